@@ -1,0 +1,668 @@
+"""The sampling and cache-page operators: what is measured of them, and their
+plain forms.
+
+Several sampled continuations of one document are decoded side by side: a
+prefilled slot is forked into others, every step draws tokens from filtered
+distributions (or accepts drafts against them), finished slots are released,
+and the pool is compacted now and then.  A case is a dict of plain values;
+``kind`` names the operator:
+
+  sample   dvs.sample_filtered: a token per row by temperature, top-k, top-p
+           and min-p from given uniforms
+  accept   dvs.accept_sampled: acceptance-rejection of drafted tokens over
+           filtered distributions, and the final token
+  fork     dvs.kv_fork: slots become continuations of others
+  release  dvs.kv_release: slots give their pages back
+  compact  dvs.kv_compact: the pages in use move to the lowest ids
+
+``own`` false: elementary torch operations.  ``own`` true: the framework's
+calls.  Lengths, tables and which slots take part follow from the case alone;
+logits, uniforms, sampling parameters and cache contents from the seed.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+PAGE = 16
+
+
+# ---------------------------------------------------------------------------
+# the cases
+# ---------------------------------------------------------------------------
+
+def _stack(name, kind, **more):
+    """A call on the cache of the 16-layer decoder stack (4 KV heads of 96)."""
+    return dict(name=name, kind=kind, layers=16, kv_heads=4, head_dim=96, dtype="bf16", **more)
+
+
+def listed():
+    return [
+        # One sequence decoded alone: the latency of a single draw from a
+        # whole vocabulary, every filter on.
+        dict(name="sample_one_row", kind="sample", rows=1, vocab=65536, dtype="f32", sigma=4.0,
+             mode="all", banned=0.0),
+        # The rows of one draft forward: 8 sequences of blocks of 16, nucleus
+        # sampling.
+        dict(name="sample_verify_rows", kind="sample", rows=136, vocab=65536, dtype="f32",
+             sigma=4.0, mode="top_p", banned=0.0),
+        # Rows that start at any alignment, a vocabulary that is no multiple
+        # of anything, half of it banned by a grammar.
+        dict(name="sample_odd_banned", kind="sample", rows=37, vocab=32003, dtype="bf16",
+             sigma=4.0, mode="mixed", banned=0.5),
+        # A large serving batch whose requests each bring their own
+        # parameters, greedy ones among them.
+        dict(name="sample_large_batch", kind="sample", rows=1024, vocab=65536, dtype="bf16",
+             sigma=4.0, mode="mixed", banned=0.0),
+        # The acceptance of a round: 8 sequences, 16 drafts each.
+        dict(name="accept_serving", kind="accept", S=8, B=16, vocab=65536, dtype="f32", sigma=4.0,
+             mode="all", noise=0.5),
+        # Few short drafts over a small vocabulary of odd size.
+        dict(name="accept_small", kind="accept", S=5, B=3, vocab=1021, dtype="bf16", sigma=2.0,
+             mode="mixed", noise=0.3),
+        # Best of 8: every document of a batch is forked seven times, pages
+        # shared but for the partly filled one.
+        _stack("fork_best_of_8", "fork", slots=64, sources=8, kv_lo=1088, kv_hi=2112, window=32,
+               share=True),
+        # One document copied to three slots, no page shared.
+        _stack("fork_private_copies", "fork", slots=4, sources=1, kv_lo=2000, kv_hi=2000,
+               window=18, share=False),
+        # Most candidates of a best-of-8 batch are dropped.
+        dict(name="release_candidates", kind="release", slots=64, sources=8, kv_lo=1088,
+             kv_hi=2112, window=32, count=48),
+        # One long sequence of a few leaves.
+        dict(name="release_one", kind="release", slots=4, sources=4, kv_lo=3001, kv_hi=9000,
+             window=18, count=1),
+        # A pool of which half is free, scattered by many commits.
+        _stack("compact_serving", "compact", slots=16, sources=16, kv_lo=500, kv_hi=1500,
+               window=32, free=0.5),
+        # A small pool that is nearly full.
+        dict(name="compact_nearly_full", kind="compact", layers=2, kv_heads=2, head_dim=64,
+             dtype="f32", slots=3, sources=3, kv_lo=40, kv_hi=300, window=9, free=0.1),
+    ]
+
+
+def _log(rng, lo, hi):
+    """An integer of [lo, hi], spread over its logarithm."""
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+MODES = ["mixed", "all", "top_p", "top_k", "min_p", "plain"]
+
+
+def draw(rng):
+    kind = rng.choice(["sample", "sample", "sample", "accept", "accept", "fork", "release",
+                       "compact"])
+    if kind == "sample":
+        V = _log(rng, 300, 160000)
+        dtype = rng.choice(["f32", "bf16"])
+        most = 134000000 // (V * (4 if dtype == "f32" else 2))
+        return dict(kind=kind, rows=_log(rng, 1, min(1024, most)), vocab=V, dtype=dtype,
+                    sigma=round(rng.uniform(0.5, 6.0), 2), mode=rng.choice(MODES),
+                    banned=rng.choice([0.0, 0.0, 0.3, 0.97]))
+    if kind == "accept":
+        V = _log(rng, 300, 100000)
+        B = _log(rng, 1, 32)
+        most = max(1, 17800000 // (V * (2 * B + 1)))
+        return dict(kind=kind, S=_log(rng, 1, min(64, most)), B=B, vocab=V,
+                    dtype=rng.choice(["f32", "bf16"]), sigma=round(rng.uniform(0.5, 6.0), 2),
+                    mode=rng.choice(MODES), noise=round(rng.uniform(0.05, 1.0), 2))
+    kv_hi = _log(rng, 20, 9000 if kind == "release" else 4000)
+    c = dict(kind=kind, kv_lo=max(1, kv_hi // rng.randint(1, 8)), kv_hi=kv_hi,
+             window=_log(rng, 1, 64), sources=_log(rng, 1, 32 if kind == "compact" else 8))
+    c["slots"] = c["sources"]
+    if kind != "compact":
+        c["slots"] = c["sources"] * rng.randint(2, 8) + rng.randint(0, 2)
+    if kind == "release":
+        c["count"] = rng.randint(1, c["slots"])
+        return c
+    if kind == "fork":
+        c["share"] = rng.random() < 0.7
+    else:
+        c["free"] = round(rng.uniform(0.05, 0.8), 2)
+    c.update(layers=rng.randint(1, 16), kv_heads=rng.choice([1, 2, 4, 8]),
+             head_dim=rng.choice([64, 96, 128]), dtype=rng.choice(["bf16", "bf16", "f32"]))
+    # no drawn case costs more than the largest listed ones
+    most = work(listed()[10])["bytes"]
+    while work(c)["bytes"] > most or _pool_bytes(c) > 1.2e9:
+        if c["layers"] > 1:
+            c["layers"] = (c["layers"] + 1) // 2
+        else:
+            c["kv_hi"] = max(20, c["kv_hi"] // 2)
+            c["kv_lo"] = min(c["kv_lo"], c["kv_hi"])
+    return c
+
+
+def _es(case):
+    return 4 if case["dtype"] == "f32" else 2
+
+
+def _pool_bytes(case):
+    return _layout(case)["pool"] * case["layers"] * 2 * _page_bytes(case)
+
+
+def _page_bytes(case):
+    return case["kv_heads"] * PAGE * case["head_dim"] * _es(case)
+
+
+def work(case):
+    kind = case["kind"]
+    if kind == "sample":
+        n = case["rows"] * case["vocab"]
+        return {"bytes": n * _es(case) + case["rows"] * 28, "flops": 10 * n}
+    if kind == "accept":
+        n = case["S"] * (2 * case["B"] + 1) * case["vocab"]
+        return {"bytes": n * _es(case), "flops": 10 * n}
+    lay = _layout(case)
+    if kind == "release":
+        return {"bytes": 12 * int(sum(lay["num_pages"][s] for s in lay["gone"])), "flops": 0}
+    page = 2 * _page_bytes(case) * case["layers"]       # K and V, every layer
+    if kind == "fork":
+        lens = np.array([lay["kv_len"][s] for s in lay["src"]])
+        copied = (int((lens % PAGE > 0).sum()) if case["share"]
+                  else int(((lens + PAGE - 1) // PAGE).sum()))
+        table = int(((lens + case["window"] + PAGE - 1) // PAGE).sum())
+        return {"bytes": 2 * copied * page + 8 * table + 8 * 256 * len(lens), "flops": 0}
+    held = np.unique(np.concatenate([lay["table"][s, :lay["num_pages"][s]]
+                                     for s in range(case["slots"])]))
+    moved = int((held >= held.size).sum())
+    return {"bytes": 2 * moved * page + 8 * int(lay["num_pages"].sum()) + 4 * lay["pool"],
+            "flops": 0}
+
+
+# ---------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------
+
+def _gen(seed, salt):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed) * 1000003 + salt)
+    return g
+
+
+def _params(mode, n, seed):
+    """Sampling parameters of n requests: temperature, top_k, top_p, min_p
+    (None where the program does not use a filter)."""
+    r = np.random.default_rng([seed, 77])
+    T = r.uniform(0.5, 1.2, n)
+    k = r.choice([10, 20, 50, 200], n)
+    p = r.uniform(0.7, 0.99, n)
+    m = r.choice([0.01, 0.02, 0.05, 0.1], n)
+    if mode == "mixed":
+        T = np.where(r.random(n) < 0.1, 0.0, T)
+        k = np.where(r.random(n) < 0.5, 0, k)
+        p = np.where(r.random(n) < 0.5, 1.0, p)
+        m = np.where(r.random(n) < 0.5, 0.0, m)
+    f32 = lambda a: torch.from_numpy(a.astype(np.float32)).cuda()   # noqa: E731
+    return dict(temperature=f32(T),
+                top_k=(torch.from_numpy(k.astype(np.int32)).cuda()
+                       if mode in ("mixed", "all", "top_k") else None),
+                top_p=f32(p) if mode in ("mixed", "all", "top_p") else None,
+                min_p=f32(m) if mode in ("mixed", "all", "min_p") else None)
+
+
+def _dt(case):
+    return torch.float32 if case["dtype"] == "f32" else torch.bfloat16
+
+
+def _layout(case):
+    """Page tables of a cache whose slots hold `sources` documents (slot s <
+    sources) and, beside them, forks of these (release) or empty slots (fork).
+    Follows from the case alone."""
+    n, docs, W = case["slots"], case["sources"], case["window"]
+    r = np.random.default_rng([n, docs, case["kv_hi"], W])
+    lens = r.integers(case["kv_lo"], case["kv_hi"] + 1, docs)
+    kv_len = np.zeros(n, np.int32)
+    kv_len[:docs] = lens
+    parent = np.arange(n) % docs
+    if case["kind"] == "release":
+        kv_len = lens[parent].astype(np.int32)
+    need = -(-(kv_len + W) // PAGE)
+    max_pages = int(-(-(int(lens.max()) + W) // PAGE)) + 2
+    shared = np.where((case["kind"] == "release") & (np.arange(n) >= docs), kv_len // PAGE, 0)
+    own_pages = need - shared
+    held = int(own_pages.sum())
+    if case["kind"] == "compact":
+        pool = int(math.ceil(held / (1 - case["free"])))
+    elif case["kind"] == "fork":
+        full = lens[parent[docs:]] // PAGE if case["share"] else 0
+        pool = held + int((-(-(lens[parent[docs:]] + W) // PAGE) - full).sum()) + 8
+    else:
+        pool = held + 8 + n
+    ids = r.permutation(pool).astype(np.int32)
+    table = np.full((n, max_pages), -1, np.int32)
+    refs = np.zeros(pool, np.int32)
+    at = 0
+    for s in range(n):
+        if shared[s]:
+            table[s, :shared[s]] = table[parent[s], :shared[s]]
+            refs[table[s, :shared[s]]] += 1
+        table[s, shared[s]:need[s]] = ids[at:at + own_pages[s]]
+        at += int(own_pages[s])
+    stack = np.full(pool, -1, np.int32)
+    stack[:pool - at] = ids[at:]
+    dst = np.arange(docs, n)
+    gone = np.sort(r.permutation(n)[:case.get("count", 0)])
+    return dict(kv_len=kv_len, num_pages=need.astype(np.int32), table=table, refs=refs,
+                stack=stack, top=pool - at, pool=pool, max_pages=max_pages,
+                src=parent[docs:].astype(np.int32), dst=dst.astype(np.int32),
+                gone=gone.astype(np.int32))
+
+
+def prepare(case, seed):
+    kind = case["kind"]
+    if kind in ("sample", "accept"):
+        return _prepare_rows(case, seed)
+    lay, pools = _layout(case), []
+    if kind != "release":                                     # a release moves no keys or values
+        g, heads, D = _gen(seed, 3), case["kv_heads"], case["head_dim"]
+        pools = [torch.randn((case["layers"], lay["pool"], heads) + page, device="cuda",
+                             generator=g, dtype=_dt(case)) for page in ((PAGE, D), (D, PAGE))]
+    n, r = case["slots"], np.random.default_rng([seed, 5])
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()  # noqa: E731
+    fields = dict(kv_len=lay["kv_len"], page_table=lay["table"], num_pages=lay["num_pages"],
+                  free_stack=lay["stack"], boundary=r.integers(0, 1000, n),
+                  draft=r.integers(0, 1000, (n, 15)), out_tokens=r.integers(0, 1000, (n, 256)),
+                  out_count=r.integers(0, 256, n), finished=np.zeros(n, np.int32))
+    st = dict(case=case, pools=pools, src=dev(lay["src"]), dst=dev(lay["dst"]), gone=dev(lay["gone"]))
+    if own:
+        from paper_2609_26638_amd import dvs, synth
+        host = synth.PagedState(free_top=lay["top"], pool_pages=lay["pool"],
+                                max_pages=lay["max_pages"],
+                                **{f: np.asarray(a, np.int32) for f, a in fields.items()})
+        st["state"], st["before"] = dvs.DeviceState(host), dvs.DeviceState(host)
+        for s in (st["state"], st["before"]):
+            s.page_refs.copy_(dev(lay["refs"]))
+        if pools:
+            st["ks"], st["vs"] = (list(p.unbind(0)) for p in pools)
+        st["workspace"] = dvs.Workspace(dvs.kv_workspace_bytes(n, n, lay["max_pages"],
+                                                               lay["pool"]))
+        st["moved"] = torch.zeros(1, dtype=torch.int32, device="cuda")
+    else:
+        fields = {f: dev(a) for f, a in fields.items()}
+        fields["free_top"], fields["page_refs"] = dev([lay["top"]]), dev(lay["refs"])
+        st["state"], st["before"] = fields, {f: a.clone() for f, a in fields.items()}
+    return st
+
+
+def _prepare_rows(case, seed):
+    V, g = case["vocab"], _gen(seed, 1)
+    if case["kind"] == "sample":
+        z = torch.randn((case["rows"], V), device="cuda", generator=g) * case["sigma"]
+        if case["banned"]:
+            ban = torch.rand((case["rows"], V), device="cuda", generator=g) < case["banned"]
+            ban[:, 0] = False
+            z.masked_fill_(ban, -math.inf)
+        st = dict(case=case, z=z.to(_dt(case)),
+                  u=torch.rand(case["rows"], device="cuda", generator=g),
+                  par=_params(case["mode"], case["rows"], seed))
+        if own:
+            from paper_2609_26638_amd import dvs
+            st["workspace"] = dvs.Workspace(dvs.sample_workspace_bytes(case["rows"], V))
+        return st
+    S, B = case["S"], case["B"]
+    zv = torch.randn((S, B + 1, V), device="cuda", generator=g) * case["sigma"]
+    zd = zv[:, :B] + torch.randn((S, B, V), device="cuda", generator=g) * case["noise"]
+    zv, zd = zv.to(_dt(case)), zd.to(_dt(case))
+    par = _params(case["mode"], S, seed)
+    # the drafts were drawn from the draft rows
+    u = torch.rand((S, 2 * B + 1), device="cuda", generator=g)
+    d = _draw_token(_filtered(zd, par), u[:, :B].double())[0].to(torch.int32)
+    st = dict(case=case, zv=zv, zd=zd, draft=d, u=u[:, B:].contiguous(), par=par)
+    if own:
+        from paper_2609_26638_amd import dvs
+        st["workspace"] = dvs.Workspace(dvs.accept_workspace_bytes(S, B, V))
+    return st
+
+
+# ---------------------------------------------------------------------------
+# one pass
+# ---------------------------------------------------------------------------
+
+def run(state):
+    return RUN[state["case"]["kind"]](state)
+
+
+def _run_sample(st):
+    if own:
+        from paper_2609_26638_amd import dvs
+        return dvs.sample_filtered(st["z"], st["u"], workspace=st["workspace"], **st["par"])
+    token, prob = _draw_token(_filtered(st["z"], st["par"]), st["u"].double())
+    return token.to(torch.int32), prob.float()
+
+
+def _run_accept(st):
+    if own:
+        from paper_2609_26638_amd import dvs
+        return dvs.accept_sampled(st["zv"], st["zd"], st["draft"], st["u"],
+                                  workspace=st["workspace"], **st["par"])
+    B = st["case"]["B"]
+    p, q = _filtered(st["zv"], st["par"]), _filtered(st["zd"], st["par"])
+    p, q = p / p.sum(-1, keepdim=True), q / q.sum(-1, keepdim=True)
+    d, u = st["draft"].long().unsqueeze(-1), st["u"].double()
+    pd, qd = p[:, :B].gather(-1, d).squeeze(-1), q.gather(-1, d).squeeze(-1)
+    A = (u[:, :B] * qd < pd).long().cumprod(-1).sum(-1)
+    at = A.view(-1, 1, 1)
+    w = p.gather(1, at.expand(-1, 1, p.shape[-1])).squeeze(1)
+    minus = q.gather(1, at.clamp(max=B - 1).expand(-1, 1, q.shape[-1])).squeeze(1)
+    rest = (w - minus).clamp(min=0)
+    w = torch.where(((A < B) & (rest.sum(-1) > 0)).unsqueeze(-1), rest, w)
+    token, _ = _draw_token(w, u[:, B])
+    return A.to(torch.int32), token.to(torch.int32)
+
+
+def _filtered(z, par):
+    """Weights exp((z - max) / T) of the tokens that the filters keep, 0 for
+    the others.  Parameters have one entry per leading index."""
+    lead = lambda a: a.view(a.shape + (1,) * (z.dim() - 1))   # noqa: E731
+    z = z.float() + 0.0                                       # -0 and +0 are equal
+    T, V = lead(par["temperature"]).double(), z.shape[-1]
+    greedy = T <= 0
+    w = ((z.double() - z.amax(-1, keepdim=True).double()) / torch.where(greedy, 1.0, T)).exp()
+    _, order = z.sort(dim=-1, descending=True, stable=True)
+    sw = w.gather(-1, order)
+    rank = torch.arange(V, device=z.device)
+    k = torch.full_like(T, V, dtype=torch.int64)
+    if par["top_k"] is not None:
+        k = lead(par["top_k"]).long()
+        k = torch.where((k <= 0) | (k > V), V, k)
+    k = torch.where(greedy, 1, k)
+    keep = rank < k
+    if par["top_p"] is not None:
+        p = lead(par["top_p"]).double()
+        before = (sw * keep).cumsum(-1)
+        keep = keep & ((before - sw < p * before[..., -1:]) | (p >= 1))
+    if par["min_p"] is not None:
+        keep = keep & (sw >= lead(par["min_p"]).double())
+    keep = keep | (rank == 0)
+    keep = keep.expand_as(w)
+    return w * torch.zeros_like(keep).scatter(-1, order, keep)
+
+
+def _draw_token(w, u):
+    """The smallest index whose running weight exceeds u times the whole."""
+    c = w.cumsum(-1)
+    token = (c <= u.unsqueeze(-1) * c[..., -1:]).sum(-1)
+    last = torch.where(w > 0, torch.arange(w.shape[-1], device=w.device), -1).amax(-1)
+    token = torch.minimum(token, last)
+    return token, w.gather(-1, token.unsqueeze(-1)).squeeze(-1) / c[..., -1]
+
+
+def _run_fork(st):
+    c = st["case"]
+    if own:
+        from paper_2609_26638_amd import dvs
+        dvs.kv_fork(st["state"], st["ks"], st["vs"], st["src"], st["dst"], c["window"],
+                    share=c["share"], workspace=st["workspace"])
+        return _outputs(st)
+    f, src, dst = st["state"], st["src"].long(), st["dst"].long()
+    L = f["kv_len"][src].long()
+    full = L // PAGE if c["share"] else torch.zeros_like(L)
+    j = torch.arange(f["page_table"].shape[1], device="cuda")
+    old = f["page_table"][src]
+    _give_back(f, dst)
+    fresh, need = _take(f, full, L + c["window"])
+    rows = torch.where(j < full.unsqueeze(1), old, fresh)
+    shared = old[j < full.unsqueeze(1)].long()
+    f["page_refs"].index_add_(0, shared, torch.ones_like(shared, dtype=torch.int32))
+    copied = (j >= full.unsqueeze(1)) & (j < ((L + PAGE - 1) // PAGE).unsqueeze(1))
+    a, b = old[copied].long(), rows[copied].long()
+    for pool in st["pools"]:
+        pool[:, b] = pool[:, a]
+    f["page_table"][dst] = rows
+    f["num_pages"][dst] = need.to(torch.int32)
+    for name in ("kv_len", "boundary", "draft", "out_tokens", "out_count", "finished"):
+        f[name][dst] = f[name][src]
+    return _outputs(st)
+
+
+def _run_release(st):
+    c = st["case"]
+    if own:
+        from paper_2609_26638_amd import dvs
+        st["state"].copy_from(st["before"])
+        dvs.kv_release(st["state"], st["gone"], c["window"], workspace=st["workspace"])
+        return _outputs(st)
+    f, gone = st["state"], st["gone"].long()
+    for name in f:
+        f[name].copy_(st["before"][name])
+    _give_back(f, gone)
+    zero = torch.zeros_like(gone)
+    rows, need = _take(f, zero, zero + c["window"])
+    f["page_table"][gone] = rows
+    f["num_pages"][gone] = need.to(torch.int32)
+    for name in ("kv_len", "boundary", "out_count"):
+        f[name][gone] = 0
+    f["finished"][gone] = 1
+    return _outputs(st)
+
+
+def _run_compact(st):
+    c = st["case"]
+    if own:
+        from paper_2609_26638_amd import dvs
+        st["state"].copy_from(st["before"])
+        dvs.kv_compact(st["state"], st["ks"], st["vs"], moved_out=st["moved"],
+                       workspace=st["workspace"])
+        return _outputs(st) + [st["moved"]]
+    f = st["state"]
+    for name in f:
+        f[name].copy_(st["before"][name])
+    table, pool = f["page_table"], f["free_stack"].shape[0]
+    valid = torch.arange(table.shape[1], device="cuda") < f["num_pages"].unsqueeze(1)
+    used = torch.zeros(pool, dtype=torch.bool, device="cuda")
+    used[table[valid].long()] = True
+    ids, U = torch.arange(pool, device="cuda"), used.sum()
+    a, b = ids[used & (ids >= U)], ids[~used & (ids < U)]
+    to = ids.clone()
+    to[a] = b
+    for p in st["pools"]:
+        p[:, b] = p[:, a]
+    table[valid] = to[table[valid].long()].to(torch.int32)
+    f["page_refs"][b] = f["page_refs"][a]
+    f["page_refs"][a] = 0
+    f["free_stack"].copy_(torch.where(ids < pool - U, pool - 1 - ids, -1))
+    return _outputs(st) + [(used & (ids >= U)).sum().to(torch.int32).view(1)]
+
+
+def _give_back(f, slots):
+    """Every page of the slots loses a holder; those without one go on the
+    free stack, the highest id first."""
+    table = f["page_table"][slots]
+    valid = torch.arange(table.shape[1], device="cuda") < f["num_pages"][slots].unsqueeze(1)
+    held = table[valid].long()
+    f["page_refs"].index_add_(0, held, torch.full_like(held, -1, dtype=torch.int32))
+    freed = f["page_refs"] < 0
+    f["page_refs"][freed] = 0
+    ids = torch.arange(freed.shape[0], device="cuda")[freed].flip(0)
+    at = f["free_top"] + torch.arange(ids.shape[0], device="cuda")
+    f["free_stack"][at] = ids.to(torch.int32)
+    f["free_top"] += ids.shape[0]
+
+
+def _take(f, first, rows):
+    """Pages for logical pages first .. ceil(rows / 16) - 1 of each slot from
+    the top of the free stack, slots in order, logical pages ascending."""
+    need = (rows + PAGE - 1) // PAGE
+    count = need - first
+    j = torch.arange(f["page_table"].shape[1], device="cuda")
+    wanted = (j >= first.unsqueeze(1)) & (j < need.unsqueeze(1))
+    at = f["free_top"] - 1 - ((count.cumsum(0) - count - first).unsqueeze(1) + j)
+    pages = torch.where(wanted, f["free_stack"][at.clamp(0, f["free_stack"].shape[0] - 1)], -1)
+    f["free_stack"][at[wanted]] = -1
+    f["free_top"] -= count.sum()
+    return pages, need
+
+
+FIELDS = ("kv_len", "page_table", "num_pages", "free_stack", "boundary", "draft", "out_tokens",
+          "out_count", "finished", "free_top", "page_refs")
+
+
+def _outputs(st):
+    s = st["state"]
+    return st["pools"] + [getattr(s, f) if own else s[f] for f in FIELDS]
+
+
+RUN = dict(sample=_run_sample, accept=_run_accept, fork=_run_fork, release=_run_release,
+           compact=_run_compact)
+
+
+# ---------------------------------------------------------------------------
+# the definition, on the host, in 64 bits
+# ---------------------------------------------------------------------------
+
+def exact(case, seed):
+    global own
+    if case["kind"] in ("sample", "accept") and work(case)["flops"] > 10 * 70e6:
+        return None
+    was, own = own, False
+    try:
+        st = prepare(case, seed)
+    finally:
+        own = was
+    if case["kind"] == "sample":
+        return _exact_sample(st)
+    if case["kind"] == "accept":
+        return _exact_accept(st)
+    return _exact_pages(st)
+
+
+def _np(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def _exact_probs(z, st, i):
+    par = {k: None if v is None else v[i].item() for k, v in st["par"].items()}
+    T, V = par["temperature"], z.size
+    order = np.argsort(-z, kind="stable")
+    if T <= 0:
+        p = np.zeros(V)
+        p[order[0]] = 1.0
+        return p
+    w = np.exp((z[order] - z[order[0]]) / T)
+    n = V
+    if par["top_k"] is not None and 0 < par["top_k"] < V:
+        n = par["top_k"]
+    if par["top_p"] is not None and par["top_p"] < 1:
+        c = np.cumsum(w[:n])
+        n = min(n, int(np.searchsorted(c, par["top_p"] * c[-1], side="left")) + 1)
+    if par["min_p"] is not None:
+        n = max(1, min(n, int((w >= par["min_p"]).sum())))
+    p = np.zeros(V)
+    p[order[:n]] = w[:n] / w[:n].sum()
+    return p
+
+
+def _exact_token(p, u):
+    c = np.cumsum(p)
+    return min(int(np.searchsorted(c, u * c[-1], side="right")), int(np.flatnonzero(p)[-1]))
+
+
+def _exact_sample(st):
+    z, u = _np(st["z"]), _np(st["u"])
+    got = []
+    for i in range(z.shape[0]):
+        p = _exact_probs(z[i], st, i)
+        t = _exact_token(p, u[i])
+        got.append((t, p[t]))
+    return (np.array([t for t, _ in got], np.int32), np.array([p for _, p in got]))
+
+
+def _exact_accept(st):
+    zv, zd, u, d = _np(st["zv"]), _np(st["zd"]), _np(st["u"]), st["draft"].cpu().numpy()
+    S, B = d.shape
+    A, tok = np.zeros(S, np.int32), np.zeros(S, np.int32)
+    for s in range(S):
+        p, q = _exact_probs(zv[s, 0], st, s), None
+        for j in range(B + 1):
+            p, q = _exact_probs(zv[s, j], st, s), None
+            if j == B:
+                break
+            q = _exact_probs(zd[s, j], st, s)
+            if not u[s, j] * q[d[s, j]] < p[d[s, j]]:
+                break
+            A[s] += 1
+        w = p if q is None else np.maximum(p - q, 0)
+        tok[s] = _exact_token(w if w.sum() > 0 else p, u[s, B])
+    return A, tok
+
+
+def _exact_pages(st):
+    """A slot at a time, a page at a time."""
+    c = st["case"]
+    f = {k: v.cpu().numpy().copy() for k, v in st["state"].items()}
+    table, stack, refs, top = f["page_table"], f["free_stack"], f["page_refs"], int(f["free_top"][0])
+    copies, more = [], []
+
+    def give_back(slots):
+        nonlocal top
+        free = []
+        for s in slots:
+            for p in table[s, :f["num_pages"][s]]:
+                refs[p] -= 1
+                if refs[p] < 0:
+                    refs[p] = 0
+                    free.append(int(p))
+        for p in sorted(free, reverse=True):
+            stack[top] = p
+            top += 1
+
+    def take():
+        nonlocal top
+        top -= 1
+        p, stack[top] = stack[top], -1
+        return p
+
+    if c["kind"] == "fork":
+        src, dst = st["src"].tolist(), st["dst"].tolist()
+        give_back(dst)
+        for a, b in zip(src, dst):
+            L = int(f["kv_len"][a])
+            need = -(-(L + c["window"]) // PAGE)
+            row = np.full(table.shape[1], -1, np.int32)
+            for j in range(need):
+                if c["share"] and (j + 1) * PAGE <= L:
+                    row[j] = table[a, j]
+                    refs[row[j]] += 1
+                else:
+                    row[j] = take()
+                    if j * PAGE < L:
+                        copies.append((int(table[a, j]), int(row[j])))
+            table[b], f["num_pages"][b] = row, need
+            for name in ("kv_len", "boundary", "draft", "out_tokens", "out_count", "finished"):
+                f[name][b] = f[name][a]
+    elif c["kind"] == "release":
+        gone = st["gone"].tolist()
+        give_back(gone)
+        for s in gone:
+            need = -(-c["window"] // PAGE)
+            table[s] = -1
+            for j in range(need):
+                table[s, j] = take()
+            f["num_pages"][s] = need
+            f["kv_len"][s] = f["boundary"][s] = f["out_count"][s] = 0
+            f["finished"][s] = 1
+    else:
+        held = sorted({int(p) for s in range(c["slots"]) for p in table[s, :f["num_pages"][s]]})
+        U, taken = len(held), set(held)
+        holes = [i for i in range(U) if i not in taken]
+        copies = list(zip([p for p in held if p >= U], holes))
+        to = dict(copies)
+        for s in range(c["slots"]):
+            for j in range(f["num_pages"][s]):
+                table[s, j] = to.get(int(table[s, j]), table[s, j])
+        for a, b in copies:
+            refs[b], refs[a] = refs[a], 0
+        stack[:] = -1
+        top = len(stack) - U
+        stack[:top] = np.arange(len(stack) - 1, U - 1, -1)
+        more = [np.array([len(copies)], np.int32)]
+    f["free_top"][0] = top
+    pools = [p.clone() for p in st["pools"]]
+    for a, b in copies:
+        for p, q in zip(pools, st["pools"]):
+            p[:, b] = q[:, a]
+    return pools + [f[name] for name in FIELDS] + more
