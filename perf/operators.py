@@ -278,8 +278,7 @@ def prepare(case, seed):
             s.page_refs.copy_(dev(lay["refs"]))
         if pools:
             st["ks"], st["vs"] = (list(p.unbind(0)) for p in pools)
-        st["workspace"] = dvs.Workspace(dvs.kv_workspace_bytes(n, n, lay["max_pages"],
-                                                               lay["pool"]))
+        st["workspace"] = dvs.Workspace(dvs.kv_workspace_bytes(n, lay["pool"]))
         st["moved"] = torch.zeros(1, dtype=torch.int32, device="cuda")
     else:
         fields = {f: dev(a) for f, a in fields.items()}
