@@ -298,9 +298,6 @@ def _prepare_rows(case, seed):
         st = dict(case=case, z=z.to(_dt(case)),
                   u=torch.rand(case["rows"], device="cuda", generator=g),
                   par=_params(case["mode"], case["rows"], seed))
-        if own:
-            from paper_2609_26638_amd import dvs
-            st["workspace"] = dvs.Workspace(dvs.sample_workspace_bytes(case["rows"], V))
         return st
     S, B = case["S"], case["B"]
     zv = torch.randn((S, B + 1, V), device="cuda", generator=g) * case["sigma"]
@@ -328,7 +325,7 @@ def run(state):
 def _run_sample(st):
     if own:
         from paper_2609_26638_amd import dvs
-        return dvs.sample_filtered(st["z"], st["u"], workspace=st["workspace"], **st["par"])
+        return dvs.sample_filtered(st["z"], st["u"], **st["par"])
     token, prob = _draw_token(_filtered(st["z"], st["par"]), st["u"].double())
     return token.to(torch.int32), prob.float()
 
