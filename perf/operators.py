@@ -277,7 +277,7 @@ def prepare(case, seed):
         for s in (st["state"], st["before"]):
             s.page_refs.copy_(dev(lay["refs"]))
         if pools:
-            st["ks"], st["vs"] = (list(p.unbind(0)) for p in pools)
+            st["handle"] = dvs.KVPools(*(list(p.unbind(0)) for p in pools))
         st["workspace"] = dvs.Workspace(dvs.kv_workspace_bytes(n, lay["pool"]))
         st["moved"] = torch.zeros(1, dtype=torch.int32, device="cuda")
     else:
@@ -391,7 +391,7 @@ def _run_fork(st):
     c = st["case"]
     if own:
         from paper_2609_26638_amd import dvs
-        dvs.kv_fork(st["state"], st["ks"], st["vs"], st["src"], st["dst"], c["window"],
+        dvs.kv_fork(st["state"], st["handle"], st["src"], st["dst"], c["window"],
                     share=c["share"], workspace=st["workspace"])
         return _outputs(st)
     f, src, dst = st["state"], st["src"].long(), st["dst"].long()
@@ -441,7 +441,7 @@ def _run_compact(st):
     if own:
         from paper_2609_26638_amd import dvs
         st["state"].copy_from(st["before"])
-        dvs.kv_compact(st["state"], st["ks"], st["vs"], moved_out=st["moved"],
+        dvs.kv_compact(st["state"], st["handle"], moved_out=st["moved"],
                        workspace=st["workspace"])
         return _outputs(st) + [st["moved"]]
     f = st["state"]
