@@ -61,6 +61,7 @@ extern "C" {
 #define DVS_ERR_NONFINITE 4       /* a logit was NaN or infinite              */
 #define DVS_ERR_BAD_PAGE 8        /* a page id outside [0, num_pool_pages)    */
 #define DVS_ERR_OPEN_BLOCK 16     /* a block commit met a masked position     */
+#define DVS_ERR_BAD_SLOT 32       /* a sequence slot out of range, or given twice */
 
 #define DVS_PAGE_SIZE 16
 
@@ -214,6 +215,74 @@ int argmax_accept(const void* logits, int32_t dtype, int32_t S, int32_t R, int32
  * ---------------------------------------------------------------------- */
 int top1_confidence(const void* logits, int32_t dtype, int32_t rows, int32_t V,
                     int32_t* argmax_out, float* conf_out, int32_t* err_word, void* stream);
+
+/* ------------------------------------------------------------------------
+ * sample_filtered
+ *
+ * One token per row of logits z, drawn from softmax(z / T) cut by top-k,
+ * top-p and min-p.  The tokens of a row are ordered by (logit descending,
+ * index ascending; -0.0 equals +0.0), with weights
+ *     w_i = exp((z_i - max z) / T)              (64-bit arithmetic):
+ *   top-k   keeps the first top_k tokens (<= 0, or >= V: all);
+ *   top-p   keeps, of these, the shortest prefix whose weight is at least
+ *           top_p times theirs, at least one token (>= 1, or NaN: all);
+ *   min-p   drops the tokens with w_i < min_p (<= 0, or NaN: none); the
+ *           first token always stays.
+ *   token_out[r] = the smallest kept index i whose running weight
+ *           sum_{j <= i, j kept} w_j exceeds u[r] * W, W the kept weight;
+ *   prob_out[r]  = w_token / W (its probability; fp32).
+ * A temperature <= 0 (or NaN) means the top-1 (lowest index among equal
+ * maxima), probability 1.  A logit of -inf is a masked token: weight 0, no
+ * error.  NaN logits have weight 0 too and set DVS_ERR_NONFINITE, as does
+ * +inf, whose row gives its lowest index.  A row that has no value above
+ * -inf sets DVS_ERR_NONFINITE and gives the index rule of argmax_accept and
+ * probability 0.  u below 0 or NaN counts as 0; u >= 1 gives the last kept
+ * token of positive weight.
+ *
+ *   logits [rows] rows of V values DVS_F32 or DVS_BF16, ld >= V elements apart
+ *   temperature, top_k, top_p, min_p  [rows / rows_per_param] each, or NULL
+ *           (temperature 1, filter off); rows [g * rows_per_param, ...) take
+ *           entry g
+ *   u [rows] fp32 uniforms in [0, 1) (the caller draws them)
+ *   token_out [rows] int32, prob_out [rows] fp32 (may be NULL); err_word may
+ *           be NULL.
+ * A row's result does not depend on the other rows.  Requirements: rows >= 1,
+ * 1 <= V <= 2^30, rows % rows_per_param == 0.
+ * ---------------------------------------------------------------------- */
+int sample_filtered(const void* logits, int32_t dtype, int32_t rows, int32_t V, int64_t ld,
+                    const float* temperature, const int32_t* top_k, const float* top_p,
+                    const float* min_p, int32_t rows_per_param, const float* u,
+                    int32_t* token_out, float* prob_out, int32_t* err_word, void* stream);
+
+/* ------------------------------------------------------------------------
+ * accept_sampled / dvs_accept_workspace_bytes
+ *
+ * Stochastic acceptance (Preliminaries, "Speculative Decoding"; the rule of
+ * literal_round_sampled) over filtered distributions.  For sequence s, p_j is
+ * the distribution of sample_filtered over verify row j-1 and q_j over draft
+ * row j-1 (the row d_j was drawn from), j = 1..B, with the parameters of s:
+ *   d_j is accepted while u[s, j-1] * q_j(d_j) < p_j(d_j) (a draft outside
+ *   [0, V) is not); accept_len[s] = A = number accepted;
+ *   token_out[s] is drawn with u[s, B] from max(0, p_{A+1} - q_{A+1}) when
+ *   A < B (from p_{A+1} where that is zero everywhere), from p_{B+1} when
+ *   A = B, by the rule of sample_filtered.
+ *   z_verify  row j of sequence s at s * verify_seq + j * verify_ld elements,
+ *             j = 0..B; z_draft likewise, j = 0..B-1; DVS_F32 or DVS_BF16
+ *   temperature, top_k, top_p, min_p [S] or NULL, as sample_filtered
+ *   draft [S, draft_width] int32, draft_width >= B; u [S, B + 1] fp32
+ *   accept_len [S], token_out [S] int32 (written); err_word may be NULL
+ *   workspace >= dvs_accept_workspace_bytes(S, B, V) bytes, no initialisation
+ *             needed.  Calls that share it must not overlap in time.
+ * Requirements: S, B >= 1, 1 <= V <= 2^30, row strides >= V.
+ * ---------------------------------------------------------------------- */
+size_t dvs_accept_workspace_bytes(int32_t S, int32_t B, int32_t V);
+int accept_sampled(const void* z_verify, int64_t verify_seq, int64_t verify_ld,
+                   const void* z_draft, int64_t draft_seq, int64_t draft_ld, int32_t dtype,
+                   int32_t S, int32_t B, int32_t V, const float* temperature,
+                   const int32_t* top_k, const float* top_p, const float* min_p,
+                   const int32_t* draft, int32_t draft_width, const float* u,
+                   int32_t* accept_len, int32_t* token_out, int32_t* err_word, void* workspace,
+                   size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * kv_commit
@@ -538,6 +607,79 @@ size_t dvs_sampled_round_workspace_bytes(const dvs_model* m, int32_t S, int32_t 
 int literal_round_sampled(const dvs_model* m, const dvs_state* st, int32_t B, float temperature,
                           const float* u, int32_t chunk_keys, float* logits_out,
                           int32_t* accept_out, void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * literal_round_filtered / dvs_filtered_round_workspace_bytes
+ *
+ * literal_round_sampled with every distribution cut by its sequence's
+ * filters: a0 and d_j are drawn by sample_filtered with u[s, 0..B], the
+ * acceptance and the final token are accept_sampled's with u[s, B+1..2B+1].
+ *   temperature, top_k, top_p, min_p [S] (device) or NULL, as sample_filtered
+ *   u [S, 2B + 2]; other arguments, outputs and pages as
+ *   literal_round_sampled.  workspace:
+ *   dvs_filtered_round_workspace_bytes(m, S, B, max_pages, chunk_keys).
+ * ---------------------------------------------------------------------- */
+size_t dvs_filtered_round_workspace_bytes(const dvs_model* m, int32_t S, int32_t B,
+                                          int32_t max_pages, int32_t chunk_keys);
+int literal_round_filtered(const dvs_model* m, const dvs_state* st, int32_t B,
+                           const float* temperature, const int32_t* top_k, const float* top_p,
+                           const float* min_p, const float* u, int32_t chunk_keys,
+                           float* logits_out, int32_t* accept_out, void* workspace,
+                           size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * kv_fork / kv_release / kv_compact / dvs_kv_workspace_bytes
+ *
+ * Sequences that continue one prefix several times over one pool.  page_refs
+ * [num_pool_pages] int32 holds, for every page, its holders beyond the first
+ * (0: one holder, or free): zero-filled by the caller before its first use,
+ * kept up by these three calls, needed by no other.  Only full committed
+ * pages are shared, which the attention never writes and the commits neither
+ * pop nor push, so shared sequences decode like any others.  It may be NULL
+ * where no page is shared; once pages are, every one of these calls takes it.
+ *
+ * kv_fork: for every pair i, slot dst[i] becomes a copy of slot src[i]
+ *   (kv_len, boundary, draft, out_tokens, out_count, finished), ready for a
+ *   window of `window` rows: it holds ceil((kv_len + window) / 16) pages.
+ *   The pages that dst[i] held are given back first: those without another
+ *   holder go on the free stack, the highest id first.  With share != 0 the
+ *   floor(kv_len / 16) full pages are src's (one holder more each) and the
+ *   partly filled page is copied, K and V, in every layer; with share == 0
+ *   every page that holds committed positions is.  New pages are popped,
+ *   pairs in order, logical pages ascending.  src and dst [n] int32; a source
+ *   may be given several times; a destination only once, and it is no source.
+ * kv_release: the slots [n] become empty: kv_len, boundary, out_count 0,
+ *   finished 1 (draft and out_tokens stay).  Their pages are given back as
+ *   above and each holds ceil(window / 16) pages again, so that the batch's
+ *   steps still run over it; with window = P + the next step's rows,
+ *   dvs_prefill can fill it again.
+ * kv_compact: with U pages held, the k-th held id >= U (ascending) moves to
+ *   the k-th free id < U, in every layer's pools, the page tables and
+ *   page_refs; afterwards the held pages are 0 .. U-1 and the free stack is
+ *   num_pool_pages-1 .. U, U on top.  st must describe every sequence that
+ *   holds pages: a page that is neither held nor on the stack, or both, is
+ *   DVS_ERR_BAD_PAGE.  *moved_out (device, may be NULL) = pages moved.
+ *
+ * Errors (nothing is changed): DVS_ERR_BAD_SLOT for a slot outside [0, S), a
+ * repeated destination or one that is a source; DVS_ERR_MAX_PAGES,
+ * DVS_ERR_POOL_EXHAUSTED as in kv_commit; DVS_ERR_BAD_PAGE for a page id
+ * outside the pool or counts that do not fit the tables.
+ *   layers: only k_pool and v_pool are read; they start on 16 bytes.
+ *   workspace >= dvs_kv_workspace_bytes(S, num_pool_pages) bytes, no
+ *   initialisation needed.  Calls that share it must not overlap in time.
+ * Requirements: 1 <= S <= 1024, max_pages <= 2^20, window >= 1, 1 <= n < S
+ * (kv_release: <= S).
+ * ---------------------------------------------------------------------- */
+size_t dvs_kv_workspace_bytes(int32_t S, int32_t num_pool_pages);
+int kv_fork(const dvs_state* st, int32_t* page_refs, const dvs_layer* layers, int32_t n_layers,
+            int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t n, const int32_t* src,
+            const int32_t* dst, int32_t window, int32_t share, void* workspace, size_t ws_bytes,
+            void* stream);
+int kv_release(const dvs_state* st, int32_t* page_refs, int32_t n, const int32_t* slots,
+               int32_t window, void* workspace, size_t ws_bytes, void* stream);
+int kv_compact(const dvs_state* st, int32_t* page_refs, const dvs_layer* layers,
+               int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+               int32_t* moved_out, void* workspace, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * dvs_prefill

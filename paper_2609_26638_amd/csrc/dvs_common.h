@@ -41,6 +41,30 @@ int launch_accept_final(int S, int B, int V, float invT, const float* zv, const 
                         const float* u, int u_stride, int32_t* accept_len, int32_t* am,
                         hipStream_t st);
 
+// Filtered sampling (filter.hip).  Parameters of a request each, device
+// arrays; NULL: temperature 1, filter off.
+struct RowParams {
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+};
+
+// Row r = s * rows_per_param + i takes the parameters s and u[s * u_stride + i].
+int launch_sample_filtered(const void* logits, int dtype, int rows, int V, long long ld,
+                           const RowParams& par, int rows_per_param, const float* u, int u_stride,
+                           int32_t* token_out, float* prob_out, int32_t* err, hipStream_t st);
+// vs, vld, ds, dld: elements from a sequence's (a row's) logits to the next's.
+// The final token of sequence s goes to token_out[s * token_stride], or to
+// slot accept_len[s] of that row (at_accepted).  ws: filter_cuts_bytes.
+size_t filter_cuts_bytes(int S, int B);
+int launch_accept_sampled(const void* zv, long long vs, long long vld, const void* zd,
+                          long long ds, long long dld, int dtype, int S, int B, int V,
+                          const RowParams& par, const int32_t* draft, int draft_width,
+                          const float* u, int u_stride, int32_t* accept_len, int32_t* token_out,
+                          int token_stride, int at_accepted, int32_t* err, void* ws,
+                          hipStream_t st);
+
 // Bytes at the start of an attention workspace that hold the split-merge
 // counters (zero between calls) for the given call shape.
 size_t attn_counter_bytes(int S, int R, int Hq, int Hkv, int D, int max_pages, int chunk_keys,

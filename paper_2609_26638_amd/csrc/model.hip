@@ -1983,6 +1983,53 @@ static int run_round_sampled(const dvs_model* m, const dvs_state* st, int B, flo
                          st->max_new, st->eos_id, st->finished, st->err_word, stream);
 }
 
+// run_round_sampled over filtered distributions (sample_filtered,
+// accept_sampled).  Draft logits and the rows' cuts live past the larger of
+// the two forwards' layouts.
+template <typename T>
+static int run_round_filtered(const dvs_model* m, const dvs_state* st, int B,
+                              const RowParams& par, const float* u, int chunk_keys,
+                              const StepLayout& Ld, const StepLayout& Lv, size_t extra, char* ws,
+                              float* logits_out, int32_t* accept_out, hipStream_t stream) {
+  const int S = st->S, R = B + 1, M = S * R, V = m->vocab, us = 2 * B + 2;
+  float* zd = (float*)(ws + extra);
+  void* cuts = ws + extra + al((size_t)M * V * 4);
+  float* zv = logits_out ? logits_out : (float*)(ws + Lv.logits);
+  int32_t* tok = (int32_t*)(ws + Lv.am);
+  int32_t* acc = accept_out ? accept_out : (int32_t*)(ws + Lv.acc);
+  int32_t* lead = (int32_t*)(ws + Lv.lead);
+  int rc;
+  hipLaunchKernelGGL(embed_rows_kernel<T>, dim3(M), dim3(256), 0, stream, (const T*)m->embed,
+                     m->hidden, V, R, 1, st->boundary, st->draft, st->draft_width, nullptr, 0,
+                     (float*)(ws + Ld.x));
+  if ((rc = launch_status("literal_round_filtered(embed)"))) return rc;
+  if ((rc = forward_layers<T>(m, st, 1, B, chunk_keys, Ld, ws, stream))) return rc;
+  if ((rc = gemm(m->dtype, ws + Ld.h, m->lm_head, M, V, m->hidden, zd, 1, 0, stream)))
+    return rc;
+  rc = launch_sample_filtered(zd, DVS_F32, M, V, V, par, R, u, us, tok, nullptr, st->err_word,
+                              stream);
+  if (rc) return rc;
+  hipLaunchKernelGGL(round_draft_kernel, dim3((S + 255) / 256), dim3(256), 0, stream, S, B, tok,
+                     st->finished, st->kv_len, lead, st->draft, st->draft_width);
+  if ((rc = launch_status("literal_round_filtered(draft)"))) return rc;
+  hipLaunchKernelGGL(embed_rows_kernel<T>, dim3(M), dim3(256), 0, stream, (const T*)m->embed,
+                     m->hidden, V, R, R, lead, st->draft, st->draft_width, nullptr, 0,
+                     (float*)(ws + Lv.x));
+  if ((rc = launch_status("literal_round_filtered(embed)"))) return rc;
+  if ((rc = forward_layers<T>(m, st, R, 0, chunk_keys, Lv, ws, stream))) return rc;
+  if ((rc = gemm(m->dtype, ws + Lv.h, m->lm_head, M, V, m->hidden, zv, 1, 0, stream)))
+    return rc;
+  const long long seq = (long long)R * V;
+  rc = launch_accept_sampled(zv, seq, V, zd + V, seq, V, DVS_F32, S, B, V, par, st->draft,
+                             st->draft_width, u + R, us, acc, tok, R, 1, st->err_word, cuts,
+                             stream);
+  if (rc) return rc;
+  return kv_commit_round(S, B, lead, acc, tok, st->kv_len, st->page_table, st->num_pages,
+                         st->max_pages, st->free_stack, st->free_top, st->num_pool_pages,
+                         st->boundary, st->draft, st->draft_width, st->out_tokens, st->out_count,
+                         st->max_new, st->eos_id, st->finished, st->err_word, stream);
+}
+
 template <typename T>
 static int run_prefill(const dvs_model* m, const dvs_state* st, int P, int n_mask,
                        const int32_t* tokens, const float* x_prefix, int chunk_keys,
@@ -2319,4 +2366,39 @@ extern "C" int literal_round_sampled(const dvs_model* m, const dvs_state* st, in
                                          (char*)workspace, logits_out, accept_out, s)
              : run_round_sampled<float>(m, st, B, temperature, u, chunk_keys, Ld, Lv, extra,
                                         (char*)workspace, logits_out, accept_out, s);
+}
+
+extern "C" size_t dvs_filtered_round_workspace_bytes(const dvs_model* m, int32_t S, int32_t B,
+                                                     int32_t max_pages, int32_t chunk_keys) {
+  if (!model_ok(m) || S < 1 || B < 1 || max_pages < 1) return 0;
+  StepLayout Ld, Lv;
+  const size_t M = (size_t)S * (B + 1);
+  return sampled_extra(m, S, B, max_pages, chunk_keys, &Ld, &Lv) + al(M * m->vocab * 4) +
+         al(filter_cuts_bytes(S, B));
+}
+
+extern "C" int literal_round_filtered(const dvs_model* m, const dvs_state* st, int32_t B,
+                                      const float* temperature, const int32_t* top_k,
+                                      const float* top_p, const float* min_p, const float* u,
+                                      int32_t chunk_keys, float* logits_out, int32_t* accept_out,
+                                      void* workspace, size_t ws_bytes, void* stream) {
+  clear_error();
+  int rc = check_model_state(m, st, "literal_round_filtered");
+  if (rc) return rc;
+  DVS_CHECK_ARG(B >= 1 && u, "literal_round_filtered: need B >= 1 and uniforms");
+  DVS_CHECK_ARG(st->draft && st->draft_width >= B, "literal_round_filtered: draft narrower than B");
+  const size_t need = dvs_filtered_round_workspace_bytes(m, st->S, B, st->max_pages, chunk_keys);
+  if (!workspace || ws_bytes < need) {
+    set_error("literal_round_filtered: workspace needs %zu bytes, got %zu", need, ws_bytes);
+    return DVS_EWORKSPACE;
+  }
+  StepLayout Ld, Lv;
+  const size_t extra = sampled_extra(m, st->S, B, st->max_pages, chunk_keys, &Ld, &Lv);
+  const RowParams par{temperature, top_k, top_p, min_p};
+  hipStream_t s = (hipStream_t)stream;
+  return m->dtype == DVS_BF16
+             ? run_round_filtered<__bf16>(m, st, B, par, u, chunk_keys, Ld, Lv, extra,
+                                          (char*)workspace, logits_out, accept_out, s)
+             : run_round_filtered<float>(m, st, B, par, u, chunk_keys, Ld, Lv, extra,
+                                         (char*)workspace, logits_out, accept_out, s);
 }

@@ -22,6 +22,7 @@ ERR_POOL_EXHAUSTED = 1
 ERR_MAX_PAGES = 2
 ERR_NONFINITE = 4
 ERR_BAD_PAGE = 8
+ERR_BAD_SLOT = 32
 
 _lib = None
 
@@ -117,6 +118,27 @@ _SIGS["dvs_prefill_workspace_bytes"] = ([ctypes.POINTER(DvsModel), _c_int, _c_in
                                          _c_int], _c_size)
 _SIGS["dvs_prefill"] = ([ctypes.POINTER(DvsModel), ctypes.POINTER(DvsState), _c_int, _c_int, _c_ptr,
                          _c_ptr, _c_int, _c_ptr, _c_ptr, _c_size, _c_ptr], _c_int)
+
+_c_long = ctypes.c_int64
+_SIGS["sample_filtered"] = ([_c_ptr, _c_int, _c_int, _c_int, _c_long, _c_ptr, _c_ptr, _c_ptr, _c_ptr,
+                             _c_int, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr], _c_int)
+_SIGS["dvs_accept_workspace_bytes"] = ([_c_int] * 3, _c_size)
+_SIGS["accept_sampled"] = ([_c_ptr, _c_long, _c_long, _c_ptr, _c_long, _c_long, _c_int, _c_int,
+                            _c_int, _c_int, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_int, _c_ptr,
+                            _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_size, _c_ptr], _c_int)
+_SIGS["dvs_filtered_round_workspace_bytes"] = _SIGS["dvs_sampled_round_workspace_bytes"]
+_SIGS["literal_round_filtered"] = ([ctypes.POINTER(DvsModel), ctypes.POINTER(DvsState), _c_int,
+                                    _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_int, _c_ptr, _c_ptr,
+                                    _c_ptr, _c_size, _c_ptr], _c_int)
+
+_SIGS["dvs_kv_workspace_bytes"] = ([_c_int, _c_int], _c_size)
+_SIGS["kv_fork"] = ([ctypes.POINTER(DvsState), _c_ptr, ctypes.POINTER(DvsLayer), _c_int, _c_int,
+                     _c_int, _c_int, _c_int, _c_ptr, _c_ptr, _c_int, _c_int, _c_ptr, _c_size,
+                     _c_ptr], _c_int)
+_SIGS["kv_release"] = ([ctypes.POINTER(DvsState), _c_ptr, _c_int, _c_ptr, _c_int, _c_ptr, _c_size,
+                        _c_ptr], _c_int)
+_SIGS["kv_compact"] = ([ctypes.POINTER(DvsState), _c_ptr, ctypes.POINTER(DvsLayer), _c_int, _c_int,
+                        _c_int, _c_int, _c_ptr, _c_ptr, _c_size, _c_ptr], _c_int)
 
 EXPORTED = tuple(_SIGS)
 
@@ -355,6 +377,129 @@ def top1_confidence(logits, argmax_out=None, conf_out=None, err=None, stream=Non
 
 
 # ---------------------------------------------------------------------------
+# sampling with filters
+# ---------------------------------------------------------------------------
+
+def _here(*tensors):
+    """Refuses tensors that are not on the current device, whose stream takes the call."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise DvsError(f"tensors must be on the current device {dev}, got {t.device}")
+
+
+def _filter_params(n, temperature, top_k, top_p, min_p):
+    """Device pointers of the sampling parameters, one entry per request."""
+    ptrs = []
+    for t, name, dt in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                        (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+        if t is not None:
+            _dev(t, dt, name, 1)
+            if n is None:
+                n = t.shape[0]
+            if t.shape[0] != n:
+                raise DvsError(f"{name} must have {n} entries, got {t.shape[0]}")
+            _here(t)
+        ptrs.append(_ptr(t))
+    return n, ptrs
+
+
+def _logit_rows(t, name, ndim=None):
+    """Checks logits whose rows are contiguous (they may lie apart)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise DvsError(f"{name} must be a CUDA (HIP) tensor")
+    if ndim is not None and t.dim() != ndim:
+        raise DvsError(f"{name} must have {ndim} dims, got {tuple(t.shape)}")
+    if t.dim() < 1 or t.shape[-1] < 1 or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise DvsError(f"{name} must have contiguous rows")
+    return _dtype_code(t)
+
+
+def sample_filtered(logits, u, temperature=None, top_k=None, top_p=None, min_p=None,
+                    token_out=None, prob_out=None, err=None, stream=None):
+    """logits [..., V] (f32/bf16; contiguous rows, evenly apart), u [...] f32 in [0, 1) ->
+    (token [...] int32, its probability [...] f32).  temperature, top_p, min_p (f32) and
+    top_k (int32) have one entry per group of rows (rows / entries rows each)."""
+    code = _logit_rows(logits, "logits")
+    lead, V = logits.shape[:-1], logits.shape[-1]
+    rows = logits.numel() // V
+    ld = V
+    if not logits.is_contiguous() and rows > 1:
+        if logits.dim() > 2:
+            raise DvsError("logits with rows apart must have 2 dims")
+        ld = logits.stride(0)
+        if ld < V:
+            raise DvsError("logits rows overlap")
+    _dev(u, torch.float32, "u")
+    if u.shape != lead:
+        raise DvsError(f"u must be {tuple(lead)}, got {tuple(u.shape)}")
+    n, par = _filter_params(None, temperature, top_k, top_p, min_p)
+    n = rows if n is None else n
+    if n < 1 or rows < 1 or rows % n:
+        raise DvsError(f"{rows} rows are no groups of {n} sampling parameters")
+    if token_out is None:
+        token_out = torch.empty(lead, dtype=torch.int32, device=logits.device)
+    if prob_out is None:
+        prob_out = torch.empty(lead, dtype=torch.float32, device=logits.device)
+    _dev(token_out, torch.int32, "token_out")
+    _dev(prob_out, torch.float32, "prob_out")
+    if token_out.numel() != rows or prob_out.numel() != rows:
+        raise DvsError("token_out / prob_out must have one entry per row")
+    _here(logits, u, token_out, prob_out, err)
+    if err is not None:
+        _dev(err, torch.int32, "err", 1)
+    rc = lib().sample_filtered(_ptr(logits), code, rows, V, ld, *par, rows // n, _ptr(u),
+                               _ptr(token_out), _ptr(prob_out), _ptr(err), _stream(stream))
+    _check(rc, "sample_filtered")
+    return token_out, prob_out
+
+
+def accept_workspace_bytes(S, B, V) -> int:
+    return int(lib().dvs_accept_workspace_bytes(S, B, V))
+
+
+def accept_sampled(z_verify, z_draft, draft, u, temperature=None, top_k=None, top_p=None,
+                   min_p=None, accept_len=None, token_out=None, err=None, workspace=None,
+                   stream=None):
+    """z_verify [S, B+1, V], z_draft [S, B, V] (f32/bf16; contiguous rows), draft [S, >= B]
+    int32, u [S, B+1] f32 -> (accept_len [S], final token [S]) int32.  Sampling parameters
+    have one entry per sequence."""
+    code = _logit_rows(z_verify, "z_verify", 3)
+    if _logit_rows(z_draft, "z_draft", 3) != code:
+        raise DvsError("z_verify and z_draft must have one dtype")
+    S, B, V = z_draft.shape
+    if tuple(z_verify.shape) != (S, B + 1, V):
+        raise DvsError("z_verify must be [S, B + 1, V] and z_draft [S, B, V]")
+    _dev(draft, torch.int32, "draft", 2)
+    _dev(u, torch.float32, "u", 2)
+    if draft.shape[0] != S or tuple(u.shape) != (S, B + 1):
+        raise DvsError("draft must have S rows and u must be [S, B + 1]")
+    _, par = _filter_params(S, temperature, top_k, top_p, min_p)
+    if accept_len is None:
+        accept_len = torch.empty((S,), dtype=torch.int32, device=z_verify.device)
+    if token_out is None:
+        token_out = torch.empty((S,), dtype=torch.int32, device=z_verify.device)
+    _dev(accept_len, torch.int32, "accept_len", 1)
+    _dev(token_out, torch.int32, "token_out", 1)
+    if accept_len.shape[0] != S or token_out.shape[0] != S:
+        raise DvsError("accept_len / token_out must have S entries")
+    _here(z_verify, z_draft, draft, u, accept_len, token_out, err)
+    if err is not None:
+        _dev(err, torch.int32, "err", 1)
+    if workspace is None:
+        workspace = Workspace(accept_workspace_bytes(S, B, V), device=z_verify.device)
+    # a sequence's only draft row has no next one to be apart from
+    draft_ld = z_draft.stride(1) if B > 1 else V
+    rc = lib().accept_sampled(_ptr(z_verify), z_verify.stride(0), z_verify.stride(1), _ptr(z_draft),
+                              z_draft.stride(0), draft_ld, code, S, B, V, *par,
+                              _ptr(draft), draft.shape[1], _ptr(u), _ptr(accept_len),
+                              _ptr(token_out), _ptr(err), _ptr(workspace.buf), workspace.nbytes,
+                              _stream(stream))
+    _check(rc, "accept_sampled")
+    return accept_len, token_out
+
+
+# ---------------------------------------------------------------------------
 # commit / rollback over a device-resident decode state
 # ---------------------------------------------------------------------------
 
@@ -380,10 +525,36 @@ class DeviceState:
             off += a.size
         self.pool_pages = int(host.pool_pages)
         self.max_pages = int(host.max_pages)
+        self._refs = [None]
+
+    @property
+    def page_refs(self):
+        """Holders of every page beyond the first (kv_fork); made when first used."""
+        if self._refs[0] is None:
+            self._refs[0] = torch.zeros(self.pool_pages, dtype=torch.int32, device=self.err.device)
+        return self._refs[0]
 
     def copy_from(self, other: "DeviceState"):
+        if self.flat is None or other.flat is None:
+            raise DvsError("copy_from needs whole states, not slots of one")
         self.flat.copy_(other.flat, non_blocking=True)
+        if other._refs[0] is not None:
+            self.page_refs.copy_(other.page_refs, non_blocking=True)
+        elif self._refs[0] is not None:
+            self._refs[0].zero_()
         return self
+
+    def slots(self, first: int, count: int) -> "DeviceState":
+        """Slots first .. first + count - 1 as a state over the same pool, free
+        stack and page counts (to prefill or step some of the sequences)."""
+        if not (0 <= first and 1 <= count and first + count <= self.kv_len.shape[0]):
+            raise DvsError("slots out of range")
+        v = object.__new__(DeviceState)
+        v.__dict__.update(self.__dict__, flat=None)
+        for f in self.FIELDS:
+            if f != "free_stack":
+                setattr(v, f, getattr(self, f)[first:first + count])
+        return v
 
     def to_host(self, host_like):
         h = host_like.copy()
@@ -748,6 +919,122 @@ def diffusion_block(model: DeviceModel, st: DeviceState, B: int, tau_c: float, b
                                _ptr(model.ws.buf), model.ws.nbytes, _stream(stream))
     _check(rc, "diffusion_block")
     return block, int(steps.value)
+
+
+def literal_round_filtered(model: DeviceModel, st: DeviceState, B: int, u, temperature=None,
+                           top_k=None, top_p=None, min_p=None,
+                           chunk_keys: int = MODEL_CHUNK_KEYS, eos_id: int = -1, logits_out=None,
+                           accept_out=None, stream=None):
+    """The two-forward round under sampling, every distribution cut by its
+    sequence's filters (one entry per sequence); u as literal_round_sampled."""
+    S = st.kv_len.shape[0]
+    _dev(u, torch.float32, "u", 2)
+    if tuple(u.shape) != (S, 2 * B + 2):
+        raise DvsError("u must be [S, 2B + 2]")
+    _, par = _filter_params(S, temperature, top_k, top_p, min_p)
+    need = int(lib().dvs_filtered_round_workspace_bytes(ctypes.byref(model.desc), S, int(B),
+                                                        st.max_pages, int(chunk_keys)))
+    if need == 0:
+        raise DvsError("literal_round_filtered: invalid configuration")
+    if model.ws is None or model.ws.nbytes < need:
+        model.ws = Workspace(need, device=st.kv_len.device)
+    if logits_out is not None:
+        _dev(logits_out, torch.float32, "logits_out")
+    if accept_out is not None:
+        _dev(accept_out, torch.int32, "accept_out", 1)
+    sd = _state_desc(st, eos_id)
+    rc = lib().literal_round_filtered(ctypes.byref(model.desc), ctypes.byref(sd), int(B), *par,
+                                      _ptr(u), int(chunk_keys), _ptr(logits_out), _ptr(accept_out),
+                                      _ptr(model.ws.buf), model.ws.nbytes, _stream(stream))
+    _check(rc, "literal_round_filtered")
+
+
+# ---------------------------------------------------------------------------
+# pages of sequences that are duplicated, dropped and moved together
+# ---------------------------------------------------------------------------
+
+class KVPools:
+    """The K and V pools of every layer (k [P,Hkv,16,D], v [P,Hkv,D,16]), as
+    kv_fork and kv_compact take them."""
+
+    def __init__(self, k_pools, v_pools):
+        if len(k_pools) != len(v_pools) or not len(k_pools):
+            raise DvsError("KVPools needs a K and a V pool per layer")
+        dt, shape = k_pools[0].dtype, tuple(k_pools[0].shape)
+        self.dtype = _dtype_code(k_pools[0])
+        self.layers = (DvsLayer * len(k_pools))()
+        for l, (k, v) in enumerate(zip(k_pools, v_pools)):
+            _dev(k, dt, "k_pool", 4)
+            _dev(v, dt, "v_pool", 4)
+            P, Hkv, _, D = shape
+            if tuple(k.shape) != (P, Hkv, 16, D) or tuple(v.shape) != (P, Hkv, D, 16):
+                raise DvsError("pools must be k [P,Hkv,16,D] and v [P,Hkv,D,16]")
+            self.layers[l].k_pool, self.layers[l].v_pool = k.data_ptr(), v.data_ptr()
+        self.pages, self.n_kv_heads, self.head_dim = shape[0], shape[1], shape[3]
+        self.keep = (list(k_pools), list(v_pools))
+
+
+def kv_workspace_bytes(S, num_pool_pages) -> int:
+    return int(lib().dvs_kv_workspace_bytes(S, num_pool_pages))
+
+
+def _kv_workspace(st, workspace):
+    if workspace is None:
+        workspace = Workspace(kv_workspace_bytes(st.kv_len.shape[0], st.pool_pages),
+                              device=st.kv_len.device)
+    return workspace
+
+
+def _check_pools(st, pools):
+    if pools.pages != st.pool_pages:
+        raise DvsError(f"the pools have {pools.pages} pages, the state's {st.pool_pages}")
+
+
+def kv_fork(st: DeviceState, pools: KVPools, src, dst, window: int, share: bool = True,
+            workspace=None, stream=None):
+    """Slot dst[i] becomes a copy of slot src[i] (int32), with pages for a window
+    of `window` rows; share: full pages are held by both, else copied."""
+    _check_pools(st, pools)
+    _dev(src, torch.int32, "src", 1)
+    _dev(dst, torch.int32, "dst", 1)
+    if src.shape != dst.shape:
+        raise DvsError("src and dst must have the same length")
+    _here(st.kv_len, src, dst)
+    workspace = _kv_workspace(st, workspace)
+    sd = _state_desc(st, -1)
+    rc = lib().kv_fork(ctypes.byref(sd), _ptr(st.page_refs), pools.layers, len(pools.layers),
+                       pools.n_kv_heads, pools.head_dim, pools.dtype, src.shape[0], _ptr(src),
+                       _ptr(dst), int(window), int(bool(share)), _ptr(workspace.buf),
+                       workspace.nbytes, _stream(stream))
+    _check(rc, "kv_fork")
+
+
+def kv_release(st: DeviceState, slots, window: int, workspace=None, stream=None):
+    """The slots (int32) become empty and keep pages for a window of `window` rows."""
+    _dev(slots, torch.int32, "slots", 1)
+    _here(st.kv_len, slots)
+    workspace = _kv_workspace(st, workspace)
+    sd = _state_desc(st, -1)
+    rc = lib().kv_release(ctypes.byref(sd), _ptr(st.page_refs), slots.shape[0], _ptr(slots),
+                          int(window), _ptr(workspace.buf), workspace.nbytes, _stream(stream))
+    _check(rc, "kv_release")
+
+
+def kv_compact(st: DeviceState, pools: KVPools, moved_out=None, workspace=None, stream=None):
+    """The pages in use move to the lowest ids, in every layer; returns the
+    number of moved pages (device int32 [1])."""
+    _check_pools(st, pools)
+    if moved_out is None:
+        moved_out = torch.empty(1, dtype=torch.int32, device=st.kv_len.device)
+    _dev(moved_out, torch.int32, "moved_out", 1)
+    _here(st.kv_len, moved_out)
+    workspace = _kv_workspace(st, workspace)
+    sd = _state_desc(st, -1)
+    rc = lib().kv_compact(ctypes.byref(sd), _ptr(st.page_refs), pools.layers, len(pools.layers),
+                          pools.n_kv_heads, pools.head_dim, pools.dtype, _ptr(moved_out),
+                          _ptr(workspace.buf), workspace.nbytes, _stream(stream))
+    _check(rc, "kv_compact")
+    return moved_out
 
 
 def prefill(model: DeviceModel, st: DeviceState, P: int, n_mask: int, prefix_tokens=None,

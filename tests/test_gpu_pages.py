@@ -1,0 +1,251 @@
+"""GPU: kv_fork, kv_release and kv_compact against the oracle (oracle/pages.py).
+
+Everything is whole numbers and moved bits: the whole integer state, the page
+counts and the pools' bits have to be equal, after every call of a random
+sequence of them; a refused call leaves all of it untouched."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages as op
+from paper_2609_26638_amd import dvs
+from tests.test_oracle_pages import make_state
+
+pytestmark = pytest.mark.gpu
+
+
+class Both:
+    """One cache on the host (oracle) and on the device."""
+
+    def __init__(self, seed, lens, window, layers=2, heads=2, D=64, dtype="bf16", **kw):
+        self.st, self.refs, _ = make_state(seed, lens, window, **kw)
+        rng = np.random.default_rng(seed + 1)
+        it = np.int16 if dtype == "bf16" else np.int32
+        P = self.st.pool_pages
+        # any bits: a copy is a copy, NaNs among them
+        draw = lambda *s: rng.integers(-30000, 30000, (P, heads) + s).astype(it)   # noqa: E731
+        self.pools = [draw(16, D) if i % 2 == 0 else draw(D, 16) for i in range(2 * layers)]
+        tt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.bits = [torch.from_numpy(a.copy()).cuda() for a in self.pools]
+        t = [b.view(tt) for b in self.bits]
+        self.handle = dvs.KVPools(t[0::2], t[1::2])
+        self.dev = dvs.DeviceState(self.st)
+
+    def same(self):
+        got = self.dev.to_host(self.st)
+        for f in dvs.DeviceState.FIELDS:
+            np.testing.assert_array_equal(getattr(got, f), getattr(self.st, f), err_msg=f)
+        assert got.free_top == self.st.free_top
+        np.testing.assert_array_equal(self.dev.page_refs.cpu().numpy(), self.refs)
+        for i, (a, b) in enumerate(zip(self.bits, self.pools)):
+            np.testing.assert_array_equal(a.cpu().numpy(), b, err_msg=f"pool {i}")
+
+    def fork(self, src, dst, window, share=True, err=0, **kw):
+        assert op.kv_fork(self.st, self.refs, self.pools, src, dst, window, share) == err
+        dvs.kv_fork(self.dev, self.handle, ids(src), ids(dst), window, share, **kw)
+        self.settle(err)
+
+    def release(self, slots, window, err=0, **kw):
+        assert op.kv_release(self.st, self.refs, slots, window) == err
+        dvs.kv_release(self.dev, ids(slots), window, **kw)
+        self.settle(err)
+
+    def compact(self, err=0, **kw):
+        want = op.kv_compact(self.st, self.refs, self.pools)
+        moved = dvs.kv_compact(self.dev, self.handle, **kw)
+        self.settle(err)
+        assert want == (err, int(moved.item()))
+
+    def settle(self, err):
+        torch.cuda.synchronize()
+        assert int(self.dev.err.item()) == err
+        self.dev.err.zero_()
+        self.same()
+
+
+def ids(a):
+    return torch.tensor(np.asarray(a, np.int32), device="cuda")
+
+
+@pytest.mark.parametrize("dtype,heads,D,layers", [("bf16", 2, 64, 2), ("f32", 1, 96, 3),
+                                                  ("bf16", 4, 128, 1), ("f32", 3, 5, 1)])
+@pytest.mark.parametrize("share", [True, False])
+def test_fork_layouts(dtype, heads, D, layers, share):
+    b = Both(1, [33, 0, 16, 5, 40, 1, 15], 9, layers, heads, D, dtype)
+    b.fork([0, 2, 0, 6], [4, 3, 5, 1], 9, share)
+    b.fork([5, 1], [0, 2], 25, share)        # forks of forks, a longer window
+    b.compact()
+
+
+@pytest.mark.parametrize("lens", [[0, 0], [1, 0], [15, 3], [16, 16], [17, 300], [4000, 1]])
+@pytest.mark.parametrize("window", [1, 16, 17, 64])
+def test_lengths_and_windows(lens, window):
+    b = Both(2, lens, window, extra=600)
+    b.fork([0], [1], window)
+    b.fork([1], [0], window, share=False)
+    b.release([0], window)
+    b.compact()
+    b.release([1, 0], window)
+    b.compact()
+
+
+def test_random_life_of_a_pool():
+    rng = np.random.default_rng(7)
+    S, W = 12, 7
+    b = Both(7, rng.integers(0, 200, S), W, extra=500)
+    ws = dvs.Workspace(dvs.kv_workspace_bytes(S, b.st.pool_pages))
+    ws.buf.fill_(0xA5)                        # needs no initialisation
+    for step in range(40):
+        kind = rng.integers(0, 4)
+        perm = rng.permutation(S)
+        if kind <= 1:
+            n = int(rng.integers(1, S))
+            b.fork(rng.choice(perm[n:], n), perm[:n], W, bool(rng.integers(0, 2)), workspace=ws)
+        elif kind == 2:
+            b.release(perm[:int(rng.integers(1, 4))], W, workspace=ws)
+        else:
+            b.compact(workspace=ws)
+
+
+def test_many_slots_and_a_large_pool():
+    """1024 slots, and more pages than one bitmap word per thread."""
+    rng = np.random.default_rng(3)
+    lens = np.zeros(1024, np.int64)
+    lens[:40] = rng.integers(500, 3000, 40)
+    b = Both(3, lens, 5, layers=1, heads=1, D=16, extra=40000, max_new=3, draft=2)
+    b.fork(np.arange(984) % 40, np.arange(40, 1024), 5)
+    b.release(rng.permutation(1024)[:700], 5)
+    b.compact()
+    b.fork([int(np.argmax(b.st.kv_len))], [int(np.argmin(b.st.kv_len))], 5, share=False)
+
+
+def test_many_layers():
+    b = Both(4, [40, 3, 0], 4, layers=70, heads=1, D=8)
+    b.fork([0, 0], [1, 2], 4)
+    b.release([0], 4)
+    b.compact()
+
+
+def test_errors_change_nothing():
+    b = Both(5, [100, 3, 3, 50], 4, extra=2)
+    b.fork([0], [1], 4)
+    b.fork([0, 0], [1, 1], 4, err=op.ERR_BAD_SLOT)
+    b.fork([0, 1], [1, 2], 4, err=op.ERR_BAD_SLOT)
+    b.fork([2], [2], 4, err=op.ERR_BAD_SLOT)
+    b.fork([4], [1], 4, err=op.ERR_BAD_SLOT)
+    b.fork([0], [-1], 4, err=op.ERR_BAD_SLOT)
+    b.release([0, 0], 4, err=op.ERR_BAD_SLOT)
+    b.release([4], 4, err=op.ERR_BAD_SLOT)
+    b.fork([0], [2], 5000, err=op.ERR_MAX_PAGES)
+    # shared pages are dropped, found missing for the fork, and come back
+    b.fork([3, 3], [1, 2], 4, share=False, err=op.ERR_POOL_EXHAUSTED)
+    b.fork([3], [2], 4)
+
+
+def test_bad_page_ids_change_nothing():
+    b = Both(6, [60, 20, 3], 4)
+    table = b.dev.page_table.clone()
+    for s, j, p in ((1, 0, -1), (1, 1, b.st.pool_pages), (0, 2, 1 << 30)):
+        b.dev.page_table[s, j] = p
+        before = b.dev.flat.clone()
+        bits = [x.clone() for x in b.bits]
+        dvs.kv_fork(b.dev, b.handle, ids([0]), ids([1]), 4)
+        if s == 1:
+            dvs.kv_release(b.dev, ids([1]), 4)
+        dvs.kv_compact(b.dev, b.handle)
+        torch.cuda.synchronize()
+        assert int(b.dev.err.item()) == op.ERR_BAD_PAGE
+        b.dev.err.zero_()
+        assert torch.equal(b.dev.flat, before) and int(b.dev.page_refs.abs().sum()) == 0
+        assert all(torch.equal(x, y) for x, y in zip(b.bits, bits))
+        b.dev.page_table.copy_(table)
+    # a page that no table holds, and one that is held and free
+    b.dev.free_top -= 1
+    dvs.kv_compact(b.dev, b.handle)
+    assert int(b.dev.err.item()) == op.ERR_BAD_PAGE
+    b.dev.err.zero_()
+    b.dev.free_top += 1
+    keep = int(b.dev.free_stack[0])
+    b.dev.free_stack[0] = int(b.st.page_table[0, 0])
+    dvs.kv_compact(b.dev, b.handle)
+    assert int(b.dev.err.item()) == op.ERR_BAD_PAGE
+    b.dev.err.zero_()
+    b.dev.free_stack[0] = keep
+    b.same()
+
+
+def test_views_of_slots():
+    """Some of the sequences as a state of their own: releases and forks see
+    the same pool; a compaction that would miss the others is refused."""
+    b = Both(8, [30, 40, 7, 0], 4)
+    v = b.dev.slots(1, 3)
+    assert op.kv_fork(b.st, b.refs, b.pools, [1], [3], 4) == 0
+    dvs.kv_fork(v, b.handle, ids([0]), ids([2]), 4)
+    b.settle(0)
+    dvs.kv_compact(v, b.handle)
+    assert int(b.dev.err.item()) == op.ERR_BAD_PAGE
+    b.dev.err.zero_()
+    b.same()
+    for bad in ((-1, 2), (2, 3), (0, 0)):
+        with pytest.raises(dvs.DvsError):
+            b.dev.slots(*bad)
+    with pytest.raises(dvs.DvsError):
+        v.copy_from(b.dev)
+
+
+def test_copy_from_restores_counts():
+    b = Both(9, [50, 0, 0], 4)
+    before = dvs.DeviceState(b.st)
+    st, refs = b.st.copy(), b.refs.copy()
+    b.fork([0, 0], [1, 2], 4)
+    assert int(b.dev.page_refs.sum()) == 6
+    b.dev.copy_from(before)
+    b.st, b.refs = st, refs
+    b.same()
+
+
+def test_capture_and_replay():
+    """Fork, release and compaction in one graph; every replay against the
+    same calls on the host, with eager work between."""
+    b = Both(10, [70, 10, 0, 33], 6, extra=60)
+    ws = dvs.Workspace(dvs.kv_workspace_bytes(4, b.st.pool_pages))
+    moved = torch.zeros(1, dtype=torch.int32, device="cuda")
+    src, dst, gone = ids([0, 0]), ids([1, 2]), ids([1])
+
+    def step():
+        dvs.kv_fork(b.dev, b.handle, src, dst, 6, workspace=ws)
+        dvs.kv_release(b.dev, gone, 6, workspace=ws)
+        dvs.kv_compact(b.dev, b.handle, moved_out=moved, workspace=ws)
+
+    def host():
+        assert op.kv_fork(b.st, b.refs, b.pools, src.tolist(), dst.tolist(), 6) == 0
+        assert op.kv_release(b.st, b.refs, gone.tolist(), 6) == 0
+        assert op.kv_compact(b.st, b.refs, b.pools)[0] == 0
+
+    step()
+    host()
+    b.settle(0)
+    g = dvs.capture(step)
+    for i in range(4):
+        src.fill_(3 if i % 2 else 0)
+        g.replay()
+        host()
+        torch.randn(1 << 20, device="cuda").sum().item()
+        b.settle(0)
+
+
+def test_binding_refusals():
+    b = Both(11, [5, 5], 4)
+    other = Both(12, [50, 5], 4)
+    for bad in (lambda: dvs.kv_fork(b.dev, other.handle, ids([0]), ids([1]), 4),
+                lambda: dvs.kv_fork(b.dev, b.handle, ids([0]), ids([1, 0]), 4),
+                lambda: dvs.kv_fork(b.dev, b.handle, ids([0]).long(), ids([1]), 4),
+                lambda: dvs.kv_fork(b.dev, b.handle, ids([0, 1]), ids([1, 0]), 4),
+                lambda: dvs.kv_release(b.dev, ids([0]), 0),
+                lambda: dvs.kv_release(b.dev, ids([0, 1, 0]), 4),
+                lambda: dvs.kv_compact(b.dev, other.handle),
+                lambda: dvs.KVPools([torch.zeros(4, 2, 16, 64, device="cuda")],
+                                    [torch.zeros(4, 2, 16, 64, device="cuda")])):
+        with pytest.raises(dvs.DvsError):
+            bad()
+    b.same()
