@@ -12,27 +12,30 @@
 // hundred.  64-bit adds and multiplies run at the 32-bit rate on this chip.
 //
 // One workgroup of 1024 threads per row.  Wave w owns one contiguous range of
-// the row, so the ranges' sums are in index order; a row of up to 65536
-// logits is read once and stays in registers.
-//   1. maximum and minimum;
-//   2. a logit that no kept token lies below, and the tokens from there up as
-//      a list in LDS: by the threads' own maxima for top-k (count_bound), by
-//      the whole weight for top-p;
-//   3. up to RANK candidates (a longer list is shortened by one histogram) are
-//      ranked against each other, which gives the cut, the kept weight and the
-//      draw at once (rank_cut);
-//   4. otherwise (a flat distribution, a large k, many equal logits) a
-//      histogram with a count and a weight sum per bin is narrowed to the bin
-//      that holds the k-th token or the share p of the weight, until few
-//      tokens are left (select_cut), over the list or over the row;
-//   5. without a cut, or after 4: the kept weight per range, the range that
-//      holds u * total, and one scan over that range's tokens (draw_kept).
-// The row's registers are dead after step 2, or after the sums of step 5
-// without a cut; what follows is kept out of line and reads the row again
-// where it needs it, so that the registers of both are never live at once.
+// the row, so the ranges' sums are in index order.
+//   1. one pass: the maximum; where the whole weight is needed, it too, each
+//      thread's sum relative to its own running maximum; and each thread's
+//      maxima over PARTS parts of its logits;
+//   2. a logit that no kept token lies below: the parts' maxima are tokens, so
+//      where their count reaches k, or their weight the share p, all of the cut
+//      is above (parts_bound);
+//   3. a second pass: the tokens from there up, as a list in LDS;
+//   4. up to SMALL of them (a longer list is first cut short by a histogram)
+//      are ranked against each other, which gives the cut, the kept weight and
+//      the draw at once (filter_small).
+// Longer lists (filter_list), and rows whose candidates do not fit the list
+// (filter_row_again: a flat distribution, a large k, many equal logits), take
+// histograms with a count and a weight sum per bin, narrowed to the tokens of
+// one wave (select_cut), and draw by the kept weight per index or range.
+//
+// A pass is a rolled loop that reads the row again, from L2 mostly: code that is
+// run once per launch is bound by fetching its instructions (16 KB of unrolled
+// passes over a row held in registers took 16,000 cycles for what the loop does
+// in 10,000), so the rest is kept small, and out of line where it is rare.
 // Weights that atomics or an unordered list add up are fixed-point integers,
 // whose sums do not depend on the order; the other sums have a fixed order.
 // Results do not depend on timing, nor on the other rows of the call.
+#include <float.h>
 #include <math.h>
 
 #include "dvs_common.h"
@@ -42,7 +45,9 @@ namespace dvs {
 constexpr int FT = 1024;          // threads of a row's workgroup
 constexpr int FW = FT / 64;
 constexpr int BINS = 1024;        // one histogram bin per thread
-constexpr int RANK = 512;         // tokens that are ranked against each other
+constexpr int RANK = 64;          // tokens that one wave ranks
+constexpr int SMALL = 256;        // tokens that the workgroup ranks
+constexpr int PARTS = 4;          // parts of a thread's logits
 constexpr int LIST = 8192;        // candidates held in LDS (64 KB)
 
 // What a row's filters keep: weight >= min_w of the tokens with z > cut.z, or
@@ -53,6 +58,7 @@ struct RowCut {
   float min_w;       // min_p
   double log2e_t;    // log2(e) / T
   double total;      // kept weight
+  double inv_total;  // 1 / total (accept_sampled)
   int single;        // 1: only token idx is kept (weight 1); -1: no token
 };
 
@@ -64,7 +70,8 @@ struct FilterShared {
   double d[FW];
   unsigned long long u[FW];
   uint32_t c[FW];
-  float f[FW], g[FW];
+  float f[FW];
+  int i[FW];
   int pick[2];
   int found, n, token;
   uint32_t fc;
@@ -133,6 +140,15 @@ __device__ __forceinline__ u32x4 load_vec(const float* p) { return *(const u32x4
 __device__ __forceinline__ u32x4 load_vec(const uint16_t* p) { return *(const u32x4_b16*)p; }
 
 template <typename E>
+__device__ __forceinline__ float vec_elem(const u32x4& x, int e);
+template <typename E>
+__device__ __forceinline__ float vec_max(const u32x4& x) {
+  float m = vec_elem<E>(x, 0);
+#pragma unroll
+  for (int e = 1; e < 16 / (int)sizeof(E); ++e) m = fmaxf(m, vec_elem<E>(x, e));
+  return m;
+}
+template <typename E>
 __device__ __forceinline__ float vec_elem(const u32x4& x, int e) {
   if constexpr (sizeof(E) == 2)
     return __uint_as_float((e & 1) ? (x[e >> 1] & 0xffff0000u) : (x[e >> 1] << 16));
@@ -140,59 +156,55 @@ __device__ __forceinline__ float vec_elem(const u32x4& x, int e) {
     return __uint_as_float(x[e]);
 }
 
-// A row of V logits, in 16-byte vectors: wave w holds the nit * 64 vectors of
-// its range, lane by lane.  NV > 0: they stay in registers (nit <= NV);
-// NV = 0: every pass reads them again, four in flight.  Past the row's end
-// the logits are -inf.
-template <typename E, int NV>
+typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
+
+// A row of V logits: 16-byte vectors, wave w with the nit * 64 vectors of its
+// range lane by lane, and the V % EPV last logits with the last wave.  A pass
+// has PARTS vectors in flight; absent ones are -inf.
+template <typename E>
 struct Row {
   static constexpr int EPV = 16 / sizeof(E);
   const E* p;
   int V, nit, base;
-  u32x4 v[NV > 0 ? NV : 1];
 
   __device__ __forceinline__ Row(const E* p_, int V_, int nit_) : p(p_), V(V_), nit(nit_) {
     base = ((threadIdx.x >> 6) * nit * 64 + (threadIdx.x & 63)) * EPV;
-    if constexpr (NV > 0) {
-#pragma unroll
-      for (int it = 0; it < NV; ++it)
-        if (it < nit) v[it] = read(it);
-    }
   }
-  __device__ __forceinline__ int at(int it) const { return base + it * 64 * EPV; }
   __device__ __forceinline__ u32x4 read(int it) const {
-    const int i = at(it);
-    if (i + EPV <= V) return load_vec(p + i);
-    u32x4 x;
-    if constexpr (sizeof(E) == 2) {
-      uint32_t b[EPV];
-#pragma unroll
-      for (int e = 0; e < EPV; ++e) b[e] = i + e < V ? (uint32_t)p[i + e] : 0xff80u;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = b[2 * k] | (b[2 * k + 1] << 16);
-    } else {
-#pragma unroll
-      for (int e = 0; e < EPV; ++e) x[e] = i + e < V ? __float_as_uint(p[i + e]) : 0xff800000u;
-    }
+    const uint32_t none = sizeof(E) == 2 ? 0xff80ff80u : 0xff800000u;
+    const int i = base + it * 64 * EPV;
+    u32x4 x = {none, none, none, none};
+    if (it < nit && i + EPV <= V) x = load_vec(p + i);
     return x;
+  }
+  // a batch of PARTS vectors
+  __device__ __forceinline__ u32x16 batch(int it) const {
+    u32x16 b;
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      const u32x4 x = read(it + k);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) b[4 * k + d] = x[d];
+    }
+    return b;
+  }
+  // vector k of a batch (k uniform: indexed registers)
+  __device__ __forceinline__ static u32x4 vec(const u32x16& b, int k) {
+    return u32x4{b[4 * k], b[4 * k + 1], b[4 * k + 2], b[4 * k + 3]};
+  }
+  // The logit behind the last vector that this thread has, or -inf.
+  __device__ __forceinline__ int rest_index() const {
+    const int i = V / EPV * EPV + (int)threadIdx.x - (FT - 64);
+    return (int)threadIdx.x >= FT - 64 && i < V ? i : -1;
   }
   // f(vector, index of its first logit)
   template <typename F>
   __device__ __forceinline__ void vectors(F f) const {
-    if constexpr (NV > 0) {
-#pragma unroll
-      for (int it = 0; it < NV; ++it)
-        if (it < nit) f(v[it], at(it));
-    } else {
-      for (int it = 0; it < nit; it += 4) {
-        u32x4 b[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (it + k < nit) b[k] = read(it + k);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (it + k < nit) f(b[k], at(it + k));
-      }
+#pragma unroll 1
+    for (int it = 0; it < nit; it += PARTS) {
+      const u32x16 b = batch(it);
+#pragma unroll 1
+      for (int k = 0; k < min(PARTS, nit - it); ++k) f(vec(b, k), base + (it + k) * 64 * EPV);
     }
   }
   template <typename F>
@@ -201,29 +213,30 @@ struct Row {
 #pragma unroll
       for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), i + e);
     });
+    const int i = rest_index();
+    if (i >= 0) f(load_logit(p + i), i);
   }
   // f(z, index) where some lane's vector reaches zlo; f decides by itself
   template <typename F>
   __device__ __forceinline__ void each_from(float zlo, F f) const {
     vectors([&](const u32x4& x, int i) {
-      float m = vec_elem<E>(x, 0);
-#pragma unroll
-      for (int e = 1; e < EPV; ++e) m = fmaxf(m, vec_elem<E>(x, e));
-      if (__ballot(m >= zlo)) {
+      if (__ballot(vec_max<E>(x) >= zlo)) {
 #pragma unroll
         for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), i + e);
       }
     });
+    const int i = rest_index();
+    if (i >= 0) f(load_logit(p + i), i);
   }
-  __device__ __forceinline__ Row<E, 0> streamed() const { return Row<E, 0>(p, V, nit); }
 };
 
-// The candidates in LDS.
-struct Candidates {
+// The n candidates in LDS.
+struct List {
   int n;
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
     const FilterShared& sh = shared();
+#pragma unroll 1
     for (int i = threadIdx.x; i < n; i += FT) f(sh.lz[i], sh.li[i]);
   }
 };
@@ -232,55 +245,106 @@ struct Candidates {
 // over the workgroup
 // ---------------------------------------------------------------------------
 
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+// A value that every thread of the workgroup has, in scalar registers: what
+// branches on it is then no divergent branch, whose both sides would keep
+// their registers.
+__device__ __forceinline__ float uniform(float v) {
+  return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ double uniform(double v) {
+  return __hiloint2double(uniform(__double2hiint(v)), uniform(__double2loint(v)));
+}
+
+// v of the lane that CTRL names in this lane's row of 16 (or a row's last lane
+// for the broadcasts), `old` where there is none: one vector move, where a
+// general shuffle takes a round trip through LDS.
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T dpp(T old, T v) {
+  if constexpr (sizeof(T) == 4) {
+    const int r = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old),
+                                              __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(T, r);
+  } else {
+    const unsigned long long o = __builtin_bit_cast(unsigned long long, old);
+    const unsigned long long x = __builtin_bit_cast(unsigned long long, v);
+    const uint32_t lo = dpp<CTRL, ROWS>((uint32_t)o, (uint32_t)x);
+    const uint32_t hi = dpp<CTRL, ROWS>((uint32_t)(o >> 32), (uint32_t)(x >> 32));
+    return __builtin_bit_cast(T, ((unsigned long long)hi << 32) | lo);
+  }
+}
+template <typename T>
+__device__ __forceinline__ T at_lane(T v, int lane) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+  } else {
+    const unsigned long long x = __builtin_bit_cast(unsigned long long, v);
+    const uint32_t lo = at_lane((uint32_t)x, lane), hi = at_lane((uint32_t)(x >> 32), lane);
+    return __builtin_bit_cast(T, ((unsigned long long)hi << 32) | lo);
+  }
+}
+struct Add {
+  template <typename T>
+  __device__ __forceinline__ T operator()(T a, T b) const { return a + b; }
+};
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+  __device__ __forceinline__ int operator()(int a, int b) const { return max(a, b); }
+};
+struct Min {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); }
+  __device__ __forceinline__ int operator()(int a, int b) const { return min(a, b); }
+};
+// Inclusive scan over each row of 16 lanes, and over the wave.  none: op's
+// neutral value.
+template <typename T, typename Op>
+__device__ __forceinline__ T row_scan(T v, T none, Op op) {
+  v = op(dpp<0x111, 0xf>(none, v), v);         // row_shr:1, 2, 4, 8
+  v = op(dpp<0x112, 0xf>(none, v), v);
+  v = op(dpp<0x114, 0xf>(none, v), v);
+  v = op(dpp<0x118, 0xf>(none, v), v);
+  return v;
+}
+template <typename T, typename Op>
+__device__ __forceinline__ T wave_scan(T v, T none, Op op) {
+  v = row_scan(v, none, op);
+  v = op(dpp<0x142, 0xa>(none, v), v);         // row_bcast:15 into rows 1 and 3
+  v = op(dpp<0x143, 0xc>(none, v), v);         // row_bcast:31 into rows 2 and 3
   return v;
 }
 
-__device__ __forceinline__ void block_min_max(float& lo, float& hi) {
-  FilterShared& sh = shared();
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    lo = fminf(lo, __shfl_xor(lo, off));
-    hi = fmaxf(hi, __shfl_xor(hi, off));
-  }
-  if (lane == 0) { sh.f[wv] = lo; sh.g[wv] = hi; }
+// v over the workgroup, in scalar registers; buf: FW values in LDS.
+template <typename T, typename Op>
+__device__ __forceinline__ T block_reduce(T v, T none, Op op, T* buf) {
+  const int lane = threadIdx.x & 63, wv = uniform((int)threadIdx.x >> 6);
+  v = wave_scan(v, none, op);
+  if (lane == 63) buf[wv] = v;
   __syncthreads();
-  for (int i = 0; i < FW; ++i) { lo = fminf(lo, sh.f[i]); hi = fmaxf(hi, sh.g[i]); }
+  v = row_scan(lane < FW ? buf[lane] : none, none, op);
   __syncthreads();
+  return at_lane(v, FW - 1);
 }
 
 // Inclusive scan over the workgroup of (count, mass), in thread order.
 __device__ __forceinline__ void scan_bins(uint32_t& c, unsigned long long& m) {
   FilterShared& sh = shared();
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint32_t oc = __shfl_up(c, off);
-    const unsigned long long om = __shfl_up(m, off);
-    if (lane >= off) { c += oc; m += om; }
-  }
-  if (lane == 63) { sh.c[w] = c; sh.u[w] = m; }
+  const int lane = threadIdx.x & 63, wv = uniform((int)threadIdx.x >> 6);
+  c = wave_scan(c, 0u, Add());
+  m = wave_scan(m, 0ull, Add());
+  if (lane == 63) { sh.c[wv] = c; sh.u[wv] = m; }
   __syncthreads();
-  uint32_t bc = 0;
-  unsigned long long bm = 0;
-  for (int i = 0; i < w; ++i) { bc += sh.c[i]; bm += sh.u[i]; }
-  c += bc;
-  m += bm;
+  const uint32_t bc = row_scan(lane < FW ? sh.c[lane] : 0u, 0u, Add());
+  const unsigned long long bm = row_scan(lane < FW ? sh.u[lane] : 0ull, 0ull, Add());
+  if (wv) {
+    c += at_lane(bc, wv - 1);
+    m += at_lane(bm, wv - 1);
+  }
   __syncthreads();
 }
 
 // Smallest index of a thread for which `yes` holds, `none` without one.
 __device__ __forceinline__ int first_index(bool yes, int i, int none) {
-  FilterShared& sh = shared();
-  if (threadIdx.x == 0) sh.found = 0x7fffffff;
-  __syncthreads();
-  if (yes) atomicMin(&sh.found, i);
-  __syncthreads();
-  const int got = sh.found;
-  __syncthreads();
+  const int got = block_reduce(yes ? i : 0x7fffffff, 0x7fffffff, Min(), shared().i);
   return got == 0x7fffffff ? none : got;
 }
 
@@ -288,86 +352,64 @@ __device__ __forceinline__ int first_index(bool yes, int i, int none) {
 // wave's range sum in sh.d; the last index of positive weight when rounding
 // (or u = 1) puts t past the sum; -1 when every weight is zero.  fn(z, i) is
 // the weight of token i.
-template <typename E, int NV, typename F>
-__device__ int pick_index(const Row<E, NV>& row, F fn, double t) {
+template <typename E, typename F>
+__device__ __forceinline__ int pick_index(const Row<E>& row, F fn, double t) {
   FilterShared& sh = shared();
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  int w = -1, last = -1;
-  double excl = 0.0, run = 0.0;
-  for (int i = 0; i < FW; ++i) {
-    const double s = sh.d[i];
-    if (s > 0.0) {
-      last = i;
-      if (w < 0 && run + s > t) { w = i; excl = run; }
-      if (w < 0) run += s;
-    }
-  }
-  if (last < 0) return -1;
-  if (w < 0) { w = last; t = INFINITY; }
-  // the range's vectors, one per thread and nit / FW more
-  constexpr int EPV = Row<E, NV>::EPV;
-  const int span = row.nit * 64 * EPV, lo = w * span, hi = min(row.V, lo + span);
-  const int per = (row.nit + FW - 1) / FW * EPV;
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
+  const double own = lane < FW ? sh.d[lane] : 0.0;
+  const double runs = row_scan(own, 0.0, Add());
+  const unsigned long long some = __ballot(own > 0.0);
+  if (!some) return -1;
+  const unsigned long long over = __ballot(own > 0.0 && runs > t);
+  const int w = over ? __ffsll((long long)over) - 1 : 63 - __clzll((long long)some);
+  const double excl = w ? at_lane(runs, w - 1) : 0.0;
+  if (!over) t = INFINITY;
+  // the range's tokens in whole vectors per thread
+  constexpr int EPV = Row<E>::EPV;
+  const int span = row.nit * 64 * EPV, lo = min(w * span, row.V / EPV * EPV);
+  const int hi = w == FW - 1 ? row.V : min(row.V / EPV * EPV, lo + span);
+  const int per = ((hi - lo + FT - 1) / FT + EPV - 1) / EPV * EPV;
   const int first = lo + tid * per;
   double part = 0.0;
   int lastpos = -1;
   auto walk = [&](auto&& f) {            // this thread's tokens, in index order
-    for (int i0 = first; i0 < min(hi, first + per); i0 += EPV) {
-      float z[EPV];
-#pragma unroll
-      for (int e = 0; e < EPV; ++e) z[e] = i0 + e < hi ? load_logit(row.p + i0 + e) : -INFINITY;
-#pragma unroll
-      for (int e = 0; e < EPV; ++e)
-        if (i0 + e < hi && f(fn(z[e], i0 + e), i0 + e)) return;
-    }
+#pragma unroll 4
+    for (int i = first; i < min(hi, first + per); ++i) f(fn(load_logit(row.p + i), i), i);
   };
   walk([&](double x, int i) {
     part += x;
     if (x > 0.0) lastpos = i;
-    return false;
   });
-  double incl = part;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const double o = __shfl_up(incl, off);
-    if (lane >= off) incl += o;
-  }
-  double before = __shfl_up(incl, 1);
-  if (lane == 0) before = 0.0;
+  const double incl = wave_scan(part, 0.0, Add());
+  const double before = dpp<0x138, 0xf>(0.0, incl);   // the lane before's
   __syncthreads();                       // sh.d has been read by every thread
   if (lane == 63) sh.d[wv] = incl;
-  if (tid == 0) { sh.pick[0] = 0x7fffffff; sh.pick[1] = -1; }
   __syncthreads();
+  const double waves = row_scan(lane < FW ? sh.d[lane] : 0.0, 0.0, Add());
   double base = excl;
-  for (int i = 0; i < wv; ++i) base += sh.d[i];
+  if (wv) base += at_lane(waves, wv - 1);
+  int at = 0x7fffffff;
   if (part > 0.0 && base + incl > t) {   // the first such thread holds the token
     double acc = base + before;
-    int at = lastpos;
+    at = lastpos;
     walk([&](double x, int i) {
       acc += x;
-      if (acc > t) at = i;
-      return acc > t;
+      if (acc > t) at = min(at, i);
     });
-    atomicMin(&sh.pick[0], at);
   }
-  if (lastpos >= 0) atomicMax(&sh.pick[1], lastpos);
-  __syncthreads();
-  const int got = sh.pick[0] != 0x7fffffff ? sh.pick[0] : sh.pick[1];
-  __syncthreads();
-  return got;
+  at = first_index(at != 0x7fffffff, at, -1);
+  return at >= 0 ? at : block_reduce(lastpos, -1, Max(), sh.i);
 }
 
 // Every wave's range sum to sh.d; returns their sum, in order.
 __device__ __forceinline__ double range_sums(double part) {
   FilterShared& sh = shared();
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  part = wave_sum(part);
+  const int lane = threadIdx.x & 63, wv = uniform((int)threadIdx.x >> 6);
+  part = wave_scan(part, 0.0, Add());
   __syncthreads();
-  if (lane == 0) sh.d[wv] = part;
+  if (lane == 63) sh.d[wv] = part;
   __syncthreads();
-  double total = 0.0;
-  for (int i = 0; i < FW; ++i) total += sh.d[i];
-  return total;
+  return at_lane(row_scan(lane < FW ? sh.d[lane] : 0.0, 0.0, Add()), FW - 1);
 }
 
 // ---------------------------------------------------------------------------
@@ -402,22 +444,46 @@ struct Binning {
     if (linear) return (int)fminf((half - z * 0.5f) * sc, (float)(BINS - 1));
     return (int)((khi - order_key(z)) >> shift);
   }
+  // a logit that none of the bins up to b lies below
+  __device__ __forceinline__ float lower_edge(int b) const {
+    if (linear) {
+      const double edge = 2.0 * ((double)half - (b + 1) / (double)sc);
+      return (float)fmax(edge - 1e-6 * (fabs(edge) + 2.0 * fabs((double)half)), -(double)FLT_MAX);
+    }
+    const unsigned long long down = ((unsigned long long)(b + 1) << shift) - 1;
+    const uint32_t key = down < khi ? khi - (uint32_t)down : 0u;
+    return fmaxf(__uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key), -FLT_MAX);
+  }
 };
 
 // The last token kept when the tokens of `src` with zlo <= z <= zhi (n of
 // them, in order) are kept up to the k-th (by_mass false), or up to the first
 // at which the weight reaches `target` (by_mass true; the last one if none
-// does).  Weights are summed only when `masses` is set.
+// does).  Weights are summed only when `masses` is set.  `row`: where equal
+// logits are counted in index order.
 template <typename Src, typename E>
-__device__ Cut select_cut(const Src& src, const Row<E, 0>& row, const RowCut& rc, double scale,
-                          int n, float zhi, float zlo, bool by_mass, bool masses, uint32_t k,
-                          double target) {
+__device__ __forceinline__ Cut select_cut(const Src& src, const Row<E>& row, const RowCut& rc,
+                                          double scale, int n, float zhi, float zlo, bool by_mass,
+                                          bool masses, uint32_t k, double target) {
   FilterShared& sh = shared();
   const int tid = threadIdx.x;
   uint32_t above_c = 0;
   unsigned long long above_m = 0;
-  for (int level = 0; n > RANK && zlo < zhi; ++level) {
-    const Binning bin(zhi, zlo, level == 0);
+  int at_bin = -1;                       // the bin looked at; -1: all of [zlo, zhi]
+  Binning bin(zhi, zlo, true);
+  auto in = [&](float z) { return z <= zhi && z >= zlo && (at_bin < 0 || bin(z) == at_bin); };
+  for (int level = 0; n > RANK; ++level) {
+    if (at_bin >= 0) {
+      float lo = INFINITY, hi = -INFINITY;
+      src.each([&](float z, int) {
+        if (in(z)) { lo = fminf(lo, z); hi = fmaxf(hi, z); }
+      });
+      zlo = block_reduce(lo, INFINITY, Min(), sh.f);
+      zhi = block_reduce(hi, -INFINITY, Max(), sh.f);
+      at_bin = -1;
+    }
+    if (zlo == zhi) break;
+    bin = Binning(zhi, zlo, level == 0);
     sh.cnt[tid] = 0;
     sh.mass[tid] = 0;
     __syncthreads();
@@ -439,16 +505,10 @@ __device__ Cut select_cut(const Src& src, const Row<E, 0>& row, const RowCut& rc
     if (b < 0) b = BINS - 1 - first_index(own_c > 0, BINS - 1 - tid, 0);   // the last bin
     if (tid == b) { sh.n = (int)own_c; sh.fc = c - own_c; sh.fm = m - own_m; }
     __syncthreads();
-    n = sh.n;
+    n = uniform(sh.n);
     above_c += sh.fc;
     above_m += sh.fm;
-    float lo = INFINITY, hi = -INFINITY;
-    src.each([&](float z, int) {
-      if (z <= zhi && z >= zlo && bin(z) == b) { lo = fminf(lo, z); hi = fmaxf(hi, z); }
-    });
-    block_min_max(lo, hi);
-    zlo = lo;
-    zhi = hi;
+    at_bin = b;
   }
   Cut cut;
   if (n > RANK) {                        // equal logits: in index order
@@ -468,42 +528,41 @@ __device__ Cut select_cut(const Src& src, const Row<E, 0>& row, const RowCut& rc
     cut.mass = above_m + w * (unsigned long long)keep;
     return cut;
   }
-  // rank what is left (at most RANK tokens), in the histogram's memory
+  // what is left, gathered in the histogram's memory and ranked by one wave
   float* lz = (float*)sh.cnt;
   int* li = (int*)sh.cnt + RANK;
   if (tid == 0) sh.n = 0;
   __syncthreads();
   src.each([&](float z, int i) {
-    if (z <= zhi && z >= zlo) {
+    if (in(z)) {
       const int at = atomicAdd(&sh.n, 1);
       if (at < RANK) { lz[at] = z; li[at] = i; }
     }
   });
   __syncthreads();
-  n = min(sh.n, RANK);
-  float z = 0.f;
-  int idx = 0, rank = 0;
-  if (tid < n) {
-    z = lz[tid];
-    idx = li[tid];
+  if (tid < 64) {
+    const bool any = tid < n;
+    const float z = any ? lz[tid] : 0.0f;
+    const int idx = any ? li[tid] : 0;
+    const unsigned long long own = any && masses ? fixed_weight(z, rc, scale) : 0;
+    const unsigned long long key =
+        any ? ((unsigned long long)order_key(z) << 32) | (uint32_t)~idx : 0ull;
+    int rank = 0;
+    unsigned long long m = above_m + own;
     for (int j = 0; j < n; ++j) {
-      const float oz = lz[j];
-      rank += oz > z || (oz == z && li[j] < idx);
+      const bool ahead = at_lane(key, j) > key;
+      rank += ahead;
+      if (masses) m += ahead ? at_lane(own, j) : 0ull;
     }
-    sh.mass[rank] = masses ? fixed_weight(z, rc, scale) : 0;
+    bool here = by_mass ? (double)m >= target : above_c + rank + 1 >= k;
+    // the lowest rank that fulfils it, the last one if none does
+    const int at = at_lane(wave_scan(any && here ? rank : RANK, RANK, Min()), 63);
+    if (any && rank == min(at, n - 1)) { sh.f[0] = z; sh.n = idx; sh.fm = m; }
   }
   __syncthreads();
-  uint32_t c = tid < n;
-  unsigned long long m = tid < n ? sh.mass[tid] : 0;
-  scan_bins(c, m);
-  const bool here = by_mass ? (double)(above_m + m) >= target : above_c + c >= k;
-  const int at = first_index(tid < n && here, tid, n - 1);
-  if (tid < n && rank == at) { sh.f[0] = z; sh.n = idx; }
-  if (tid == at) sh.fm = m;
-  __syncthreads();
-  cut.z = sh.f[0];
-  cut.idx = sh.n;
-  cut.mass = above_m + sh.fm;
+  cut.z = uniform(sh.f[0]);
+  cut.idx = uniform(sh.n);
+  cut.mass = sh.fm;
   __syncthreads();
   return cut;
 }
@@ -514,7 +573,7 @@ template <typename E>
 __device__ __noinline__ void draw_kept(const E* p, int V, int nit, float u) {
   FilterShared& sh = shared();
   const RowCut rc = sh.rc;
-  const Row<E, 0> row(p, V, nit);
+  const Row<E> row(p, V, nit);
   const int t = pick_index(row, [&](float z, int i) { return kept_weight(z, i, rc); },
                            (double)u * rc.total);
   if (threadIdx.x == 0) {
@@ -524,34 +583,42 @@ __device__ __noinline__ void draw_kept(const E* p, int V, int nit, float u) {
   __syncthreads();
 }
 
-// Cut, kept weight and draw in general; n tokens reach `bound`, in LDS if they
-// are at most LIST.  whole: weight that top-p is a share of, < 0: of the kept
-// by top-k.  u < 0: no draw.
-template <typename E>
-__device__ __noinline__ void filter_general(const E* p, int V, int nit, int n, float bound, int k,
-                                            double top_p, double whole, float u) {
-  FilterShared& sh = shared();
-  RowCut rc = sh.rc;
-  const Row<E, 0> row(p, V, nit);
-  const Candidates list{n};
-  const float hi = rc.zmax;
-  const double scale = ldexp(1.0, __clz(V) + 30);   // V * scale <= 2^62
+// Both cuts of the tokens of `src` that reach `bound` (n of them): rc.z, rc.idx.
+// whole: the weight that top-p is a share of, < 0: that of the k tokens.
+template <typename Src, typename E>
+__device__ __forceinline__ void both_cuts(const Src& src, const Row<E>& row, RowCut& rc, int n,
+                                          float bound, int k, double top_p, double whole,
+                                          double scale) {
   const bool need_p = top_p < 1.0;
   whole *= scale;
   for (int step = k < n ? 0 : 1; step < (need_p ? 2 : 1); ++step) {   // top-k, top-p
     if (step && whole < 0.0) {                      // top-k keeps all
       double part = 0.0;
-      row.each([&](float z, int) { part += weight(z, rc); });
+      src.each([&](float z, int) { part += z >= bound ? weight(z, rc) : 0.0; });
       whole = range_sums(part) * scale;
+      __syncthreads();
     }
-    const double target = fmax(top_p, 0.0) * whole;
-    const Cut c = n <= LIST ? select_cut(list, row, rc, scale, n, hi, bound, step == 1, need_p,
-                                         (uint32_t)k, target)
-                            : select_cut(row, row, rc, scale, n, hi, bound, step == 1, need_p,
-                                         (uint32_t)k, target);
+    const Cut c = select_cut(src, row, rc, scale, n, rc.zmax, bound, step == 1, need_p,
+                             (uint32_t)k, fmax(top_p, 0.0) * whole);
     if (c.z > rc.z || (c.z == rc.z && c.idx < rc.idx)) { rc.z = c.z; rc.idx = c.idx; }
     if (!step) whole = (double)c.mass;
   }
+  rc.z = fmaxf(rc.z, bound);                        // without a cut: the candidates
+}
+
+// Cut, kept weight and draw over the row; n tokens reach `bound`.  u < 0: no
+// draw.
+template <typename E>
+__device__ __noinline__ void filter_row_again(const E* p, int V, int nit, int n, float bound, int k,
+                                            double top_p, double whole, float u) {
+  FilterShared& sh = shared();
+  RowCut rc = sh.rc;
+  const Row<E> row(p, V, nit);
+  float lo = INFINITY;                              // the smallest candidate
+  row.each([&](float z, int) { lo = z >= bound ? fminf(lo, z) : lo; });
+  lo = block_reduce(lo, INFINITY, Min(), sh.f);
+  // V weights of at most 2^(clz(V) + 30) stay below 2^62
+  both_cuts(row, row, rc, n, lo, k, top_p, whole, ldexp(1.0, __clz(V) + 30));
   double part = 0.0;
   row.each_from(rc.z, [&](float z, int i) { part += kept_weight(z, i, rc); });
   rc.total = range_sums(part);
@@ -560,32 +627,96 @@ __device__ __noinline__ void filter_general(const E* p, int V, int nit, int n, f
   if (u >= 0.0f) draw_kept(p, V, nit, u);
 }
 
-// Shortens a list of RANK < n <= LIST candidates to those in the histogram
+// The same over the n <= LIST candidates in LDS.
+template <typename E>
+__device__ __noinline__ void filter_list(const E* p, int V, int nit, int n, float bound, int k,
+                                         double top_p, double whole, float u) {
+  FilterShared& sh = shared();
+  RowCut rc = sh.rc;
+  const int tid = threadIdx.x;
+  const Row<E> row(p, V, nit);
+  const List list{n};
+  const double scale = 562949953421312.0;           // 2^49: LIST weights stay below 2^63
+  both_cuts(list, row, rc, n, bound, k, top_p, whole, scale);
+  // kept weights by index; a positive one counts for 1 at least
+  auto fixed = [&](float z, int i) -> unsigned long long {
+    const double w = kept_weight(z, i, rc);
+    return w > 0.0 ? max((unsigned long long)(w * scale + 0.5), 1ull) : 0ull;
+  };
+  const int shift = max(0, 22 - __clz(V - 1));      // BINS bins over [0, V)
+  sh.mass[tid] = 0;
+  __syncthreads();
+  list.each([&](float z, int i) {
+    const unsigned long long w = fixed(z, i);
+    if (w) atomicAdd(&sh.mass[i >> shift], w);
+  });
+  __syncthreads();
+  uint32_t none = 0;
+  unsigned long long m = sh.mass[tid];
+  const unsigned long long own = m;
+  scan_bins(none, m);
+  if (tid == BINS - 1) {
+    sh.fm = m;
+    rc.total = (double)m / scale;
+    sh.rc = rc;
+  }
+  __syncthreads();
+  if (u < 0.0f) return;
+  const double t = (double)u * (double)sh.fm;
+  int b = first_index(own && (double)m > t, tid, -1);
+  const bool past = b < 0;                          // u = 1, or by rounding: the last token
+  if (past) b = BINS - 1 - first_index(own > 0, BINS - 1 - tid, 0);
+  if (tid == b) sh.fm = m - own;
+  __syncthreads();
+  if (tid < 64) {                                   // the bin's tokens, a run per lane
+    const unsigned long long base = sh.fm;
+    const int run = max(1, (1 << shift) / 64), first = (b << shift) + tid * run;
+    const int end = min(min(V, first + run), (b + 1) << shift);
+    unsigned long long part = 0;
+    int last = -1;
+    for (int i = first; i < end; ++i) {
+      const unsigned long long w = fixed(load_logit(p + i), i);
+      part += w;
+      if (w) last = i;
+    }
+    const unsigned long long incl = wave_scan(part, 0ull, Add());
+    unsigned long long acc = base + incl - part;
+    const unsigned long long hit = __ballot(part && !past && (double)(base + incl) > t);
+    const unsigned long long any = __ballot(part > 0);
+    const int lane = hit ? __ffsll((long long)hit) - 1 : 63 - __clzll((long long)any);
+    if (tid == lane) {
+      int at = last;
+      if (hit)
+        for (int i = first; i < end; ++i) {
+          acc += fixed(load_logit(p + i), i);
+          if ((double)acc > t) { at = i; break; }
+        }
+      sh.token = at;
+      sh.w = kept_weight(load_logit(p + at), at, rc);
+    }
+  }
+  __syncthreads();
+}
+
+// Shortens a list of SMALL < n <= LIST candidates to those in the histogram
 // bins up to the one that holds the k-th token, or (by_mass) in which the
 // weight reaches `target`.  Returns how many they are; n, and the list as it
-// was, if more than RANK.
+// was, if more than SMALL.
 __device__ __noinline__ int shorten_list(int n, float bound, bool by_mass, int k, double target) {
   FilterShared& sh = shared();
   const RowCut rc = sh.rc;
   const int tid = threadIdx.x;
   const double scale = 562949953421312.0;      // 2^49: LIST weights stay below 2^63
   const Binning bin(rc.zmax, bound, true);
+  const List list{n};
   sh.cnt[tid] = 0;
   sh.mass[tid] = 0;
   __syncthreads();
-  float z[LIST / FT];
-  int idx[LIST / FT];
-#pragma unroll
-  for (int j = 0; j < LIST / FT; ++j) {
-    const int i = j * FT + tid;
-    if (i < n) {
-      z[j] = sh.lz[i];
-      idx[j] = sh.li[i];
-      const int b = bin(z[j]);
-      atomicAdd(&sh.cnt[b], 1u);
-      if (by_mass) atomicAdd(&sh.mass[b], fixed_weight(z[j], rc, scale));
-    }
-  }
+  list.each([&](float z, int) {
+    const int b = bin(z);
+    atomicAdd(&sh.cnt[b], 1u);
+    if (by_mass) atomicAdd(&sh.mass[b], fixed_weight(z, rc, scale));
+  });
   __syncthreads();
   uint32_t c = sh.cnt[tid];
   unsigned long long m = sh.mass[tid];
@@ -595,154 +726,218 @@ __device__ __noinline__ int shorten_list(int n, float bound, bool by_mass, int k
   if (tid == b) sh.found = (int)c;
   if (tid == 0) sh.n = 0;
   __syncthreads();
-  const int left = sh.found;
+  const int left = uniform(sh.found);
+  if (left > SMALL) return n;
+  // gathered behind the histogram, then put in front
+  float* gz = (float*)sh.mass;
+  int* gi = (int*)sh.mass + SMALL;
   __syncthreads();
-  if (left > RANK) return n;
-#pragma unroll
-  for (int j = 0; j < LIST / FT; ++j) {
-    const int i = j * FT + tid;
-    if (i < n && bin(z[j]) <= b) {
+  list.each([&](float z, int i) {
+    if (bin(z) <= b) {
       const int at = atomicAdd(&sh.n, 1);
-      sh.lz[at] = z[j];
-      sh.li[at] = idx[j];
+      gz[at] = z;
+      gi[at] = i;
     }
-  }
+  });
+  __syncthreads();
+  if (tid < left) { sh.lz[tid] = gz[tid]; sh.li[tid] = gi[tid]; }
   __syncthreads();
   return left;
 }
 
-// All cuts and the draw over the n <= RANK candidates in LDS: each thread
-// counts the candidates ahead of its own; sorted by that rank, a scan of the
-// weights gives the prefixes.  Kept tokens then find their running weight in
-// index order by another count.  k: tokens kept by top-k (n: all); top_p < 1:
-// top-p of `whole` (< 0: of the k tokens').  u < 0: no draw.
-__device__ __noinline__ void rank_cut(int n, int k, double top_p, double whole, float u) {
+// Both cuts and the draw over the n <= SMALL candidates in LDS.  A token is
+// kept by top-k if fewer than k are ahead of it, by top-p if the weight ahead
+// of it is below the target; a drawn one is the lowest whose running weight in
+// index order exceeds u * total.  Both take a comparison of every pair: the
+// waves share the candidates out as (64 of them, a part of the others) and add
+// up in LDS.  whole: the weight that top-p is a share of, < 0: that of the k
+// tokens.  u < 0: no draw.
+__device__ __noinline__ void filter_small(int n, int k, double top_p, double whole, float u) {
   FilterShared& sh = shared();
-  RowCut rc = sh.rc;
-  const int tid = threadIdx.x;
-  const double scale = 9007199254740992.0;     // 2^53: RANK weights stay below 2^63
+  const RowCut rc = sh.rc;
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
+  const double scale = 18014398509481984.0;    // 2^54: SMALL weights stay below 2^63
   unsigned long long* key = sh.mass;           // larger logit, then lower index, first
-  unsigned long long* w = sh.mass + RANK;      // by rank
+  unsigned long long* w = sh.mass + SMALL;
+  unsigned long long* sum = sh.mass + 2 * SMALL;
+  uint32_t* rank = sh.cnt;
   float z = 0.f;
   int idx = 0;
-  unsigned long long mine = 0, own = 0;
-  bool big = false;
   double x = 0.0;
+  unsigned long long own = 0;
   if (tid < n) {
     z = sh.lz[tid];
     idx = sh.li[tid];
     x = weight(z, rc);
-    big = x >= (double)rc.min_w;
     own = x > 0.0 ? max((unsigned long long)(x * scale + 0.5), 1ull) : 0ull;
-    mine = ((unsigned long long)order_key(z) << 32) | (uint32_t)~idx;
-    key[tid] = mine;
+    key[tid] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~idx;
+    w[tid] = own;
+  }
+  if (tid < SMALL) { rank[tid] = 0; sum[tid] = 0; }
+  __syncthreads();
+  const int groups = (n + 63) >> 6, parts = FW / groups;   // waves: part * groups + group
+  const int part = wv / groups, cand = (wv - part * groups) * 64 + lane;
+  const bool works = part < parts && cand < n;
+  const unsigned long long mine = works ? key[cand] : ~0ull;
+  if (works) {
+    uint32_t r = 0;
+    unsigned long long a = 0;
+#pragma unroll 2
+    for (int j = part; j < n; j += parts) {
+      const bool ahead = key[j] > mine;
+      r += ahead;
+      a += ahead ? w[j] : 0ull;
+    }
+    atomicAdd(&rank[cand], r);
+    atomicAdd(&sum[cand], a);
   }
   __syncthreads();
-  int rank = 0;
-  if (tid < n) {
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) rank += key[j] > mine;
-    w[rank] = own;
-  }
-  __syncthreads();
-  uint32_t c = tid < n;
-  unsigned long long m = tid < n ? w[tid] : 0;
-  scan_bins(c, m);
-  int keep = k;
+  const int r = tid < n ? (int)rank[tid] : SMALL;
+  const unsigned long long ahead = tid < n ? sum[tid] : 0;
+  bool kept = r < k;
   if (top_p < 1.0) {
-    if (tid == k - 1) sh.fm = m;
-    __syncthreads();
-    const double target = fmax(top_p, 0.0) * (whole < 0.0 ? (double)sh.fm : whole * scale);
-    keep = first_index(tid < k && (double)m >= target, tid, k - 1) + 1;
+    const double all = whole < 0.0
+                           ? (double)block_reduce(kept ? own : 0ull, 0ull, Add(), sh.u)
+                           : whole * scale;
+    kept = kept && (r == 0 || (double)ahead < fmax(top_p, 0.0) * all);
   }
-  const bool kept = tid < n && rank < keep && (big || rank == 0);
-  if (tid < n) w[tid] = kept ? own : 0;        // now by candidate
-  if (tid < n && rank == keep - 1) { sh.rc.z = z; sh.rc.idx = idx; }
-  if (tid == 0) { sh.pick[0] = 0x7fffffff; sh.pick[1] = -1; }
+  const int last = block_reduce(kept ? r : -1, -1, Max(), sh.i);
+  if (r == last) { sh.rc.z = z; sh.rc.idx = idx; }
+  if (!(kept && (x >= (double)rc.min_w || r == 0))) own = 0;
+  const unsigned long long total = block_reduce(own, 0ull, Add(), sh.u);
+  if (tid == 0) sh.rc.total = (double)total / scale;
+  if (tid < n) { w[tid] = own; sum[tid] = 0; }
   __syncthreads();
-  unsigned long long all = 0, run = 0;
-  if (kept || tid == 0) {
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) {
-      const unsigned long long o = w[j];
-      all += o;
-      run += (int)~(uint32_t)key[j] <= idx ? o : 0;
-    }
-    if (tid == 0) sh.rc.total = (double)all / scale;
-    if (u >= 0.0f && kept && own > 0) {
-      if ((double)run > (double)u * (double)all) atomicMin(&sh.pick[0], idx);
-      atomicMax(&sh.pick[1], idx);
-    }
+  if (u < 0.0f) return;
+  if (works) {
+    unsigned long long a = 0;
+    const uint32_t lim = (uint32_t)mine;       // ~index: the lower the index, the larger
+#pragma unroll 2
+    for (int j = part; j < n; j += parts) a += (uint32_t)key[j] >= lim ? w[j] : 0ull;
+    atomicAdd(&sum[cand], a);
   }
   __syncthreads();
-  const int token = sh.pick[0] != 0x7fffffff ? sh.pick[0] : sh.pick[1];
-  if (kept && idx == token) { sh.token = token; sh.w = x; }
+  const bool over = own > 0 && (double)sum[tid < n ? tid : 0] > (double)u * (double)total;
+  int token = first_index(over, idx, -1);
+  if (token < 0) token = block_reduce(own > 0 ? idx : -1, -1, Max(), sh.i);
+  if (own > 0 && idx == token) { sh.token = token; sh.w = x; }
   __syncthreads();
 }
 
-// A logit that at least k tokens of the row reach: the k-th largest of the
-// threads' own maxima is one; here the smallest of those in the histogram bins
-// up to the one where their count reaches k.
-__device__ __forceinline__ float count_bound(float mine, float hi, uint32_t k) {
+// A logit that every token before the cut reaches.  part[]: maxima over parts
+// of this thread's logits, each a token of the row, lo the smallest of them.
+// Where their count reaches k (k > 0), or their weight `target` (k = 0), the
+// row's does; the bound is the lower edge of the histogram bin where that
+// happens.  -FLT_MAX if it does not.
+__device__ __forceinline__ float parts_bound(const float (&part)[PARTS], const RowCut& rc, float lo,
+                                             int k, double target) {
   FilterShared& sh = shared();
   const int tid = threadIdx.x;
-  const bool any = mine > -INFINITY;
-  float lo = any ? mine : INFINITY, top = hi;
-  block_min_max(lo, top);
-  if (!(lo < hi)) return -INFINITY;
-  const Binning bin(hi, lo, true);
-  sh.cnt[tid] = 0;
+  const double scale = 1125899906842624.0;     // 2^50: PARTS * FT weights stay below 2^63
+  if (!(lo < rc.zmax)) return -FLT_MAX;
+  // (linear bins would be one bin where tokens are masked by a lowest number)
+  const Binning bin(rc.zmax, lo, rc.zmax * 0.5f - lo * 0.5f <= 32.0f * (fabsf(rc.zmax) + 1.0f));
+  sh.mass[tid] = 0;
   __syncthreads();
-  const int b = any ? bin(mine) : BINS;
-  if (any) atomicAdd(&sh.cnt[b], 1u);
+#pragma unroll
+  for (int j = 0; j < PARTS; ++j)
+    if (part[j] > -INFINITY)
+      // weights rounded down: what they reach, the row's reach
+      atomicAdd(&sh.mass[bin(part[j])],
+                k ? 1ull : (unsigned long long)(weight(part[j], rc) * scale));
   __syncthreads();
-  uint32_t c = sh.cnt[tid];
-  unsigned long long none = 0;
-  scan_bins(c, none);
-  const int at = first_index(c >= k, tid, -1);
-  if (at < 0) return -INFINITY;                // fewer threads than k hold a logit
-  lo = b <= at ? mine : INFINITY;
-  top = hi;
-  block_min_max(lo, top);
-  return lo;
+  unsigned long long m = sh.mass[tid];
+  uint32_t none = 0;
+  scan_bins(none, m);
+  const bool there = k ? m >= (unsigned long long)k : (double)m >= target * scale;
+  const int at = first_index(there, tid, -1);
+  if (at < 0) return -FLT_MAX;
+  return bin.lower_edge(at);
+}
+
+// A logit such that exp((z - hi) / T) is below w for every smaller one,
+// whatever the roundings on the way.
+__device__ __forceinline__ float weight_bound(float hi, double T, double w) {
+  // (the largest: also for T infinite, whose products may be no number)
+  return fmaxf((float)((double)hi + T * log(w) * (1.0 + 1e-6)) - fabsf(hi) * 1e-6f, -FLT_MAX);
 }
 
 // Reads a row, finds what its filters keep (sh.rc) and, for u >= 0, draws a
 // token (sh.token, sh.w: its weight).
-template <typename E, int NV>
-__device__ __forceinline__ void filter_row(const Row<E, NV>& row, const RowParams& par, int pi,
+template <typename E>
+__device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& par, int pi,
                                            float u, int32_t* err) {
   FilterShared& sh = shared();
+  constexpr int EPV = Row<E>::EPV;
   const int tid = threadIdx.x, V = row.V;
-  const float T = par.temperature ? par.temperature[pi] : 1.0f;
-  const int k = par.top_k ? par.top_k[pi] : 0;
-  const double top_p = par.top_p ? (double)par.top_p[pi] : 1.0;
-  float hi = -INFINITY, lo = INFINITY;
-  bool bad = false;
-  row.each([&](float z, int) {
-    bad |= !(z < INFINITY);
-    hi = fmaxf(hi, z);
-    lo = fminf(lo, z > -INFINITY ? z : INFINITY);
-  });
-  const float mine = hi;
-  if (bad) set_err(err, DVS_ERR_NONFINITE);
-  block_min_max(lo, hi);
-
+  const float T = uniform(par.temperature ? par.temperature[pi] : 1.0f);
+  const int k = uniform(par.top_k ? par.top_k[pi] : 0);
+  const double top_p = (double)uniform(par.top_p ? par.top_p[pi] : 1.0f);
   RowCut rc;
-  rc.zmax = hi;
   rc.z = -INFINITY;
   rc.idx = 0x7fffffff;
-  rc.min_w = par.min_p ? par.min_p[pi] : 0.0f;
+  rc.min_w = uniform(par.min_p ? par.min_p[pi] : 0.0f);
   if (!(rc.min_w > 0.0f)) rc.min_w = 0.0f;
   rc.log2e_t = 1.4426950408889634 / (double)T;
   rc.total = 0.0;
   rc.single = 0;
+  const bool greedy = !(T > 0.0f) || k == 1 || rc.min_w > 1.0f;
+  const bool need_k = k > 0 && k < V, need_p = top_p < 1.0;
+  const bool need_sum = !greedy && !need_k && (need_p || rc.min_w == 0.0f);
+
+  float part[PARTS], mine = -INFINITY;
+  double sum = 0.0;                            // of exp((z - mine) / T)
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < PARTS; ++j) part[j] = -INFINITY;
+#pragma unroll 1
+  for (int it = 0; it < row.nit; it += PARTS) {
+    const u32x16 b = row.batch(it);
+    float most = mine;
+#pragma unroll
+    for (int j = 0; j < PARTS; ++j) {
+      const u32x4 x = Row<E>::vec(b, j);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) {
+        const float z = vec_elem<E>(x, e);
+        bad |= !(z < INFINITY);
+        part[j] = fmaxf(part[j], z);
+      }
+      most = fmaxf(most, part[j]);
+    }
+    if (need_sum) {
+      // the sum so far in terms of the new maximum (an infinite one: no sum)
+      sum *= exp2_neg(((double)mine - (double)most) * rc.log2e_t);
+#pragma unroll 1
+      for (int j = 0; j < PARTS; ++j) {
+        const u32x4 x = Row<E>::vec(b, j);
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+          sum += exp2_neg(((double)vec_elem<E>(x, e) - (double)most) * rc.log2e_t);
+      }
+    }
+    mine = most;
+  }
+  const int ri = row.rest_index();
+  if (ri >= 0) {
+    const float z = load_logit(row.p + ri);
+    bad |= !(z < INFINITY);
+    const float most = fmaxf(mine, z);
+    if (need_sum)
+      sum = sum * exp2_neg(((double)mine - (double)most) * rc.log2e_t) +
+            exp2_neg(((double)z - (double)most) * rc.log2e_t);
+    part[0] = fmaxf(part[0], z);
+    mine = most;
+  }
+  const float hi = block_reduce(mine, -INFINITY, Max(), sh.f);
+  if (bad) set_err(err, DVS_ERR_NONFINITE);
+  rc.zmax = hi;
   const bool empty = hi == -INFINITY;
   if (empty && tid == 0) set_err(err, DVS_ERR_NONFINITE);
-  if (!(T > 0.0f) || k == 1 || rc.min_w > 1.0f || empty || hi == INFINITY) {
+  if (greedy || empty || hi == INFINITY) {
     // top-1: the lowest index of the maximum
     int at = 0x7fffffff;
-    row.each([&](float z, int i) { if (z == hi && i < V) at = min(at, i); });
+    row.each_from(hi, [&](float z, int i) { if (z == hi && i < V) at = min(at, i); });
     at = first_index(at != 0x7fffffff, at, -1);
     rc.z = hi;
     rc.idx = at;
@@ -756,75 +951,73 @@ __device__ __forceinline__ void filter_row(const Row<E, NV>& row, const RowParam
     __syncthreads();
     return;
   }
-  const bool need_k = k > 0 && k < V, need_p = top_p < 1.0;
-  float bound = lo;                            // tokens below are not kept
-  if (rc.min_w > 0.0f && !(need_k && need_p)) {
-    // w < min_p surely, whatever the roundings on the way
-    const double d = (double)T * log((double)rc.min_w);
-    bound = fmaxf(bound, (float)((double)hi + d * (1.0 + 1e-6)) - fabsf(hi) * 1e-6f);
-  }
-  double whole = -1.0;
-  if (need_k) {
-    if (k <= FT) bound = fmaxf(bound, count_bound(mine, hi, (uint32_t)k));
-  } else {
-    // the whole weight: for top-p, and as the kept weight where nothing cuts
-    const double least = need_p ? 0.0 : (double)rc.min_w;
-    double part = 0.0;
-    row.each_from(need_p ? lo : bound, [&](float z, int) {
-      const double w = weight(z, rc);
-      part += w >= least ? w : 0.0;
-    });
-    whole = range_sums(part);
-    if (!need_p) {
-      rc.z = bound;
-      rc.total = whole;
-      if (tid == 0) sh.rc = rc;
-      __syncthreads();
-      if (u >= 0.0f) draw_kept(row.p, V, row.nit, u);
-      return;
+  double whole = -1.0;                         // the row's weight
+  if (need_sum)
+    whole = range_sums(sum * exp2_neg(((double)mine - (double)hi) * rc.log2e_t));
+  float bound = -FLT_MAX;                      // tokens below are not kept
+  if (!need_k && !need_p) {
+    if (rc.min_w > 0.0f) {
+      bound = weight_bound(hi, (double)T, (double)rc.min_w);
+      double kept = 0.0;
+      row.each_from(bound, [&](float z, int) {
+        const double w = weight(z, rc);
+        kept += w >= (double)rc.min_w ? w : 0.0;
+      });
+      whole = range_sums(kept);
     }
+    rc.z = bound;
+    rc.total = whole;
+    if (tid == 0) sh.rc = rc;
+    __syncthreads();
+    if (u >= 0.0f) draw_kept(row.p, V, row.nit, u);
+    return;
+  }
+  float least = INFINITY;
+#pragma unroll
+  for (int j = 0; j < PARTS; ++j) least = fminf(least, part[j] > -INFINITY ? part[j] : INFINITY);
+  const float lo = block_reduce(least, INFINITY, Min(), sh.f);
+  const double target = fmax(top_p, 0.0) * whole;   // (top-p alone)
+  bound = parts_bound(part, rc, lo, need_k ? k : 0, target * (1.0 + 1e-9));
+  if (!need_k) {
     // tokens of less than (1 - p) / V of the weight each cannot hold 1 - p of it
-    const double d = (double)T * log((1.0 - fmax(top_p, 0.0)) * whole / (double)V);
-    bound = fmaxf(bound, (float)((double)hi + d * (1.0 + 1e-6)) - fabsf(hi) * 1e-6f);
+    bound = fmaxf(bound, weight_bound(hi, (double)T, (1.0 - fmax(top_p, 0.0)) * whole / (double)V));
+    if (rc.min_w > 0.0f) bound = fmaxf(bound, weight_bound(hi, (double)T, (double)rc.min_w));
   }
   if (tid == 0) { sh.n = 0; sh.rc = rc; }
   __syncthreads();
   row.each_from(bound, [&](float z, int i) {
-    const unsigned long long m = __ballot(z >= bound);
-    if (m) {
-      const int lane = tid & 63, leader = __ffsll((long long)m) - 1;
-      int first = 0;
-      if (lane == leader) first = atomicAdd(&sh.n, (int)__popcll(m));
-      const int at = __shfl(first, leader) + __popcll(m & ((1ull << lane) - 1));
-      if (z >= bound && at < LIST) { sh.lz[at] = z; sh.li[at] = i; }
+    if (z >= bound) {
+      const int at = atomicAdd(&sh.n, 1);
+      if (at < LIST) { sh.lz[at] = z; sh.li[at] = i; }
     }
   });
   __syncthreads();
-  int n = sh.n;
+  int n = uniform(sh.n);
   __syncthreads();
   const int kk = need_k ? min(k, n) : n;
-  if (n > RANK && n <= LIST && kk <= RANK)
-    n = shorten_list(n, bound, false, kk, 0.0);
-  else if (n > RANK && n <= LIST && !need_k)
-    n = shorten_list(n, bound, true, 0, fmax(top_p, 0.0) * whole);
-  if (n <= RANK)
-    rank_cut(n, min(kk, n), need_p ? top_p : 1.0, whole, u);
+  const double share = need_p ? top_p : 1.0;
+  if (n > SMALL && n <= LIST && (!need_k || kk <= SMALL))
+    n = shorten_list(n, bound, !need_k, kk, target);
+  if (n <= SMALL)
+    filter_small(n, min(kk, n), share, whole, u);
+  else if (n <= LIST)
+    filter_list(row.p, V, row.nit, n, bound, kk, share, whole, u);
   else
-    filter_general(row.p, V, row.nit, n, bound, kk, need_p ? top_p : 1.0, whole, u);
+    filter_row_again(row.p, V, row.nit, n, bound, kk, share, whole, u);
 }
 
 // ---------------------------------------------------------------------------
 // kernels
 // ---------------------------------------------------------------------------
 
-template <typename E, int NV>
+template <typename E>
 __global__ void __launch_bounds__(FT) sample_filtered_kernel(
     const E* __restrict__ logits, long long ld, int V, int nit, RowParams par, int rows_per_param,
     const float* __restrict__ u, int u_stride, int32_t* __restrict__ token_out,
     float* __restrict__ prob_out, int32_t* err) {
   FilterShared& sh = shared();
   const int r = blockIdx.x, s = r / rows_per_param;
-  const Row<E, NV> row(logits + (size_t)r * ld, V, nit);
+  const Row<E> row(logits + (size_t)r * ld, V, nit);
   float uu = u[(size_t)s * u_stride + (r - s * rows_per_param)];
   if (!(uu > 0.0f)) uu = 0.0f;
   filter_row(row, par, s, uu, err);
@@ -835,7 +1028,7 @@ __global__ void __launch_bounds__(FT) sample_filtered_kernel(
 }
 
 // Cuts of the verify rows (first S * (B + 1)) and draft rows (S * B) of a call.
-template <typename E, int NV>
+template <typename E>
 __global__ void __launch_bounds__(FT) filter_rows_kernel(
     const E* __restrict__ zv, long long vs, long long vld, const E* __restrict__ zd, long long ds,
     long long dld, int B, int nv, int V, int nit, RowParams par, RowCut* __restrict__ cuts,
@@ -844,15 +1037,18 @@ __global__ void __launch_bounds__(FT) filter_rows_kernel(
   const int per = r < nv ? B + 1 : B, i = r < nv ? r : r - nv;
   const int s = i / per, j = i - s * per;
   const E* z = r < nv ? zv + (size_t)s * vs + (size_t)j * vld : zd + (size_t)s * ds + (size_t)j * dld;
-  const Row<E, NV> row(z, V, nit);
+  const Row<E> row(z, V, nit);
   filter_row(row, par, s, -1.0f, err);
-  if (threadIdx.x == 0) cuts[r] = shared().rc;
+  if (threadIdx.x == 0) {
+    RowCut rc = shared().rc;
+    rc.inv_total = rc.total > 0.0 ? 1.0 / rc.total : 0.0;
+    cuts[r] = rc;
+  }
 }
 
 __device__ __forceinline__ double prob_of(float z, int i, const RowCut& c) {
   if (c.single) return c.single > 0 && i == c.idx ? 1.0 : 0.0;
-  const double w = kept_weight(z, i, c);
-  return w > 0.0 ? w / c.total : 0.0;
+  return kept_weight(z, i, c) * c.inv_total;
 }
 
 // One workgroup per sequence: d_j accepted while u q_j(d_j) < p_j(d_j), then
@@ -889,26 +1085,23 @@ __global__ void __launch_bounds__(FT) accept_filtered_kernel(
   float uu = u[(size_t)s * u_stride + B];
   if (!(uu > 0.0f)) uu = 0.0f;
   const RowCut p = cv[A];
-  const Row<E, 0> row(v + (size_t)A * vld, V, nit);
-  auto alone = [&](float z, int i) { return i < V ? prob_of(z, i, p) : 0.0; };
+  const Row<E> row(v + (size_t)A * vld, V, nit);
+  const RowCut q = cd[A < B ? A : 0];
+  const E* zq = d + (size_t)(A < B ? A : 0) * dld;
   int t = -1;
-  if (A < B) {
-    const RowCut q = cd[A];
-    const E* zq = d + (size_t)A * dld;
+  // p - q, or p alone: after B acceptances, and where p and q are equal to the
+  // last bit
+  for (int step = A < B ? 0 : 1; step < 2 && t < 0; ++step) {
     auto rest = [&](float z, int i) {
-      const double a = alone(z, i);
-      return a > 0.0 ? fmax(a - prob_of(load_logit(zq + i), i, q), 0.0) : 0.0;
+      double a = i < V ? prob_of(z, i, p) : 0.0;
+      if (step == 0 && a > 0.0) a = fmax(a - prob_of(load_logit(zq + i), i, q), 0.0);
+      return a;
     };
     double part = 0.0;
     row.each_from(p.z, [&](float z, int i) { part += rest(z, i); });
     const double total = range_sums(part);
     t = pick_index(row, rest, (double)uu * total);
-  }
-  if (t < 0) {                           // all accepted, or p and q equal to the last bit
-    double part = 0.0;
-    row.each_from(p.z, [&](float z, int i) { part += alone(z, i); });
-    const double total = range_sums(part);
-    t = pick_index(row, alone, (double)uu * total);
+    __syncthreads();
   }
   if (t < 0) t = max(p.idx, 0);          // a row without a number above -inf
   if (tid == 0) {
@@ -919,18 +1112,11 @@ __global__ void __launch_bounds__(FT) accept_filtered_kernel(
 
 size_t filter_cuts_bytes(int S, int B) { return (size_t)S * (2 * B + 1) * sizeof(RowCut); }
 
-// Calls f(integral constant NV) with the vectors per lane that hold a row of
-// nit: a workgroup of more registers than the row needs would spill nothing
-// but leave the loops over absent vectors in.  0: the row is read again by
-// each pass.
-template <typename E, typename F>
-static void by_vectors(int V, F f) {
-  const int per = FT * 16 / (int)sizeof(E), nit = (V + per - 1) / per;
-  constexpr int MOST = sizeof(E) == 4 ? 16 : 8;
-  if (nit <= 1) f(IC<1>{}, nit);
-  else if (nit <= 4) f(IC<4>{}, nit);
-  else if (nit <= MOST) f(IC<MOST>{}, nit);
-  else f(IC<0>{}, nit);
+// Vectors per lane of a row.
+template <typename E>
+static int row_vectors(int V) {
+  const int epv = 16 / (int)sizeof(E);
+  return (V / epv + FT - 1) / FT;
 }
 
 template <typename E>
@@ -940,15 +1126,12 @@ static int launch_accept(const void* zv, long long vs, long long vld, const void
                          int32_t* accept_len, int32_t* token_out, int token_stride,
                          int at_accepted, int32_t* err, void* ws, hipStream_t st) {
   RowCut* cuts = (RowCut*)ws;
-  by_vectors<E>(V, [&](auto nv, int nit) {
-    constexpr int NV = decltype(nv)::value;
-    hipLaunchKernelGGL((filter_rows_kernel<E, NV>), dim3(S * (2 * B + 1)), dim3(FT), 0, st,
-                       (const E*)zv, vs, vld, (const E*)zd, ds, dld, B, S * (B + 1), V, nit, par,
-                       cuts, err);
-    hipLaunchKernelGGL(accept_filtered_kernel<E>, dim3(S), dim3(FT), 0, st, (const E*)zv, vs,
-                       vld, (const E*)zd, ds, dld, S, B, V, nit, cuts, draft, draft_width, u,
-                       u_stride, accept_len, token_out, token_stride, at_accepted);
-  });
+  const int nit = row_vectors<E>(V);
+  hipLaunchKernelGGL(filter_rows_kernel<E>, dim3(S * (2 * B + 1)), dim3(FT), 0, st, (const E*)zv,
+                     vs, vld, (const E*)zd, ds, dld, B, S * (B + 1), V, nit, par, cuts, err);
+  hipLaunchKernelGGL(accept_filtered_kernel<E>, dim3(S), dim3(FT), 0, st, (const E*)zv, vs, vld,
+                     (const E*)zd, ds, dld, S, B, V, nit, cuts, draft, draft_width, u, u_stride,
+                     accept_len, token_out, token_stride, at_accepted);
   return launch_status("accept_sampled");
 }
 
@@ -956,12 +1139,9 @@ template <typename E>
 static void launch_sample(const void* logits, int rows, int V, long long ld, const RowParams& par,
                           int rows_per_param, const float* u, int u_stride, int32_t* token_out,
                           float* prob_out, int32_t* err, hipStream_t st) {
-  by_vectors<E>(V, [&](auto nv, int nit) {
-    constexpr int NV = decltype(nv)::value;
-    hipLaunchKernelGGL((sample_filtered_kernel<E, NV>), dim3(rows), dim3(FT), 0, st,
-                       (const E*)logits, ld, V, nit, par, rows_per_param, u, u_stride, token_out,
-                       prob_out, err);
-  });
+  hipLaunchKernelGGL(sample_filtered_kernel<E>, dim3(rows), dim3(FT), 0, st, (const E*)logits, ld,
+                     V, row_vectors<E>(V), par, rows_per_param, u, u_stride, token_out, prob_out,
+                     err);
 }
 
 int launch_sample_filtered(const void* logits, int dtype, int rows, int V, long long ld,
