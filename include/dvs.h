@@ -247,7 +247,7 @@ int top1_confidence(const void* logits, int32_t dtype, int32_t rows, int32_t V,
  *   token_out [rows] int32, prob_out [rows] fp32 (may be NULL); err_word may
  *           be NULL.
  * A row's result does not depend on the other rows.  Requirements: rows >= 1,
- * 1 <= V <= 2^30, rows % rows_per_param == 0.
+ * 1 <= V <= 2^22, rows % rows_per_param == 0.
  * ---------------------------------------------------------------------- */
 int sample_filtered(const void* logits, int32_t dtype, int32_t rows, int32_t V, int64_t ld,
                     const float* temperature, const int32_t* top_k, const float* top_p,
@@ -273,7 +273,7 @@ int sample_filtered(const void* logits, int32_t dtype, int32_t rows, int32_t V, 
  *   accept_len [S], token_out [S] int32 (written); err_word may be NULL
  *   workspace >= dvs_accept_workspace_bytes(S, B, V) bytes, no initialisation
  *             needed.  Calls that share it must not overlap in time.
- * Requirements: S, B >= 1, 1 <= V <= 2^30, row strides >= V.
+ * Requirements: S, B >= 1, 1 <= V <= 2^22, row strides >= V.
  * ---------------------------------------------------------------------- */
 size_t dvs_accept_workspace_bytes(int32_t S, int32_t B, int32_t V);
 int accept_sampled(const void* z_verify, int64_t verify_seq, int64_t verify_ld,

@@ -16,10 +16,15 @@
 //   1. one pass: the maximum; where the whole weight is needed, it too, each
 //      thread's sum relative to its own running maximum; and each thread's
 //      maxima over PARTS parts of its logits;
-//   2. a logit that no kept token lies below: the parts' maxima are tokens, so
-//      where their count reaches k, or their weight the share p, all of the cut
-//      is above (parts_bound);
-//   3. a second pass: the tokens from there up, as a list in LDS;
+//   2. a logit that no kept token lies below (parts_bound).  The parts' maxima
+//      are tokens: where their count reaches k, the row's does.  For top-p
+//      they are a sample: a maximum that a share q of the parts exceeds stands
+//      for 1 / (1 - q) tokens, and where the weights so counted reach a little
+//      more than the share p, the cut is likely above, which step 3 checks;
+//   3. a second pass: the tokens from there up, as a list in LDS, and whether
+//      they do weigh the share p (otherwise, and where the list overflows,
+//      again from a bound that is sure: tokens of less than (1 - p) / V of the
+//      weight each, or row_bound);
 //   4. up to SMALL of them (a longer list is first cut short by a histogram)
 //      are ranked against each other, which gives the cut, the kept weight and
 //      the draw at once (filter_small).
@@ -42,13 +47,16 @@
 
 namespace dvs {
 
+#define NOINLINE __attribute__((noinline))
+
 constexpr int FT = 1024;          // threads of a row's workgroup
 constexpr int FW = FT / 64;
 constexpr int BINS = 1024;        // one histogram bin per thread
 constexpr int RANK = 64;          // tokens that one wave ranks
 constexpr int SMALL = 256;        // tokens that the workgroup ranks
 constexpr int PARTS = 4;          // parts of a thread's logits
-constexpr int LIST = 8192;        // candidates held in LDS (64 KB)
+constexpr int BATCH = 16;         // logits that a thread has in flight
+constexpr int LIST = 16384;       // candidates held in LDS (128 KB: one workgroup per CU)
 
 // What a row's filters keep: weight >= min_w of the tokens with z > cut.z, or
 // z == cut.z and index <= cut.idx.
@@ -70,7 +78,7 @@ struct FilterShared {
   double d[FW];
   unsigned long long u[FW];
   uint32_t c[FW];
-  float f[FW];
+  float f[FW], g[FW];
   int i[FW];
   int pick[2];
   int found, n, token;
@@ -86,13 +94,12 @@ __device__ __forceinline__ FilterShared& shared() {
   return sh;
 }
 
-// 2^t for t <= 0: 2^n (1 + f P(f)), t = n + f, |f| <= 1/2.  P interpolates
-// (2^f - 1) / f at Chebyshev nodes: 3.7e-14 relative.  0 for t below -1021,
-// -inf and NaN (a masked logit, or one that is not a number).
-__device__ __forceinline__ double exp2_neg(double t) {
+// 2^(d c) for -1021 < d c <= 0: 2^n (1 + f P(f)), d c = n + f, |f| <= 1/2.  P
+// interpolates (2^f - 1) / f at Chebyshev nodes: 3.7e-14 relative.
+__device__ __forceinline__ double exp2_normal(double d, double c) {
   const double shift = 6755399441055744.0;     // 1.5 * 2^52: n in the low word
-  const double s = t + shift;
-  const double f = t - (s - shift);
+  const double s = fma(d, c, shift);
+  const double f = fma(d, c, shift - s);
   double q = 1.02031210633917290e-07;
   q = fma(q, f, 1.32552248786688168e-06);
   q = fma(q, f, 1.52526868462677196e-05);
@@ -103,13 +110,19 @@ __device__ __forceinline__ double exp2_neg(double t) {
   q = fma(q, f, 2.40226506958129887e-01);
   q = fma(q, f, 6.93147180559945286e-01);
   q = fma(q, f, 1.0);
-  const int hi = __double2hiint(q) + (__double2loint(s) << 20);
-  return t > -1021.0 ? __hiloint2double(hi, __double2loint(q)) : 0.0;
+  return __hiloint2double(__double2hiint(q) + (__double2loint(s) << 20), __double2loint(q));
+}
+
+// The same for every d <= 0, 0 for d c below -1021, -inf and NaN (a masked
+// logit, or one that is not a number).
+__device__ __forceinline__ double exp2_neg(double d, double c) {
+  const double w = exp2_normal(d, c);
+  return d * c > -1021.0 ? w : 0.0;
 }
 
 // exp((z - zmax) / T), zmax finite.
 __device__ __forceinline__ double weight(float z, const RowCut& c) {
-  return exp2_neg(((double)z - (double)c.zmax) * c.log2e_t);
+  return exp2_neg((double)z - (double)c.zmax, c.log2e_t);
 }
 
 __device__ __forceinline__ bool before_cut(float z, int idx, const RowCut& c) {
@@ -160,52 +173,63 @@ typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
 
 // A row of V logits: 16-byte vectors, wave w with the nit * 64 vectors of its
 // range lane by lane, and the V % EPV last logits with the last wave.  A pass
-// has PARTS vectors in flight; absent ones are -inf.
+// has BATCH logits in flight; absent ones are -inf.
 template <typename E>
 struct Row {
-  static constexpr int EPV = 16 / sizeof(E);
+  static constexpr int EPV = 16 / sizeof(E), AHEAD = BATCH / EPV;
   const E* p;
   int V, nit, base;
 
   __device__ __forceinline__ Row(const E* p_, int V_, int nit_) : p(p_), V(V_), nit(nit_) {
     base = ((threadIdx.x >> 6) * nit * 64 + (threadIdx.x & 63)) * EPV;
   }
-  __device__ __forceinline__ u32x4 read(int it) const {
-    const uint32_t none = sizeof(E) == 2 ? 0xff80ff80u : 0xff800000u;
-    const int i = base + it * 64 * EPV;
-    u32x4 x = {none, none, none, none};
-    if (it < nit && i + EPV <= V) x = load_vec(p + i);
-    return x;
-  }
-  // a batch of PARTS vectors
+  __device__ __forceinline__ int at(int it) const { return base + it * 64 * EPV; }
+  // A batch of AHEAD vectors.  No branches: a wait for each load would stand in
+  // them.  (The first vector stands in for absent ones; a pass begins a batch
+  // only if there is one.)
   __device__ __forceinline__ u32x16 batch(int it) const {
+    const uint32_t none = sizeof(E) == 2 ? 0xff80ff80u : 0xff800000u;
+    u32x4 x[AHEAD];
+    bool there[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = at(it + k);
+      there[k] = it + k < nit && i + EPV <= V;
+      x[k] = load_vec(p + (there[k] ? i : 0));
+    }
     u32x16 b;
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k) {
-      const u32x4 x = read(it + k);
+    for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
-      for (int d = 0; d < 4; ++d) b[4 * k + d] = x[d];
-    }
+      for (int d = 0; d < 4; ++d) b[4 * k + d] = there[k] ? x[k][d] : none;
     return b;
   }
   // vector k of a batch (k uniform: indexed registers)
   __device__ __forceinline__ static u32x4 vec(const u32x16& b, int k) {
     return u32x4{b[4 * k], b[4 * k + 1], b[4 * k + 2], b[4 * k + 3]};
   }
-  // The logit behind the last vector that this thread has, or -inf.
+  // logit e of a batch (e constant)
+  __device__ __forceinline__ static float logit(const u32x16& b, int e) {
+    return vec_elem<E>(vec(b, e / EPV), e % EPV);
+  }
+  // The logit behind the last vector that this thread has, or -1.
   __device__ __forceinline__ int rest_index() const {
     const int i = V / EPV * EPV + (int)threadIdx.x - (FT - 64);
     return (int)threadIdx.x >= FT - 64 && i < V ? i : -1;
   }
+  // f(batch, number of its first vector)
+  template <typename F>
+  __device__ __forceinline__ void batches(F f) const {
+#pragma unroll 1
+    for (int it = 0; it < nit; it += AHEAD) f(batch(it), it);
+  }
   // f(vector, index of its first logit)
   template <typename F>
   __device__ __forceinline__ void vectors(F f) const {
+    batches([&](const u32x16& b, int it) {
 #pragma unroll 1
-    for (int it = 0; it < nit; it += PARTS) {
-      const u32x16 b = batch(it);
-#pragma unroll 1
-      for (int k = 0; k < min(PARTS, nit - it); ++k) f(vec(b, k), base + (it + k) * 64 * EPV);
-    }
+      for (int k = 0; k < min(AHEAD, nit - it); ++k) f(vec(b, k), at(it + k));
+    });
   }
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
@@ -219,10 +243,18 @@ struct Row {
   // f(z, index) where some lane's vector reaches zlo; f decides by itself
   template <typename F>
   __device__ __forceinline__ void each_from(float zlo, F f) const {
-    vectors([&](const u32x4& x, int i) {
-      if (__ballot(vec_max<E>(x) >= zlo)) {
+    batches([&](const u32x16& b, int it) {
+      float m = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), i + e);
+      for (int e = 0; e < BATCH; ++e) m = fmaxf(m, logit(b, e));
+      if (!__ballot(m >= zlo)) return;
+#pragma unroll 1
+      for (int k = 0; k < min(AHEAD, nit - it); ++k) {
+        const u32x4 x = vec(b, k);
+        if (__ballot(vec_max<E>(x) >= zlo)) {
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), at(it + k) + e);
+        }
       }
     });
     const int i = rest_index();
@@ -323,6 +355,18 @@ __device__ __forceinline__ T block_reduce(T v, T none, Op op, T* buf) {
   v = row_scan(lane < FW ? buf[lane] : none, none, op);
   __syncthreads();
   return at_lane(v, FW - 1);
+}
+
+__device__ __forceinline__ void block_max_min(float& hi, float& lo) {
+  FilterShared& sh = shared();
+  const int lane = threadIdx.x & 63, wv = uniform((int)threadIdx.x >> 6);
+  hi = wave_scan(hi, -INFINITY, Max());
+  lo = wave_scan(lo, INFINITY, Min());
+  if (lane == 63) { sh.f[wv] = hi; sh.g[wv] = lo; }
+  __syncthreads();
+  hi = at_lane(row_scan(lane < FW ? sh.f[lane] : -INFINITY, -INFINITY, Max()), FW - 1);
+  lo = at_lane(row_scan(lane < FW ? sh.g[lane] : INFINITY, INFINITY, Min()), FW - 1);
+  __syncthreads();
 }
 
 // Inclusive scan over the workgroup of (count, mass), in thread order.
@@ -430,13 +474,14 @@ __device__ __forceinline__ unsigned long long fixed_weight(float z, const RowCut
 // row's logits well, or ones of the numbers' ordered keys, which end at single
 // values whatever the spread.
 struct Binning {
-  float half, sc;
+  float half, sc, width;   // half the largest logit, bins per half a unit, half a bin
   uint32_t khi;
   int shift;
   bool linear;
   __device__ __forceinline__ Binning(float zhi, float zlo, bool lin) : linear(lin) {
     half = zhi * 0.5f;
-    sc = fminf((float)BINS / (half - zlo * 0.5f), 3.0e38f);
+    width = fmaxf((half - zlo * 0.5f) * (1.0f / BINS), 1e-36f);
+    sc = __builtin_amdgcn_rcpf(width);
     khi = order_key(zhi);
     shift = max(0, 22 - __clz(khi - order_key(zlo)));
   }
@@ -447,7 +492,7 @@ struct Binning {
   // a logit that none of the bins up to b lies below
   __device__ __forceinline__ float lower_edge(int b) const {
     if (linear) {
-      const double edge = 2.0 * ((double)half - (b + 1) / (double)sc);
+      const double edge = 2.0 * ((double)half - (b + 1) * (double)width);
       return (float)fmax(edge - 1e-6 * (fabs(edge) + 2.0 * fabs((double)half)), -(double)FLT_MAX);
     }
     const unsigned long long down = ((unsigned long long)(b + 1) << shift) - 1;
@@ -570,7 +615,7 @@ __device__ __forceinline__ Cut select_cut(const Src& src, const Row<E>& row, con
 // The draw among the kept tokens, given each wave's kept weight in sh.d;
 // sh.token and sh.w (its weight).
 template <typename E>
-__device__ __noinline__ void draw_kept(const E* p, int V, int nit, float u) {
+static __device__ NOINLINE void draw_kept(const E* p, int V, int nit, float u) {
   FilterShared& sh = shared();
   const RowCut rc = sh.rc;
   const Row<E> row(p, V, nit);
@@ -609,7 +654,7 @@ __device__ __forceinline__ void both_cuts(const Src& src, const Row<E>& row, Row
 // Cut, kept weight and draw over the row; n tokens reach `bound`.  u < 0: no
 // draw.
 template <typename E>
-__device__ __noinline__ void filter_row_again(const E* p, int V, int nit, int n, float bound, int k,
+static __device__ NOINLINE void filter_row_again(const E* p, int V, int nit, int n, float bound, int k,
                                             double top_p, double whole, float u) {
   FilterShared& sh = shared();
   RowCut rc = sh.rc;
@@ -629,14 +674,14 @@ __device__ __noinline__ void filter_row_again(const E* p, int V, int nit, int n,
 
 // The same over the n <= LIST candidates in LDS.
 template <typename E>
-__device__ __noinline__ void filter_list(const E* p, int V, int nit, int n, float bound, int k,
+static __device__ NOINLINE void filter_list(const E* p, int V, int nit, int n, float bound, int k,
                                          double top_p, double whole, float u) {
   FilterShared& sh = shared();
   RowCut rc = sh.rc;
   const int tid = threadIdx.x;
   const Row<E> row(p, V, nit);
   const List list{n};
-  const double scale = 562949953421312.0;           // 2^49: LIST weights stay below 2^63
+  const double scale = 281474976710656.0;           // 2^48: LIST weights stay below 2^63
   both_cuts(list, row, rc, n, bound, k, top_p, whole, scale);
   // kept weights by index; a positive one counts for 1 at least
   auto fixed = [&](float z, int i) -> unsigned long long {
@@ -701,12 +746,12 @@ __device__ __noinline__ void filter_list(const E* p, int V, int nit, int n, floa
 // Shortens a list of SMALL < n <= LIST candidates to those in the histogram
 // bins up to the one that holds the k-th token, or (by_mass) in which the
 // weight reaches `target`.  Returns how many they are; n, and the list as it
-// was, if more than SMALL.
-__device__ __noinline__ int shorten_list(int n, float bound, bool by_mass, int k, double target) {
+// was, if more than SMALL; -1 if the list does not weigh `target`.
+static __device__ NOINLINE int shorten_list(int n, float bound, bool by_mass, int k, double target) {
   FilterShared& sh = shared();
   const RowCut rc = sh.rc;
   const int tid = threadIdx.x;
-  const double scale = 562949953421312.0;      // 2^49: LIST weights stay below 2^63
+  const double scale = 281474976710656.0;      // 2^48: LIST weights stay below 2^63
   const Binning bin(rc.zmax, bound, true);
   const List list{n};
   sh.cnt[tid] = 0;
@@ -721,8 +766,8 @@ __device__ __noinline__ int shorten_list(int n, float bound, bool by_mass, int k
   uint32_t c = sh.cnt[tid];
   unsigned long long m = sh.mass[tid];
   scan_bins(c, m);
-  // (a target past every weight by rounding: the last bin)
-  const int b = first_index(by_mass ? (double)m >= target * scale : c >= (uint32_t)k, tid, BINS - 1);
+  const int b = first_index(by_mass ? (double)m >= target * scale : c >= (uint32_t)k, tid, -1);
+  if (b < 0) return -1;
   if (tid == b) sh.found = (int)c;
   if (tid == 0) sh.n = 0;
   __syncthreads();
@@ -751,8 +796,10 @@ __device__ __noinline__ int shorten_list(int n, float bound, bool by_mass, int k
 // index order exceeds u * total.  Both take a comparison of every pair: the
 // waves share the candidates out as (64 of them, a part of the others) and add
 // up in LDS.  whole: the weight that top-p is a share of, < 0: that of the k
-// tokens.  u < 0: no draw.
-__device__ __noinline__ void filter_small(int n, int k, double top_p, double whole, float u) {
+// tokens.  u < 0: no draw.  check: false if the candidates do not weigh that
+// share.
+static __device__ NOINLINE bool filter_small(int n, int k, double top_p, double whole, float u,
+                                            bool check) {
   FilterShared& sh = shared();
   const RowCut rc = sh.rc;
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
@@ -796,9 +843,9 @@ __device__ __noinline__ void filter_small(int n, int k, double top_p, double who
   const unsigned long long ahead = tid < n ? sum[tid] : 0;
   bool kept = r < k;
   if (top_p < 1.0) {
-    const double all = whole < 0.0
-                           ? (double)block_reduce(kept ? own : 0ull, 0ull, Add(), sh.u)
-                           : whole * scale;
+    const double sum_k = (double)block_reduce(kept ? own : 0ull, 0ull, Add(), sh.u);
+    const double all = whole < 0.0 ? sum_k : whole * scale;
+    if (check && sum_k < fmax(top_p, 0.0) * all) return false;
     kept = kept && (r == 0 || (double)ahead < fmax(top_p, 0.0) * all);
   }
   const int last = block_reduce(kept ? r : -1, -1, Max(), sh.i);
@@ -808,7 +855,7 @@ __device__ __noinline__ void filter_small(int n, int k, double top_p, double who
   if (tid == 0) sh.rc.total = (double)total / scale;
   if (tid < n) { w[tid] = own; sum[tid] = 0; }
   __syncthreads();
-  if (u < 0.0f) return;
+  if (u < 0.0f) return true;
   if (works) {
     unsigned long long a = 0;
     const uint32_t lim = (uint32_t)mine;       // ~index: the lower the index, the larger
@@ -822,37 +869,98 @@ __device__ __noinline__ void filter_small(int n, int k, double top_p, double who
   if (token < 0) token = block_reduce(own > 0 ? idx : -1, -1, Max(), sh.i);
   if (own > 0 && idx == token) { sh.token = token; sh.w = x; }
   __syncthreads();
+  return true;
 }
 
-// A logit that every token before the cut reaches.  part[]: maxima over parts
-// of this thread's logits, each a token of the row, lo the smallest of them.
-// Where their count reaches k (k > 0), or their weight `target` (k = 0), the
-// row's does; the bound is the lower edge of the histogram bin where that
-// happens.  -FLT_MAX if it does not.
+// A logit that every token before the cut reaches (k > 0), or is likely to
+// (top-p).  part[]: maxima over parts of this thread's logits, lo the smallest
+// of them.  The lower edge of the histogram bin where their count reaches k,
+// or their weight, each taken for the tokens that it stands for, `target`;
+// -FLT_MAX if it does not, or where a part stands for too many.
 __device__ __forceinline__ float parts_bound(const float (&part)[PARTS], const RowCut& rc, float lo,
-                                             int k, double target) {
+                                             int k, float target) {
   FilterShared& sh = shared();
   const int tid = threadIdx.x;
-  const double scale = 1125899906842624.0;     // 2^50: PARTS * FT weights stay below 2^63
   if (!(lo < rc.zmax)) return -FLT_MAX;
   // (linear bins would be one bin where tokens are masked by a lowest number)
   const Binning bin(rc.zmax, lo, rc.zmax * 0.5f - lo * 0.5f <= 32.0f * (fabsf(rc.zmax) + 1.0f));
-  sh.mass[tid] = 0;
+  const float scale = 262144.0f, log2e_t = (float)rc.log2e_t;   // 2^18: sums below 2^31
+  uint32_t* mass = (uint32_t*)sh.mass;
+  sh.cnt[tid] = 0;
+  mass[tid] = 0;
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < PARTS; ++j)
-    if (part[j] > -INFINITY)
-      // weights rounded down: what they reach, the row's reach
-      atomicAdd(&sh.mass[bin(part[j])],
-                k ? 1ull : (unsigned long long)(weight(part[j], rc) * scale));
+  for (int j = 0; j < PARTS; ++j) {
+    if (part[j] > -INFINITY) {
+      const int b = bin(part[j]);
+      atomicAdd(&sh.cnt[b], 1u);
+      if (!k)
+        atomicAdd(&mass[b],
+                  (uint32_t)(__builtin_amdgcn_exp2f((part[j] - rc.zmax) * log2e_t) * scale));
+    }
+  }
   __syncthreads();
-  unsigned long long m = sh.mass[tid];
+  uint32_t c = sh.cnt[tid];
+  unsigned long long m = mass[tid];
+  scan_bins(c, m);
+  bool there = c >= (uint32_t)k;
+  if (!k) {
+    if (tid == FT - 1) sh.fc = c;
+    const float own = (float)mass[tid];
+    __syncthreads();
+    const float left = 1.0f - (float)c * __builtin_amdgcn_rcpf((float)sh.fc);
+    // parts that more than four fifths exceed say little
+    uint32_t few = left < 0.2f;
+    m = few ? 0ull : (unsigned long long)(own * __builtin_amdgcn_rcpf(left));
+    scan_bins(few, m);
+    there = !few && (float)m >= target * scale;
+  }
+  const int at = first_index(there, tid, -1);
+  return at < 0 ? -FLT_MAX : bin.lower_edge(at);
+}
+
+// A bound as parts_bound's, by a histogram over the row, where the parts do
+// not hold enough.  No weights: a bin adds up its tokens' count and, in 2^-16
+// of the bin's width, how far they lie below its upper edge, rounded up.  As
+// exp is convex, the count times the weight at their mean is no more than they
+// weigh, and less by (width / T)^2 / 24 at most.
+template <typename E>
+static __device__ NOINLINE float row_bound(const E* p, int V, int nit, float bound, int k, double target) {
+  FilterShared& sh = shared();
+  const RowCut rc = sh.rc;
+  const int tid = threadIdx.x;
+  const Row<E> row(p, V, nit);
+  const double scale = ldexp(1.0, __clz(V) + 30);   // V * scale <= 2^62
+  const Binning bin(rc.zmax, bound, rc.zmax * 0.5f - bound * 0.5f <= 32.0f * (fabsf(rc.zmax) + 1.0f));
+  sh.mass[tid] = 0;
+  __syncthreads();
+  row.each_from(bound, [&](float z, int) {
+    if (z >= bound) {
+      const float x = (bin.half - z * 0.5f) * bin.sc;
+      const int b = bin(z);
+      const uint32_t below = bin.linear ? (uint32_t)((x - (float)b) * 65536.0f) + 1u : 0u;
+      atomicAdd(&sh.mass[b], (1ull << 40) | below);   // V <= 2^22
+    }
+  });
+  __syncthreads();
+  const unsigned long long got = sh.mass[tid];
+  const double count = (double)(got >> 40);
+  unsigned long long m = got >> 40;
+  if (!k && m) {
+    float z = bin.lower_edge(tid);
+    if (bin.linear) {
+      const double mean = tid + (double)(got & ((1ull << 40) - 1)) / (65536.0 * count);
+      z = fmaxf(z, (float)(2.0 * ((double)bin.half - mean * (double)bin.width)));
+    }
+    // (1e-5 less: the roundings of x, sc and z move a mean by less at any T
+    // whose weights reach this far)
+    m = (unsigned long long)(count * weight(z, rc) * (1.0 - 1e-5) * scale);
+  }
   uint32_t none = 0;
   scan_bins(none, m);
   const bool there = k ? m >= (unsigned long long)k : (double)m >= target * scale;
   const int at = first_index(there, tid, -1);
-  if (at < 0) return -FLT_MAX;
-  return bin.lower_edge(at);
+  return at < 0 ? bound : fmaxf(bound, bin.lower_edge(at));
 }
 
 // A logit such that exp((z - hi) / T) is below w for every smaller one,
@@ -870,7 +978,8 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
   FilterShared& sh = shared();
   constexpr int EPV = Row<E>::EPV;
   const int tid = threadIdx.x, V = row.V;
-  const float T = uniform(par.temperature ? par.temperature[pi] : 1.0f);
+  float T = uniform(par.temperature ? par.temperature[pi] : 1.0f);
+  if (T > FLT_MAX) T = FLT_MAX;
   const int k = uniform(par.top_k ? par.top_k[pi] : 0);
   const double top_p = (double)uniform(par.top_p ? par.top_p[pi] : 1.0f);
   RowCut rc;
@@ -890,46 +999,44 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
   bool bad = false;
 #pragma unroll
   for (int j = 0; j < PARTS; ++j) part[j] = -INFINITY;
-#pragma unroll 1
-  for (int it = 0; it < row.nit; it += PARTS) {
-    const u32x16 b = row.batch(it);
+  // below `floor` a weight counts as 2^-1000 in the sum, in place of less
+  const double floor = -1000.0 / rc.log2e_t;
+  row.batches([&](const u32x16& b, int) {
     float most = mine;
 #pragma unroll
-    for (int j = 0; j < PARTS; ++j) {
-      const u32x4 x = Row<E>::vec(b, j);
-#pragma unroll
-      for (int e = 0; e < EPV; ++e) {
-        const float z = vec_elem<E>(x, e);
-        bad |= !(z < INFINITY);
-        part[j] = fmaxf(part[j], z);
-      }
-      most = fmaxf(most, part[j]);
+    for (int e = 0; e < BATCH; ++e) {
+      const float z = Row<E>::logit(b, e);
+      bad |= !(z < INFINITY);
+      part[e * PARTS / BATCH] = fmaxf(part[e * PARTS / BATCH], z);
     }
+#pragma unroll
+    for (int j = 0; j < PARTS; ++j) most = fmaxf(most, part[j]);
     if (need_sum) {
       // the sum so far in terms of the new maximum (an infinite one: no sum)
-      sum *= exp2_neg(((double)mine - (double)most) * rc.log2e_t);
-#pragma unroll 1
-      for (int j = 0; j < PARTS; ++j) {
-        const u32x4 x = Row<E>::vec(b, j);
+      const double top = (double)most;
+      sum *= exp2_normal(fmax((double)mine - top, floor), rc.log2e_t);
 #pragma unroll
-        for (int e = 0; e < EPV; ++e)
-          sum += exp2_neg(((double)vec_elem<E>(x, e) - (double)most) * rc.log2e_t);
-      }
+      for (int e = 0; e < BATCH; ++e)
+        sum += exp2_normal(fmax((double)Row<E>::logit(b, e) - top, floor), rc.log2e_t);
     }
     mine = most;
-  }
+  });
   const int ri = row.rest_index();
   if (ri >= 0) {
     const float z = load_logit(row.p + ri);
     bad |= !(z < INFINITY);
     const float most = fmaxf(mine, z);
     if (need_sum)
-      sum = sum * exp2_neg(((double)mine - (double)most) * rc.log2e_t) +
-            exp2_neg(((double)z - (double)most) * rc.log2e_t);
+      sum = sum * exp2_neg((double)mine - (double)most, rc.log2e_t) +
+            exp2_neg((double)z - (double)most, rc.log2e_t);
     part[0] = fmaxf(part[0], z);
     mine = most;
   }
-  const float hi = block_reduce(mine, -INFINITY, Max(), sh.f);
+  float least = INFINITY;
+#pragma unroll
+  for (int j = 0; j < PARTS; ++j) least = fminf(least, part[j] > -INFINITY ? part[j] : INFINITY);
+  float hi = mine, lo = least;
+  block_max_min(hi, lo);
   if (bad) set_err(err, DVS_ERR_NONFINITE);
   rc.zmax = hi;
   const bool empty = hi == -INFINITY;
@@ -953,7 +1060,7 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
   }
   double whole = -1.0;                         // the row's weight
   if (need_sum)
-    whole = range_sums(sum * exp2_neg(((double)mine - (double)hi) * rc.log2e_t));
+    whole = range_sums(sum * exp2_neg((double)mine - (double)hi, rc.log2e_t));
   float bound = -FLT_MAX;                      // tokens below are not kept
   if (!need_k && !need_p) {
     if (rc.min_w > 0.0f) {
@@ -972,38 +1079,57 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
     if (u >= 0.0f) draw_kept(row.p, V, row.nit, u);
     return;
   }
-  float least = INFINITY;
-#pragma unroll
-  for (int j = 0; j < PARTS; ++j) least = fminf(least, part[j] > -INFINITY ? part[j] : INFINITY);
-  const float lo = block_reduce(least, INFINITY, Min(), sh.f);
   const double target = fmax(top_p, 0.0) * whole;   // (top-p alone)
-  bound = parts_bound(part, rc, lo, need_k ? k : 0, target * (1.0 + 1e-9));
+  const int kk = need_k ? k : 0;
+  // (a third of the way from the share p to all: room for the sample's error)
+  float sure = -FLT_MAX;
+  bound = parts_bound(part, rc, lo, kk, (float)(target + 0.3 * (whole - target)));
   if (!need_k) {
     // tokens of less than (1 - p) / V of the weight each cannot hold 1 - p of it
-    bound = fmaxf(bound, weight_bound(hi, (double)T, (1.0 - fmax(top_p, 0.0)) * whole / (double)V));
-    if (rc.min_w > 0.0f) bound = fmaxf(bound, weight_bound(hi, (double)T, (double)rc.min_w));
+    sure = weight_bound(hi, (double)T, (1.0 - fmax(top_p, 0.0)) * whole / (double)V);
+    if (rc.min_w > 0.0f) sure = fmaxf(sure, weight_bound(hi, (double)T, (double)rc.min_w));
   }
-  if (tid == 0) { sh.n = 0; sh.rc = rc; }
-  __syncthreads();
-  row.each_from(bound, [&](float z, int i) {
-    if (z >= bound) {
-      const int at = atomicAdd(&sh.n, 1);
-      if (at < LIST) { sh.lz[at] = z; sh.li[at] = i; }
-    }
-  });
-  __syncthreads();
-  int n = uniform(sh.n);
-  __syncthreads();
-  const int kk = need_k ? min(k, n) : n;
   const double share = need_p ? top_p : 1.0;
-  if (n > SMALL && n <= LIST && (!need_k || kk <= SMALL))
-    n = shorten_list(n, bound, !need_k, kk, target);
-  if (n <= SMALL)
-    filter_small(n, min(kk, n), share, whole, u);
-  else if (n <= LIST)
-    filter_list(row.p, V, row.nit, n, bound, kk, share, whole, u);
-  else
-    filter_row_again(row.p, V, row.nit, n, bound, kk, share, whole, u);
+  // bounds: 0 the parts', 1 the sure one, 2 the row's
+  for (int level = bound > sure || need_k ? 0 : 1;;) {
+    if (level == 1) bound = sure;
+    if (tid == 0) { sh.n = 0; sh.rc = rc; }
+    __syncthreads();
+    if (level == 2) bound = row_bound(row.p, V, row.nit, sure, kk, target * (1.0 + 1e-9));
+    row.each_from(bound, [&](float z, int i) {
+      if (z >= bound) {
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < LIST) { sh.lz[at] = z; sh.li[at] = i; }
+      }
+    });
+    __syncthreads();
+    int n = uniform(sh.n);
+    __syncthreads();
+    if (n > LIST && level < 2) {
+      level = 2;
+      continue;
+    }
+    const int keep = need_k ? min(k, n) : n;
+    if (n > SMALL && n <= LIST && (!need_k || keep <= SMALL)) {
+      const int left = shorten_list(n, bound, !need_k, keep, target);
+      if (left < 0 && level == 0) {
+        level = 1;
+        continue;
+      }
+      n = left < 0 ? n : left;
+    }
+    if (n <= SMALL) {
+      if (!filter_small(n, min(keep, n), share, whole, u, level == 0)) {
+        level = 1;
+        continue;
+      }
+    } else if (n <= LIST) {
+      filter_list(row.p, V, row.nit, n, bound, keep, share, whole, u);
+    } else {
+      filter_row_again(row.p, V, row.nit, n, bound, keep, share, whole, u);
+    }
+    return;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -1183,7 +1309,7 @@ extern "C" int sample_filtered(const void* logits, int32_t dtype, int32_t rows, 
   clear_error();
   DVS_CHECK_ARG(logits && u && token_out, "sample_filtered: NULL array argument");
   DVS_CHECK_SUPPORTED(dtype == DVS_F32 || dtype == DVS_BF16, "sample_filtered: dtype %d", dtype);
-  DVS_CHECK_ARG(rows >= 1 && V >= 1 && V <= (1 << 30), "sample_filtered: need rows >= 1 and 1 <= V <= 2^30");
+  DVS_CHECK_ARG(rows >= 1 && V >= 1 && V <= (1 << 22), "sample_filtered: need rows >= 1 and 1 <= V <= 2^22");
   DVS_CHECK_ARG(ld >= V, "sample_filtered: row stride %lld < V", (long long)ld);
   DVS_CHECK_ARG(rows_per_param >= 1 && rows % rows_per_param == 0,
                 "sample_filtered: rows (%d) must be groups of rows_per_param (%d)", rows,
@@ -1194,7 +1320,7 @@ extern "C" int sample_filtered(const void* logits, int32_t dtype, int32_t rows, 
 }
 
 extern "C" size_t dvs_accept_workspace_bytes(int32_t S, int32_t B, int32_t V) {
-  if (S < 1 || B < 1 || V < 1 || V > (1 << 30)) return 0;
+  if (S < 1 || B < 1 || V < 1 || V > (1 << 22)) return 0;
   return (filter_cuts_bytes(S, B) + 255) & ~(size_t)255;
 }
 
@@ -1209,8 +1335,8 @@ extern "C" int accept_sampled(const void* z_verify, int64_t verify_seq, int64_t 
   DVS_CHECK_ARG(z_verify && z_draft && draft && u && accept_len && token_out,
                 "accept_sampled: NULL array argument");
   DVS_CHECK_SUPPORTED(dtype == DVS_F32 || dtype == DVS_BF16, "accept_sampled: dtype %d", dtype);
-  DVS_CHECK_ARG(S >= 1 && B >= 1 && V >= 1 && V <= (1 << 30),
-                "accept_sampled: need S, B >= 1 and 1 <= V <= 2^30");
+  DVS_CHECK_ARG(S >= 1 && B >= 1 && V >= 1 && V <= (1 << 22),
+                "accept_sampled: need S, B >= 1 and 1 <= V <= 2^22");
   DVS_CHECK_ARG((int64_t)S * (2 * (int64_t)B + 1) <= 0x7fffffff, "accept_sampled: too many rows");
   DVS_CHECK_ARG(verify_ld >= V && draft_ld >= V && verify_seq >= 0 && draft_seq >= 0,
                 "accept_sampled: a row stride is less than V");
