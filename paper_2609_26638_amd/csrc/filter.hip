@@ -70,6 +70,14 @@ struct RowCut {
   int single;        // 1: only token idx is kept (weight 1); -1: no token
 };
 
+// What a histogram over all the tokens has found: the bin of the cut, its
+// tokens, and the count and weight above it.  bin < 0: nothing yet.
+struct Found {
+  int bin, n;
+  uint32_t above_c;
+  unsigned long long above_m;
+};
+
 struct FilterShared {
   uint32_t cnt[BINS];
   unsigned long long mass[BINS];
@@ -86,6 +94,7 @@ struct FilterShared {
   unsigned long long fm;
   double w;
   RowCut rc;
+  Found so_far;
 };
 
 // The workgroup's LDS, for the functions that are kept out of line too.
@@ -501,6 +510,17 @@ struct Binning {
   }
 };
 
+// The r-th lowest index (r >= 1) whose logit equals z.
+template <typename E>
+static __device__ NOINLINE int nth_equal(const E* p, int V, int nit, float z, int r) {
+  const Row<E> row(p, V, nit);
+  auto one = [&](float x, int) { return x == z ? 1.0 : 0.0; };
+  double part = 0.0;
+  row.each([&](float x, int i) { part += one(x, i); });
+  range_sums(part);
+  return pick_index(row, one, (double)r - 0.5);
+}
+
 // The last token kept when the tokens of `src` with zlo <= z <= zhi (n of
 // them, in order) are kept up to the k-th (by_mass false), or up to the first
 // at which the weight reaches `target` (by_mass true; the last one if none
@@ -509,15 +529,16 @@ struct Binning {
 template <typename Src, typename E>
 __device__ __forceinline__ Cut select_cut(const Src& src, const Row<E>& row, const RowCut& rc,
                                           double scale, int n, float zhi, float zlo, bool by_mass,
-                                          bool masses, uint32_t k, double target) {
+                                          bool masses, uint32_t k, double target, Found so_far) {
   FilterShared& sh = shared();
   const int tid = threadIdx.x;
-  uint32_t above_c = 0;
-  unsigned long long above_m = 0;
-  int at_bin = -1;                       // the bin looked at; -1: all of [zlo, zhi]
+  uint32_t above_c = so_far.above_c;
+  unsigned long long above_m = so_far.above_m;
+  int at_bin = so_far.bin;               // the bin looked at; -1: all of [zlo, zhi]
+  if (at_bin >= 0) n = so_far.n;
   Binning bin(zhi, zlo, true);
   auto in = [&](float z) { return z <= zhi && z >= zlo && (at_bin < 0 || bin(z) == at_bin); };
-  for (int level = 0; n > RANK; ++level) {
+  for (int level = at_bin >= 0; n > RANK; ++level) {
     if (at_bin >= 0) {
       float lo = INFINITY, hi = -INFINITY;
       src.each([&](float z, int) {
@@ -564,12 +585,8 @@ __device__ __forceinline__ Cut select_cut(const Src& src, const Row<E>& row, con
       keep = more < 1.0 ? 1 : more < (double)n ? (int)more : n;
     }
     keep = min(max(keep, 1), n);
-    auto one = [&](float z, int) { return z == zhi ? 1.0 : 0.0; };
-    double part = 0.0;
-    row.each([&](float z, int i) { part += one(z, i); });
-    range_sums(part);
     cut.z = zhi;
-    cut.idx = pick_index(row, one, (double)keep - 0.5);
+    cut.idx = nth_equal(row.p, row.V, row.nit, zhi, keep);
     cut.mass = above_m + w * (unsigned long long)keep;
     return cut;
   }
@@ -633,7 +650,7 @@ static __device__ NOINLINE void draw_kept(const E* p, int V, int nit, float u) {
 template <typename Src, typename E>
 __device__ __forceinline__ void both_cuts(const Src& src, const Row<E>& row, RowCut& rc, int n,
                                           float bound, int k, double top_p, double whole,
-                                          double scale) {
+                                          double scale, Found so_far) {
   const bool need_p = top_p < 1.0;
   whole *= scale;
   for (int step = k < n ? 0 : 1; step < (need_p ? 2 : 1); ++step) {   // top-k, top-p
@@ -644,7 +661,8 @@ __device__ __forceinline__ void both_cuts(const Src& src, const Row<E>& row, Row
       __syncthreads();
     }
     const Cut c = select_cut(src, row, rc, scale, n, rc.zmax, bound, step == 1, need_p,
-                             (uint32_t)k, fmax(top_p, 0.0) * whole);
+                             (uint32_t)k, fmax(top_p, 0.0) * whole,
+                             step == 1 ? so_far : Found{-1, 0, 0u, 0ull});
     if (c.z > rc.z || (c.z == rc.z && c.idx < rc.idx)) { rc.z = c.z; rc.idx = c.idx; }
     if (!step) whole = (double)c.mass;
   }
@@ -663,7 +681,8 @@ static __device__ NOINLINE void filter_row_again(const E* p, int V, int nit, int
   row.each([&](float z, int) { lo = z >= bound ? fminf(lo, z) : lo; });
   lo = block_reduce(lo, INFINITY, Min(), sh.f);
   // V weights of at most 2^(clz(V) + 30) stay below 2^62
-  both_cuts(row, row, rc, n, lo, k, top_p, whole, ldexp(1.0, __clz(V) + 30));
+  both_cuts(row, row, rc, n, lo, k, top_p, whole, ldexp(1.0, __clz(V) + 30),
+            Found{-1, 0, 0u, 0ull});
   double part = 0.0;
   row.each_from(rc.z, [&](float z, int i) { part += kept_weight(z, i, rc); });
   rc.total = range_sums(part);
@@ -672,17 +691,19 @@ static __device__ NOINLINE void filter_row_again(const E* p, int V, int nit, int
   if (u >= 0.0f) draw_kept(p, V, nit, u);
 }
 
-// The same over the n <= LIST candidates in LDS.
+// The same over the n <= LIST candidates in LDS.  found: shorten_list has left
+// its histogram's bin of the weight.
 template <typename E>
 static __device__ NOINLINE void filter_list(const E* p, int V, int nit, int n, float bound, int k,
-                                         double top_p, double whole, float u) {
+                                         double top_p, double whole, float u, bool found) {
   FilterShared& sh = shared();
   RowCut rc = sh.rc;
   const int tid = threadIdx.x;
   const Row<E> row(p, V, nit);
   const List list{n};
+  const Found so_far = found ? sh.so_far : Found{-1, 0, 0u, 0ull};
   const double scale = 281474976710656.0;           // 2^48: LIST weights stay below 2^63
-  both_cuts(list, row, rc, n, bound, k, top_p, whole, scale);
+  both_cuts(list, row, rc, n, bound, k, top_p, whole, scale, so_far);
   // kept weights by index; a positive one counts for 1 at least
   auto fixed = [&](float z, int i) -> unsigned long long {
     const double w = kept_weight(z, i, rc);
@@ -768,7 +789,11 @@ static __device__ NOINLINE int shorten_list(int n, float bound, bool by_mass, in
   scan_bins(c, m);
   const int b = first_index(by_mass ? (double)m >= target * scale : c >= (uint32_t)k, tid, -1);
   if (b < 0) return -1;
-  if (tid == b) sh.found = (int)c;
+  if (tid == b) {
+    const uint32_t own_c = sh.cnt[tid];
+    sh.found = (int)c;
+    sh.so_far = Found{b, (int)own_c, c - own_c, m - sh.mass[tid]};
+  }
   if (tid == 0) sh.n = 0;
   __syncthreads();
   const int left = uniform(sh.found);
@@ -934,14 +959,20 @@ static __device__ NOINLINE float row_bound(const E* p, int V, int nit, float bou
   const Binning bin(rc.zmax, bound, rc.zmax * 0.5f - bound * 0.5f <= 32.0f * (fabsf(rc.zmax) + 1.0f));
   sh.mass[tid] = 0;
   __syncthreads();
-  row.each_from(bound, [&](float z, int) {
+  auto add = [&](float z) {
     if (z >= bound) {
       const float x = (bin.half - z * 0.5f) * bin.sc;
       const int b = bin(z);
       const uint32_t below = bin.linear ? (uint32_t)((x - (float)b) * 65536.0f) + 1u : 0u;
       atomicAdd(&sh.mass[b], (1ull << 40) | below);   // V <= 2^22
     }
+  };
+  row.batches([&](const u32x16& b, int) {
+#pragma unroll
+    for (int e = 0; e < BATCH; ++e) add(Row<E>::logit(b, e));
   });
+  const int ri = row.rest_index();
+  if (ri >= 0) add(load_logit(p + ri));
   __syncthreads();
   const unsigned long long got = sh.mass[tid];
   const double count = (double)(got >> 40);
@@ -1091,17 +1122,36 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
   }
   const double share = need_p ? top_p : 1.0;
   // bounds: 0 the parts', 1 the sure one, 2 the row's
-  for (int level = bound > sure || need_k ? 0 : 1;;) {
+  for (int level = bound > sure || need_k ? 0 : bound > -FLT_MAX ? 1 : 2;;) {
     if (level == 1) bound = sure;
     if (tid == 0) { sh.n = 0; sh.rc = rc; }
     __syncthreads();
     if (level == 2) bound = row_bound(row.p, V, row.nit, sure, kk, target * (1.0 + 1e-9));
-    row.each_from(bound, [&](float z, int i) {
-      if (z >= bound) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < LIST) { sh.lz[at] = z; sh.li[at] = i; }
+    row.batches([&](const u32x16& b, int it) {
+      uint32_t c = 0;
+#pragma unroll
+      for (int e = 0; e < BATCH; ++e) c += Row<E>::logit(b, e) >= bound;
+      if (!__ballot(c)) return;
+      const uint32_t incl = wave_scan(c, 0u, Add());   // a place for each, one count-in per wave
+      int at = 0;
+      if ((tid & 63) == 63) at = atomicAdd(&sh.n, (int)incl);
+      at = at_lane(at, 63) + (int)(incl - c);
+#pragma unroll
+      for (int e = 0; e < BATCH; ++e) {
+        const float z = Row<E>::logit(b, e);
+        if (z >= bound) {
+          if (at < LIST) { sh.lz[at] = z; sh.li[at] = row.at(it + e / EPV) + e % EPV; }
+          ++at;
+        }
       }
     });
+    if (ri >= 0) {
+      const float z = load_logit(row.p + ri);
+      if (z >= bound) {
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < LIST) { sh.lz[at] = z; sh.li[at] = ri; }
+      }
+    }
     __syncthreads();
     int n = uniform(sh.n);
     __syncthreads();
@@ -1110,6 +1160,7 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
       continue;
     }
     const int keep = need_k ? min(k, n) : n;
+    bool found = false;
     if (n > SMALL && n <= LIST && (!need_k || keep <= SMALL)) {
       const int left = shorten_list(n, bound, !need_k, keep, target);
       if (left < 0 && level == 0) {
@@ -1117,6 +1168,7 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
         continue;
       }
       n = left < 0 ? n : left;
+      found = !need_k && left > SMALL;
     }
     if (n <= SMALL) {
       if (!filter_small(n, min(keep, n), share, whole, u, level == 0)) {
@@ -1124,7 +1176,7 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
         continue;
       }
     } else if (n <= LIST) {
-      filter_list(row.p, V, row.nit, n, bound, keep, share, whole, u);
+      filter_list(row.p, V, row.nit, n, bound, keep, share, whole, u, found);
     } else {
       filter_row_again(row.p, V, row.nit, n, bound, keep, share, whole, u);
     }
