@@ -11,7 +11,7 @@
 // 32-bit weights (1e-7 relative) would draw a neighbour for one row in a few
 // hundred.  64-bit adds and multiplies run at the 32-bit rate on this chip.
 //
-// One workgroup of 1024 threads per row.  Wave w owns one contiguous range of
+// One workgroup per row (RowFilter).  Wave w owns one contiguous range of
 // the row, so the ranges' sums are in index order.
 //   1. one pass: the maximum; where the whole weight is needed, it too, each
 //      thread's sum relative to its own running maximum; and each thread's
@@ -49,14 +49,10 @@ namespace dvs {
 
 #define NOINLINE __attribute__((noinline))
 
-constexpr int FT = 1024;          // threads of a row's workgroup
-constexpr int FW = FT / 64;
-constexpr int BINS = 1024;        // one histogram bin per thread
 constexpr int RANK = 64;          // tokens that one wave ranks
 constexpr int SMALL = 256;        // tokens that the workgroup ranks
 constexpr int PARTS = 4;          // parts of a thread's logits
 constexpr int BATCH = 16;         // logits that a thread has in flight
-constexpr int LIST = 16384;       // candidates held in LDS (128 KB: one workgroup per CU)
 
 // What a row's filters keep: weight >= min_w of the tokens with z > cut.z, or
 // z == cut.z and index <= cut.idx.
@@ -77,31 +73,6 @@ struct Found {
   uint32_t above_c;
   unsigned long long above_m;
 };
-
-struct FilterShared {
-  uint32_t cnt[BINS];
-  unsigned long long mass[BINS];
-  float lz[LIST];
-  int li[LIST];
-  double d[FW];
-  unsigned long long u[FW];
-  uint32_t c[FW];
-  float f[FW], g[FW];
-  int i[FW];
-  int pick[2];
-  int found, n, token;
-  uint32_t fc;
-  unsigned long long fm;
-  double w;
-  RowCut rc;
-  Found so_far;
-};
-
-// The workgroup's LDS, for the functions that are kept out of line too.
-__device__ __forceinline__ FilterShared& shared() {
-  __shared__ FilterShared sh;
-  return sh;
-}
 
 // 2^(d c) for -1021 < d c <= 0: 2^n (1 + f P(f)), d c = n + f, |f| <= 1/2.  P
 // interpolates (2^f - 1) / f at Chebyshev nodes: 3.7e-14 relative.
@@ -180,112 +151,6 @@ __device__ __forceinline__ float vec_elem(const u32x4& x, int e) {
 
 typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
 
-// A row of V logits: 16-byte vectors, wave w with the nit * 64 vectors of its
-// range lane by lane, and the V % EPV last logits with the last wave.  A pass
-// has BATCH logits in flight; absent ones are -inf.
-template <typename E>
-struct Row {
-  static constexpr int EPV = 16 / sizeof(E), AHEAD = BATCH / EPV;
-  const E* p;
-  int V, nit, base;
-
-  __device__ __forceinline__ Row(const E* p_, int V_, int nit_) : p(p_), V(V_), nit(nit_) {
-    base = ((threadIdx.x >> 6) * nit * 64 + (threadIdx.x & 63)) * EPV;
-  }
-  __device__ __forceinline__ int at(int it) const { return base + it * 64 * EPV; }
-  // A batch of AHEAD vectors.  No branches: a wait for each load would stand in
-  // them.  (The first vector stands in for absent ones; a pass begins a batch
-  // only if there is one.)
-  __device__ __forceinline__ u32x16 batch(int it) const {
-    const uint32_t none = sizeof(E) == 2 ? 0xff80ff80u : 0xff800000u;
-    u32x4 x[AHEAD];
-    bool there[AHEAD];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const int i = at(it + k);
-      there[k] = it + k < nit && i + EPV <= V;
-      x[k] = load_vec(p + (there[k] ? i : 0));
-    }
-    u32x16 b;
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-      for (int d = 0; d < 4; ++d) b[4 * k + d] = there[k] ? x[k][d] : none;
-    return b;
-  }
-  // vector k of a batch (k uniform: indexed registers)
-  __device__ __forceinline__ static u32x4 vec(const u32x16& b, int k) {
-    return u32x4{b[4 * k], b[4 * k + 1], b[4 * k + 2], b[4 * k + 3]};
-  }
-  // logit e of a batch (e constant)
-  __device__ __forceinline__ static float logit(const u32x16& b, int e) {
-    return vec_elem<E>(vec(b, e / EPV), e % EPV);
-  }
-  // The logit behind the last vector that this thread has, or -1.
-  __device__ __forceinline__ int rest_index() const {
-    const int i = V / EPV * EPV + (int)threadIdx.x - (FT - 64);
-    return (int)threadIdx.x >= FT - 64 && i < V ? i : -1;
-  }
-  // f(batch, number of its first vector)
-  template <typename F>
-  __device__ __forceinline__ void batches(F f) const {
-#pragma unroll 1
-    for (int it = 0; it < nit; it += AHEAD) f(batch(it), it);
-  }
-  // f(vector, index of its first logit)
-  template <typename F>
-  __device__ __forceinline__ void vectors(F f) const {
-    batches([&](const u32x16& b, int it) {
-#pragma unroll 1
-      for (int k = 0; k < min(AHEAD, nit - it); ++k) f(vec(b, k), at(it + k));
-    });
-  }
-  template <typename F>
-  __device__ __forceinline__ void each(F f) const {
-    vectors([&](const u32x4& x, int i) {
-#pragma unroll
-      for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), i + e);
-    });
-    const int i = rest_index();
-    if (i >= 0) f(load_logit(p + i), i);
-  }
-  // f(z, index) where some lane's vector reaches zlo; f decides by itself
-  template <typename F>
-  __device__ __forceinline__ void each_from(float zlo, F f) const {
-    batches([&](const u32x16& b, int it) {
-      float m = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < BATCH; ++e) m = fmaxf(m, logit(b, e));
-      if (!__ballot(m >= zlo)) return;
-#pragma unroll 1
-      for (int k = 0; k < min(AHEAD, nit - it); ++k) {
-        const u32x4 x = vec(b, k);
-        if (__ballot(vec_max<E>(x) >= zlo)) {
-#pragma unroll
-          for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), at(it + k) + e);
-        }
-      }
-    });
-    const int i = rest_index();
-    if (i >= 0) f(load_logit(p + i), i);
-  }
-};
-
-// The n candidates in LDS.
-struct List {
-  int n;
-  template <typename F>
-  __device__ __forceinline__ void each(F f) const {
-    const FilterShared& sh = shared();
-#pragma unroll 1
-    for (int i = threadIdx.x; i < n; i += FT) f(sh.lz[i], sh.li[i]);
-  }
-};
-
-// ---------------------------------------------------------------------------
-// over the workgroup
-// ---------------------------------------------------------------------------
-
 // A value that every thread of the workgroup has, in scalar registers: what
 // branches on it is then no divergent branch, whose both sides would keep
 // their registers.
@@ -354,9 +219,166 @@ __device__ __forceinline__ T wave_scan(T v, T none, Op op) {
   return v;
 }
 
+struct Cut {
+  float z;
+  int idx;
+  unsigned long long mass;   // fixed-point weight through the cut
+};
+
+__device__ __forceinline__ unsigned long long fixed_weight(float z, const RowCut& c, double scale) {
+  return (unsigned long long)(weight(z, c) * scale + 0.5);
+}
+
+// A logit such that exp((z - hi) / T) is below w for every smaller one,
+// whatever the roundings on the way.
+__device__ __forceinline__ float weight_bound(float hi, double T, double w) {
+  // (the largest: also for T infinite, whose products may be no number)
+  return fmaxf((float)((double)hi + T * (log(w) * (1.0 + 1e-6) - 1e-9)) - fabsf(hi) * 1e-6f,
+               -FLT_MAX);
+}
+
+// A row by a workgroup of FT threads: 1024 (one workgroup per CU, for calls of
+// few rows, where a row's latency counts) or 512 (two per CU, so that the
+// latencies of one row run under the passes of the other).
+template <int FT>
+struct RowFilter {
+
+static constexpr int FW = FT / 64;
+static constexpr int BINS = FT, BIN_BITS = FT == 1024 ? 10 : 9;   // one bin per thread
+static constexpr int LIST = 16 * FT;   // candidates held in LDS (128 KB or 64 KB)
+
+struct FilterShared {
+  uint32_t cnt[BINS];
+  unsigned long long mass[BINS > 3 * SMALL ? BINS : 3 * SMALL];
+  float lz[LIST];
+  int li[LIST];
+  double d[FW];
+  unsigned long long u[FW];
+  uint32_t c[FW];
+  float f[FW], g[FW];
+  int i[FW];
+  int pick[2];
+  int found, n, token;
+  uint32_t fc;
+  unsigned long long fm;
+  double w;
+  RowCut rc;
+  Found so_far;
+};
+
+// The workgroup's LDS, for the functions that are kept out of line too.
+static __device__ __forceinline__ FilterShared& shared() {
+  __shared__ FilterShared sh;
+  return sh;
+}
+
+// A row of V logits: 16-byte vectors, wave w with the nit * 64 vectors of its
+// range lane by lane, and the V % EPV last logits with the last wave.  A pass
+// has BATCH logits in flight; absent ones are -inf.
+template <typename E>
+struct Row {
+  static constexpr int EPV = 16 / sizeof(E), AHEAD = BATCH / EPV;
+  const E* p;
+  int V, nit, base;
+
+  __device__ __forceinline__ Row(const E* p_, int V_, int nit_) : p(p_), V(V_), nit(nit_) {
+    base = ((threadIdx.x >> 6) * nit * 64 + (threadIdx.x & 63)) * EPV;
+  }
+  __device__ __forceinline__ int at(int it) const { return base + it * 64 * EPV; }
+  // A batch of AHEAD vectors.  No branches: a wait for each load would stand in
+  // them.  (The first vector stands in for absent ones; a pass begins a batch
+  // only if there is one.)
+  __device__ __forceinline__ u32x16 batch(int it) const {
+    const uint32_t none = sizeof(E) == 2 ? 0xff80ff80u : 0xff800000u;
+    u32x4 x[AHEAD];
+    bool there[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = at(it + k);
+      there[k] = it + k < nit && i + EPV <= V;
+      x[k] = load_vec(p + (there[k] ? i : 0));
+    }
+    u32x16 b;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) b[4 * k + d] = there[k] ? x[k][d] : none;
+    return b;
+  }
+  // vector k of a batch (k uniform: indexed registers)
+  static __device__ __forceinline__ u32x4 vec(const u32x16& b, int k) {
+    return u32x4{b[4 * k], b[4 * k + 1], b[4 * k + 2], b[4 * k + 3]};
+  }
+  // logit e of a batch (e constant)
+  static __device__ __forceinline__ float logit(const u32x16& b, int e) {
+    return vec_elem<E>(vec(b, e / EPV), e % EPV);
+  }
+  // The logit behind the last vector that this thread has, or -1.
+  __device__ __forceinline__ int rest_index() const {
+    const int i = V / EPV * EPV + (int)threadIdx.x - (FT - 64);
+    return (int)threadIdx.x >= FT - 64 && i < V ? i : -1;
+  }
+  // f(batch, number of its first vector)
+  template <typename F>
+  __device__ __forceinline__ void batches(F f) const {
+#pragma unroll 1
+    for (int it = 0; it < nit; it += AHEAD) f(batch(it), it);
+  }
+  // f(vector, index of its first logit)
+  template <typename F>
+  __device__ __forceinline__ void vectors(F f) const {
+    batches([&](const u32x16& b, int it) {
+#pragma unroll 1
+      for (int k = 0; k < min(AHEAD, nit - it); ++k) f(vec(b, k), at(it + k));
+    });
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    vectors([&](const u32x4& x, int i) {
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), i + e);
+    });
+    const int i = rest_index();
+    if (i >= 0) f(load_logit(p + i), i);
+  }
+  // f(z, index) where some lane's vector reaches zlo; f decides by itself
+  template <typename F>
+  __device__ __forceinline__ void each_from(float zlo, F f) const {
+    batches([&](const u32x16& b, int it) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < BATCH; ++e) m = fmaxf(m, logit(b, e));
+      if (!__ballot(m >= zlo)) return;
+#pragma unroll 1
+      for (int k = 0; k < min(AHEAD, nit - it); ++k) {
+        const u32x4 x = vec(b, k);
+        if (__ballot(vec_max<E>(x) >= zlo)) {
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), at(it + k) + e);
+        }
+      }
+    });
+    const int i = rest_index();
+    if (i >= 0) f(load_logit(p + i), i);
+  }
+};
+
+// The n candidates in LDS.
+struct List {
+  int n;
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    const FilterShared& sh = shared();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += FT) f(sh.lz[i], sh.li[i]);
+  }
+};
+
+  // -- over the workgroup
+
 // v over the workgroup, in scalar registers; buf: FW values in LDS.
 template <typename T, typename Op>
-__device__ __forceinline__ T block_reduce(T v, T none, Op op, T* buf) {
+static __device__ __forceinline__ T block_reduce(T v, T none, Op op, T* buf) {
   const int lane = threadIdx.x & 63, wv = uniform((int)threadIdx.x >> 6);
   v = wave_scan(v, none, op);
   if (lane == 63) buf[wv] = v;
@@ -366,7 +388,7 @@ __device__ __forceinline__ T block_reduce(T v, T none, Op op, T* buf) {
   return at_lane(v, FW - 1);
 }
 
-__device__ __forceinline__ void block_max_min(float& hi, float& lo) {
+static __device__ __forceinline__ void block_max_min(float& hi, float& lo) {
   FilterShared& sh = shared();
   const int lane = threadIdx.x & 63, wv = uniform((int)threadIdx.x >> 6);
   hi = wave_scan(hi, -INFINITY, Max());
@@ -379,7 +401,7 @@ __device__ __forceinline__ void block_max_min(float& hi, float& lo) {
 }
 
 // Inclusive scan over the workgroup of (count, mass), in thread order.
-__device__ __forceinline__ void scan_bins(uint32_t& c, unsigned long long& m) {
+static __device__ __forceinline__ void scan_bins(uint32_t& c, unsigned long long& m) {
   FilterShared& sh = shared();
   const int lane = threadIdx.x & 63, wv = uniform((int)threadIdx.x >> 6);
   c = wave_scan(c, 0u, Add());
@@ -396,7 +418,7 @@ __device__ __forceinline__ void scan_bins(uint32_t& c, unsigned long long& m) {
 }
 
 // Smallest index of a thread for which `yes` holds, `none` without one.
-__device__ __forceinline__ int first_index(bool yes, int i, int none) {
+static __device__ __forceinline__ int first_index(bool yes, int i, int none) {
   const int got = block_reduce(yes ? i : 0x7fffffff, 0x7fffffff, Min(), shared().i);
   return got == 0x7fffffff ? none : got;
 }
@@ -406,7 +428,7 @@ __device__ __forceinline__ int first_index(bool yes, int i, int none) {
 // (or u = 1) puts t past the sum; -1 when every weight is zero.  fn(z, i) is
 // the weight of token i.
 template <typename E, typename F>
-__device__ __forceinline__ int pick_index(const Row<E>& row, F fn, double t) {
+static __device__ __forceinline__ int pick_index(const Row<E>& row, F fn, double t) {
   FilterShared& sh = shared();
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   const double own = lane < FW ? sh.d[lane] : 0.0;
@@ -455,7 +477,7 @@ __device__ __forceinline__ int pick_index(const Row<E>& row, F fn, double t) {
 }
 
 // Every wave's range sum to sh.d; returns their sum, in order.
-__device__ __forceinline__ double range_sums(double part) {
+static __device__ __forceinline__ double range_sums(double part) {
   FilterShared& sh = shared();
   const int lane = threadIdx.x & 63, wv = uniform((int)threadIdx.x >> 6);
   part = wave_scan(part, 0.0, Add());
@@ -465,19 +487,7 @@ __device__ __forceinline__ double range_sums(double part) {
   return at_lane(row_scan(lane < FW ? sh.d[lane] : 0.0, 0.0, Add()), FW - 1);
 }
 
-// ---------------------------------------------------------------------------
-// the cut
-// ---------------------------------------------------------------------------
-
-struct Cut {
-  float z;
-  int idx;
-  unsigned long long mass;   // fixed-point weight through the cut
-};
-
-__device__ __forceinline__ unsigned long long fixed_weight(float z, const RowCut& c, double scale) {
-  return (unsigned long long)(weight(z, c) * scale + 0.5);
-}
+  // -- the cut
 
 // Bins over [zlo, zhi], the largest logits first: linear ones, which spread a
 // row's logits well, or ones of the numbers' ordered keys, which end at single
@@ -492,7 +502,7 @@ struct Binning {
     width = fmaxf((half - zlo * 0.5f) * (1.0f / BINS), 1e-36f);
     sc = __builtin_amdgcn_rcpf(width);
     khi = order_key(zhi);
-    shift = max(0, 22 - __clz(khi - order_key(zlo)));
+    shift = max(0, 32 - BIN_BITS - __clz(khi - order_key(zlo)));
   }
   __device__ __forceinline__ int operator()(float z) const {
     if (linear) return (int)fminf((half - z * 0.5f) * sc, (float)(BINS - 1));
@@ -527,7 +537,7 @@ static __device__ NOINLINE int nth_equal(const E* p, int V, int nit, float z, in
 // does).  Weights are summed only when `masses` is set.  `row`: where equal
 // logits are counted in index order.
 template <typename Src, typename E>
-__device__ __forceinline__ Cut select_cut(const Src& src, const Row<E>& row, const RowCut& rc,
+static __device__ __forceinline__ Cut select_cut(const Src& src, const Row<E>& row, const RowCut& rc,
                                           double scale, int n, float zhi, float zlo, bool by_mass,
                                           bool masses, uint32_t k, double target, Found so_far) {
   FilterShared& sh = shared();
@@ -648,7 +658,7 @@ static __device__ NOINLINE void draw_kept(const E* p, int V, int nit, float u) {
 // Both cuts of the tokens of `src` that reach `bound` (n of them): rc.z, rc.idx.
 // whole: the weight that top-p is a share of, < 0: that of the k tokens.
 template <typename Src, typename E>
-__device__ __forceinline__ void both_cuts(const Src& src, const Row<E>& row, RowCut& rc, int n,
+static __device__ __forceinline__ void both_cuts(const Src& src, const Row<E>& row, RowCut& rc, int n,
                                           float bound, int k, double top_p, double whole,
                                           double scale, Found so_far) {
   const bool need_p = top_p < 1.0;
@@ -709,7 +719,7 @@ static __device__ NOINLINE void filter_list(const E* p, int V, int nit, int n, f
     const double w = kept_weight(z, i, rc);
     return w > 0.0 ? max((unsigned long long)(w * scale + 0.5), 1ull) : 0ull;
   };
-  const int shift = max(0, 22 - __clz(V - 1));      // BINS bins over [0, V)
+  const int shift = max(0, 32 - BIN_BITS - __clz(V - 1));      // BINS bins over [0, V)
   sh.mass[tid] = 0;
   __syncthreads();
   list.each([&](float z, int i) {
@@ -902,7 +912,7 @@ static __device__ NOINLINE bool filter_small(int n, int k, double top_p, double 
 // of them.  The lower edge of the histogram bin where their count reaches k,
 // or their weight, each taken for the tokens that it stands for, `target`;
 // -FLT_MAX if it does not, or where a part stands for too many.
-__device__ __forceinline__ float parts_bound(const float (&part)[PARTS], const RowCut& rc, float lo,
+static __device__ __forceinline__ float parts_bound(const float (&part)[PARTS], const RowCut& rc, float lo,
                                              int k, float target) {
   FilterShared& sh = shared();
   const int tid = threadIdx.x;
@@ -994,23 +1004,15 @@ static __device__ NOINLINE float row_bound(const E* p, int V, int nit, float bou
   return at < 0 ? bound : fmaxf(bound, bin.lower_edge(at));
 }
 
-// A logit such that exp((z - hi) / T) is below w for every smaller one,
-// whatever the roundings on the way.
-__device__ __forceinline__ float weight_bound(float hi, double T, double w) {
-  // (the largest: also for T infinite, whose products may be no number)
-  return fmaxf((float)((double)hi + T * log(w) * (1.0 + 1e-6)) - fabsf(hi) * 1e-6f, -FLT_MAX);
-}
-
 // Reads a row, finds what its filters keep (sh.rc) and, for u >= 0, draws a
 // token (sh.token, sh.w: its weight).
 template <typename E>
-__device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& par, int pi,
+static __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& par, int pi,
                                            float u, int32_t* err) {
   FilterShared& sh = shared();
   constexpr int EPV = Row<E>::EPV;
   const int tid = threadIdx.x, V = row.V;
-  float T = uniform(par.temperature ? par.temperature[pi] : 1.0f);
-  if (T > FLT_MAX) T = FLT_MAX;
+  const float T = uniform(par.temperature ? par.temperature[pi] : 1.0f);
   const int k = uniform(par.top_k ? par.top_k[pi] : 0);
   const double top_p = (double)uniform(par.top_p ? par.top_p[pi] : 1.0f);
   RowCut rc;
@@ -1090,8 +1092,14 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
     return;
   }
   double whole = -1.0;                         // the row's weight
-  if (need_sum)
-    whole = range_sums(sum * exp2_neg((double)mine - (double)hi, rc.log2e_t));
+  if (need_sum) {
+    sum *= exp2_neg((double)mine - (double)hi, rc.log2e_t);
+    if (T > FLT_MAX) {                         // infinite: every token but the masked ones, once
+      sum = 0.0;
+      row.each([&](float z, int) { sum += weight(z, rc); });
+    }
+    whole = range_sums(sum);
+  }
   float bound = -FLT_MAX;                      // tokens below are not kept
   if (!need_k && !need_p) {
     if (rc.min_w > 0.0f) {
@@ -1184,21 +1192,23 @@ __device__ __forceinline__ void filter_row(const Row<E>& row, const RowParams& p
   }
 }
 
+};  // RowFilter
+
 // ---------------------------------------------------------------------------
 // kernels
 // ---------------------------------------------------------------------------
 
-template <typename E>
-__global__ void __launch_bounds__(FT) sample_filtered_kernel(
+template <int FT, typename E>
+__global__ void __launch_bounds__(FT, 4) sample_filtered_kernel(
     const E* __restrict__ logits, long long ld, int V, int nit, RowParams par, int rows_per_param,
     const float* __restrict__ u, int u_stride, int32_t* __restrict__ token_out,
     float* __restrict__ prob_out, int32_t* err) {
-  FilterShared& sh = shared();
+  auto& sh = RowFilter<FT>::shared();
   const int r = blockIdx.x, s = r / rows_per_param;
-  const Row<E> row(logits + (size_t)r * ld, V, nit);
+  const typename RowFilter<FT>::template Row<E> row(logits + (size_t)r * ld, V, nit);
   float uu = u[(size_t)s * u_stride + (r - s * rows_per_param)];
   if (!(uu > 0.0f)) uu = 0.0f;
-  filter_row(row, par, s, uu, err);
+  RowFilter<FT>::filter_row(row, par, s, uu, err);
   if (threadIdx.x == 0) {
     token_out[r] = sh.token;
     if (prob_out) prob_out[r] = sh.rc.total > 0.0 ? (float)(sh.w / sh.rc.total) : 0.0f;
@@ -1206,8 +1216,8 @@ __global__ void __launch_bounds__(FT) sample_filtered_kernel(
 }
 
 // Cuts of the verify rows (first S * (B + 1)) and draft rows (S * B) of a call.
-template <typename E>
-__global__ void __launch_bounds__(FT) filter_rows_kernel(
+template <int FT, typename E>
+__global__ void __launch_bounds__(FT, 4) filter_rows_kernel(
     const E* __restrict__ zv, long long vs, long long vld, const E* __restrict__ zd, long long ds,
     long long dld, int B, int nv, int V, int nit, RowParams par, RowCut* __restrict__ cuts,
     int32_t* err) {
@@ -1215,10 +1225,10 @@ __global__ void __launch_bounds__(FT) filter_rows_kernel(
   const int per = r < nv ? B + 1 : B, i = r < nv ? r : r - nv;
   const int s = i / per, j = i - s * per;
   const E* z = r < nv ? zv + (size_t)s * vs + (size_t)j * vld : zd + (size_t)s * ds + (size_t)j * dld;
-  const Row<E> row(z, V, nit);
-  filter_row(row, par, s, -1.0f, err);
+  const typename RowFilter<FT>::template Row<E> row(z, V, nit);
+  RowFilter<FT>::filter_row(row, par, s, -1.0f, err);
   if (threadIdx.x == 0) {
-    RowCut rc = shared().rc;
+    RowCut rc = RowFilter<FT>::shared().rc;
     rc.inv_total = rc.total > 0.0 ? 1.0 / rc.total : 0.0;
     cuts[r] = rc;
   }
@@ -1233,13 +1243,14 @@ __device__ __forceinline__ double prob_of(float z, int i, const RowCut& c) {
 // the final token from max(0, p - q) of the rejected draft's rows, or from the
 // last verify row.
 template <typename E>
-__global__ void __launch_bounds__(FT) accept_filtered_kernel(
+__global__ void __launch_bounds__(1024) accept_filtered_kernel(
     const E* __restrict__ zv, long long vs, long long vld, const E* __restrict__ zd, long long ds,
     long long dld, int S, int B, int V, int nit, const RowCut* __restrict__ cuts,
     const int32_t* __restrict__ draft, int draft_width, const float* __restrict__ u, int u_stride,
     int32_t* __restrict__ accept_len, int32_t* __restrict__ token_out, int token_stride,
     int at_accepted) {
-  FilterShared& sh = shared();
+  using F = RowFilter<1024>;
+  auto& sh = F::shared();
   const int s = blockIdx.x, tid = threadIdx.x;
   const RowCut* cv = cuts + (size_t)s * (B + 1);
   const RowCut* cd = cuts + (size_t)S * (B + 1) + (size_t)s * B;
@@ -1247,7 +1258,7 @@ __global__ void __launch_bounds__(FT) accept_filtered_kernel(
   const E* d = zd + (size_t)s * ds;
   if (tid == 0) sh.found = B;
   __syncthreads();
-  for (int j = tid; j < B; j += FT) {    // the first rejected draft
+  for (int j = tid; j < B; j += 1024) {    // the first rejected draft
     const int t = draft[(size_t)s * draft_width + j];
     bool ok = false;
     if (t >= 0 && t < V) {
@@ -1263,7 +1274,7 @@ __global__ void __launch_bounds__(FT) accept_filtered_kernel(
   float uu = u[(size_t)s * u_stride + B];
   if (!(uu > 0.0f)) uu = 0.0f;
   const RowCut p = cv[A];
-  const Row<E> row(v + (size_t)A * vld, V, nit);
+  const typename F::template Row<E> row(v + (size_t)A * vld, V, nit);
   const RowCut q = cd[A < B ? A : 0];
   const E* zq = d + (size_t)(A < B ? A : 0) * dld;
   int t = -1;
@@ -1277,8 +1288,8 @@ __global__ void __launch_bounds__(FT) accept_filtered_kernel(
     };
     double part = 0.0;
     row.each_from(p.z, [&](float z, int i) { part += rest(z, i); });
-    const double total = range_sums(part);
-    t = pick_index(row, rest, (double)uu * total);
+    const double total = F::range_sums(part);
+    t = F::pick_index(row, rest, (double)uu * total);
     __syncthreads();
   }
   if (t < 0) t = max(p.idx, 0);          // a row without a number above -inf
@@ -1292,9 +1303,18 @@ size_t filter_cuts_bytes(int S, int B) { return (size_t)S * (2 * B + 1) * sizeof
 
 // Vectors per lane of a row.
 template <typename E>
-static int row_vectors(int V) {
+static int row_vectors(int V, int threads) {
   const int epv = 16 / (int)sizeof(E);
-  return (V / epv + FT - 1) / FT;
+  return (V / epv + threads - 1) / threads;
+}
+
+// Calls f(threads): 1024 while every row has a CU of its own, else 512.
+template <typename F>
+static void by_rows(int rows, F f) {
+  if (rows <= device_cus())
+    f(IC<1024>{});
+  else
+    f(IC<512>{});
 }
 
 template <typename E>
@@ -1304,10 +1324,14 @@ static int launch_accept(const void* zv, long long vs, long long vld, const void
                          int32_t* accept_len, int32_t* token_out, int token_stride,
                          int at_accepted, int32_t* err, void* ws, hipStream_t st) {
   RowCut* cuts = (RowCut*)ws;
-  const int nit = row_vectors<E>(V);
-  hipLaunchKernelGGL(filter_rows_kernel<E>, dim3(S * (2 * B + 1)), dim3(FT), 0, st, (const E*)zv,
-                     vs, vld, (const E*)zd, ds, dld, B, S * (B + 1), V, nit, par, cuts, err);
-  hipLaunchKernelGGL(accept_filtered_kernel<E>, dim3(S), dim3(FT), 0, st, (const E*)zv, vs, vld,
+  by_rows(S * (2 * B + 1), [&](auto threads) {
+    constexpr int FT = decltype(threads)::value;
+    hipLaunchKernelGGL((filter_rows_kernel<FT, E>), dim3(S * (2 * B + 1)), dim3(FT), 0, st,
+                       (const E*)zv, vs, vld, (const E*)zd, ds, dld, B, S * (B + 1), V,
+                       row_vectors<E>(V, FT), par, cuts, err);
+  });
+  const int nit = row_vectors<E>(V, 1024);
+  hipLaunchKernelGGL(accept_filtered_kernel<E>, dim3(S), dim3(1024), 0, st, (const E*)zv, vs, vld,
                      (const E*)zd, ds, dld, S, B, V, nit, cuts, draft, draft_width, u, u_stride,
                      accept_len, token_out, token_stride, at_accepted);
   return launch_status("accept_sampled");
@@ -1317,9 +1341,12 @@ template <typename E>
 static void launch_sample(const void* logits, int rows, int V, long long ld, const RowParams& par,
                           int rows_per_param, const float* u, int u_stride, int32_t* token_out,
                           float* prob_out, int32_t* err, hipStream_t st) {
-  hipLaunchKernelGGL(sample_filtered_kernel<E>, dim3(rows), dim3(FT), 0, st, (const E*)logits, ld,
-                     V, row_vectors<E>(V), par, rows_per_param, u, u_stride, token_out, prob_out,
-                     err);
+  by_rows(rows, [&](auto threads) {
+    constexpr int FT = decltype(threads)::value;
+    hipLaunchKernelGGL((sample_filtered_kernel<FT, E>), dim3(rows), dim3(FT), 0, st,
+                       (const E*)logits, ld, V, row_vectors<E>(V, FT), par, rows_per_param, u,
+                       u_stride, token_out, prob_out, err);
+  });
 }
 
 int launch_sample_filtered(const void* logits, int dtype, int rows, int V, long long ld,

@@ -104,6 +104,23 @@ def test_large_vocabularies(dtype, kind, V):
     _check(z64, par, got_t.cpu().numpy(), got_p.cpu().numpy())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,kind", [(3, "levels"), (65, "masked"), (511, "flat"), (1025, "normal"),
+                                    (4099, "equal"), (8192, "normal"), (20011, "flat"),
+                                    (20011, "masked"), (9001, "spread"), (70001, "normal")])
+def test_more_rows_than_the_chip_runs_at_once(V, kind, dtype):
+    rows = 330
+    rng = np.random.default_rng([V, len(kind), 7])
+    zt, z64 = _rounded(_logits(kind, rows, V, rng), dtype)
+    par = _params(rows)
+    if kind in ("normal", "flat"):
+        par["T"] = np.where(rng.random(rows) < 0.8, rng.uniform(0.3, 1.5, rows),
+                            par["T"]).astype(np.float32)
+    par["u"] = np.where(rng.random(rows) < 0.8, rng.random(rows), par["u"]).astype(np.float32)
+    got_t, got_p = _call(zt, _dev(par))
+    _check(z64, par, got_t.cpu().numpy(), got_p.cpu().numpy())
+
+
 @pytest.mark.parametrize("name", ["none", "k", "p", "m", "kp", "T"])
 def test_each_filter_alone(name):
     rows, V = 16, 5003
