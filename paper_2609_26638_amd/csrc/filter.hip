@@ -18,9 +18,11 @@
 //      maxima over PARTS parts of its logits;
 //   2. a logit that no kept token lies below (parts_bound).  The parts' maxima
 //      are tokens: where their count reaches k, the row's does.  For top-p
-//      they are a sample: a maximum that a share q of the parts exceeds stands
-//      for 1 / (1 - q) tokens, and where the weights so counted reach a little
-//      more than the share p, the cut is likely above, which step 3 checks;
+//      they are a sample: one of s tokens that a share q of the parts exceeds
+//      stands for (1 - q)^(1/s - 1) tokens (a share x of all tokens exceeds it,
+//      (1 - x)^s = 1 - q, and (1 - x)^(s - 1) of its like are maxima), and
+//      where the weights so counted reach a little more than the share p, the
+//      cut is likely above, which step 3 checks;
 //   3. a second pass: the tokens from there up, as a list in LDS, and whether
 //      they do weigh the share p (otherwise, and where the list overflows,
 //      again from a bound that is sure: tokens of less than (1 - p) / V of the
@@ -51,7 +53,7 @@ namespace dvs {
 
 constexpr int RANK = 64;          // tokens that one wave ranks
 constexpr int SMALL = 256;        // tokens that the workgroup ranks
-constexpr int PARTS = 4;          // parts of a thread's logits
+constexpr int PARTS = 8;          // parts of a thread's logits
 constexpr int BATCH = 16;         // logits that a thread has in flight
 
 // What a row's filters keep: weight >= min_w of the tokens with z > cut.z, or
@@ -476,6 +478,46 @@ static __device__ __forceinline__ int pick_index(const Row<E>& row, F fn, double
   return at >= 0 ? at : block_reduce(lastpos, -1, Max(), sh.i);
 }
 
+// The tokens from `bound` (> -inf) up, as a list in LDS if at most LIST;
+// returns how many they are.
+template <typename E>
+static __device__ __forceinline__ int gather(const Row<E>& row, float bound) {
+  FilterShared& sh = shared();
+  if (threadIdx.x == 0) sh.n = 0;
+  __syncthreads();
+  row.batches([&](const u32x16& b, int it) {
+    uint32_t c = 0;
+#pragma unroll
+    for (int e = 0; e < BATCH; ++e) c += Row<E>::logit(b, e) >= bound;
+    if (!__ballot(c)) return;
+    const uint32_t incl = wave_scan(c, 0u, Add());   // a place for each, one count-in per wave
+    int at = 0;
+    if ((threadIdx.x & 63) == 63) at = atomicAdd(&sh.n, (int)incl);
+    at = at_lane(at, 63) + (int)(incl - c);
+    constexpr int EPV = Row<E>::EPV;
+#pragma unroll
+    for (int e = 0; e < BATCH; ++e) {
+      const float z = Row<E>::logit(b, e);
+      if (z >= bound) {
+        if (at < LIST) { sh.lz[at] = z; sh.li[at] = row.at(it + e / EPV) + e % EPV; }
+        ++at;
+      }
+    }
+  });
+  const int ri = row.rest_index();
+  if (ri >= 0) {
+    const float z = load_logit(row.p + ri);
+    if (z >= bound) {
+      const int at = atomicAdd(&sh.n, 1);
+      if (at < LIST) { sh.lz[at] = z; sh.li[at] = ri; }
+    }
+  }
+  __syncthreads();
+  const int n = uniform(sh.n);
+  __syncthreads();
+  return n;
+}
+
 // Every wave's range sum to sh.d; returns their sum, in order.
 static __device__ __forceinline__ double range_sums(double part) {
   FilterShared& sh = shared();
@@ -701,28 +743,20 @@ static __device__ NOINLINE void filter_row_again(const E* p, int V, int nit, int
   if (u >= 0.0f) draw_kept(p, V, nit, u);
 }
 
-// The same over the n <= LIST candidates in LDS.  found: shorten_list has left
-// its histogram's bin of the weight.
-template <typename E>
-static __device__ NOINLINE void filter_list(const E* p, int V, int nit, int n, float bound, int k,
-                                         double top_p, double whole, float u, bool found) {
+// The draw among the n tokens of the list, -1 if they weigh nothing or u < 0.
+// fixed(z, i): a token's weight, integers; 0 for tokens that are not in the
+// list.  They are added up in bins of the index, and the drawn bin's tokens
+// walked by one wave.
+template <typename E, typename F>
+static __device__ __forceinline__ int draw_list(const E* p, int V, int n, F fixed, float u,
+                                                unsigned long long& total) {
   FilterShared& sh = shared();
-  RowCut rc = sh.rc;
   const int tid = threadIdx.x;
-  const Row<E> row(p, V, nit);
-  const List list{n};
-  const Found so_far = found ? sh.so_far : Found{-1, 0, 0u, 0ull};
-  const double scale = 281474976710656.0;           // 2^48: LIST weights stay below 2^63
-  both_cuts(list, row, rc, n, bound, k, top_p, whole, scale, so_far);
-  // kept weights by index; a positive one counts for 1 at least
-  auto fixed = [&](float z, int i) -> unsigned long long {
-    const double w = kept_weight(z, i, rc);
-    return w > 0.0 ? max((unsigned long long)(w * scale + 0.5), 1ull) : 0ull;
-  };
   const int shift = max(0, 32 - BIN_BITS - __clz(V - 1));      // BINS bins over [0, V)
+  __syncthreads();
   sh.mass[tid] = 0;
   __syncthreads();
-  list.each([&](float z, int i) {
+  List{n}.each([&](float z, int i) {
     const unsigned long long w = fixed(z, i);
     if (w) atomicAdd(&sh.mass[i >> shift], w);
   });
@@ -731,14 +765,11 @@ static __device__ NOINLINE void filter_list(const E* p, int V, int nit, int n, f
   unsigned long long m = sh.mass[tid];
   const unsigned long long own = m;
   scan_bins(none, m);
-  if (tid == BINS - 1) {
-    sh.fm = m;
-    rc.total = (double)m / scale;
-    sh.rc = rc;
-  }
+  if (tid == BINS - 1) sh.fm = m;
   __syncthreads();
-  if (u < 0.0f) return;
-  const double t = (double)u * (double)sh.fm;
+  total = sh.fm;
+  if (u < 0.0f || !total) return -1;
+  const double t = (double)u * (double)total;
   int b = first_index(own && (double)m > t, tid, -1);
   const bool past = b < 0;                          // u = 1, or by rounding: the last token
   if (past) b = BINS - 1 - first_index(own > 0, BINS - 1 - tid, 0);
@@ -767,8 +798,38 @@ static __device__ NOINLINE void filter_list(const E* p, int V, int nit, int n, f
           acc += fixed(load_logit(p + i), i);
           if ((double)acc > t) { at = i; break; }
         }
-      sh.token = at;
-      sh.w = kept_weight(load_logit(p + at), at, rc);
+      sh.i[0] = at;
+    }
+  }
+  __syncthreads();
+  return uniform(sh.i[0]);
+}
+
+// The same over the n <= LIST candidates in LDS.  found: shorten_list has left
+// its histogram's bin of the weight.
+template <typename E>
+static __device__ NOINLINE void filter_list(const E* p, int V, int nit, int n, float bound, int k,
+                                         double top_p, double whole, float u, bool found) {
+  FilterShared& sh = shared();
+  RowCut rc = sh.rc;
+  const Row<E> row(p, V, nit);
+  const List list{n};
+  const Found so_far = found ? sh.so_far : Found{-1, 0, 0u, 0ull};
+  const double scale = 281474976710656.0;           // 2^48: LIST weights stay below 2^63
+  both_cuts(list, row, rc, n, bound, k, top_p, whole, scale, so_far);
+  // a positive weight counts for 1 at least
+  auto fixed = [&](float z, int i) -> unsigned long long {
+    const double w = kept_weight(z, i, rc);
+    return w > 0.0 ? max((unsigned long long)(w * scale + 0.5), 1ull) : 0ull;
+  };
+  unsigned long long total;
+  const int t = draw_list(p, V, n, fixed, u, total);
+  if (threadIdx.x == 0) {
+    rc.total = (double)total / scale;
+    sh.rc = rc;
+    if (u >= 0.0f) {
+      sh.token = t;
+      sh.w = t < 0 ? 0.0 : kept_weight(load_logit(p + t), t, rc);
     }
   }
   __syncthreads();
@@ -912,41 +973,40 @@ static __device__ NOINLINE bool filter_small(int n, int k, double top_p, double 
 // of them.  The lower edge of the histogram bin where their count reaches k,
 // or their weight, each taken for the tokens that it stands for, `target`;
 // -FLT_MAX if it does not, or where a part stands for too many.
-static __device__ __forceinline__ float parts_bound(const float (&part)[PARTS], const RowCut& rc, float lo,
-                                             int k, float target) {
+static __device__ __forceinline__ float parts_bound(const float (&part)[PARTS], const RowCut& rc,
+                                                    int V, float lo, int k, float target) {
   FilterShared& sh = shared();
   const int tid = threadIdx.x;
   if (!(lo < rc.zmax)) return -FLT_MAX;
   // (linear bins would be one bin where tokens are masked by a lowest number)
   const Binning bin(rc.zmax, lo, rc.zmax * 0.5f - lo * 0.5f <= 32.0f * (fabsf(rc.zmax) + 1.0f));
-  const float scale = 262144.0f, log2e_t = (float)rc.log2e_t;   // 2^18: sums below 2^31
-  uint32_t* mass = (uint32_t*)sh.mass;
-  sh.cnt[tid] = 0;
-  mass[tid] = 0;
+  // a bin: its count above 40 bits of weight, in 2^-26 (at most 2^13 parts)
+  const float scale = 67108864.0f, log2e_t = (float)rc.log2e_t;
+  sh.mass[tid] = 0;
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < PARTS; ++j) {
     if (part[j] > -INFINITY) {
-      const int b = bin(part[j]);
-      atomicAdd(&sh.cnt[b], 1u);
-      if (!k)
-        atomicAdd(&mass[b],
-                  (uint32_t)(__builtin_amdgcn_exp2f((part[j] - rc.zmax) * log2e_t) * scale));
+      const float w = __builtin_amdgcn_exp2f((part[j] - rc.zmax) * log2e_t) * scale;
+      atomicAdd(&sh.mass[bin(part[j])], (1ull << 40) | (uint32_t)w);
     }
   }
   __syncthreads();
-  uint32_t c = sh.cnt[tid];
-  unsigned long long m = mass[tid];
+  const unsigned long long got = sh.mass[tid];
+  uint32_t c = (uint32_t)(got >> 40);
+  unsigned long long m = 0;
   scan_bins(c, m);
   bool there = c >= (uint32_t)k;
   if (!k) {
     if (tid == FT - 1) sh.fc = c;
-    const float own = (float)mass[tid];
+    const float own = (float)(got & ((1ull << 40) - 1));
     __syncthreads();
-    const float left = 1.0f - (float)c * __builtin_amdgcn_rcpf((float)sh.fc);
-    // parts that more than four fifths exceed say little
-    uint32_t few = left < 0.2f;
-    m = few ? 0ull : (unsigned long long)(own * __builtin_amdgcn_rcpf(left));
+    const float parts = (float)sh.fc;
+    const float left = 1.0f - (float)c * __builtin_amdgcn_rcpf(parts);
+    // parts that more than nine tenths exceed say little
+    uint32_t few = left < 0.1f;
+    const float others = 1.0f - parts / (float)V;
+    m = few ? 0ull : (unsigned long long)(own * __builtin_amdgcn_exp2f(-others * __builtin_amdgcn_logf(left)));
     scan_bins(few, m);
     there = !few && (float)m >= target * scale;
   }
@@ -1122,7 +1182,7 @@ static __device__ __forceinline__ void filter_row(const Row<E>& row, const RowPa
   const int kk = need_k ? k : 0;
   // (a third of the way from the share p to all: room for the sample's error)
   float sure = -FLT_MAX;
-  bound = parts_bound(part, rc, lo, kk, (float)(target + 0.3 * (whole - target)));
+  bound = parts_bound(part, rc, V, lo, kk, (float)(target + 0.3 * (whole - target)));
   if (!need_k) {
     // tokens of less than (1 - p) / V of the weight each cannot hold 1 - p of it
     sure = weight_bound(hi, (double)T, (1.0 - fmax(top_p, 0.0)) * whole / (double)V);
@@ -1132,37 +1192,10 @@ static __device__ __forceinline__ void filter_row(const Row<E>& row, const RowPa
   // bounds: 0 the parts', 1 the sure one, 2 the row's
   for (int level = bound > sure || need_k ? 0 : bound > -FLT_MAX ? 1 : 2;;) {
     if (level == 1) bound = sure;
-    if (tid == 0) { sh.n = 0; sh.rc = rc; }
+    if (tid == 0) sh.rc = rc;
     __syncthreads();
     if (level == 2) bound = row_bound(row.p, V, row.nit, sure, kk, target * (1.0 + 1e-9));
-    row.batches([&](const u32x16& b, int it) {
-      uint32_t c = 0;
-#pragma unroll
-      for (int e = 0; e < BATCH; ++e) c += Row<E>::logit(b, e) >= bound;
-      if (!__ballot(c)) return;
-      const uint32_t incl = wave_scan(c, 0u, Add());   // a place for each, one count-in per wave
-      int at = 0;
-      if ((tid & 63) == 63) at = atomicAdd(&sh.n, (int)incl);
-      at = at_lane(at, 63) + (int)(incl - c);
-#pragma unroll
-      for (int e = 0; e < BATCH; ++e) {
-        const float z = Row<E>::logit(b, e);
-        if (z >= bound) {
-          if (at < LIST) { sh.lz[at] = z; sh.li[at] = row.at(it + e / EPV) + e % EPV; }
-          ++at;
-        }
-      }
-    });
-    if (ri >= 0) {
-      const float z = load_logit(row.p + ri);
-      if (z >= bound) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < LIST) { sh.lz[at] = z; sh.li[at] = ri; }
-      }
-    }
-    __syncthreads();
-    int n = uniform(sh.n);
-    __syncthreads();
+    int n = gather(row, bound);
     if (n > LIST && level < 2) {
       level = 2;
       continue;
@@ -1278,18 +1311,30 @@ __global__ void __launch_bounds__(1024) accept_filtered_kernel(
   const RowCut q = cd[A < B ? A : 0];
   const E* zq = d + (size_t)(A < B ? A : 0) * dld;
   int t = -1;
+  // the tokens of p, if they fit (no row without a number above -inf)
+  int n = F::LIST + 1;
+  if (p.single >= 0 && (p.z > -FLT_MAX || V <= F::LIST)) n = F::gather(row, p.z);
   // p - q, or p alone: after B acceptances, and where p and q are equal to the
   // last bit
-  for (int step = A < B ? 0 : 1; step < 2 && t < 0; ++step) {
+  for (int step = A < B ? 0 : 1; step < 2 && t < 0 && p.single >= 0; ++step) {
     auto rest = [&](float z, int i) {
       double a = i < V ? prob_of(z, i, p) : 0.0;
       if (step == 0 && a > 0.0) a = fmax(a - prob_of(load_logit(zq + i), i, q), 0.0);
       return a;
     };
-    double part = 0.0;
-    row.each_from(p.z, [&](float z, int i) { part += rest(z, i); });
-    const double total = F::range_sums(part);
-    t = F::pick_index(row, rest, (double)uu * total);
+    if (n <= F::LIST) {
+      auto fixed = [&](float z, int i) -> unsigned long long {   // sums of up to 1
+        const double a = rest(z, i);
+        return a > 0.0 ? max((unsigned long long)(a * 1152921504606846976.0 + 0.5), 1ull) : 0ull;
+      };
+      unsigned long long total;
+      t = F::draw_list(v + (size_t)A * vld, V, n, fixed, uu, total);
+    } else {
+      double part = 0.0;
+      row.each_from(p.z, [&](float z, int i) { part += rest(z, i); });
+      const double total = F::range_sums(part);
+      t = F::pick_index(row, rest, (double)uu * total);
+    }
     __syncthreads();
   }
   if (t < 0) t = max(p.idx, 0);          // a row without a number above -inf
