@@ -886,14 +886,16 @@ static __device__ NOINLINE int shorten_list(int n, float bound, bool by_mass, in
   return left;
 }
 
-// Both cuts and the draw over the n <= SMALL candidates in LDS.  A token is
-// kept by top-k if fewer than k are ahead of it, by top-p if the weight ahead
-// of it is below the target; a drawn one is the lowest whose running weight in
-// index order exceeds u * total.  Both take a comparison of every pair: the
-// waves share the candidates out as (64 of them, a part of the others) and add
-// up in LDS.  whole: the weight that top-p is a share of, < 0: that of the k
-// tokens.  u < 0: no draw.  check: false if the candidates do not weigh that
-// share.
+// Both cuts and the draw over the n <= SMALL candidates in LDS.  Every pair is
+// compared, by logit and by index (the waves share the candidates out as 64 of
+// them and a part of the others), which gives the tokens' places in both
+// orders.  In the first, scanned weights give the cuts: kept by top-k are the
+// first k, by top-p those whose weight ahead is below the target.  In the
+// second, the lowest kept token whose running weight exceeds u * total is
+// drawn.  (Adding up weights in the comparisons in place of the two scans: 32000
+// cycles for 219 candidates, two rows to a CU.)  whole: the weight that top-p is
+// a share of, < 0: that of the k tokens.  u < 0: no draw.  check: false if the
+// candidates do not weigh that share.
 static __device__ NOINLINE bool filter_small(int n, int k, double top_p, double whole, float u,
                                             bool check) {
   FilterShared& sh = shared();
@@ -902,68 +904,89 @@ static __device__ NOINLINE bool filter_small(int n, int k, double top_p, double 
   const double scale = 18014398509481984.0;    // 2^54: SMALL weights stay below 2^63
   unsigned long long* key = sh.mass;           // larger logit, then lower index, first
   unsigned long long* w = sh.mass + SMALL;
-  unsigned long long* sum = sh.mass + 2 * SMALL;
-  uint32_t* rank = sh.cnt;
+  float* zi = (float*)(sh.mass + 2 * SMALL);
+  uint32_t *places = sh.cnt, *after = sh.cnt + SMALL;
   float z = 0.f;
   int idx = 0;
-  double x = 0.0;
   unsigned long long own = 0;
+  uint32_t heavy = 0;                          // not below min_p
   if (tid < n) {
     z = sh.lz[tid];
     idx = sh.li[tid];
-    x = weight(z, rc);
+    const double x = weight(z, rc);
     own = x > 0.0 ? max((unsigned long long)(x * scale + 0.5), 1ull) : 0ull;
+    heavy = x >= (double)rc.min_w;
     key[tid] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~idx;
-    w[tid] = own;
   }
-  if (tid < SMALL) { rank[tid] = 0; sum[tid] = 0; }
+  if (tid < SMALL) places[tid] = 0;
   __syncthreads();
   const int groups = (n + 63) >> 6, parts = FW / groups;   // waves: part * groups + group
   const int part = wv / groups, cand = (wv - part * groups) * 64 + lane;
-  const bool works = part < parts && cand < n;
-  const unsigned long long mine = works ? key[cand] : ~0ull;
-  if (works) {
-    uint32_t r = 0;
-    unsigned long long a = 0;
-#pragma unroll 2
+  if (part < parts && cand < n) {
+    const unsigned long long mine = key[cand];
+    uint32_t ahead = 0, lower = 0;
+#pragma unroll 4
     for (int j = part; j < n; j += parts) {
-      const bool ahead = key[j] > mine;
-      r += ahead;
-      a += ahead ? w[j] : 0ull;
+      const unsigned long long other = key[j];
+      ahead += other > mine;
+      lower += (uint32_t)other > (uint32_t)mine;           // ~index
     }
-    atomicAdd(&rank[cand], r);
-    atomicAdd(&sum[cand], a);
+    atomicAdd(&places[cand], ahead | lower << 16);
   }
   __syncthreads();
-  const int r = tid < n ? (int)rank[tid] : SMALL;
-  const unsigned long long ahead = tid < n ? sum[tid] : 0;
-  bool kept = r < k;
+  if (tid < n) {
+    const uint32_t both = places[tid], r = both & 0xffffu;
+    sh.lz[r] = z;
+    sh.li[r] = idx;
+    w[r] = own;
+    after[r] = both >> 16 | heavy << 31;
+  }
+  __syncthreads();
+  // thread t: the t-th token by logit
+  const int first_k = min(k, n);
+  uint32_t at = 0, none = 0;
+  own = 0;
+  if (tid < n) {
+    z = sh.lz[tid];
+    idx = sh.li[tid];
+    own = w[tid];
+    at = after[tid];
+  }
+  bool kept = tid < first_k, next = tid + 1 < first_k;
   if (top_p < 1.0) {
-    const double sum_k = (double)block_reduce(kept ? own : 0ull, 0ull, Add(), sh.u);
-    const double all = whole < 0.0 ? sum_k : whole * scale;
-    if (check && sum_k < fmax(top_p, 0.0) * all) return false;
-    kept = kept && (r == 0 || (double)ahead < fmax(top_p, 0.0) * all);
+    unsigned long long run = own;
+    scan_bins(none, run);
+    if (tid == first_k - 1) sh.fm = run;
+    __syncthreads();
+    const double sum_k = (double)sh.fm;
+    const double target = fmax(top_p, 0.0) * (whole < 0.0 ? sum_k : whole * scale);
+    if (check && sum_k < target) return false;
+    next = next && (double)run < target;
+    kept = kept && (tid == 0 || (double)(run - own) < target);
   }
-  const int last = block_reduce(kept ? r : -1, -1, Max(), sh.i);
-  if (r == last) { sh.rc.z = z; sh.rc.idx = idx; }
-  if (!(kept && (x >= (double)rc.min_w || r == 0))) own = 0;
-  const unsigned long long total = block_reduce(own, 0ull, Add(), sh.u);
+  if (kept && !next) { sh.rc.z = z; sh.rc.idx = idx; }     // the last one
+  if (!(kept && (at >> 31 || tid == 0))) own = 0;
+  if (u < 0.0f) {
+    const unsigned long long total = block_reduce(own, 0ull, Add(), sh.u);
+    if (tid == 0) sh.rc.total = (double)total / scale;
+    __syncthreads();
+    return true;
+  }
+  at &= 0xffffu;
+  if (tid < n) { key[at] = own; places[at] = idx; zi[at] = z; }
+  __syncthreads();
+  // thread t: the t-th by index
+  own = tid < n ? key[tid] : 0;
+  idx = tid < n ? (int)places[tid] : 0;
+  unsigned long long run = own;
+  scan_bins(none, run);
+  if (tid == n - 1) sh.fm = run;
+  __syncthreads();
+  const unsigned long long total = sh.fm;
   if (tid == 0) sh.rc.total = (double)total / scale;
-  if (tid < n) { w[tid] = own; sum[tid] = 0; }
-  __syncthreads();
-  if (u < 0.0f) return true;
-  if (works) {
-    unsigned long long a = 0;
-    const uint32_t lim = (uint32_t)mine;       // ~index: the lower the index, the larger
-#pragma unroll 2
-    for (int j = part; j < n; j += parts) a += (uint32_t)key[j] >= lim ? w[j] : 0ull;
-    atomicAdd(&sum[cand], a);
-  }
-  __syncthreads();
-  const bool over = own > 0 && (double)sum[tid < n ? tid : 0] > (double)u * (double)total;
-  int token = first_index(over, idx, -1);
+  int token = first_index(own > 0 && (double)run > (double)u * (double)total, idx, -1);
   if (token < 0) token = block_reduce(own > 0 ? idx : -1, -1, Max(), sh.i);
-  if (own > 0 && idx == token) { sh.token = token; sh.w = x; }
+  if (own > 0 && idx == token) { sh.token = token; sh.w = weight(zi[tid], rc); }
   __syncthreads();
   return true;
 }
