@@ -246,8 +246,9 @@ int top1_confidence(const void* logits, int32_t dtype, int32_t rows, int32_t V,
  *   u [rows] fp32 uniforms in [0, 1) (the caller draws them)
  *   token_out [rows] int32, prob_out [rows] fp32 (may be NULL); err_word may
  *           be NULL.
- * A row's result does not depend on the other rows.  Requirements: rows >= 1,
- * 1 <= V <= 2^22, rows % rows_per_param == 0.
+ * A row's result does not depend on the other rows' values (their number may
+ * change the order in which its 64-bit weights are added up).  Requirements:
+ * rows >= 1, 1 <= V <= 2^22, rows % rows_per_param == 0.
  * ---------------------------------------------------------------------- */
 int sample_filtered(const void* logits, int32_t dtype, int32_t rows, int32_t V, int64_t ld,
                     const float* temperature, const int32_t* top_k, const float* top_p,

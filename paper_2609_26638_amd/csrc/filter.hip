@@ -9,7 +9,7 @@
 // with weight w = exp((z - max z) / T) in 64 bits: the running sums of a
 // vocabulary of 65536 are compared with u * total at every token, and sums of
 // 32-bit weights (1e-7 relative) would draw a neighbour for one row in a few
-// hundred.  64-bit adds and multiplies run at the 32-bit rate on this chip.
+// hundred.  (A 64-bit FMA takes 4.3 cycles per wave, a 32-bit one 2.7.)
 //
 // One workgroup per row (RowFilter).  Wave w owns one contiguous range of
 // the row, so the ranges' sums are in index order.
@@ -41,7 +41,16 @@
 // in 10,000), so the rest is kept small, and out of line where it is rare.
 // Weights that atomics or an unordered list add up are fixed-point integers,
 // whose sums do not depend on the order; the other sums have a fixed order.
-// Results do not depend on timing, nor on the other rows of the call.
+// Results do not depend on timing, nor on the other rows of the call (the
+// number of rows may choose another order of the 64-bit sums).
+//
+// What bounds it, at V = 65536 f32, in cycles of 65,000 (n of 80) to 105,000
+// (n of 7500): the first pass 31,000 where it sums weights (21,000 of them the
+// 64-bit exponentials), 10,000 where it does not; the bound 9,000; the second
+// pass 12,000 to 19,000 (the rows of an XCD's CUs together exceed its L2); then
+// 12,000 for a short list, which is barriers and LDS latency, up to 45,000 for a
+// long one.  136 such rows: 49 us, 0.73 TB/s of logits read once; 1024 rows of
+// bf16 with top-k, two to a CU: 65 us, 2.1 TB/s.
 #include <float.h>
 #include <math.h>
 
@@ -239,9 +248,8 @@ __device__ __forceinline__ float weight_bound(float hi, double T, double w) {
                -FLT_MAX);
 }
 
-// A row by a workgroup of FT threads: 1024 (one workgroup per CU, for calls of
-// few rows, where a row's latency counts) or 512 (two per CU, so that the
-// latencies of one row run under the passes of the other).
+// A row by a workgroup of FT threads: 1024 (one workgroup per CU) or 512 (two
+// per CU, so that the latencies of one row run under the passes of the other).
 template <int FT>
 struct RowFilter {
 
@@ -259,7 +267,6 @@ struct FilterShared {
   uint32_t c[FW];
   float f[FW], g[FW];
   int i[FW];
-  int pick[2];
   int found, n, token;
   uint32_t fc;
   unsigned long long fm;
@@ -1376,13 +1383,19 @@ static int row_vectors(int V, int threads) {
   return (V / epv + threads - 1) / threads;
 }
 
-// Calls f(threads): 1024 while every row has a CU of its own, else 512.
+// Calls f(threads): 1024, or 512 where rows wait for a CU and top-k keeps the
+// lists short (a list of 512 threads is half as long, and a flat row of top-p
+// alone outgrows it).  V = 65536, us with 1024 / 512 threads:
+//   rows           256 f32, top-p   1024 f32, top-p   1024 f32, top-k   1024 bf16, top-k
+//                     58 / 102         169 / 211         103 / 99           80 / 65
+// (one row 27 / 26, 32 rows of top-p 43 / 51; 1024 f32 rows without a filter
+// 94 / 97, with min-p 102 / 112).
 template <typename F>
-static void by_rows(int rows, F f) {
-  if (rows <= device_cus())
-    f(IC<1024>{});
-  else
+static void by_rows(int rows, const RowParams& par, F f) {
+  if (rows > device_cus() && par.top_k)
     f(IC<512>{});
+  else
+    f(IC<1024>{});
 }
 
 template <typename E>
@@ -1392,7 +1405,7 @@ static int launch_accept(const void* zv, long long vs, long long vld, const void
                          int32_t* accept_len, int32_t* token_out, int token_stride,
                          int at_accepted, int32_t* err, void* ws, hipStream_t st) {
   RowCut* cuts = (RowCut*)ws;
-  by_rows(S * (2 * B + 1), [&](auto threads) {
+  by_rows(S * (2 * B + 1), par, [&](auto threads) {
     constexpr int FT = decltype(threads)::value;
     hipLaunchKernelGGL((filter_rows_kernel<FT, E>), dim3(S * (2 * B + 1)), dim3(FT), 0, st,
                        (const E*)zv, vs, vld, (const E*)zd, ds, dld, B, S * (B + 1), V,
@@ -1409,7 +1422,7 @@ template <typename E>
 static void launch_sample(const void* logits, int rows, int V, long long ld, const RowParams& par,
                           int rows_per_param, const float* u, int u_stride, int32_t* token_out,
                           float* prob_out, int32_t* err, hipStream_t st) {
-  by_rows(rows, [&](auto threads) {
+  by_rows(rows, par, [&](auto threads) {
     constexpr int FT = decltype(threads)::value;
     hipLaunchKernelGGL((sample_filtered_kernel<FT, E>), dim3(rows), dim3(FT), 0, st,
                        (const E*)logits, ld, V, row_vectors<E>(V, FT), par, rows_per_param, u,
