@@ -273,6 +273,8 @@ struct FilterShared {
   double w;
   RowCut rc;
   Found so_far;
+  float lo, hi;
+  int inside;
 };
 
 // The workgroup's LDS, for the functions that are kept out of line too.
@@ -485,17 +487,22 @@ static __device__ __forceinline__ int pick_index(const Row<E>& row, F fn, double
   return at >= 0 ? at : block_reduce(lastpos, -1, Max(), sh.i);
 }
 
-// The tokens from `bound` (> -inf) up, as a list in LDS if at most LIST;
-// returns how many they are.
-template <typename E>
-static __device__ __forceinline__ int gather(const Row<E>& row, float bound) {
+// The tokens for which in(z) holds (not for -inf), as a list in LDS if at most
+// LIST; returns how many they are.  each(z): called for all of the row (-inf for
+// absent ones).
+template <typename E, typename I, typename F>
+static __device__ __forceinline__ int gather(const Row<E>& row, I in, F each) {
   FilterShared& sh = shared();
   if (threadIdx.x == 0) sh.n = 0;
   __syncthreads();
   row.batches([&](const u32x16& b, int it) {
     uint32_t c = 0;
 #pragma unroll
-    for (int e = 0; e < BATCH; ++e) c += Row<E>::logit(b, e) >= bound;
+    for (int e = 0; e < BATCH; ++e) {
+      const float z = Row<E>::logit(b, e);
+      each(z);
+      c += in(z);
+    }
     if (!__ballot(c)) return;
     const uint32_t incl = wave_scan(c, 0u, Add());   // a place for each, one count-in per wave
     int at = 0;
@@ -505,7 +512,7 @@ static __device__ __forceinline__ int gather(const Row<E>& row, float bound) {
 #pragma unroll
     for (int e = 0; e < BATCH; ++e) {
       const float z = Row<E>::logit(b, e);
-      if (z >= bound) {
+      if (in(z)) {
         if (at < LIST) { sh.lz[at] = z; sh.li[at] = row.at(it + e / EPV) + e % EPV; }
         ++at;
       }
@@ -514,7 +521,8 @@ static __device__ __forceinline__ int gather(const Row<E>& row, float bound) {
   const int ri = row.rest_index();
   if (ri >= 0) {
     const float z = load_logit(row.p + ri);
-    if (z >= bound) {
+    each(z);
+    if (in(z)) {
       const int at = atomicAdd(&sh.n, 1);
       if (at < LIST) { sh.lz[at] = z; sh.li[at] = ri; }
     }
@@ -523,6 +531,11 @@ static __device__ __forceinline__ int gather(const Row<E>& row, float bound) {
   const int n = uniform(sh.n);
   __syncthreads();
   return n;
+}
+// The tokens from `lo` up.
+template <typename E>
+static __device__ __forceinline__ int gather(const Row<E>& row, float lo) {
+  return gather(row, [=](float z) { return z >= lo; }, [](float) {});
 }
 
 // Every wave's range sum to sh.d; returns their sum, in order.
@@ -1048,9 +1061,12 @@ static __device__ __forceinline__ float parts_bound(const float (&part)[PARTS], 
 // not hold enough.  No weights: a bin adds up its tokens' count and, in 2^-16
 // of the bin's width, how far they lie below its upper edge, rounded up.  As
 // exp is convex, the count times the weight at their mean is no more than they
-// weigh, and less by (width / T)^2 / 24 at most.
+// weigh, and less by (width / T)^2 / 8 at most.  sh.lo: the bound; sh.found: how
+// many tokens reach it (about; V + 1: the row ends before the target).  For
+// top-p also sh.hi, a logit from which the tokens up weigh less than the target,
+// and sh.inside, how many lie between the two.
 template <typename E>
-static __device__ NOINLINE float row_bound(const E* p, int V, int nit, float bound, int k, double target) {
+static __device__ __forceinline__ void row_bound(const E* p, int V, int nit, float bound, int k, double target) {
   FilterShared& sh = shared();
   const RowCut rc = sh.rc;
   const int tid = threadIdx.x;
@@ -1087,11 +1103,104 @@ static __device__ NOINLINE float row_bound(const E* p, int V, int nit, float bou
     // whose weights reach this far)
     m = (unsigned long long)(count * weight(z, rc) * (1.0 - 1e-5) * scale);
   }
-  uint32_t none = 0;
-  scan_bins(none, m);
+  uint32_t c = (uint32_t)(got >> 40);
+  scan_bins(c, m);
   const bool there = k ? m >= (unsigned long long)k : (double)m >= target * scale;
   const int at = first_index(there, tid, -1);
-  return at < 0 ? bound : fmaxf(bound, bin.lower_edge(at));
+  int over = 0;                                     // the bins before may be above
+  if (!k && bin.linear) {
+    const double h = 1.3863 * (double)bin.width * rc.log2e_t;
+    over = first_index((double)m * (1.0 + 0.125 * h * h + 1e-4) >= target * scale, tid, 0);
+  }
+  if (tid == 0) {
+    sh.inside = sh.found = V + 1;
+    sh.hi = over ? bin.lower_edge(over - 1) : INFINITY;
+  }
+  __syncthreads();
+  if (tid == at) sh.found = (int)c;
+  if (tid == over - 1) sh.fc = c;
+  __syncthreads();
+  if (tid == 0) {
+    if (at >= 0) sh.inside = sh.found - (over ? (int)sh.fc : 0);
+    sh.lo = at < 0 ? bound : fmaxf(bound, bin.lower_edge(at));
+  }
+  __syncthreads();
+}
+
+// The weight of min-p's tokens, none of them below `bound`.
+template <typename E>
+static __device__ __forceinline__ double min_p_sum(const Row<E>& row, const RowCut& rc,
+                                                   float bound) {
+  double kept = 0.0;
+  row.each_from(bound, [&](float z, int) {
+    const double w = weight(z, rc);
+    kept += w >= (double)rc.min_w ? w : 0.0;
+  });
+  return range_sums(kept);
+}
+
+// Bound (sh.lo) and, for a flat row of top-p, the cut and the draw: the tokens
+// from sh.hi up, too many for a list, are added up, those of [sh.lo, sh.hi) are
+// the list.  Where min-p's tokens weigh less than the target, they are kept.
+// false if there is no cut yet.  65536 normal logits of sigma / T about 0.6, one
+// row: 56 us, 124 by filter_row_again (26 where a list holds the cut).
+template <typename E>
+static __device__ NOINLINE bool filter_flat(const E* p, int V, int nit, float sure, int k,
+                                            double target, float u) {
+  FilterShared& sh = shared();
+  RowCut rc = sh.rc;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const Row<E> row(p, V, nit);
+  row_bound(p, V, nit, sure, k, target * (1.0 + 1e-9));
+  const float lo = uniform(sh.lo), hi = uniform(sh.hi);
+  if (k || uniform(sh.found) <= LIST) return false;
+  if (rc.min_w > 0.0f && uniform(sh.found) > V) {
+    const double kept = min_p_sum(row, rc, lo);
+    if (!(kept < target)) return false;
+    rc.z = lo;
+    rc.total = kept;
+    if (tid == 0) sh.rc = rc;
+    __syncthreads();
+    if (u >= 0.0f) draw_kept(p, V, nit, u);
+    return true;
+  }
+  if (uniform(sh.inside) > LIST) return false;
+  const double floor = -1000.0 / rc.log2e_t;        // 2^-1000 stands for less
+  double part = 0.0;
+  const double top = (double)rc.zmax;
+  const int n = gather(
+      row, [=](float z) { return z >= lo && z < hi; },
+      [&](float z) {
+        const double w = exp2_normal(fmax((double)z - top, floor), rc.log2e_t);
+        part += z >= hi ? w : 0.0;
+      });
+  const double above = range_sums(part);
+  if (n < 1 || n > LIST || !(above < target)) return false;
+  const double range = lane < FW ? sh.d[lane] : 0.0;
+  const double scale = ldexp(1.0, __clz(V) + 30);   // V weights stay below 2^62
+  const List list{n};
+  const Cut cut = select_cut(list, row, rc, scale, n, fminf(hi, rc.zmax), lo, true, true, 0u,
+                             target * scale,
+                             Found{-1, 0, 0u, (unsigned long long)(above * scale + 0.5)});
+  if ((double)cut.mass < target * scale || weight(cut.z, rc) < (double)rc.min_w) return false;
+  rc.z = cut.z;
+  rc.idx = cut.idx;
+  // the kept weight of each wave's range
+  if (tid < FW) sh.mass[tid] = 0;
+  __syncthreads();
+  const int span = nit * 64 * Row<E>::EPV, whole = V / Row<E>::EPV * Row<E>::EPV;
+  list.each([&](float z, int i) {
+    if (before_cut(z, i, rc))
+      atomicAdd(&sh.mass[i < whole ? i / span : FW - 1], fixed_weight(z, rc, 281474976710656.0));
+  });
+  __syncthreads();
+  const double kept = lane < FW ? range + (double)sh.mass[lane] * 3.552713678800501e-15 : 0.0;
+  if (tid < FW) sh.d[tid] = kept;
+  rc.total = at_lane(row_scan(kept, 0.0, Add()), FW - 1);
+  if (tid == 0) sh.rc = rc;
+  __syncthreads();
+  if (u >= 0.0f) draw_kept(p, V, nit, u);
+  return true;
 }
 
 // Reads a row, finds what its filters keep (sh.rc) and, for u >= 0, draws a
@@ -1194,12 +1303,7 @@ static __device__ __forceinline__ void filter_row(const Row<E>& row, const RowPa
   if (!need_k && !need_p) {
     if (rc.min_w > 0.0f) {
       bound = weight_bound(hi, (double)T, (double)rc.min_w);
-      double kept = 0.0;
-      row.each_from(bound, [&](float z, int) {
-        const double w = weight(z, rc);
-        kept += w >= (double)rc.min_w ? w : 0.0;
-      });
-      whole = range_sums(kept);
+      whole = min_p_sum(row, rc, bound);
     }
     rc.z = bound;
     rc.total = whole;
@@ -1222,9 +1326,12 @@ static __device__ __forceinline__ void filter_row(const Row<E>& row, const RowPa
   // bounds: 0 the parts', 1 the sure one, 2 the row's
   for (int level = bound > sure || need_k ? 0 : bound > -FLT_MAX ? 1 : 2;;) {
     if (level == 1) bound = sure;
-    if (tid == 0) sh.rc = rc;
-    __syncthreads();
-    if (level == 2) bound = row_bound(row.p, V, row.nit, sure, kk, target * (1.0 + 1e-9));
+    if (tid == 0) sh.rc = rc;                  // (seen after gather)
+    if (level == 2) {
+      __syncthreads();
+      if (filter_flat(row.p, V, row.nit, sure, kk, target, u)) return;
+      bound = uniform(sh.lo);
+    }
     int n = gather(row, bound);
     if (n > LIST && level < 2) {
       level = 2;

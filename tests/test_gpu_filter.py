@@ -121,6 +121,27 @@ def test_more_rows_than_the_chip_runs_at_once(V, kind, dtype):
     _check(z64, par, got_t.cpu().numpy(), got_p.cpu().numpy())
 
 
+@pytest.mark.parametrize("dtype,V,rows,step", [("f32", 65536, 40, 0.0), ("bf16", 40007, 40, 0.0),
+                                               ("f32", 17003, 40, 0.0), ("f32", 40007, 40, 0.25),
+                                               ("f32", 65536, 40, 2.0), ("bf16", 20011, 300, 0.0),
+                                               ("f32", 9007, 300, 0.5)])
+def test_flat_rows_keep_more_than_a_list(V, rows, step, dtype):
+    """Top-p over rows whose kept tokens are many thousands: cut by top-p, by
+    min-p where it leaves less, by either; steps of equal logits; half masked."""
+    rng = np.random.default_rng([V, rows, 17])
+    z = rng.standard_normal((rows, V)) * rng.choice([0.1, 0.5, 1.0, 2.0], (rows, 1))
+    if step:
+        z = np.round(z / step) * step
+    z[1::5][rng.random((len(z[1::5]), V)) < 0.5] = -np.inf
+    zt, z64 = _rounded(z, dtype)
+    c = lambda a: np.array([a[i % len(a)] for i in range(rows)], np.float32)   # noqa: E731
+    par = dict(T=rng.choice([0.6, 1.0, 1.3, 50.0, 1e30], rows, p=[.3, .3, .2, .1, .1]).astype(np.float32),
+               k=np.zeros(rows, np.int32), p=c([0.9, 0.5, 0.99, 0.7, 0.999, 0.95, 0.05]),
+               m=c([0.0, 0.0, 0.02, 0.1, 0.0, 0.3, 1e-4, 0.9]), u=rng.random(rows).astype(np.float32))
+    got_t, got_p = _call(zt, _dev(par))
+    _check(z64, par, got_t.cpu().numpy(), got_p.cpu().numpy())
+
+
 @pytest.mark.parametrize("name", ["none", "k", "p", "m", "kp", "T"])
 def test_each_filter_alone(name):
     rows, V = 16, 5003
@@ -266,6 +287,28 @@ def test_accept_matches_oracle(S, B, V, noise, dtype):
     A, tok = dvs.accept_sampled(zvt, zdt, wide, torch.from_numpy(u).cuda(), d["T"], d["k"], d["p"],
                                 d["m"])
     A, tok = A.cpu().numpy(), tok.cpu().numpy()
+    for s in range(S):
+        want = of.accept(pv[s], qd[s], draft[s], u[s].astype(np.float64))
+        assert (int(A[s]), int(tok[s])) == want, f"sequence {s}"
+
+
+@pytest.mark.parametrize("sigma,p", [(0.3, 0.9), (1.0, 0.99), (2.5, 1.0)])
+def test_accept_over_flat_rows(sigma, p):
+    """More kept tokens than fit a list, in the draft rows and in the verify rows."""
+    S, B, V = 3, 2, 20011
+    rng = np.random.default_rng([S, V, 23])
+    zv = rng.standard_normal((S, B + 1, V)) * sigma
+    zd = zv[:, :B] + rng.standard_normal((S, B, V)) * 0.3
+    zvt, zv64 = _rounded(zv, "f32")
+    zdt, zd64 = _rounded(zd, "f32")
+    pp = np.float32(p)
+    pv = np.array([[of.probs(of.kept_weights(r, 1.0, 0, float(pp), 0.0)) for r in q] for q in zv64])
+    qd = np.array([[of.probs(of.kept_weights(r, 1.0, 0, float(pp), 0.0)) for r in q] for q in zd64])
+    draft = np.array([[of.draw(q, rng.random()) for q in row] for row in qd], np.int32)
+    u = rng.random((S, B + 1)).astype(np.float32)
+    u[0], u[1, :B], u[2, :B] = 0.999, 0.0, 0.5
+    A, tok = dvs.accept_sampled(zvt, zdt, torch.from_numpy(draft).cuda(), torch.from_numpy(u).cuda(),
+                                None, None, torch.full((S,), p, device="cuda"), None)
     for s in range(S):
         want = of.accept(pv[s], qd[s], draft[s], u[s].astype(np.float64))
         assert (int(A[s]), int(tok[s])) == want, f"sequence {s}"
