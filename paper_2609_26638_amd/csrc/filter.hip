@@ -50,7 +50,7 @@
 // pass 12,000 to 19,000 (the rows of an XCD's CUs together exceed its L2); then
 // 12,000 for a short list, which is barriers and LDS latency, up to 45,000 for a
 // long one.  136 such rows: 49 us, 0.73 TB/s of logits read once; 1024 rows of
-// bf16 with top-k, two to a CU: 65 us, 2.1 TB/s.
+// bf16 with top-k, two to a CU: 67 us, 2.0 TB/s.
 #include <float.h>
 #include <math.h>
 
@@ -1490,19 +1490,18 @@ static int row_vectors(int V, int threads) {
   return (V / epv + threads - 1) / threads;
 }
 
-// Calls f(threads): 1024, or 512 where rows wait for a CU and top-k keeps the
-// lists short (a list of 512 threads is half as long, and a flat row of top-p
-// alone outgrows it).  V = 65536, us with 1024 / 512 threads:
-//   rows           256 f32, top-p   1024 f32, top-p   1024 f32, top-k   1024 bf16, top-k
-//                     58 / 102         169 / 211         103 / 99           80 / 65
-// (one row 27 / 26, 32 rows of top-p 43 / 51; 1024 f32 rows without a filter
-// 94 / 97, with min-p 102 / 112).
+// Calls f(threads): 1024 while every row has a CU of its own, else 512.
+// V = 65536, us with 1024 / 512 threads:
+//   rows      f32, top-p    f32, top-k    f32, min-p    bf16, top-k    bf16, mixed
+//     32       43 / 52
+//    256       58 / 78
+//   1024      171 / 147     105 / 99      103 / 112      83 / 67       116 / 90
 template <typename F>
-static void by_rows(int rows, const RowParams& par, F f) {
-  if (rows > device_cus() && par.top_k)
-    f(IC<512>{});
-  else
+static void by_rows(int rows, F f) {
+  if (rows <= device_cus())
     f(IC<1024>{});
+  else
+    f(IC<512>{});
 }
 
 template <typename E>
@@ -1512,7 +1511,7 @@ static int launch_accept(const void* zv, long long vs, long long vld, const void
                          int32_t* accept_len, int32_t* token_out, int token_stride,
                          int at_accepted, int32_t* err, void* ws, hipStream_t st) {
   RowCut* cuts = (RowCut*)ws;
-  by_rows(S * (2 * B + 1), par, [&](auto threads) {
+  by_rows(S * (2 * B + 1), [&](auto threads) {
     constexpr int FT = decltype(threads)::value;
     hipLaunchKernelGGL((filter_rows_kernel<FT, E>), dim3(S * (2 * B + 1)), dim3(FT), 0, st,
                        (const E*)zv, vs, vld, (const E*)zd, ds, dld, B, S * (B + 1), V,
@@ -1529,7 +1528,7 @@ template <typename E>
 static void launch_sample(const void* logits, int rows, int V, long long ld, const RowParams& par,
                           int rows_per_param, const float* u, int u_stride, int32_t* token_out,
                           float* prob_out, int32_t* err, hipStream_t st) {
-  by_rows(rows, par, [&](auto threads) {
+  by_rows(rows, [&](auto threads) {
     constexpr int FT = decltype(threads)::value;
     hipLaunchKernelGGL((sample_filtered_kernel<FT, E>), dim3(rows), dim3(FT), 0, st,
                        (const E*)logits, ld, V, row_vectors<E>(V, FT), par, rows_per_param, u,
