@@ -29,7 +29,7 @@
 // follow.  Sources and targets are disjoint, so the copies need no order.
 //
 // The copies are bound by HBM (fork of one sequence of 2000 rows to three slots
-// of their own, 64 pools: 295 MB in 40 us; compaction of 418 MB in 86 us); the
+// of their own, 32 pools: 295 MB in 40 us; compaction of 418 MB in 86 us); the
 // rest by the latency of a few dependent loads.  Calls of up to SMALL_ENTRIES
 // table entries over pools of up to SMALL_POOL pages do everything up to the
 // settling (a release all of it) in one workgroup with its bitmaps in LDS; page
@@ -301,7 +301,9 @@ __device__ __forceinline__ void apply_fields(const PageState& st, const Pair& pr
 
 // Everything up to the settling in one workgroup, a release whole.  The
 // holders that a page loses are counted in LDS, in 16 bits (a call has at most
-// SMALL_ENTRIES of them).
+// 2 * SMALL_ENTRIES of them): 16 us for 56 forks of 8 prefixes, where seven
+// destinations give up the same pages, 19.5 with an atomic on page_refs for
+// each.
 __global__ void __launch_bounds__(PLAN_THREADS) assign_small_kernel(PageState st, PageWork wk,
                                                                     Assign as) {
   __shared__ uint32_t bits[SMALL_POOL / 32];
@@ -717,20 +719,24 @@ static int page_bytes(int n_kv_heads, int head_dim, int dtype) {
 //      4 x 252          12.9 / 14.9      14.6 / 20.9
 //     32 x 134          15.9 / 16.7      15.9 / 20.1
 //     64 x 252          23.1 / 23.4      17.9 / 20.3
-static bool one_workgroup(const PageState& st, int rows) {
-  return (long long)rows * st.max_pages <= SMALL_ENTRIES && st.pool <= SMALL_POOL;
+// A release is one launch instead of four, for up to twice the entries: 48 slots
+// of 134 pages, called one by one, 19.2 / 22.8.
+static bool one_workgroup(const PageState& st, int rows, int entries) {
+  return (long long)rows * st.max_pages <= entries && st.pool <= SMALL_POOL;
 }
 
-static void launch_assign(const PageState& st, const PageWork& wk, const Assign& as,
+// true: in one workgroup, a release to its end.
+static bool launch_assign(const PageState& st, const PageWork& wk, const Assign& as,
                           hipStream_t s) {
-  if (one_workgroup(st, as.n)) {
+  if (one_workgroup(st, as.n, as.src ? SMALL_ENTRIES : 2 * SMALL_ENTRIES)) {
     hipLaunchKernelGGL(assign_small_kernel, dim3(1), dim3(PLAN_THREADS), 0, s, st, wk, as);
-    return;
+    return true;
   }
   hipLaunchKernelGGL(assign_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, s, st, wk, as);
   hipLaunchKernelGGL(assign_drop_kernel, dim3((st.max_pages + 255) / 256, as.n), dim3(256), 0, s,
                      st, wk, as);
   hipLaunchKernelGGL(assign_settle_kernel, dim3(1), dim3(PLAN_THREADS), 0, s, st, wk, as);
+  return false;
 }
 
 extern "C" int kv_fork(const dvs_state* st, int32_t* page_refs, const dvs_layer* layers,
@@ -775,8 +781,7 @@ extern "C" int kv_release(const dvs_state* st, int32_t* page_refs, int32_t n, co
   DVS_CHECK_ARG(window >= 1, "kv_release: need window >= 1");
   const PageWork wk = work_layout((char*)workspace, st->S, st->num_pool_pages);
   const Assign as{nullptr, slots, n, window, 0};
-  launch_assign(p, wk, as, (hipStream_t)stream);
-  if (!one_workgroup(p, n)) {
+  if (!launch_assign(p, wk, as, (hipStream_t)stream)) {
     const int per_row = (p.max_pages + COPY_THREADS - 1) / COPY_THREADS;
     hipLaunchKernelGGL(assign_apply_kernel, dim3(n * per_row), dim3(COPY_THREADS), 0,
                        (hipStream_t)stream, p, wk, as, per_row, n * per_row, Pools{}, 0, 0);
@@ -794,7 +799,7 @@ extern "C" int kv_compact(const dvs_state* st, int32_t* page_refs, const dvs_lay
   if ((rc = check_pools("kv_compact", layers, n_layers, n_kv_heads, head_dim, dtype))) return rc;
   const PageWork wk = work_layout((char*)workspace, st->S, st->num_pool_pages);
   hipStream_t s = (hipStream_t)stream;
-  if (one_workgroup(p, st->S)) {
+  if (one_workgroup(p, st->S, SMALL_ENTRIES)) {
     hipLaunchKernelGGL(compact_small_kernel, dim3(1), dim3(PLAN_THREADS), 0, s, p, wk, moved_out);
   } else {
     hipLaunchKernelGGL(compact_clear_kernel, dim3((wk.words + 255) / 256), dim3(256), 0, s, wk);
