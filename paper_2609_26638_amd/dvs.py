@@ -388,6 +388,19 @@ def _here(*tensors):
             raise DvsError(f"tensors must be on the current device {dev}, got {t.device}")
 
 
+def _new(shape, dtype, device, stream):
+    """An output or scratch that the call leaves to its stream: memory that another
+    stream may still be using would not do."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _scratch(workspace, nbytes, device, stream):
+    return workspace.buf if workspace is not None else _new(nbytes, torch.uint8, device, stream)
+
+
 def _filter_params(n, temperature, top_k, top_p, min_p):
     """Device pointers of the sampling parameters, one entry per request."""
     ptrs = []
@@ -438,9 +451,9 @@ def sample_filtered(logits, u, temperature=None, top_k=None, top_p=None, min_p=N
     if n < 1 or rows < 1 or rows % n:
         raise DvsError(f"{rows} rows are no groups of {n} sampling parameters")
     if token_out is None:
-        token_out = torch.empty(lead, dtype=torch.int32, device=logits.device)
+        token_out = _new(lead, torch.int32, logits.device, stream)
     if prob_out is None:
-        prob_out = torch.empty(lead, dtype=torch.float32, device=logits.device)
+        prob_out = _new(lead, torch.float32, logits.device, stream)
     _dev(token_out, torch.int32, "token_out")
     _dev(prob_out, torch.float32, "prob_out")
     if token_out.numel() != rows or prob_out.numel() != rows:
@@ -476,9 +489,9 @@ def accept_sampled(z_verify, z_draft, draft, u, temperature=None, top_k=None, to
         raise DvsError("draft must have S rows and u must be [S, B + 1]")
     _, par = _filter_params(S, temperature, top_k, top_p, min_p)
     if accept_len is None:
-        accept_len = torch.empty((S,), dtype=torch.int32, device=z_verify.device)
+        accept_len = _new((S,), torch.int32, z_verify.device, stream)
     if token_out is None:
-        token_out = torch.empty((S,), dtype=torch.int32, device=z_verify.device)
+        token_out = _new((S,), torch.int32, z_verify.device, stream)
     _dev(accept_len, torch.int32, "accept_len", 1)
     _dev(token_out, torch.int32, "token_out", 1)
     if accept_len.shape[0] != S or token_out.shape[0] != S:
@@ -486,15 +499,13 @@ def accept_sampled(z_verify, z_draft, draft, u, temperature=None, top_k=None, to
     _here(z_verify, z_draft, draft, u, accept_len, token_out, err)
     if err is not None:
         _dev(err, torch.int32, "err", 1)
-    if workspace is None:
-        workspace = Workspace(accept_workspace_bytes(S, B, V), device=z_verify.device)
+    ws = _scratch(workspace, accept_workspace_bytes(S, B, V), z_verify.device, stream)
     # a sequence's only draft row has no next one to be apart from
     draft_ld = z_draft.stride(1) if B > 1 else V
     rc = lib().accept_sampled(_ptr(z_verify), z_verify.stride(0), z_verify.stride(1), _ptr(z_draft),
                               z_draft.stride(0), draft_ld, code, S, B, V, *par,
                               _ptr(draft), draft.shape[1], _ptr(u), _ptr(accept_len),
-                              _ptr(token_out), _ptr(err), _ptr(workspace.buf), workspace.nbytes,
-                              _stream(stream))
+                              _ptr(token_out), _ptr(err), _ptr(ws), ws.numel(), _stream(stream))
     _check(rc, "accept_sampled")
     return accept_len, token_out
 
@@ -531,7 +542,11 @@ class DeviceState:
     def page_refs(self):
         """Holders of every page beyond the first (kv_fork); made when first used."""
         if self._refs[0] is None:
+            if self.err.is_cuda and torch.cuda.is_current_stream_capturing():
+                raise DvsError("page_refs must be made before a capture (one eager call does it)")
             self._refs[0] = torch.zeros(self.pool_pages, dtype=torch.int32, device=self.err.device)
+            if self.err.is_cuda:         # zero for the call's stream, whichever it is
+                torch.cuda.current_stream(self.err.device).synchronize()
         return self._refs[0]
 
     def copy_from(self, other: "DeviceState"):
@@ -796,13 +811,15 @@ def literal_round(model: DeviceModel, st: DeviceState, B: int, chunk_keys: int =
 
 def capture(fn) -> "torch.cuda.CUDAGraph":
     """Record the launches of ``fn`` (calls of this module that only enqueue:
-    draft_verify_step, literal_round, attn_hybrid_block, argmax_accept, the
-    commits; not diffusion_block or literal_round_refined, which read a count
+    draft_verify_step, literal_round, attn_hybrid_block, argmax_accept,
+    sample_filtered, accept_sampled, the commits, kv_fork, kv_release,
+    kv_compact; not diffusion_block or literal_round_refined, which read a count
     back from the device) into a HIP graph.  ``replay()`` re-runs them on the
     buffers' current contents: every input of a step (kv_len, pages, boundary,
     draft, ...) is read from device memory, so a replay is the next step.
     The library clears its counters with kernels, never with a memset node.
-    Workspaces must be allocated before the capture (one eager call does it)
+    Workspaces and a state's page counts must be allocated before the capture
+    (one eager call does it)
     and must not be replaced (by a call needing a larger one) while the
     graph is replayed."""
     g = torch.cuda.CUDAGraph()
@@ -978,11 +995,9 @@ def kv_workspace_bytes(S, num_pool_pages) -> int:
     return int(lib().dvs_kv_workspace_bytes(S, num_pool_pages))
 
 
-def _kv_workspace(st, workspace):
-    if workspace is None:
-        workspace = Workspace(kv_workspace_bytes(st.kv_len.shape[0], st.pool_pages),
-                              device=st.kv_len.device)
-    return workspace
+def _kv_workspace(st, workspace, stream):
+    return _scratch(workspace, kv_workspace_bytes(st.kv_len.shape[0], st.pool_pages),
+                    st.kv_len.device, stream)
 
 
 def _check_pools(st, pools):
@@ -1000,12 +1015,12 @@ def kv_fork(st: DeviceState, pools: KVPools, src, dst, window: int, share: bool 
     if src.shape != dst.shape:
         raise DvsError("src and dst must have the same length")
     _here(st.kv_len, src, dst)
-    workspace = _kv_workspace(st, workspace)
+    ws = _kv_workspace(st, workspace, stream)
     sd = _state_desc(st, -1)
     rc = lib().kv_fork(ctypes.byref(sd), _ptr(st.page_refs), pools.layers, len(pools.layers),
                        pools.n_kv_heads, pools.head_dim, pools.dtype, src.shape[0], _ptr(src),
-                       _ptr(dst), int(window), int(bool(share)), _ptr(workspace.buf),
-                       workspace.nbytes, _stream(stream))
+                       _ptr(dst), int(window), int(bool(share)), _ptr(ws), ws.numel(),
+                       _stream(stream))
     _check(rc, "kv_fork")
 
 
@@ -1013,10 +1028,10 @@ def kv_release(st: DeviceState, slots, window: int, workspace=None, stream=None)
     """The slots (int32) become empty and keep pages for a window of `window` rows."""
     _dev(slots, torch.int32, "slots", 1)
     _here(st.kv_len, slots)
-    workspace = _kv_workspace(st, workspace)
+    ws = _kv_workspace(st, workspace, stream)
     sd = _state_desc(st, -1)
     rc = lib().kv_release(ctypes.byref(sd), _ptr(st.page_refs), slots.shape[0], _ptr(slots),
-                          int(window), _ptr(workspace.buf), workspace.nbytes, _stream(stream))
+                          int(window), _ptr(ws), ws.numel(), _stream(stream))
     _check(rc, "kv_release")
 
 
@@ -1025,14 +1040,14 @@ def kv_compact(st: DeviceState, pools: KVPools, moved_out=None, workspace=None, 
     number of moved pages (device int32 [1])."""
     _check_pools(st, pools)
     if moved_out is None:
-        moved_out = torch.empty(1, dtype=torch.int32, device=st.kv_len.device)
+        moved_out = _new(1, torch.int32, st.kv_len.device, stream)
     _dev(moved_out, torch.int32, "moved_out", 1)
     _here(st.kv_len, moved_out)
-    workspace = _kv_workspace(st, workspace)
+    ws = _kv_workspace(st, workspace, stream)
     sd = _state_desc(st, -1)
     rc = lib().kv_compact(ctypes.byref(sd), _ptr(st.page_refs), pools.layers, len(pools.layers),
                           pools.n_kv_heads, pools.head_dim, pools.dtype, _ptr(moved_out),
-                          _ptr(workspace.buf), workspace.nbytes, _stream(stream))
+                          _ptr(ws), ws.numel(), _stream(stream))
     _check(rc, "kv_compact")
     return moved_out
 

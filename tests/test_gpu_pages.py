@@ -249,3 +249,79 @@ def test_binding_refusals():
         with pytest.raises(dvs.DvsError):
             bad()
     b.same()
+
+
+def test_page_counts_are_not_made_inside_a_capture():
+    b = Both(13, [20, 5], 4, extra=8)
+    ws = dvs.Workspace(dvs.kv_workspace_bytes(2, b.st.pool_pages))
+    src, dst = ids([0]), ids([1])
+    b.dev._refs[0] = None
+    torch.cuda.synchronize()
+    with pytest.raises(dvs.DvsError, match="before a capture"):
+        dvs.capture(lambda: dvs.kv_fork(b.dev, b.handle, src, dst, 4, workspace=ws))
+    b.fork([0], [1], 4)
+    b.same()
+
+
+def test_explicit_stream_without_workspace():
+    """Scratch, counts and outputs of a call on a stream that is not the current one."""
+    b = Both(14, [70, 10, 0], 6, extra=60)
+    src, dst, gone = ids([0]), ids([1]), ids([1])
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        dvs.kv_fork(b.dev, b.handle, src, dst, 6, stream=s)
+        dvs.kv_release(b.dev, gone, 6, stream=s)
+        moved = dvs.kv_compact(b.dev, b.handle, stream=s)
+        torch.ones(1 << 22, device="cuda").sum()       # work of the current stream
+        assert op.kv_fork(b.st, b.refs, b.pools, [0], [1], 6) == 0
+        assert op.kv_release(b.st, b.refs, [1], 6) == 0
+        rc, n = op.kv_compact(b.st, b.refs, b.pools)[:2]
+        s.synchronize()
+        assert rc == 0 and int(moved.item()) == n
+        b.settle(0)
+
+
+LONG = [34000, 100, 3, 3, 50, 5, 0, 70]    # page tables that one workgroup does not take
+
+
+def test_large_tables_errors_change_nothing():
+    b = Both(15, LONG, 4, layers=1, heads=1, D=8, extra=2)
+    b.fork([1, 4], [2, 3], 2000, share=False, err=op.ERR_POOL_EXHAUSTED)
+    b.fork([1, 1], [2, 2], 4, err=op.ERR_BAD_SLOT)
+    b.fork([1, 2], [2, 3], 4, err=op.ERR_BAD_SLOT)
+    b.fork([0, 1], [2, 3], 40000, err=op.ERR_MAX_PAGES)
+    b.release([1, 2, 3, 4, 1], 4, err=op.ERR_BAD_SLOT)
+    b.fork([1, 1], [2, 3], 4)              # shared pages dropped, missing, and back
+    b.fork([4, 7], [2, 3], 2000, share=False, err=op.ERR_POOL_EXHAUSTED)
+    b.release([1, 2, 3, 4, 5], 4)
+    b.compact()
+    table = b.dev.page_table.clone()
+    for s, j, p in ((7, 0, -1), (7, 1, b.st.pool_pages), (0, 2100, 1 << 30)):
+        b.dev.page_table[s, j] = p
+        before, refs = b.dev.flat.clone(), b.dev.page_refs.clone()
+        dvs.kv_fork(b.dev, b.handle, ids([0, 1]), ids([7, 2]), 4)
+        if s == 7:
+            dvs.kv_release(b.dev, ids([1, 7, 2, 3, 4]), 4)
+        dvs.kv_compact(b.dev, b.handle)
+        torch.cuda.synchronize()
+        assert int(b.dev.err.item()) & op.ERR_BAD_PAGE
+        b.dev.err.zero_()
+        assert torch.equal(b.dev.flat, before) and torch.equal(b.dev.page_refs, refs)
+        b.dev.page_table.copy_(table)
+    b.same()
+
+
+def test_large_tables_random_life():
+    rng = np.random.default_rng(16)
+    b = Both(16, LONG, 4, layers=1, heads=1, D=8, extra=9000)
+    S = len(LONG)
+    for step in range(24):
+        kind, perm = rng.integers(0, 4), rng.permutation(S)
+        if kind <= 1:
+            n = int(rng.integers(2, 4))
+            b.fork(rng.choice(perm[n:], n), perm[:n], 4, bool(rng.integers(0, 2)))
+        elif kind == 2:
+            b.release(perm[perm != 0][:5], 4)
+        else:
+            b.compact()
