@@ -619,6 +619,7 @@ int literal_round_sampled(const dvs_model* m, const dvs_state* st, int32_t B, fl
  *   u [S, 2B + 2]; other arguments, outputs and pages as
  *   literal_round_sampled.  workspace:
  *   dvs_filtered_round_workspace_bytes(m, S, B, max_pages, chunk_keys).
+ *   Requirements: vocab <= 2^22.
  * ---------------------------------------------------------------------- */
 size_t dvs_filtered_round_workspace_bytes(const dvs_model* m, int32_t S, int32_t B,
                                           int32_t max_pages, int32_t chunk_keys);

@@ -2370,7 +2370,7 @@ extern "C" int literal_round_sampled(const dvs_model* m, const dvs_state* st, in
 
 extern "C" size_t dvs_filtered_round_workspace_bytes(const dvs_model* m, int32_t S, int32_t B,
                                                      int32_t max_pages, int32_t chunk_keys) {
-  if (!model_ok(m) || S < 1 || B < 1 || max_pages < 1) return 0;
+  if (!model_ok(m) || S < 1 || B < 1 || max_pages < 1 || m->vocab > (1 << 22)) return 0;
   StepLayout Ld, Lv;
   const size_t M = (size_t)S * (B + 1);
   return sampled_extra(m, S, B, max_pages, chunk_keys, &Ld, &Lv) + al(M * m->vocab * 4) +
@@ -2386,6 +2386,7 @@ extern "C" int literal_round_filtered(const dvs_model* m, const dvs_state* st, i
   int rc = check_model_state(m, st, "literal_round_filtered");
   if (rc) return rc;
   DVS_CHECK_ARG(B >= 1 && u, "literal_round_filtered: need B >= 1 and uniforms");
+  DVS_CHECK_ARG(m->vocab <= (1 << 22), "literal_round_filtered: vocab over 2^22");
   DVS_CHECK_ARG(st->draft && st->draft_width >= B, "literal_round_filtered: draft narrower than B");
   const size_t need = dvs_filtered_round_workspace_bytes(m, st->S, B, st->max_pages, chunk_keys);
   if (!workspace || ws_bytes < need) {

@@ -117,6 +117,20 @@ def test_round_refuses():
     assert b"literal_round_filtered" in L.dvs_last_error()
 
 
+@pytest.mark.parametrize("vocab,B,rc", [((1 << 22) + 1, 2, -1), (1 << 22, 0, -1), (1 << 22, 4, -1),
+                                        (1 << 22, 2, -4)])
+def test_round_refuses_models_and_blocks(vocab, B, rc):
+    L = dvs.lib()
+    layers = (dvs.DvsLayer * 1)()
+    for n, _ in dvs.DvsLayer._fields_:
+        setattr(layers[0], n, 0x1000)
+    m = dvs.DvsModel(0, 1, vocab, 64, 1, 1, 64, 64, 1e4, 1e-6, 0x1000, 0x1000, 0x1000, layers)
+    assert (L.dvs_filtered_round_workspace_bytes(ctypes.byref(m), 4, 2, 8, 0) == 0) == (vocab > 1 << 22)
+    assert L.literal_round_filtered(ctypes.byref(m), ctypes.byref(_state()), B, N, N, N, N, F, 0, N,
+                                    N, F, 16, N) == rc
+    assert b"literal_round_filtered" in L.dvs_last_error()
+
+
 def test_binding_refuses_host_tensors():
     z, u = torch.zeros(2, 8), torch.zeros(2)
     with pytest.raises(dvs.DvsError, match="logits"):
