@@ -1094,14 +1094,18 @@ static __device__ __forceinline__ void row_bound(const E* p, int V, int nit, flo
   const double count = (double)(got >> 40);
   unsigned long long m = got >> 40;
   if (!k && m) {
-    float z = bin.lower_edge(tid);
+    double w;
     if (bin.linear) {
+      // below the largest logit, not as a logit: those far from zero are
+      // further apart than this may be off
       const double mean = tid + (double)(got & ((1ull << 40) - 1)) / (65536.0 * count);
-      z = fmaxf(z, (float)(2.0 * ((double)bin.half - mean * (double)bin.width)));
+      w = exp2_neg(-2.0 * mean * (double)bin.width, rc.log2e_t);
+    } else {
+      w = weight(bin.lower_edge(tid), rc);
     }
-    // (1e-5 less: the roundings of x, sc and z move a mean by less at any T
-    // whose weights reach this far)
-    m = (unsigned long long)(count * weight(z, rc) * (1.0 - 1e-5) * scale);
+    // (1e-5 less: the roundings of x and sc move a mean by less at any T whose
+    // weights reach this far)
+    m = (unsigned long long)(count * w * (1.0 - 1e-5) * scale);
   }
   uint32_t c = (uint32_t)(got >> 40);
   scan_bins(c, m);

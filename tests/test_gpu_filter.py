@@ -142,6 +142,21 @@ def test_flat_rows_keep_more_than_a_list(V, rows, step, dtype):
     _check(z64, par, got_t.cpu().numpy(), got_p.cpu().numpy())
 
 
+@pytest.mark.parametrize("offset", [-1e4, 1e3, 3e5])
+@pytest.mark.parametrize("V,rows", [(257, 3000), (511, 3000), (4095, 600), (8193, 600)])
+def test_logits_far_from_zero(V, rows, offset):
+    """Their spacing is no longer small against T; shares close to 1."""
+    rng = np.random.default_rng([V, int(abs(offset)), 29])
+    z = rng.standard_normal((rows, V)) * rng.choice([0.05, 0.3, 1.0, 2.0], (rows, 1)) + offset
+    zt, z64 = _rounded(z, "f32")
+    par = dict(T=(10 ** rng.uniform(-2, 1, rows)).astype(np.float32), k=np.zeros(rows, np.int32),
+               p=(1 - 10 ** rng.uniform(-4, -3, rows)).astype(np.float32),
+               m=np.where(rng.random(rows) < 0.7, 0, 10 ** rng.uniform(-6, -3, rows)).astype(np.float32),
+               u=rng.random(rows).astype(np.float32))
+    got_t, got_p = _call(zt, _dev(par))
+    _check(z64, par, got_t.cpu().numpy(), got_p.cpu().numpy())
+
+
 @pytest.mark.parametrize("name", ["none", "k", "p", "m", "kp", "T"])
 def test_each_filter_alone(name):
     rows, V = 16, 5003
