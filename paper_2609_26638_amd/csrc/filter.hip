@@ -30,10 +30,11 @@
 //   4. up to SMALL of them (a longer list is first cut short by a histogram)
 //      are ranked against each other, which gives the cut, the kept weight and
 //      the draw at once (filter_small).
-// Longer lists (filter_list), and rows whose candidates do not fit the list
-// (filter_row_again: a flat distribution, a large k, many equal logits), take
-// histograms with a count and a weight sum per bin, narrowed to the tokens of
-// one wave (select_cut), and draw by the kept weight per index or range.
+// Longer lists (filter_list) take histograms with a count and a weight sum per
+// bin, narrowed to the tokens of one wave (select_cut), and draw by the kept
+// weight per index.  Rows whose candidates do not fit a list: flat ones of top-p
+// add up what lies above a window around the cut (filter_flat); a large k and
+// many equal logits take the histograms over the row (filter_row_again).
 //
 // A pass is a rolled loop that reads the row again, from L2 mostly: code that is
 // run once per launch is bound by fetching its instructions (16 KB of unrolled
@@ -1415,7 +1416,9 @@ __device__ __forceinline__ double prob_of(float z, int i, const RowCut& c) {
 
 // One workgroup per sequence: d_j accepted while u q_j(d_j) < p_j(d_j), then
 // the final token from max(0, p - q) of the rejected draft's rows, or from the
-// last verify row.
+// last verify row: a list in LDS of the tokens that p keeps, weighed together
+// (8 sequences of V = 65536: 13 us, 17 by two walks over the row; those remain
+// for tokens that do not fit a list).
 template <typename E>
 __global__ void __launch_bounds__(1024) accept_filtered_kernel(
     const E* __restrict__ zv, long long vs, long long vld, const E* __restrict__ zd, long long ds,
