@@ -266,7 +266,8 @@ int sample_filtered(const void* logits, int32_t dtype, int32_t rows, int32_t V, 
  *   [0, V) is not); accept_len[s] = A = number accepted;
  *   token_out[s] is drawn with u[s, B] from max(0, p_{A+1} - q_{A+1}) when
  *   A < B (from p_{A+1} where that is zero everywhere), from p_{B+1} when
- *   A = B, by the rule of sample_filtered.
+ *   A = B, by the rule of sample_filtered, which also holds for a row that has
+ *   no value above -inf (p or q is then 0).
  *   z_verify  row j of sequence s at s * verify_seq + j * verify_ld elements,
  *             j = 0..B; z_draft likewise, j = 0..B-1; DVS_F32 or DVS_BF16
  *   temperature, top_k, top_p, min_p [S] or NULL, as sample_filtered

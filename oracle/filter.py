@@ -74,13 +74,20 @@ def sample(z, u, T=1.0, k=0, p=1.0, m=0.0):
     t = draw(w, u)
     if t >= 0:
         return t, float(probs(w)[t])
-    masked = np.flatnonzero(z == -np.inf)
-    return (int(masked[0]) if masked.size else 0), 0.0
+    return no_number(z), 0.0
 
 
-def accept(pv, qd, d, u):
+def no_number(z) -> int:
+    """Token of a row without a value above -inf: its lowest index of -inf, 0
+    when every value is NaN."""
+    masked = np.flatnonzero(np.asarray(z) == -np.inf)
+    return int(masked[0]) if masked.size else 0
+
+
+def accept(pv, qd, d, u, zv=None):
     """(A, final token): pv [B+1, V], qd [B, V] probabilities, d [B] drafts,
-    u [B+1] uniforms."""
+    u [B+1] uniforms; zv [B+1, V] the logits of pv, where rows without a value
+    above -inf are among them."""
     B, V = qd.shape
     A = 0
     while A < B:
@@ -91,4 +98,5 @@ def accept(pv, qd, d, u):
     w = pv[A] if A == B else np.maximum(pv[A] - qd[A], 0.0)
     if not np.any(w > 0):
         w = pv[A]
-    return A, max(draw(w, u[B]), 0)
+    t = draw(w, u[B])
+    return A, t if t >= 0 else 0 if zv is None else no_number(zv[A])

@@ -336,19 +336,20 @@ struct Row {
 #pragma unroll 1
     for (int it = 0; it < nit; it += AHEAD) f(batch(it), it);
   }
-  // f(vector, index of its first logit)
-  template <typename F>
-  __device__ __forceinline__ void vectors(F f) const {
-    batches([&](const u32x16& b, int it) {
-#pragma unroll 1
-      for (int k = 0; k < min(AHEAD, nit - it); ++k) f(vec(b, k), at(it + k));
-    });
-  }
+  // f(z, index) for every token.  A vector that is absent has an index past the
+  // whole ones, which the tokens behind them have too.
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    vectors([&](const u32x4& x, int i) {
+    batches([&](const u32x16& b, int it) {
+#pragma unroll 1
+      for (int k = 0; k < min(AHEAD, nit - it); ++k) {
+        const u32x4 x = vec(b, k);
+        const int first = at(it + k);
+        if (first + EPV <= V) {
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), i + e);
+          for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), first + e);
+        }
+      }
     });
     const int i = rest_index();
     if (i >= 0) f(load_logit(p + i), i);
@@ -364,9 +365,11 @@ struct Row {
 #pragma unroll 1
       for (int k = 0; k < min(AHEAD, nit - it); ++k) {
         const u32x4 x = vec(b, k);
-        if (__ballot(vec_max<E>(x) >= zlo)) {
+        const int first = at(it + k);
+        const bool there = first + EPV <= V;
+        if (__ballot(there && vec_max<E>(x) >= zlo) && there) {
 #pragma unroll
-          for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), at(it + k) + e);
+          for (int e = 0; e < EPV; ++e) f(vec_elem<E>(x, e), first + e);
         }
       }
     });
@@ -1281,7 +1284,7 @@ static __device__ __forceinline__ void filter_row(const Row<E>& row, const RowPa
   if (greedy || empty || hi == INFINITY) {
     // top-1: the lowest index of the maximum
     int at = 0x7fffffff;
-    row.each_from(hi, [&](float z, int i) { if (z == hi && i < V) at = min(at, i); });
+    row.each_from(hi, [&](float z, int i) { if (z == hi) at = min(at, i); });
     at = first_index(at != 0x7fffffff, at, -1);
     rc.z = hi;
     rc.idx = at;
@@ -1462,7 +1465,7 @@ __global__ void __launch_bounds__(1024) accept_filtered_kernel(
   // last bit
   for (int step = A < B ? 0 : 1; step < 2 && t < 0 && p.single >= 0; ++step) {
     auto rest = [&](float z, int i) {
-      double a = i < V ? prob_of(z, i, p) : 0.0;
+      double a = prob_of(z, i, p);
       if (step == 0 && a > 0.0) a = fmax(a - prob_of(load_logit(zq + i), i, q), 0.0);
       return a;
     };
