@@ -727,14 +727,14 @@ template <typename Src, typename E>
 static __device__ __forceinline__ void both_cuts(const Src& src, const Row<E>& row, RowCut& rc, int n,
                                           float bound, int k, double top_p, double whole,
                                           double scale, Found so_far) {
+  FilterShared& sh = shared();
   const bool need_p = top_p < 1.0;
   whole *= scale;
   for (int step = k < n ? 0 : 1; step < (need_p ? 2 : 1); ++step) {   // top-k, top-p
     if (step && whole < 0.0) {                      // top-k keeps all
-      double part = 0.0;
-      src.each([&](float z, int) { part += z >= bound ? weight(z, rc) : 0.0; });
-      whole = range_sums(part) * scale;
-      __syncthreads();
+      unsigned long long part = 0;                  // (a list has no order)
+      src.each([&](float z, int) { part += z >= bound ? fixed_weight(z, rc, scale) : 0ull; });
+      whole = (double)block_reduce(part, 0ull, Add(), sh.u);
     }
     const Cut c = select_cut(src, row, rc, scale, n, rc.zmax, bound, step == 1, need_p,
                              (uint32_t)k, fmax(top_p, 0.0) * whole,
