@@ -222,7 +222,9 @@ int top1_confidence(const void* logits, int32_t dtype, int32_t rows, int32_t V,
  * One token per row of logits z, drawn from softmax(z / T) cut by top-k,
  * top-p and min-p.  The tokens of a row are ordered by (logit descending,
  * index ascending; -0.0 equals +0.0), with weights
- *     w_i = exp((z_i - max z) / T)              (64-bit arithmetic):
+ *     w_i = exp((z_i - max z) / T)
+ * in 64 bits (within 1e-13 of themselves, 0 below 2^-1021; sums of them within
+ * 2^-40 of the weight of all the tokens summed):
  *   top-k   keeps the first top_k tokens (<= 0, or >= V: all);
  *   top-p   keeps, of these, the shortest prefix whose weight is at least
  *           top_p times theirs, at least one token (>= 1, or NaN: all);

@@ -65,6 +65,7 @@ constexpr int RANK = 64;          // tokens that one wave ranks
 constexpr int SMALL = 256;        // tokens that the workgroup ranks
 constexpr int PARTS = 8;          // parts of a thread's logits
 constexpr int BATCH = 16;         // logits that a thread has in flight
+constexpr double LIST_SCALE = 281474976710656.0;   // 2^48: a list's weights stay below 2^63
 
 // What a row's filters keep: weight >= min_w of the tokens with z > cut.z, or
 // z == cut.z and index <= cut.idx.
@@ -239,6 +240,15 @@ struct Cut {
 
 __device__ __forceinline__ unsigned long long fixed_weight(float z, const RowCut& c, double scale) {
   return (unsigned long long)(weight(z, c) * scale + 0.5);
+}
+
+// Scale of weights that integers add up: base, whose sums stay below 2^63 by the
+// number of the tokens, or more where these weigh `whole` at most (< 0: not
+// known).  Each weight is rounded by half a unit, so a sum over 2^22 of them is
+// off by 2^-40 of the whole at most; by 2^-18 of the largest weight with the
+// base alone, where 4 million tokens of 2^-40 each would count as nothing.
+__device__ __forceinline__ double mass_scale(double base, double whole) {
+  return whole > 0.0 ? fmax(base, ldexp(1.0, 61 - ilogb(whole))) : base;
 }
 
 // A logit such that exp((z - hi) / T) is below w for every smaller one,
@@ -722,20 +732,23 @@ static __device__ NOINLINE void draw_kept(const E* p, int V, int nit, float u) {
 }
 
 // Both cuts of the tokens of `src` that reach `bound` (n of them): rc.z, rc.idx.
-// whole: the weight that top-p is a share of, < 0: that of the k tokens.
+// whole: the weight that top-p is a share of, < 0: that of the k tokens.  scale:
+// the weights', raised where these tokens' weight has to be found first.
 template <typename Src, typename E>
 static __device__ __forceinline__ void both_cuts(const Src& src, const Row<E>& row, RowCut& rc, int n,
                                           float bound, int k, double top_p, double whole,
-                                          double scale, Found so_far) {
+                                          double& scale, Found so_far) {
   FilterShared& sh = shared();
   const bool need_p = top_p < 1.0;
+  auto sum = [&] {                                  // (a list has no order)
+    unsigned long long part = 0;
+    src.each([&](float z, int) { part += z >= bound ? fixed_weight(z, rc, scale) : 0ull; });
+    return (double)block_reduce(part, 0ull, Add(), sh.u);
+  };
+  if (need_p && whole < 0.0) scale = mass_scale(scale, sum() / scale);
   whole *= scale;
   for (int step = k < n ? 0 : 1; step < (need_p ? 2 : 1); ++step) {   // top-k, top-p
-    if (step && whole < 0.0) {                      // top-k keeps all
-      unsigned long long part = 0;                  // (a list has no order)
-      src.each([&](float z, int) { part += z >= bound ? fixed_weight(z, rc, scale) : 0ull; });
-      whole = (double)block_reduce(part, 0ull, Add(), sh.u);
-    }
+    if (step && whole < 0.0) whole = sum();         // top-k keeps all
     const Cut c = select_cut(src, row, rc, scale, n, rc.zmax, bound, step == 1, need_p,
                              (uint32_t)k, fmax(top_p, 0.0) * whole,
                              step == 1 ? so_far : Found{-1, 0, 0u, 0ull});
@@ -757,8 +770,8 @@ static __device__ NOINLINE void filter_row_again(const E* p, int V, int nit, int
   row.each([&](float z, int) { lo = z >= bound ? fminf(lo, z) : lo; });
   lo = block_reduce(lo, INFINITY, Min(), sh.f);
   // V weights of at most 2^(clz(V) + 30) stay below 2^62
-  both_cuts(row, row, rc, n, lo, k, top_p, whole, ldexp(1.0, __clz(V) + 30),
-            Found{-1, 0, 0u, 0ull});
+  double scale = mass_scale(ldexp(1.0, __clz(V) + 30), whole);
+  both_cuts(row, row, rc, n, lo, k, top_p, whole, scale, Found{-1, 0, 0u, 0ull});
   double part = 0.0;
   row.each_from(rc.z, [&](float z, int i) { part += kept_weight(z, i, rc); });
   rc.total = range_sums(part);
@@ -839,7 +852,7 @@ static __device__ NOINLINE void filter_list(const E* p, int V, int nit, int n, f
   const Row<E> row(p, V, nit);
   const List list{n};
   const Found so_far = found ? sh.so_far : Found{-1, 0, 0u, 0ull};
-  const double scale = 281474976710656.0;           // 2^48: LIST weights stay below 2^63
+  double scale = mass_scale(LIST_SCALE, whole);
   both_cuts(list, row, rc, n, bound, k, top_p, whole, scale, so_far);
   // a positive weight counts for 1 at least
   auto fixed = [&](float z, int i) -> unsigned long long {
@@ -861,13 +874,14 @@ static __device__ NOINLINE void filter_list(const E* p, int V, int nit, int n, f
 
 // Shortens a list of SMALL < n <= LIST candidates to those in the histogram
 // bins up to the one that holds the k-th token, or (by_mass) in which the
-// weight reaches `target`.  Returns how many they are; n, and the list as it
+// weight reaches `target` of `whole`.  Returns how many they are; n, and the list as it
 // was, if more than SMALL; -1 if the list does not weigh `target`.
-static __device__ NOINLINE int shorten_list(int n, float bound, bool by_mass, int k, double target) {
+static __device__ NOINLINE int shorten_list(int n, float bound, bool by_mass, int k, double target,
+                                            double whole) {
   FilterShared& sh = shared();
   const RowCut rc = sh.rc;
   const int tid = threadIdx.x;
-  const double scale = 281474976710656.0;      // 2^48: LIST weights stay below 2^63
+  const double scale = mass_scale(LIST_SCALE, whole);   // filter_list's
   const Binning bin(rc.zmax, bound, true);
   const List list{n};
   sh.cnt[tid] = 0;
@@ -1070,12 +1084,12 @@ static __device__ __forceinline__ float parts_bound(const float (&part)[PARTS], 
 // top-p also sh.hi, a logit from which the tokens up weigh less than the target,
 // and sh.inside, how many lie between the two.
 template <typename E>
-static __device__ __forceinline__ void row_bound(const E* p, int V, int nit, float bound, int k, double target) {
+static __device__ __forceinline__ void row_bound(const E* p, int V, int nit, float bound, int k,
+                                                 double target, double scale) {
   FilterShared& sh = shared();
   const RowCut rc = sh.rc;
   const int tid = threadIdx.x;
   const Row<E> row(p, V, nit);
-  const double scale = ldexp(1.0, __clz(V) + 30);   // V * scale <= 2^62
   const Binning bin(rc.zmax, bound, rc.zmax * 0.5f - bound * 0.5f <= 32.0f * (fabsf(rc.zmax) + 1.0f));
   sh.mass[tid] = 0;
   __syncthreads();
@@ -1154,12 +1168,13 @@ static __device__ __forceinline__ double min_p_sum(const Row<E>& row, const RowC
 // row: 56 us, 124 by filter_row_again (26 where a list holds the cut).
 template <typename E>
 static __device__ NOINLINE bool filter_flat(const E* p, int V, int nit, float sure, int k,
-                                            double target, float u) {
+                                            double target, double whole_w, float u) {
   FilterShared& sh = shared();
   RowCut rc = sh.rc;
   const int tid = threadIdx.x, lane = tid & 63;
   const Row<E> row(p, V, nit);
-  row_bound(p, V, nit, sure, k, target * (1.0 + 1e-9));
+  const double scale = mass_scale(ldexp(1.0, __clz(V) + 30), whole_w);   // as filter_row_again
+  row_bound(p, V, nit, sure, k, target * (1.0 + 1e-9), scale);
   const float lo = uniform(sh.lo), hi = uniform(sh.hi);
   if (k || uniform(sh.found) <= LIST) return false;
   if (rc.min_w > 0.0f && uniform(sh.found) > V) {
@@ -1185,7 +1200,6 @@ static __device__ NOINLINE bool filter_flat(const E* p, int V, int nit, float su
   const double above = range_sums(part);
   if (n < 1 || n > LIST || !(above < target)) return false;
   const double range = lane < FW ? sh.d[lane] : 0.0;
-  const double scale = ldexp(1.0, __clz(V) + 30);   // V weights stay below 2^62
   const List list{n};
   const Cut cut = select_cut(list, row, rc, scale, n, fminf(hi, rc.zmax), lo, true, true, 0u,
                              target * scale,
@@ -1199,10 +1213,10 @@ static __device__ NOINLINE bool filter_flat(const E* p, int V, int nit, float su
   const int span = nit * 64 * Row<E>::EPV, whole = V / Row<E>::EPV * Row<E>::EPV;
   list.each([&](float z, int i) {
     if (before_cut(z, i, rc))
-      atomicAdd(&sh.mass[i < whole ? i / span : FW - 1], fixed_weight(z, rc, 281474976710656.0));
+      atomicAdd(&sh.mass[i < whole ? i / span : FW - 1], fixed_weight(z, rc, scale));
   });
   __syncthreads();
-  const double kept = lane < FW ? range + (double)sh.mass[lane] * 3.552713678800501e-15 : 0.0;
+  const double kept = lane < FW ? range + (double)sh.mass[lane] / scale : 0.0;
   if (tid < FW) sh.d[tid] = kept;
   rc.total = at_lane(row_scan(kept, 0.0, Add()), FW - 1);
   if (tid == 0) sh.rc = rc;
@@ -1337,7 +1351,7 @@ static __device__ __forceinline__ void filter_row(const Row<E>& row, const RowPa
     if (tid == 0) sh.rc = rc;                  // (seen after gather)
     if (level == 2) {
       __syncthreads();
-      if (filter_flat(row.p, V, row.nit, sure, kk, target, u)) return;
+      if (filter_flat(row.p, V, row.nit, sure, kk, target, whole, u)) return;
       bound = uniform(sh.lo);
     }
     int n = gather(row, bound);
@@ -1348,7 +1362,7 @@ static __device__ __forceinline__ void filter_row(const Row<E>& row, const RowPa
     const int keep = need_k ? min(k, n) : n;
     bool found = false;
     if (n > SMALL && n <= LIST && (!need_k || keep <= SMALL)) {
-      const int left = shorten_list(n, bound, !need_k, keep, target);
+      const int left = shorten_list(n, bound, !need_k, keep, target, whole);
       if (left < 0 && level == 0) {
         level = 1;
         continue;
