@@ -949,16 +949,21 @@ def literal_round_filtered(model: DeviceModel, st: DeviceState, B: int, u, tempe
     if tuple(u.shape) != (S, 2 * B + 2):
         raise DvsError("u must be [S, 2B + 2]")
     _, par = _filter_params(S, temperature, top_k, top_p, min_p)
+    if logits_out is not None:
+        _dev(logits_out, torch.float32, "logits_out")
+        if logits_out.numel() != S * (B + 1) * model.V:
+            raise DvsError("logits_out must be [S, B + 1, V]")
+    if accept_out is not None:
+        _dev(accept_out, torch.int32, "accept_out", 1)
+        if accept_out.shape[0] != S:
+            raise DvsError("accept_out must have S entries")
+    _here(st.kv_len, u, logits_out, accept_out)
     need = int(lib().dvs_filtered_round_workspace_bytes(ctypes.byref(model.desc), S, int(B),
                                                         st.max_pages, int(chunk_keys)))
     if need == 0:
         raise DvsError("literal_round_filtered: invalid configuration")
     if model.ws is None or model.ws.nbytes < need:
         model.ws = Workspace(need, device=st.kv_len.device)
-    if logits_out is not None:
-        _dev(logits_out, torch.float32, "logits_out")
-    if accept_out is not None:
-        _dev(accept_out, torch.int32, "accept_out", 1)
     sd = _state_desc(st, eos_id)
     rc = lib().literal_round_filtered(ctypes.byref(model.desc), ctypes.byref(sd), int(B), *par,
                                       _ptr(u), int(chunk_keys), _ptr(logits_out), _ptr(accept_out),
