@@ -217,6 +217,7 @@ class Workspace:
     def __init__(self, nbytes: int, device="cuda"):
         self.buf = torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=device)
         self.shape = None
+        self.streams = set()             # of the model calls that used it
 
     def prepare(self, nbytes: int, shape):
         self.ensure(nbytes)
@@ -726,6 +727,20 @@ def _state_desc(st: DeviceState, eos_id: int) -> DvsState:
                     st.out_count.data_ptr(), st.finished.data_ptr(), st.err.data_ptr())
 
 
+def _model_workspace(model, nbytes: int, device, stream):
+    """Makes model.ws hold nbytes for a call on `stream` (None: the current one):
+    cleared in that stream's order, and left to the allocator only when every
+    stream that a call used it on is past that call."""
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    if model.ws is None or model.ws.nbytes < nbytes:
+        with torch.cuda.stream(s):
+            model.ws = Workspace(nbytes, device=device)
+        model.ws.streams = {s.cuda_stream}
+    elif s.cuda_stream not in model.ws.streams:
+        model.ws.buf.record_stream(s)
+        model.ws.streams.add(s.cuda_stream)
+
+
 def draft_verify_step(model: DeviceModel, st: DeviceState, n_causal: int, n_mask: int,
                       chunk_keys: int = MODEL_CHUNK_KEYS, eos_id: int = -1, logits_out=None, argmax_out=None,
                       accept_out=None, stream=None):
@@ -734,8 +749,7 @@ def draft_verify_step(model: DeviceModel, st: DeviceState, n_causal: int, n_mask
     need = model.workspace_bytes(S, n_causal, n_mask, st.max_pages, chunk_keys)
     if need == 0:
         raise DvsError("draft_verify_step: invalid configuration")
-    if model.ws is None or model.ws.nbytes < need:
-        model.ws = Workspace(need, device=st.kv_len.device)
+    _model_workspace(model, need, st.kv_len.device, stream)
     for t, name in ((logits_out, "logits_out"), (argmax_out, "argmax_out"), (accept_out, "accept_out")):
         if t is not None:
             _dev(t, torch.float32 if name == "logits_out" else torch.int32, name)
@@ -756,8 +770,7 @@ def multidraft_step(model: DeviceModel, st: DeviceState, B: int,
     need = model.workspace_bytes(S, B, B * B, st.max_pages, chunk_keys)
     if need == 0:
         raise DvsError("multidraft_step: invalid configuration")
-    if model.ws is None or model.ws.nbytes < need:
-        model.ws = Workspace(need, device=st.kv_len.device)
+    _model_workspace(model, need, st.kv_len.device, stream)
     for t, name in ((logits_out, "logits_out"), (argmax_out, "argmax_out"), (accept_out, "accept_out")):
         if t is not None:
             _dev(t, torch.float32 if name == "logits_out" else torch.int32, name)
@@ -797,8 +810,7 @@ def literal_round(model: DeviceModel, st: DeviceState, B: int, chunk_keys: int =
     need = model.workspace_bytes(S, B + 1, 0, st.max_pages, chunk_keys)
     if need == 0:
         raise DvsError("literal_round: invalid configuration")
-    if model.ws is None or model.ws.nbytes < need:
-        model.ws = Workspace(need, device=st.kv_len.device)
+    _model_workspace(model, need, st.kv_len.device, stream)
     for t, name in ((logits_out, "logits_out"), (argmax_out, "argmax_out"), (accept_out, "accept_out")):
         if t is not None:
             _dev(t, torch.float32 if name == "logits_out" else torch.int32, name)
@@ -838,8 +850,7 @@ def literal_round_refined(model: DeviceModel, st: DeviceState, B: int, tau_d: fl
                model.workspace_bytes(S, B + 1, 0, st.max_pages, chunk_keys))
     if need == 0:
         raise DvsError("literal_round_refined: invalid configuration")
-    if model.ws is None or model.ws.nbytes < need:
-        model.ws = Workspace(need, device=st.kv_len.device)
+    _model_workspace(model, need, st.kv_len.device, stream)
     for t, name in ((logits_out, "logits_out"), (argmax_out, "argmax_out"), (accept_out, "accept_out")):
         if t is not None:
             _dev(t, torch.float32 if name == "logits_out" else torch.int32, name)
@@ -866,8 +877,7 @@ def literal_round_sampled(model: DeviceModel, st: DeviceState, B: int, temperatu
                                                        st.max_pages, int(chunk_keys)))
     if need == 0:
         raise DvsError("literal_round_sampled: invalid configuration")
-    if model.ws is None or model.ws.nbytes < need:
-        model.ws = Workspace(need, device=st.kv_len.device)
+    _model_workspace(model, need, st.kv_len.device, stream)
     if logits_out is not None:
         _dev(logits_out, torch.float32, "logits_out")
     if accept_out is not None:
@@ -894,8 +904,7 @@ def diffusion_denoise(model: DeviceModel, st: DeviceState, block, tau_c: float, 
     need = model.workspace_bytes(S, 1, B, st.max_pages, chunk_keys)
     if need == 0:
         raise DvsError("diffusion_denoise: invalid configuration")
-    if model.ws is None or model.ws.nbytes < need:
-        model.ws = Workspace(need, device=st.kv_len.device)
+    _model_workspace(model, need, st.kv_len.device, stream)
     if n_open is None:
         n_open = torch.empty(1, dtype=torch.int32, device=st.kv_len.device)
     _dev(n_open, torch.int32, "n_open", 1)
@@ -922,8 +931,7 @@ def diffusion_block(model: DeviceModel, st: DeviceState, B: int, tau_c: float, b
                                                    st.max_pages, int(chunk_keys)))
     if need == 0:
         raise DvsError("diffusion_block: invalid configuration")
-    if model.ws is None or model.ws.nbytes < need:
-        model.ws = Workspace(need, device=st.kv_len.device)
+    _model_workspace(model, need, st.kv_len.device, stream)
     if block is None:
         block = torch.empty((S, B), dtype=torch.int32, device=st.kv_len.device)
     _dev(block, torch.int32, "block", 2)
@@ -962,8 +970,7 @@ def literal_round_filtered(model: DeviceModel, st: DeviceState, B: int, u, tempe
                                                         st.max_pages, int(chunk_keys)))
     if need == 0:
         raise DvsError("literal_round_filtered: invalid configuration")
-    if model.ws is None or model.ws.nbytes < need:
-        model.ws = Workspace(need, device=st.kv_len.device)
+    _model_workspace(model, need, st.kv_len.device, stream)
     sd = _state_desc(st, eos_id)
     rc = lib().literal_round_filtered(ctypes.byref(model.desc), ctypes.byref(sd), int(B), *par,
                                       _ptr(u), int(chunk_keys), _ptr(logits_out), _ptr(accept_out),
@@ -1070,8 +1077,7 @@ def prefill(model: DeviceModel, st: DeviceState, P: int, n_mask: int, prefix_tok
                                                  st.max_pages, chunk_keys))
     if need == 0:
         raise DvsError("dvs_prefill: invalid configuration")
-    if model.ws is None or model.ws.nbytes < need:
-        model.ws = Workspace(need, device=st.kv_len.device)
+    _model_workspace(model, need, st.kv_len.device, stream)
     sd = _state_desc(st, eos_id)
     rc = lib().dvs_prefill(ctypes.byref(model.desc), ctypes.byref(sd), P, n_mask,
                            _ptr(prefix_tokens), _ptr(x_prefix), int(chunk_keys), _ptr(logits_out),
