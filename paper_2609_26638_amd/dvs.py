@@ -7,6 +7,7 @@ call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -178,6 +179,18 @@ def _stream(stream=None):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _on(stream):
+    """The stream as the current one, for what a call allocates or clears: memory
+    that another stream may still be using, or clears later, would not do."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _new(shape, dtype, device, stream):
+    """An output or scratch that the call leaves to its stream."""
+    with _on(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _dev(t, dtype, name, ndim=None):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise DvsError(f"{name} must be a CUDA (HIP) tensor")
@@ -237,7 +250,8 @@ class Workspace:
         return self
 
 
-def _attn_args(q, k_new, v_new, k_pool, v_pool, page_table, kv_len, n_causal, n_mask, out, err):
+def _attn_args(q, k_new, v_new, k_pool, v_pool, page_table, kv_len, n_causal, n_mask, out, err,
+               stream):
     """Shape and dtype checks shared by the two attention entry points."""
     dt = q.dtype
     _dev(q, dt, "q", 4)
@@ -259,7 +273,7 @@ def _attn_args(q, k_new, v_new, k_pool, v_pool, page_table, kv_len, n_causal, n_
     if R != n_causal + n_mask:
         raise DvsError("R must equal n_causal + n_mask")
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(q.shape, dt, q.device, stream)
     _dev(out, dt, "out", 4)
     if err is not None:
         _dev(err, torch.int32, "err", 1)
@@ -272,7 +286,7 @@ def attn_hybrid_block_noalloc(q, k_new, v_new, k_pool, v_pool, page_table, kv_le
     """attn_hybrid_block with the library's own scratch array as workspace (the C
     call allocates nothing; ``out`` is allocated here when not given)."""
     S, R, Hq, Hkv, D, P, max_pages, out = _attn_args(q, k_new, v_new, k_pool, v_pool, page_table,
-                                                     kv_len, n_causal, n_mask, out, err)
+                                                     kv_len, n_causal, n_mask, out, err, stream)
     rc = lib().attn_hybrid_block_noalloc(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_pool),
                                          _ptr(v_pool), _ptr(page_table), _ptr(kv_len), S, n_causal,
                                          n_mask, Hq, Hkv, D, max_pages, P, float(softmax_scale),
@@ -308,15 +322,16 @@ def attn_hybrid_block(q, k_new, v_new, k_pool, v_pool, page_table, kv_len, n_cau
         raise DvsError("R must equal n_causal + n_mask")
     max_pages = page_table.shape[1]
     if out is None:
-        out = torch.empty_like(q)
+        out = _new(q.shape, dt, q.device, stream)
     _dev(out, dt, "out", 4)
     if err is not None:
         _dev(err, torch.int32, "err", 1)
     code = _dtype_code(q)
     need = attn_workspace_bytes(S, n_causal, n_mask, Hq, Hkv, D, max_pages, chunk_keys, code)
-    if workspace is None:
-        workspace = Workspace(need, device=q.device)
-    workspace.prepare(need, ("attn", S, R, Hq, Hkv, D, max_pages, int(chunk_keys), code))
+    with _on(stream):
+        if workspace is None:
+            workspace = Workspace(need, device=q.device)
+        workspace.prepare(need, ("attn", S, R, Hq, Hkv, D, max_pages, int(chunk_keys), code))
     rc = lib().attn_hybrid_block(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_pool), _ptr(v_pool),
                                  _ptr(page_table), _ptr(kv_len), S, n_causal, n_mask, Hq, Hkv, D,
                                  max_pages, P, float(softmax_scale), code, int(chunk_keys),
@@ -338,9 +353,9 @@ def argmax_accept(logits, n_causal: int, draft, argmax_out=None, accept_len=None
     S, R, V = logits.shape
     _dev(draft, torch.int32, "draft", 2)
     if argmax_out is None:
-        argmax_out = torch.empty((S, R), dtype=torch.int32, device=logits.device)
+        argmax_out = _new((S, R), torch.int32, logits.device, stream)
     if accept and accept_len is None:
-        accept_len = torch.empty((S,), dtype=torch.int32, device=logits.device)
+        accept_len = _new((S,), torch.int32, logits.device, stream)
     if not accept:
         accept_len = None
     _dev(argmax_out, torch.int32, "argmax_out", 2)
@@ -362,9 +377,9 @@ def top1_confidence(logits, argmax_out=None, conf_out=None, err=None, stream=Non
     lead, V = logits.shape[:-1], logits.shape[-1]
     rows = int(np.prod(lead)) if len(lead) else 1
     if argmax_out is None:
-        argmax_out = torch.empty(lead, dtype=torch.int32, device=logits.device)
+        argmax_out = _new(lead, torch.int32, logits.device, stream)
     if conf_out is None:
-        conf_out = torch.empty(lead, dtype=torch.float32, device=logits.device)
+        conf_out = _new(lead, torch.float32, logits.device, stream)
     _dev(argmax_out, torch.int32, "argmax_out")
     _dev(conf_out, torch.float32, "conf_out")
     if argmax_out.numel() != rows or conf_out.numel() != rows:
@@ -387,15 +402,6 @@ def _here(*tensors):
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise DvsError(f"tensors must be on the current device {dev}, got {t.device}")
-
-
-def _new(shape, dtype, device, stream):
-    """An output or scratch that the call leaves to its stream: memory that another
-    stream may still be using would not do."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _scratch(workspace, nbytes, device, stream):
@@ -588,7 +594,7 @@ def accept_commit(st: DeviceState, argmax, n_causal: int, n_mask: int, accept_ou
     if argmax.shape != (S, n_causal + n_mask):
         raise DvsError("argmax must be [S, n_causal + n_mask]")
     if accept_out is None:
-        accept_out = torch.empty((S,), dtype=torch.int32, device=argmax.device)
+        accept_out = _new((S,), torch.int32, argmax.device, stream)
     _dev(accept_out, torch.int32, "accept_out", 1)
     rc = lib().accept_commit(S, n_causal, n_mask, int(draft_group), _ptr(argmax), _ptr(accept_out), _ptr(st.kv_len),
                              _ptr(st.page_table), _ptr(st.num_pages), st.max_pages,
@@ -786,12 +792,13 @@ def attn_hybrid_block_grouped(q, k_new, v_new, k_pool, v_pool, page_table, kv_le
                               err=None, workspace=None, chunk_keys: int = 0, stream=None):
     """attn_hybrid_block with the mask rows in groups of mask_group rows."""
     S, R, Hq, Hkv, D, P, max_pages, out = _attn_args(q, k_new, v_new, k_pool, v_pool, page_table,
-                                                     kv_len, n_causal, n_mask, out, err)
+                                                     kv_len, n_causal, n_mask, out, err, stream)
     code = _dtype_code(q)
     need = attn_workspace_bytes(S, n_causal, n_mask, Hq, Hkv, D, max_pages, chunk_keys, code)
-    if workspace is None:
-        workspace = Workspace(need, device=q.device)
-    workspace.prepare(need, ("attn", S, R, Hq, Hkv, D, max_pages, int(chunk_keys), code))
+    with _on(stream):
+        if workspace is None:
+            workspace = Workspace(need, device=q.device)
+        workspace.prepare(need, ("attn", S, R, Hq, Hkv, D, max_pages, int(chunk_keys), code))
     rc = lib().attn_hybrid_block_grouped(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_pool),
                                          _ptr(v_pool), _ptr(page_table), _ptr(kv_len), S, n_causal,
                                          n_mask, int(mask_group), Hq, Hkv, D, max_pages, P,
@@ -906,7 +913,7 @@ def diffusion_denoise(model: DeviceModel, st: DeviceState, block, tau_c: float, 
         raise DvsError("diffusion_denoise: invalid configuration")
     _model_workspace(model, need, st.kv_len.device, stream)
     if n_open is None:
-        n_open = torch.empty(1, dtype=torch.int32, device=st.kv_len.device)
+        n_open = _new(1, torch.int32, st.kv_len.device, stream)
     _dev(n_open, torch.int32, "n_open", 1)
     for t, name, dt in ((logits_out, "logits_out", torch.float32),
                         (argmax_out, "argmax_out", torch.int32), (conf_out, "conf_out", torch.float32)):
@@ -933,7 +940,7 @@ def diffusion_block(model: DeviceModel, st: DeviceState, B: int, tau_c: float, b
         raise DvsError("diffusion_block: invalid configuration")
     _model_workspace(model, need, st.kv_len.device, stream)
     if block is None:
-        block = torch.empty((S, B), dtype=torch.int32, device=st.kv_len.device)
+        block = _new((S, B), torch.int32, st.kv_len.device, stream)
     _dev(block, torch.int32, "block", 2)
     if tuple(block.shape) != (S, B):
         raise DvsError("block must be [S, B]")
