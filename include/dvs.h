@@ -91,7 +91,8 @@ const char* dvs_last_error(void);
  *   v_pool  [num_pool_pages, Hkv, D, 16]  paged V cache, head-dim-major (updated)
  *   page_table [S, max_pages] int32, kv_len [S] int32 (read only)
  *   out     [S, R, Hq, D]     attention output, same dtype as q
- *   chunk_keys   key-range split per workgroup (multiple of 64), or 0 for
+ *   chunk_keys   key-range split per workgroup (a multiple of 64 up to 16384;
+ *                others are refused, size queries give 0), or 0 for
  *                the balanced split.  Chunks start at absolute positions that
  *                are multiples of it, so a row's arithmetic does not depend on
  *                the other rows (a causal row equals an AR call bit for bit).

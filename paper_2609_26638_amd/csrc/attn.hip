@@ -1938,6 +1938,11 @@ struct AttnPlan {
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 
+// Chunks of whole tiles, or the balanced split.
+bool attn_chunk_ok(int chunk_keys) {
+  return chunk_keys >= 0 && chunk_keys % KT == 0 && chunk_keys <= MAX_CHUNK_KEYS;
+}
+
 static AttnPlan plan_attn(int S, int R, int Hq, int Hkv, int D, int max_pages, int chunk_keys,
                           int dtype) {
   AttnPlan pl{};
@@ -2119,7 +2124,7 @@ extern "C" size_t dvs_attn_workspace_bytes(int32_t S, int32_t n_causal, int32_t 
                                            int32_t Hq, int32_t Hkv, int32_t D, int32_t max_pages,
                                            int32_t chunk_keys, int32_t dtype) {
   if (S < 1 || n_causal < 0 || n_mask < 0 || n_causal + n_mask < 1 || Hkv < 1 || Hq < Hkv ||
-      Hq % Hkv != 0 || max_pages < 1 || chunk_keys < 0)
+      Hq % Hkv != 0 || max_pages < 1 || !attn_chunk_ok(chunk_keys))
     return 0;
   return plan_attn(S, n_causal + n_mask, Hq, Hkv, D, max_pages, chunk_keys, dtype).bytes;
 }
@@ -2143,7 +2148,7 @@ static int attn_launch(const void* q, const void* k_new, const void* v_new, void
   DVS_CHECK_ARG(max_pages >= 1 && num_pool_pages >= 1, "attn_hybrid_block: empty page table/pool");
   DVS_CHECK_ARG(softmax_scale > 0.f && isfinite(softmax_scale),
                 "attn_hybrid_block: softmax_scale must be positive");
-  DVS_CHECK_ARG(chunk_keys >= 0 && chunk_keys % KT == 0 && chunk_keys <= MAX_CHUNK_KEYS,
+  DVS_CHECK_ARG(attn_chunk_ok(chunk_keys),
                 "attn_hybrid_block: chunk_keys must be a multiple of 64 and <= %d", MAX_CHUNK_KEYS);
   DVS_CHECK_SUPPORTED(dtype == DVS_F32 || dtype == DVS_BF16, "attn_hybrid_block: dtype %d", dtype);
   DVS_CHECK_SUPPORTED(D == 64 || D == 96 || D == 128, "attn_hybrid_block: head_dim %d", D);

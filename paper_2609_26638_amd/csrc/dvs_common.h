@@ -65,6 +65,8 @@ int launch_accept_sampled(const void* zv, long long vs, long long vld, const voi
                           int token_stride, int at_accepted, int32_t* err, void* ws,
                           hipStream_t st);
 
+// Whether an attention call takes this chunk_keys (what plans its shape needs it).
+bool attn_chunk_ok(int chunk_keys);
 // Bytes at the start of an attention workspace that hold the split-merge
 // counters (zero between calls) for the given call shape.
 size_t attn_counter_bytes(int S, int R, int Hq, int Hkv, int D, int max_pages, int chunk_keys,

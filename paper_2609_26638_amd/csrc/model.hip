@@ -2063,7 +2063,9 @@ using namespace dvs;
 
 extern "C" size_t dvs_step_workspace_bytes(const dvs_model* m, int32_t S, int32_t n_causal,
                                            int32_t n_mask, int32_t max_pages, int32_t chunk_keys) {
-  if (!model_ok(m) || S < 1 || n_causal < 1 || n_mask < 0 || max_pages < 1) return 0;
+  if (!model_ok(m) || !attn_chunk_ok(chunk_keys) || S < 1 || n_causal < 1 || n_mask < 0 ||
+      max_pages < 1)
+    return 0;
   return step_layout(m, S, n_causal, n_mask, max_pages, chunk_keys,
                      (size_t)S * (n_causal + n_mask)).total;
 }
@@ -2074,6 +2076,7 @@ extern "C" int draft_verify_step(const dvs_model* m, const dvs_state* st, int32_
                                  size_t ws_bytes, void* stream) {
   clear_error();
   DVS_CHECK_ARG(model_ok(m), "draft_verify_step: invalid model description");
+  DVS_CHECK_ARG(attn_chunk_ok(chunk_keys), "draft_verify_step: chunk_keys %d", chunk_keys);
   DVS_CHECK_ARG(st && st->S >= 1 && st->kv_len && st->page_table && st->num_pages &&
                     st->free_stack && st->free_top && st->boundary && st->out_tokens &&
                     st->out_count && st->finished,
@@ -2104,7 +2107,8 @@ extern "C" int draft_verify_step(const dvs_model* m, const dvs_state* st, int32_
                          argmax_out, accept_out, s);
 }
 
-static int check_model_state(const dvs_model* m, const dvs_state* st, const char* who);
+static int check_model_state(const dvs_model* m, const dvs_state* st, int chunk_keys,
+                             const char* who);
 
 extern "C" int multidraft_step(const dvs_model* m, const dvs_state* st, int32_t B,
                                int32_t chunk_keys, float* logits_out, int32_t* argmax_out,
@@ -2113,7 +2117,7 @@ extern "C" int multidraft_step(const dvs_model* m, const dvs_state* st, int32_t 
   clear_error();
   DVS_CHECK_ARG(model_ok(m), "multidraft_step: invalid model description");
   DVS_CHECK_ARG(B >= 1 && B <= 64, "multidraft_step: need 1 <= B <= 64");
-  int rc = check_model_state(m, st, "multidraft_step");
+  int rc = check_model_state(m, st, chunk_keys, "multidraft_step");
   if (rc) return rc;
   DVS_CHECK_ARG(st->draft_width >= B - 1 && st->draft_width <= B,
                 "multidraft_step: draft width must be B - 1 or B");
@@ -2137,6 +2141,7 @@ extern "C" int literal_round(const dvs_model* m, const dvs_state* st, int32_t B,
                              int32_t* accept_out, void* workspace, size_t ws_bytes, void* stream) {
   clear_error();
   DVS_CHECK_ARG(model_ok(m), "literal_round: invalid model description");
+  DVS_CHECK_ARG(attn_chunk_ok(chunk_keys), "literal_round: chunk_keys %d", chunk_keys);
   DVS_CHECK_ARG(st && st->S >= 1 && st->kv_len && st->page_table && st->num_pages &&
                     st->free_stack && st->free_top && st->boundary && st->out_tokens &&
                     st->out_count && st->finished,
@@ -2169,7 +2174,8 @@ extern "C" int literal_round(const dvs_model* m, const dvs_state* st, int32_t B,
 extern "C" size_t dvs_prefill_workspace_bytes(const dvs_model* m, int32_t S, int32_t P,
                                               int32_t n_mask, int32_t max_pages,
                                               int32_t chunk_keys) {
-  if (!model_ok(m) || S < 1 || P < 1 || n_mask < 0 || max_pages < 1) return 0;
+  if (!model_ok(m) || !attn_chunk_ok(chunk_keys) || S < 1 || P < 1 || n_mask < 0 || max_pages < 1)
+    return 0;
   return step_layout(m, S, P, n_mask, max_pages, chunk_keys, (size_t)S * (n_mask + 1)).total;
 }
 
@@ -2178,6 +2184,7 @@ extern "C" int dvs_prefill(const dvs_model* m, const dvs_state* st, int32_t P, i
                            float* logits_out, void* workspace, size_t ws_bytes, void* stream) {
   clear_error();
   DVS_CHECK_ARG(model_ok(m), "dvs_prefill: invalid model description");
+  DVS_CHECK_ARG(attn_chunk_ok(chunk_keys), "dvs_prefill: chunk_keys %d", chunk_keys);
   DVS_CHECK_ARG(st && st->S >= 1 && st->kv_len && st->page_table && st->boundary &&
                     st->out_tokens && st->out_count && st->finished,
                 "dvs_prefill: invalid state description");
@@ -2202,12 +2209,14 @@ extern "C" int dvs_prefill(const dvs_model* m, const dvs_state* st, int32_t P, i
                             (char*)workspace, logits_out, s);
 }
 
-static int check_model_state(const dvs_model* m, const dvs_state* st, const char* who) {
+static int check_model_state(const dvs_model* m, const dvs_state* st, int chunk_keys,
+                             const char* who) {
   DVS_CHECK_ARG(model_ok(m), "%s: invalid model description", who);
   DVS_CHECK_ARG(st && st->S >= 1 && st->kv_len && st->page_table && st->num_pages &&
                     st->free_stack && st->free_top && st->boundary && st->out_tokens &&
                     st->out_count && st->finished,
                 "%s: invalid state description", who);
+  DVS_CHECK_ARG(attn_chunk_ok(chunk_keys), "%s: chunk_keys %d", who, chunk_keys);
   for (int l = 0; l < m->n_layers; ++l) {
     const dvs_layer& ly = m->layers[l];
     DVS_CHECK_ARG(ly.wq && ly.wk && ly.wv && ly.wo && ly.g_attn && ly.k_pool && ly.v_pool,
@@ -2222,7 +2231,7 @@ static int check_model_state(const dvs_model* m, const dvs_state* st, const char
 
 extern "C" size_t dvs_diffusion_workspace_bytes(const dvs_model* m, int32_t S, int32_t B,
                                                 int32_t max_pages, int32_t chunk_keys) {
-  if (!model_ok(m) || S < 1 || B < 1 || max_pages < 1) return 0;
+  if (!model_ok(m) || !attn_chunk_ok(chunk_keys) || S < 1 || B < 1 || max_pages < 1) return 0;
   return std::max(step_layout(m, S, 1, B, max_pages, chunk_keys, (size_t)S * (B + 1)).total,
                   step_layout(m, S, B, 0, max_pages, chunk_keys, 0).total);
 }
@@ -2232,7 +2241,7 @@ extern "C" int diffusion_denoise(const dvs_model* m, const dvs_state* st, int32_
                                  float* logits_out, int32_t* argmax_out, float* conf_out,
                                  void* workspace, size_t ws_bytes, void* stream) {
   clear_error();
-  int rc = check_model_state(m, st, "diffusion_denoise");
+  int rc = check_model_state(m, st, chunk_keys, "diffusion_denoise");
   if (rc) return rc;
   DVS_CHECK_ARG(B >= 1 && block && n_open, "diffusion_denoise: need B >= 1, block, n_open");
   const StepLayout L = step_layout(m, st->S, 1, B, st->max_pages, chunk_keys,
@@ -2253,7 +2262,7 @@ extern "C" int diffusion_block(const dvs_model* m, const dvs_state* st, int32_t 
                                int32_t* block, int32_t chunk_keys, int32_t* steps_out,
                                void* workspace, size_t ws_bytes, void* stream) {
   clear_error();
-  int rc = check_model_state(m, st, "diffusion_block");
+  int rc = check_model_state(m, st, chunk_keys, "diffusion_block");
   if (rc) return rc;
   DVS_CHECK_ARG(B >= 1 && block, "diffusion_block: need B >= 1 and a block array");
   const int S = st->S;
@@ -2301,7 +2310,7 @@ extern "C" int literal_round_refined(const dvs_model* m, const dvs_state* st, in
                                      int32_t* draft_steps_out, void* workspace, size_t ws_bytes,
                                      void* stream) {
   clear_error();
-  int rc = check_model_state(m, st, "literal_round_refined");
+  int rc = check_model_state(m, st, chunk_keys, "literal_round_refined");
   if (rc) return rc;
   DVS_CHECK_ARG(B >= 1, "literal_round_refined: need B >= 1");
   DVS_CHECK_ARG(st->draft && st->draft_width >= B, "literal_round_refined: draft narrower than B");
@@ -2335,7 +2344,7 @@ static size_t sampled_extra(const dvs_model* m, int S, int B, int max_pages, int
 
 extern "C" size_t dvs_sampled_round_workspace_bytes(const dvs_model* m, int32_t S, int32_t B,
                                                     int32_t max_pages, int32_t chunk_keys) {
-  if (!model_ok(m) || S < 1 || B < 1 || max_pages < 1) return 0;
+  if (!model_ok(m) || !attn_chunk_ok(chunk_keys) || S < 1 || B < 1 || max_pages < 1) return 0;
   StepLayout Ld, Lv;
   const size_t M = (size_t)S * (B + 1);
   return sampled_extra(m, S, B, max_pages, chunk_keys, &Ld, &Lv) + al(M * m->vocab * 4) +
@@ -2347,7 +2356,7 @@ extern "C" int literal_round_sampled(const dvs_model* m, const dvs_state* st, in
                                      float* logits_out, int32_t* accept_out, void* workspace,
                                      size_t ws_bytes, void* stream) {
   clear_error();
-  int rc = check_model_state(m, st, "literal_round_sampled");
+  int rc = check_model_state(m, st, chunk_keys, "literal_round_sampled");
   if (rc) return rc;
   DVS_CHECK_ARG(B >= 1 && u, "literal_round_sampled: need B >= 1 and uniforms");
   DVS_CHECK_ARG(temperature > 0.f && temperature < 1e30f,
@@ -2370,7 +2379,9 @@ extern "C" int literal_round_sampled(const dvs_model* m, const dvs_state* st, in
 
 extern "C" size_t dvs_filtered_round_workspace_bytes(const dvs_model* m, int32_t S, int32_t B,
                                                      int32_t max_pages, int32_t chunk_keys) {
-  if (!model_ok(m) || S < 1 || B < 1 || max_pages < 1 || m->vocab > (1 << 22)) return 0;
+  if (!model_ok(m) || !attn_chunk_ok(chunk_keys) || S < 1 || B < 1 || max_pages < 1 ||
+      m->vocab > (1 << 22))
+    return 0;
   StepLayout Ld, Lv;
   const size_t M = (size_t)S * (B + 1);
   return sampled_extra(m, S, B, max_pages, chunk_keys, &Ld, &Lv) + al(M * m->vocab * 4) +
@@ -2383,7 +2394,7 @@ extern "C" int literal_round_filtered(const dvs_model* m, const dvs_state* st, i
                                       int32_t chunk_keys, float* logits_out, int32_t* accept_out,
                                       void* workspace, size_t ws_bytes, void* stream) {
   clear_error();
-  int rc = check_model_state(m, st, "literal_round_filtered");
+  int rc = check_model_state(m, st, chunk_keys, "literal_round_filtered");
   if (rc) return rc;
   DVS_CHECK_ARG(B >= 1 && u, "literal_round_filtered: need B >= 1 and uniforms");
   DVS_CHECK_ARG(m->vocab <= (1 << 22), "literal_round_filtered: vocab over 2^22");
