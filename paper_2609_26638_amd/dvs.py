@@ -185,6 +185,11 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _check_err(err):
+    if err is not None and not _dev(err, torch.int32, "err", 1).shape[0]:
+        raise DvsError("err must have an entry")
+
+
 def _new(shape, dtype, device, stream):
     """An output or scratch that the call leaves to its stream."""
     with _on(stream):
@@ -405,7 +410,10 @@ def _here(*tensors):
 
 
 def _scratch(workspace, nbytes, device, stream):
-    return workspace.buf if workspace is not None else _new(nbytes, torch.uint8, device, stream)
+    if workspace is None:
+        return _new(nbytes, torch.uint8, device, stream)
+    _here(workspace.buf)
+    return workspace.buf
 
 
 def _filter_params(n, temperature, top_k, top_p, min_p):
@@ -437,8 +445,8 @@ def _logit_rows(t, name, ndim=None):
 
 def sample_filtered(logits, u, temperature=None, top_k=None, top_p=None, min_p=None,
                     token_out=None, prob_out=None, err=None, stream=None):
-    """logits [..., V] (f32/bf16; contiguous rows, evenly apart), u [...] f32 in [0, 1) ->
-    (token [...] int32, its probability [...] f32).  temperature, top_p, min_p (f32) and
+    """logits [..., V] (f32/bf16; contiguous rows, which may lie apart in 2 dims), u [...] f32
+    in [0, 1) -> (token [...] int32, its probability [...] f32).  temperature, top_p, min_p (f32) and
     top_k (int32) have one entry per group of rows (rows / entries rows each)."""
     code = _logit_rows(logits, "logits")
     lead, V = logits.shape[:-1], logits.shape[-1]
@@ -466,8 +474,7 @@ def sample_filtered(logits, u, temperature=None, top_k=None, top_p=None, min_p=N
     if token_out.numel() != rows or prob_out.numel() != rows:
         raise DvsError("token_out / prob_out must have one entry per row")
     _here(logits, u, token_out, prob_out, err)
-    if err is not None:
-        _dev(err, torch.int32, "err", 1)
+    _check_err(err)
     rc = lib().sample_filtered(_ptr(logits), code, rows, V, ld, *par, rows // n, _ptr(u),
                                _ptr(token_out), _ptr(prob_out), _ptr(err), _stream(stream))
     _check(rc, "sample_filtered")
@@ -504,8 +511,7 @@ def accept_sampled(z_verify, z_draft, draft, u, temperature=None, top_k=None, to
     if accept_len.shape[0] != S or token_out.shape[0] != S:
         raise DvsError("accept_len / token_out must have S entries")
     _here(z_verify, z_draft, draft, u, accept_len, token_out, err)
-    if err is not None:
-        _dev(err, torch.int32, "err", 1)
+    _check_err(err)
     ws = _scratch(workspace, accept_workspace_bytes(S, B, V), z_verify.device, stream)
     # a sequence's only draft row has no next one to be apart from
     draft_ld = z_draft.stride(1) if B > 1 else V
@@ -1005,6 +1011,8 @@ class KVPools:
             P, Hkv, _, D = shape
             if tuple(k.shape) != (P, Hkv, 16, D) or tuple(v.shape) != (P, Hkv, D, 16):
                 raise DvsError("pools must be k [P,Hkv,16,D] and v [P,Hkv,D,16]")
+            if k.device != k_pools[0].device or v.device != k.device:
+                raise DvsError("the pools must be on one device")
             self.layers[l].k_pool, self.layers[l].v_pool = k.data_ptr(), v.data_ptr()
         self.pages, self.n_kv_heads, self.head_dim = shape[0], shape[1], shape[3]
         self.keep = (list(k_pools), list(v_pools))
@@ -1020,6 +1028,7 @@ def _kv_workspace(st, workspace, stream):
 
 
 def _check_pools(st, pools):
+    _here(pools.keep[0][0])
     if pools.pages != st.pool_pages:
         raise DvsError(f"the pools have {pools.pages} pages, the state's {st.pool_pages}")
 
@@ -1061,6 +1070,8 @@ def kv_compact(st: DeviceState, pools: KVPools, moved_out=None, workspace=None, 
     if moved_out is None:
         moved_out = _new(1, torch.int32, st.kv_len.device, stream)
     _dev(moved_out, torch.int32, "moved_out", 1)
+    if moved_out.shape[0] != 1:
+        raise DvsError("moved_out must have one entry")
     _here(st.kv_len, moved_out)
     ws = _kv_workspace(st, workspace, stream)
     sd = _state_desc(st, -1)
