@@ -1394,9 +1394,9 @@ template <int FT, typename E>
 __global__ void __launch_bounds__(FT, 4) sample_filtered_kernel(
     const E* __restrict__ logits, long long ld, int V, int nit, RowParams par, int rows_per_param,
     const float* __restrict__ u, int u_stride, int32_t* __restrict__ token_out,
-    float* __restrict__ prob_out, int32_t* err) {
+    float* __restrict__ prob_out, int32_t* err, int first) {
   auto& sh = RowFilter<FT>::shared();
-  const int r = blockIdx.x, s = r / rows_per_param;
+  const int r = first + blockIdx.x, s = r / rows_per_param;
   const typename RowFilter<FT>::template Row<E> row(logits + (size_t)r * ld, V, nit);
   float uu = u[(size_t)s * u_stride + (r - s * rows_per_param)];
   if (!(uu > 0.0f)) uu = 0.0f;
@@ -1412,8 +1412,8 @@ template <int FT, typename E>
 __global__ void __launch_bounds__(FT, 4) filter_rows_kernel(
     const E* __restrict__ zv, long long vs, long long vld, const E* __restrict__ zd, long long ds,
     long long dld, int B, int nv, int V, int nit, RowParams par, RowCut* __restrict__ cuts,
-    int32_t* err) {
-  const int r = blockIdx.x;
+    int32_t* err, int first) {
+  const int r = first + blockIdx.x;
   const int per = r < nv ? B + 1 : B, i = r < nv ? r : r - nv;
   const int s = i / per, j = i - s * per;
   const E* z = r < nv ? zv + (size_t)s * vs + (size_t)j * vld : zd + (size_t)s * ds + (size_t)j * dld;
@@ -1442,10 +1442,10 @@ __global__ void __launch_bounds__(1024) accept_filtered_kernel(
     long long dld, int S, int B, int V, int nit, const RowCut* __restrict__ cuts,
     const int32_t* __restrict__ draft, int draft_width, const float* __restrict__ u, int u_stride,
     int32_t* __restrict__ accept_len, int32_t* __restrict__ token_out, int token_stride,
-    int at_accepted) {
+    int at_accepted, int first) {
   using F = RowFilter<1024>;
   auto& sh = F::shared();
-  const int s = blockIdx.x, tid = threadIdx.x;
+  const int s = first + blockIdx.x, tid = threadIdx.x;
   const RowCut* cv = cuts + (size_t)s * (B + 1);
   const RowCut* cd = cuts + (size_t)S * (B + 1) + (size_t)s * B;
   const E* v = zv + (size_t)s * vs;
@@ -1528,6 +1528,15 @@ static void by_rows(int rows, F f) {
     f(IC<512>{});
 }
 
+// Calls f(first, count) for `groups` workgroups, 2^21 at a time: a launch has less
+// than 2^32 threads.
+template <typename F>
+static void by_launches(int groups, F f) {
+  constexpr int MOST = 1 << 21;
+  for (long long first = 0; first < groups; first += MOST)
+    f((int)first, (int)(groups - first < MOST ? groups - first : MOST));
+}
+
 template <typename E>
 static int launch_accept(const void* zv, long long vs, long long vld, const void* zd, long long ds,
                          long long dld, int S, int B, int V, const RowParams& par,
@@ -1535,16 +1544,21 @@ static int launch_accept(const void* zv, long long vs, long long vld, const void
                          int32_t* accept_len, int32_t* token_out, int token_stride,
                          int at_accepted, int32_t* err, void* ws, hipStream_t st) {
   RowCut* cuts = (RowCut*)ws;
-  by_rows(S * (2 * B + 1), [&](auto threads) {
+  const int rows = S * (2 * B + 1);
+  by_rows(rows, [&](auto threads) {
     constexpr int FT = decltype(threads)::value;
-    hipLaunchKernelGGL((filter_rows_kernel<FT, E>), dim3(S * (2 * B + 1)), dim3(FT), 0, st,
-                       (const E*)zv, vs, vld, (const E*)zd, ds, dld, B, S * (B + 1), V,
-                       row_vectors<E>(V, FT), par, cuts, err);
+    by_launches(rows, [&](int first, int n) {
+      hipLaunchKernelGGL((filter_rows_kernel<FT, E>), dim3(n), dim3(FT), 0, st, (const E*)zv, vs,
+                         vld, (const E*)zd, ds, dld, B, S * (B + 1), V, row_vectors<E>(V, FT), par,
+                         cuts, err, first);
+    });
   });
   const int nit = row_vectors<E>(V, 1024);
-  hipLaunchKernelGGL(accept_filtered_kernel<E>, dim3(S), dim3(1024), 0, st, (const E*)zv, vs, vld,
-                     (const E*)zd, ds, dld, S, B, V, nit, cuts, draft, draft_width, u, u_stride,
-                     accept_len, token_out, token_stride, at_accepted);
+  by_launches(S, [&](int first, int n) {
+    hipLaunchKernelGGL(accept_filtered_kernel<E>, dim3(n), dim3(1024), 0, st, (const E*)zv, vs, vld,
+                       (const E*)zd, ds, dld, S, B, V, nit, cuts, draft, draft_width, u, u_stride,
+                       accept_len, token_out, token_stride, at_accepted, first);
+  });
   return launch_status("accept_sampled");
 }
 
@@ -1554,9 +1568,11 @@ static void launch_sample(const void* logits, int rows, int V, long long ld, con
                           float* prob_out, int32_t* err, hipStream_t st) {
   by_rows(rows, [&](auto threads) {
     constexpr int FT = decltype(threads)::value;
-    hipLaunchKernelGGL((sample_filtered_kernel<FT, E>), dim3(rows), dim3(FT), 0, st,
-                       (const E*)logits, ld, V, row_vectors<E>(V, FT), par, rows_per_param, u,
-                       u_stride, token_out, prob_out, err);
+    by_launches(rows, [&](int first, int n) {
+      hipLaunchKernelGGL((sample_filtered_kernel<FT, E>), dim3(n), dim3(FT), 0, st,
+                         (const E*)logits, ld, V, row_vectors<E>(V, FT), par, rows_per_param, u,
+                         u_stride, token_out, prob_out, err, first);
+    });
   });
 }
 
