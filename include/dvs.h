@@ -673,8 +673,8 @@ int literal_round_filtered(const dvs_model* m, const dvs_state* st, int32_t B,
  *   layers: only k_pool and v_pool are read; they start on 16 bytes.
  *   workspace >= dvs_kv_workspace_bytes(S, num_pool_pages) bytes, no
  *   initialisation needed.  Calls that share it must not overlap in time.
- * Requirements: 1 <= S <= 1024, max_pages <= 2^20, window >= 1, 1 <= n < S
- * (kv_release: <= S).
+ * Requirements: 1 <= S <= 1024, max_pages <= 2^20, num_pool_pages <= 2^29,
+ * window >= 1, 1 <= n < S (kv_release: <= S).
  * ---------------------------------------------------------------------- */
 size_t dvs_kv_workspace_bytes(int32_t S, int32_t num_pool_pages);
 int kv_fork(const dvs_state* st, int32_t* page_refs, const dvs_layer* layers, int32_t n_layers,

@@ -42,6 +42,7 @@ constexpr int PLAN_THREADS = 1024;
 constexpr int COPY_THREADS = 256;
 constexpr int SMALL_ENTRIES = 4096, SMALL_POOL = 32768;
 constexpr int COPY_LAYERS = 64;    // pools per launch (as kernel arguments)
+constexpr int MAX_POOL = 1 << 29;  // sums of two page counts, and ids by whole words, fit 31 bits
 
 struct PageState {   // of dvs_state, as the kernels take it
   int S, max_pages, pool, draft_width, max_new;
@@ -633,7 +634,7 @@ using namespace dvs;
 static size_t al(size_t v) { return (v + 255) & ~(size_t)255; }
 
 extern "C" size_t dvs_kv_workspace_bytes(int32_t S, int32_t num_pool_pages) {
-  if (S < 1 || S > PLAN_THREADS || num_pool_pages < 1) return 0;
+  if (S < 1 || S > PLAN_THREADS || num_pool_pages < 1 || num_pool_pages > MAX_POOL) return 0;
   const size_t words = ((size_t)num_pool_pages + 31) / 32;
   return 256 + 4 * al((size_t)S * 4) + 2 * al(words * 4) + 3 * al((size_t)num_pool_pages * 4);
 }
@@ -664,6 +665,7 @@ static int check_state(const char* who, const dvs_state* st, PageState& p, int32
   DVS_CHECK_ARG(st->max_pages >= 1 && st->num_pool_pages >= 1 && st->max_new >= 1,
                 "%s: need max_pages, num_pool_pages, max_new >= 1", who);
   DVS_CHECK_ARG(st->max_pages <= (1 << 20), "%s: max_pages over 2^20", who);
+  DVS_CHECK_ARG(st->num_pool_pages <= MAX_POOL, "%s: num_pool_pages over 2^29", who);
   DVS_CHECK_ARG(st->draft_width >= 0 && (st->draft || st->draft_width == 0), "%s: bad draft", who);
   const size_t need = dvs_kv_workspace_bytes(st->S, st->num_pool_pages);
   if (!workspace || ws_bytes < need) {
