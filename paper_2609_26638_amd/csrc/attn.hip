@@ -1994,7 +1994,7 @@ static AttnPlan plan_attn(int S, int R, int Hq, int Hkv, int D, int max_pages, i
     // and the count-in (32 sequences of 1k-4k cached tokens, four layers of a
     // fused step: 1.14 / 1.09 / 1.15 / 1.15 ms with 1 / 2 / 3 / 4 per CU).
     const int want = 2 * device_cus();
-    pl.wgs_per_item = std::min(pl.n_chunks_max, (want + pl.n_items - 1) / pl.n_items);
+    pl.wgs_per_item = std::min(pl.n_chunks_max, (want + pl.n_items - 1) / std::max(1, pl.n_items));
     // Two workgroups per CU also where one would do, except for the 128-wide
     // heads, whose 256 registers per thread then spill a few (steps of one
     // sequence, D = 96: 155 -> 148 and 181 -> 172 us; D = 128: 140.7 -> 142.6).
