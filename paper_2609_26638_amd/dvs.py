@@ -410,10 +410,11 @@ def _here(*tensors):
 
 
 def _scratch(workspace, nbytes, device, stream):
-    if workspace is None:
-        return _new(nbytes, torch.uint8, device, stream)
-    _here(workspace.buf)
-    return workspace.buf
+    return workspace.buf if workspace is not None else _new(nbytes, torch.uint8, device, stream)
+
+
+def _buf(workspace):
+    return None if workspace is None else workspace.buf
 
 
 def _filter_params(n, temperature, top_k, top_p, min_p):
@@ -510,7 +511,7 @@ def accept_sampled(z_verify, z_draft, draft, u, temperature=None, top_k=None, to
     _dev(token_out, torch.int32, "token_out", 1)
     if accept_len.shape[0] != S or token_out.shape[0] != S:
         raise DvsError("accept_len / token_out must have S entries")
-    _here(z_verify, z_draft, draft, u, accept_len, token_out, err)
+    _here(z_verify, z_draft, draft, u, accept_len, token_out, err, _buf(workspace))
     _check_err(err)
     ws = _scratch(workspace, accept_workspace_bytes(S, B, V), z_verify.device, stream)
     # a sequence's only draft row has no next one to be apart from
@@ -1028,7 +1029,6 @@ def _kv_workspace(st, workspace, stream):
 
 
 def _check_pools(st, pools):
-    _here(pools.keep[0][0])
     if pools.pages != st.pool_pages:
         raise DvsError(f"the pools have {pools.pages} pages, the state's {st.pool_pages}")
 
@@ -1042,7 +1042,7 @@ def kv_fork(st: DeviceState, pools: KVPools, src, dst, window: int, share: bool 
     _dev(dst, torch.int32, "dst", 1)
     if src.shape != dst.shape:
         raise DvsError("src and dst must have the same length")
-    _here(st.kv_len, src, dst)
+    _here(st.kv_len, src, dst, pools.keep[0][0], _buf(workspace))
     ws = _kv_workspace(st, workspace, stream)
     sd = _state_desc(st, -1)
     rc = lib().kv_fork(ctypes.byref(sd), _ptr(st.page_refs), pools.layers, len(pools.layers),
@@ -1055,7 +1055,7 @@ def kv_fork(st: DeviceState, pools: KVPools, src, dst, window: int, share: bool 
 def kv_release(st: DeviceState, slots, window: int, workspace=None, stream=None):
     """The slots (int32) become empty and keep pages for a window of `window` rows."""
     _dev(slots, torch.int32, "slots", 1)
-    _here(st.kv_len, slots)
+    _here(st.kv_len, slots, _buf(workspace))
     ws = _kv_workspace(st, workspace, stream)
     sd = _state_desc(st, -1)
     rc = lib().kv_release(ctypes.byref(sd), _ptr(st.page_refs), slots.shape[0], _ptr(slots),
@@ -1072,7 +1072,7 @@ def kv_compact(st: DeviceState, pools: KVPools, moved_out=None, workspace=None, 
     _dev(moved_out, torch.int32, "moved_out", 1)
     if moved_out.shape[0] != 1:
         raise DvsError("moved_out must have one entry")
-    _here(st.kv_len, moved_out)
+    _here(st.kv_len, moved_out, pools.keep[0][0], _buf(workspace))
     ws = _kv_workspace(st, workspace, stream)
     sd = _state_desc(st, -1)
     rc = lib().kv_compact(ctypes.byref(sd), _ptr(st.page_refs), pools.layers, len(pools.layers),
