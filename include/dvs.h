@@ -647,6 +647,8 @@ int literal_round_filtered(const dvs_model* m, const dvs_state* st, int32_t B,
  * kv_fork: for every pair i, slot dst[i] becomes a copy of slot src[i]
  *   (kv_len, boundary, draft, out_tokens, out_count, finished), ready for a
  *   window of `window` rows: it holds ceil((kv_len + window) / 16) pages.
+ *   (Forks of a slot that has just been prefilled all start from its first
+ *   token, dvs_prefill's top-1.)
  *   The pages that dst[i] held are given back first: those without another
  *   holder go on the free stack, the highest id first.  With share != 0 the
  *   floor(kv_len / 16) full pages are src's (one holder more each) and the
@@ -667,9 +669,13 @@ int literal_round_filtered(const dvs_model* m, const dvs_state* st, int32_t B,
  *   DVS_ERR_BAD_PAGE.  *moved_out (device, may be NULL) = pages moved.
  *
  * Errors (nothing is changed): DVS_ERR_BAD_SLOT for a slot outside [0, S), a
- * repeated destination or one that is a source; DVS_ERR_MAX_PAGES,
- * DVS_ERR_POOL_EXHAUSTED as in kv_commit; DVS_ERR_BAD_PAGE for a page id
- * outside the pool or counts that do not fit the tables.
+ * repeated destination or one that is a source; DVS_ERR_MAX_PAGES for a table
+ * that would exceed max_pages, and for a num_pages outside [0, max_pages] of a
+ * slot that gives its pages up (kv_compact: of any, and a free_top outside the
+ * pool); DVS_ERR_POOL_EXHAUSTED for too few free pages, and for a free_top
+ * outside the pool (kv_fork, kv_release); DVS_ERR_BAD_PAGE for a page id outside
+ * the pool, a page given up more often than it is held, and a source whose
+ * num_pages does not cover its kv_len.
  *   layers: only k_pool and v_pool are read; they start on 16 bytes.
  *   workspace >= dvs_kv_workspace_bytes(S, num_pool_pages) bytes, no
  *   initialisation needed.  Calls that share it must not overlap in time.

@@ -29,11 +29,13 @@
 // follow.  Sources and targets are disjoint, so the copies need no order.
 //
 // The copies are bound by HBM (fork of one sequence of 2000 rows to three slots
-// of their own, 32 pools: 295 MB in 40 us; compaction of 418 MB in 86 us); the
-// rest by the latency of a few dependent loads.  Calls of up to SMALL_ENTRIES
-// table entries over pools of up to SMALL_POOL pages do everything up to the
-// settling (a release all of it) in one workgroup with its bitmaps in LDS; page
-// rows and copies share a launch.  A release of one sequence: 9 us.
+// of their own, 32 pools: 49 MB read and 147 written in 40 us; compaction of
+// 209 MB read and written in 86 us); the rest by the latency of a few dependent
+// loads.  Forks and compactions of up to SMALL_ENTRIES table entries, and
+// releases of up to twice as many, over pools of up to SMALL_POOL pages do
+// everything up to the settling (a release all of it) in one workgroup with its
+// bitmaps in LDS; page rows and copies share a launch.  A release of one
+// sequence: 9 us.
 #include "dvs_common.h"
 
 namespace dvs {
