@@ -62,6 +62,7 @@ extern "C" {
 #define DVS_ERR_BAD_PAGE 8        /* a page id outside [0, num_pool_pages)    */
 #define DVS_ERR_OPEN_BLOCK 16     /* a block commit met a masked position     */
 #define DVS_ERR_BAD_SLOT 32       /* a sequence slot out of range, or given twice */
+#define DVS_ERR_BAD_TREE 64       /* a row's parent is the row itself or a later one */
 
 #define DVS_PAGE_SIZE 16
 
@@ -692,6 +693,127 @@ int kv_release(const dvs_state* st, int32_t* page_refs, int32_t n, const int32_t
 int kv_compact(const dvs_state* st, int32_t* page_refs, const dvs_layer* layers,
                int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                int32_t* moved_out, void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * A step over a tree of drafted tokens
+ *
+ * A window of R rows per sequence verifies several continuations at once: row
+ * 0 is the last committed token x0, row r a drafted token that continues row
+ * parent[s, r] < r.  parent -1: a root (attached to the cache alone; row 0 is
+ * one); parent < -1: padding, as is every row below a padding row, so trees
+ * of fewer than R rows share a call.  A parent >= its row is padding too and
+ * sets DVS_ERR_BAD_TREE (in tree_masks).  Row r sits in the cache slot
+ * kv_len + r, at the position kv_len + depth.  A step is
+ *     tree_masks      once: masks and depths from the parents;
+ *     kv_append_rope  per layer: rotated queries, keys and values appended;
+ *     attn_tree       per layer: attention over the cache and the ancestors;
+ *     accept_commit_tree  once, after the verifier's top-1 of every row.
+ * The middle two serve ordinary windows as well: depth NULL and tree_mask NULL
+ * are a token-level causal window (decode: R = 1; a chunk of a prefill).
+ *
+ * tree_masks: mask_out [S, R, ceil(R / 32)]: bit j % 32 of word j / 32 of row
+ *   r is set iff j is r or one of its ancestors (padding: no bit);
+ *   depth_out [S, R] (may be NULL): ancestors of r (padding: -1).
+ *   parent [S, R]; all int32.  Requirements: S >= 1, 1 <= R <= 1024, mask_out
+ *   on 8 bytes.
+ * ---------------------------------------------------------------------- */
+int tree_masks(const int32_t* parent, int32_t S, int32_t R, int32_t* mask_out, int32_t* depth_out,
+               int32_t* err_word, void* stream);
+
+/* ------------------------------------------------------------------------
+ * kv_append_rope
+ *
+ * Rotates the window's queries and keys and appends keys and values to the
+ * paged cache.  Row r of sequence s is at position p = kv_len[s] + depth[s, r]
+ * (depth NULL: + r); with h = rot_dim / 2, elements (i, i + h), i < h, of each
+ * query and key head turn by p * theta^(-i / h):
+ *     x_i' = x_i cos - x_{i+h} sin,   x_{i+h}' = x_{i+h} cos + x_i sin
+ * (angles in 64 bits, the products in 32, one rounding to the dtype); elements
+ * from rot_dim on are copied.  Keys and values go to slot kv_len[s] + r.
+ *   q      row r of sequence s at s * q_seq + r * q_ld elements, Hq heads of D
+ *          side by side; may be NULL, with q_out
+ *   k_new, v_new  likewise, Hkv heads (a fused projection's rows can be given
+ *          as they are)
+ *   q_out  [S, R, Hq, D] (written); may be q where q has these strides, and
+ *          overlaps no other row
+ *   pools, page_table [S, max_pages], kv_len [S] as attn_hybrid_block; the
+ *          pools start on 16 bytes
+ *   depth  [S, R] int32 or NULL.  Rows of depth < 0 (padding) are left as they
+ *          were, in q_out and in the cache.
+ *   err_word  DVS_ERR_MAX_PAGES if kv_len + R > max_pages * 16 (the sequence
+ *          is skipped), DVS_ERR_BAD_PAGE for a page id outside the pool (its
+ *          slots are skipped).
+ * The cache outside the appended slots is neither read nor written.
+ * Requirements: S, R, Hkv >= 1 (with q: Hq >= 1), D in {64, 96, 128}, rot_dim
+ * a multiple of 16 in [0, D], theta > 0, rows at the alignment of their
+ * elements (ones that start on 16 bytes take the faster copies).
+ * ---------------------------------------------------------------------- */
+int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const void* k_new, int64_t k_seq,
+                   int64_t k_ld, const void* v_new, int64_t v_seq, int64_t v_ld, void* k_pool,
+                   void* v_pool, const int32_t* page_table, const int32_t* kv_len,
+                   const int32_t* depth, int32_t S, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
+                   int32_t rot_dim, float theta, int32_t max_pages, int32_t num_pool_pages,
+                   int32_t dtype, void* q_out, int32_t* err_word, void* stream);
+
+/* ------------------------------------------------------------------------
+ * attn_tree / dvs_tree_workspace_bytes
+ *
+ * Masked softmax attention of a window whose keys and values are in the cache
+ * (slots [L, L + R), L = kv_len[s]).  Row r sees key position k iff
+ *     k < L,  or  L <= k < L + R and bit k - L of its mask is set
+ * (tree_mask NULL: k <= L + r); a row without any bit sees nothing, not the
+ * cache either: its output is 0.  Slots that a row does not see may hold
+ * anything.  out[s,r,h,:] = sum_k softmax_k(softmax_scale <q[s,r,h], K_k>) V_k,
+ * query head h reading KV head h / (Hq / Hkv).
+ *   q, out [S, R, Hq, D]; pools, page_table, kv_len as attn_hybrid_block;
+ *   tree_mask [S, R, ceil(R / 32)] int32 (tree_masks makes it; any other bits
+ *   do as well) or NULL.
+ *   err_word  DVS_ERR_MAX_PAGES if L + R > max_pages * 16 (the sequence is
+ *   skipped), DVS_ERR_BAD_PAGE for a page id outside the pool (the outputs of
+ *   the sequence then mean nothing).
+ *   workspace >= dvs_tree_workspace_bytes(...) bytes on 256, no initialisation
+ *   needed.  Calls that share it must not overlap in time.
+ * Requirements: Hq % Hkv == 0, D in {64, 96, 128}, S >= 1, 1 <= R <= 1024, q,
+ * out and the pools on 16 bytes, softmax_scale > 0.
+ * ---------------------------------------------------------------------- */
+size_t dvs_tree_workspace_bytes(int32_t S, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
+                                int32_t max_pages, int32_t dtype);
+int attn_tree(const void* q, const void* k_pool, const void* v_pool, const int32_t* page_table,
+              const int32_t* kv_len, const int32_t* tree_mask, int32_t S, int32_t R, int32_t Hq,
+              int32_t Hkv, int32_t D, int32_t max_pages, int32_t num_pool_pages,
+              float softmax_scale, int32_t dtype, void* out, int32_t* err_word, void* workspace,
+              size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * accept_commit_tree / dvs_accept_tree_workspace_bytes
+ *
+ * Acceptance, commit and KV rollback of a tree window.  For every sequence
+ * with finished[s] == 0 and parent[s, 0] == -1 the accepted path is p_0 = 0,
+ * p_{i+1} = the lowest row c with parent[s, c] == p_i (c > p_i) and tokens[s, c]
+ * == argmax[s, p_i], as long as there is one; A = its rows below row 0.  Then
+ *   run   = argmax[s, p_0], ..., argmax[s, p_A], truncated as kv_commit's
+ *           (eos_id, max_new); k tokens are kept, appended to out_tokens;
+ *   cache: slots kv_len + p_i move to kv_len + i, i < k, in every layer;
+ *   kv_len += k, out_count, boundary, finished and the pages as kv_commit with
+ *           R window rows (every sequence then holds ceil((kv_len + R) / 16)
+ *           pages); draft is not changed.
+ * Other sequences are left unchanged but for their pages, which also become
+ * ceil((kv_len + R) / 16).  Errors as kv_commit (nothing is changed, the cache
+ * neither).
+ *   layers: only k_pool and v_pool are read; they start on 16 bytes.
+ *   parent, tokens, argmax [S, R] int32 (tokens[s, 0] is not read)
+ *   accept_out [S] = A, path_out [S, R] = p_0 .. p_A, then -1 (A = 0 and all
+ *           -1 for the other sequences); both may be NULL.
+ *   workspace >= dvs_accept_tree_workspace_bytes(S, R) bytes, no
+ *           initialisation needed.  Calls that share it must not overlap.
+ * Requirements: 1 <= S <= 1024, 1 <= R <= 1024, head_dim in {64, 96, 128}.
+ * ---------------------------------------------------------------------- */
+size_t dvs_accept_tree_workspace_bytes(int32_t S, int32_t R);
+int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, int32_t n_layers,
+                       int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t R,
+                       const int32_t* parent, const int32_t* tokens, const int32_t* argmax,
+                       int32_t* accept_out, int32_t* path_out, void* workspace, size_t ws_bytes,
+                       void* stream);
 
 /* ------------------------------------------------------------------------
  * dvs_prefill

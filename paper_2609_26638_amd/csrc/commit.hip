@@ -61,6 +61,7 @@ struct CommitParams {
   int accept_here;             // 1: A computed in this kernel from argmax and draft
   int32_t* accept_out;         // accept_here: A per sequence (may be NULL)
   int draft_group;             // > 0: next draft from mask group A (groups of this many rows)
+  int idle_below;              // accept_len < idle_below: the sequence sits this step out
   const int32_t* argmax;
   int32_t* kv_len;
   int32_t* page_table;
@@ -156,7 +157,7 @@ __global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(CommitParams 
     L = p.kv_len[s];
     n = p.num_pages[s];
     cnt = p.out_count[s];
-    fin = p.finished[s] != 0;
+    fin = p.finished[s] != 0 || (p.accept_len && p.accept_len[s] < p.idle_below);
     if (!fin && p.accept_here) {
       // longest prefix with d_j == a_j = argmax[s, j-1], j <= n_causal - 1,
       // compared RUN_CHUNK positions at a time (independent loads first)
@@ -305,7 +306,7 @@ static int launch_commit(const char* who, int32_t S, int32_t n_causal, int32_t n
                          int32_t* free_top, int32_t num_pool_pages, int32_t* boundary,
                          int32_t* draft, int32_t draft_width, int32_t* out_tokens,
                          int32_t* out_count, int32_t max_new, int32_t eos_id, int32_t* finished,
-                         int32_t* err_word, void* stream) {
+                         int32_t* err_word, void* stream, int32_t idle_below = INT32_MIN) {
   DVS_CHECK_ARG(argmax && kv_len && page_table && num_pages && free_stack &&
                     free_top && boundary && out_tokens && out_count && finished,
                 "%s: NULL array argument", who);
@@ -327,6 +328,7 @@ static int launch_commit(const char* who, int32_t S, int32_t n_causal, int32_t n
                                      (n_mask == n_causal * draft_group && draft_group >= draft_width)),
                 "%s: mask rows must be n_causal groups of draft_group >= draft_width rows", who);
   p.accept_len = accept_len; p.accept_here = accept_here; p.accept_out = accept_out;
+  p.idle_below = idle_below;
   p.draft_group = draft_group;
   p.argmax = argmax; p.kv_len = kv_len; p.page_table = page_table;
   p.num_pages = num_pages; p.free_stack = free_stack; p.free_top = free_top;
@@ -343,6 +345,22 @@ static int launch_commit(const char* who, int32_t S, int32_t n_causal, int32_t n
     hipLaunchKernelGGL(kv_commit_kernel<false>, dim3(1), dim3(threads), 0, (hipStream_t)stream, p);
   return launch_status(who);
 }
+
+namespace dvs {
+
+// accept_commit_tree: run[s, 0 .. run_len[s]] are the tokens that the accepted
+// path commits (both the run's drafts and its last token); run_len < 0: the
+// sequence has no tree this step.
+int commit_tree_run(const dvs_state* st, int R, const int32_t* run_len, const int32_t* run,
+                    void* stream) {
+  return launch_commit("accept_commit_tree", st->S, R, 0, R, nullptr, run_len, 0, nullptr, 0, run,
+                       st->kv_len, st->page_table, st->num_pages, st->max_pages, st->free_stack,
+                       st->free_top, st->num_pool_pages, st->boundary, const_cast<int32_t*>(run), R,
+                       st->out_tokens, st->out_count, st->max_new, st->eos_id, st->finished,
+                       st->err_word, stream, 0);
+}
+
+}  // namespace dvs
 
 extern "C" int kv_commit(int32_t S, int32_t n_causal, int32_t n_mask, const int32_t* accept_len,
                          const int32_t* argmax, int32_t* kv_len, int32_t* page_table,

@@ -72,6 +72,10 @@ bool attn_chunk_ok(int chunk_keys);
 size_t attn_counter_bytes(int S, int R, int Hq, int Hkv, int D, int max_pages, int chunk_keys,
                           int dtype);
 
+// The commit of accept_commit_tree (commit.hip).
+int commit_tree_run(const dvs_state* st, int R, const int32_t* run_len, const int32_t* run,
+                    void* stream);
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

@@ -1,0 +1,550 @@
+// A step over a tree of drafted tokens: tree_masks, kv_append_rope and
+// accept_commit_tree (the attention between them is in tree_attn.hip).
+//
+// Row 0 of a window is the last committed token x0, every other row a drafted
+// token whose parent is an earlier row.  A row attends to the cache and to its
+// ancestors, is rotated at position kv_len + depth, and sits in the cache slot
+// kv_len + row, so that siblings share a position but not a slot.  The commit
+// keeps the slots of one path and moves them to the front of the window.
+#include <math.h>
+
+#include <algorithm>
+
+#include "dvs_common.h"
+
+namespace dvs {
+
+constexpr int TREE_MAX_ROWS = 1024;
+
+// ---------------------------------------------------------------------------
+// tree_masks
+//
+// mask(r) = {r} U mask(parent r).  A wave holds 64 consecutive rows, a row a
+// lane.  Pointer doubling inside the wave (log2 64 rounds of mask(r) |=
+// mask(up r), up r = up(up r)) gives every row's ancestors among the 64 as one
+// 64-bit word; the topmost of them, its lowest bit, names the parent further
+// up by which the chain leaves the wave's rows.  The waves then finish in
+// order, 64 rows a step, each row taking over the words of that parent, which
+// an earlier wave has finished.
+// ---------------------------------------------------------------------------
+struct MaskRow {
+  uint64_t in;   // ancestors among the wave's rows, itself among them
+  int up;        // the parent by which the chain leaves them; < 0: it ends
+};
+
+__device__ __forceinline__ uint64_t shfl64(uint64_t v, int src) {
+  const uint32_t lo = __shfl((int)(uint32_t)v, src), hi = __shfl((int)(uint32_t)(v >> 32), src);
+  return (uint64_t)hi << 32 | lo;
+}
+
+// p: the row's parent, or below -1 for a row of the padding.
+__device__ __forceinline__ MaskRow wave_ancestors(int p, int first, int lane) {
+  uint64_t in = 1ull << lane;
+  int up = p >= first ? p - first : -1;
+#pragma unroll
+  for (int round = 0; round < 6; ++round) {
+    const int src = up >= 0 ? up : lane;
+    const uint64_t other = shfl64(in, src);
+    const int next = __shfl(up, src);
+    in |= other;
+    up = up >= 0 ? next : -1;
+  }
+  return MaskRow{in, __shfl(p, __ffsll((unsigned long long)in) - 1)};
+}
+
+// A row's parent as the kernels take it: a row that names itself or a later
+// one is no tree's.
+__device__ __forceinline__ int checked_parent(int p, int r, int32_t* err) {
+  if (p >= r) {
+    set_err(err, DVS_ERR_BAD_TREE);
+    return -2;
+  }
+  return p;
+}
+
+// Up to 64 rows: a wave a sequence.
+__global__ void __launch_bounds__(256) tree_masks_small_kernel(const int32_t* __restrict__ parent,
+                                                               int S, int R,
+                                                               int32_t* __restrict__ mask,
+                                                               int32_t* __restrict__ depth,
+                                                               int32_t* __restrict__ err) {
+  const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (s >= S) return;
+  int p = -2;
+  if (lane < R) p = checked_parent(parent[(size_t)s * R + lane], lane, err);
+  const MaskRow m = wave_ancestors(p, 0, lane);
+  if (lane >= R) return;
+  const bool in_tree = m.up == -1;
+  const size_t at = (size_t)s * R + lane;
+  if (depth) depth[at] = in_tree ? __popcll(m.in) - 1 : -1;
+  const uint64_t w = in_tree ? m.in : 0;
+  if (R > 32)
+    *(u32x2*)(mask + 2 * at) = u32x2{(uint32_t)w, (uint32_t)(w >> 32)};
+  else
+    mask[at] = (int32_t)(uint32_t)w;
+}
+
+// More rows: a workgroup a sequence, the masks in LDS.  Rows are 16 bytes more
+// than their words apart, which spreads the lanes' 16-byte accesses over the
+// banks.
+__global__ void __launch_bounds__(1024) tree_masks_kernel(const int32_t* __restrict__ parent, int R,
+                                                          int32_t* __restrict__ mask,
+                                                          int32_t* __restrict__ depth,
+                                                          int32_t* __restrict__ err) {
+  extern __shared__ __attribute__((aligned(16))) uint32_t rows_lds[];
+  const int W = (R + 31) / 32, W4 = (W + 3) / 4 * 4, ld = W4 + 4;
+  int* s_depth = (int*)(rows_lds + (size_t)R * ld);
+  const int s = blockIdx.x, r = threadIdx.x, lane = r & 63, first = r & ~63;
+  const size_t base = (size_t)s * R;
+  int p = -2;
+  if (r < R) p = checked_parent(parent[base + r], r, err);
+  const MaskRow m = wave_ancestors(p, first, lane);
+  for (int f = 0; f < R; f += 64) {
+    if (f == first && r < R) {
+      int d = -1;
+      if (m.up == -1) d = 0;
+      else if (m.up >= 0) d = s_depth[m.up] < 0 ? -1 : s_depth[m.up] + 1;
+      if (d >= 0) d += __popcll(m.in) - 1;
+      s_depth[r] = d;
+      uint32_t* row = rows_lds + (size_t)r * ld;
+      const uint32_t* over = m.up >= 0 && d >= 0 ? rows_lds + (size_t)m.up * ld : nullptr;
+      for (int w = 0; w < W4; w += 4)
+        *(u32x4*)(row + w) = over && w < first / 32 ? *(const u32x4*)(over + w) : u32x4{0, 0, 0, 0};
+      if (d >= 0) *(u32x2*)(row + first / 32) = u32x2{(uint32_t)m.in, (uint32_t)(m.in >> 32)};
+    }
+    __syncthreads();
+  }
+  if (r < R && depth) depth[base + r] = s_depth[r];
+  for (int i = r; i < R * W; i += blockDim.x) {
+    const int row = i / W, w = i - row * W;
+    mask[base * W + i] = (int32_t)rows_lds[(size_t)row * ld + w];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// kv_append_rope
+//
+// A pair (a, b) = (x_i, x_{i + h}), h = rot_dim / 2, turns by the angle
+// pos * theta^(-i / h):  (a cos - b sin, b cos + a sin).  A workgroup takes the
+// rows of one page of the window (up to 16) and a run of heads (queries, then
+// keys, then values): the page's sines and cosines are made once for all of
+// its heads.  Values go through LDS, so that the head-dim-major page of V is
+// written in whole 16-byte pieces (8 or 4 slots of an element).
+// ---------------------------------------------------------------------------
+struct AppendParams {
+  const void *q, *k, *v;
+  long long q_seq, q_ld, k_seq, k_ld, v_seq, v_ld;
+  void *k_pool, *v_pool, *q_out;
+  const int32_t *table, *kv_len, *depth;
+  int32_t* err;
+  int S, R, Hq, Hkv, max_pages, pool_pages, half, n_pages, n_groups, per_group;
+  // quarter turns a position: theta^(-i / half) * 2 / pi, in 64 bits, so that
+  // far positions keep their angle (what is left after whole quarters is
+  // taken in 32)
+  double turns[64];
+};
+
+template <typename T, bool ALIGNED>
+struct Piece {   // 16 bytes of a head's row
+  static constexpr int N = 16 / sizeof(T);
+  T e[N];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (ALIGNED) {
+      *(u32x4*)e = *(const u32x4*)p;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) e[i] = p[i];
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (ALIGNED) {
+      *(u32x4*)p = *(const u32x4*)e;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = e[i];
+    }
+  }
+};
+
+// T: float or __bf16.  ALIGNED: every row of q, k, v and q_out starts on 16
+// bytes (pool rows always do).
+template <typename T, int D, bool ALIGNED>
+__global__ void __launch_bounds__(256) append_rope_kernel(AppendParams p) {
+  constexpr int N = 16 / sizeof(T);
+  constexpr int PAIRS = D / (2 * N);    // items of a row: two pieces each
+  constexpr int VLD = D + 16 / sizeof(T);
+  __shared__ float2 s_cs[16][65];
+  __shared__ __attribute__((aligned(16))) T s_v[16 * VLD];
+  __shared__ int s_live[16];
+  const int tid = threadIdx.x;
+  const int g = blockIdx.x % p.n_groups, sp = blockIdx.x / p.n_groups;
+  const int pi = sp % p.n_pages, s = sp / p.n_pages;
+  const int L = p.kv_len[s];
+  if (L < 0 || (long long)L + p.R > (long long)p.max_pages * DVS_PAGE_SIZE) {
+    if (g == 0 && pi == 0 && tid == 0) set_err(p.err, DVS_ERR_MAX_PAGES);
+    return;
+  }
+  const int pg = L / DVS_PAGE_SIZE + pi;             // logical page
+  const int r0 = pg * DVS_PAGE_SIZE - L;             // row of its slot 0
+  if (r0 >= p.R) return;
+  const int page = p.table[(size_t)s * p.max_pages + pg];
+  const bool in_pool = page >= 0 && page < p.pool_pages;
+  if (!in_pool && g == 0 && tid == 0) set_err(p.err, DVS_ERR_BAD_PAGE);
+  const int u0 = g * p.per_group, u1 = min(u0 + p.per_group, p.Hq + 2 * p.Hkv);
+  // live rows and their angles
+  for (int i = tid; i < 16 * max(p.half, 1); i += 256) {
+    const int j = i % 16, e = i / 16, r = r0 + j;
+    int d = -1;
+    if (r >= 0 && r < p.R) d = p.depth ? p.depth[(size_t)s * p.R + r] : r;
+    if (e == 0) s_live[j] = d >= 0;
+    if (d < 0 || p.half == 0) continue;
+    const double t = (double)((long long)L + d) * p.turns[e];
+    const double n = rint(t);
+    float sn, cs;
+    sincospif(0.5f * (float)(t - n), &sn, &cs);
+    switch ((long long)n & 3) {
+      case 0: s_cs[j][e] = float2{cs, sn}; break;
+      case 1: s_cs[j][e] = float2{-sn, cs}; break;
+      case 2: s_cs[j][e] = float2{-cs, -sn}; break;
+      default: s_cs[j][e] = float2{sn, -cs}; break;
+    }
+  }
+  __syncthreads();
+  const T* q = (const T*)p.q + s * p.q_seq;
+  const T* k = (const T*)p.k + s * p.k_seq;
+  const T* v = (const T*)p.v + s * p.v_seq;
+  // queries and keys
+  const int ur = min(u1, p.Hq + p.Hkv);
+  for (int i = tid; i < (ur - u0) * 16 * PAIRS; i += 256) {
+    const int c = i % PAIRS, j = i / PAIRS % 16, u = u0 + i / (16 * PAIRS), r = r0 + j;
+    const bool key = u >= p.Hq;
+    if (!s_live[j] || (key && !in_pool)) continue;
+    const T* src = key ? k + r * p.k_ld + (u - p.Hq) * D : q + r * p.q_ld + (long long)u * D;
+    const bool turn = c * N < p.half;
+    const int lo = turn ? c * N : 2 * p.half + 2 * (c * N - p.half), hi = turn ? p.half + c * N : lo + N;
+    Piece<T, ALIGNED> a, b;
+    a.load(src + lo);
+    b.load(src + hi);
+    if (turn) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float2 w = s_cs[j][lo + e];
+        const float x = (float)a.e[e], y = (float)b.e[e];
+        a.e[e] = (T)(x * w.x - y * w.y);
+        b.e[e] = (T)(y * w.x + x * w.y);
+      }
+    }
+    if (key) {
+      T* dst = (T*)p.k_pool + (((size_t)page * p.Hkv + (u - p.Hq)) * 16 + j) * D;
+      ((Piece<T, true>&)a).store(dst + lo);
+      ((Piece<T, true>&)b).store(dst + hi);
+    } else if (p.q_out) {
+      T* dst = (T*)p.q_out + (((size_t)s * p.R + r) * p.Hq + u) * D;
+      a.store(dst + lo);
+      b.store(dst + hi);
+    }
+  }
+  if (!in_pool) return;
+  // values
+  for (int u = max(u0, p.Hq + p.Hkv); u < u1; ++u) {
+    const int h = u - p.Hq - p.Hkv;
+    __syncthreads();
+    for (int i = tid; i < 16 * (D / N); i += 256) {
+      const int c = i % (D / N), j = i / (D / N);
+      if (!s_live[j]) continue;
+      Piece<T, ALIGNED> x;
+      x.load(v + (r0 + j) * p.v_ld + h * D + c * N);
+      ((Piece<T, true>&)x).store(s_v + j * VLD + c * N);
+    }
+    __syncthreads();
+    T* dst = (T*)p.v_pool + ((size_t)page * p.Hkv + h) * D * 16;
+    for (int i = tid; i < D * (16 / N); i += 256) {
+      const int d = i / (16 / N), j0 = i % (16 / N) * N;
+      Piece<T, true> x;
+      int live = 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        x.e[e] = s_v[(j0 + e) * VLD + d];
+        live += s_live[j0 + e];
+      }
+      if (live == N) {
+        x.store(dst + d * 16 + j0);
+      } else if (live) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (s_live[j0 + e]) dst[d * 16 + j0 + e] = x.e[e];
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// accept_commit_tree
+//
+// follow(p) = the lowest child of row p whose token is the verifier's top-1 at
+// p; the accepted path is 0, follow(0), follow(follow(0)), ...  The committed
+// tokens are the verifier's at the path's rows, which kv_commit's kernel
+// commits with its pages; the path's cache slots then move from kv_len +
+// path[i] to kv_len + i in every layer.  The commit may give pages of the
+// window back before the move: the move goes by the page ids noted here, and
+// nothing writes to a page that was given back in between.
+// ---------------------------------------------------------------------------
+struct TreeCommit {
+  int S, R, max_pages, pool_pages, n_window_pages;
+  const int32_t *parent, *tokens, *argmax, *kv_len, *table, *finished;
+  int32_t *accept, *path;                      // outputs (or workspace)
+  int32_t *run_len, *old_len, *pages, *run;    // workspace
+};
+
+__global__ void __launch_bounds__(256) tree_accept_kernel(TreeCommit t) {
+  __shared__ int s_next[TREE_MAX_ROWS];
+  __shared__ int s_path[TREE_MAX_ROWS];
+  __shared__ int s_A;
+  const int s = blockIdx.x, tid = threadIdx.x, R = t.R;
+  const size_t base = (size_t)s * R;
+  const int32_t *parent = t.parent + base, *argmax = t.argmax + base;
+  const int L = t.kv_len[s];
+  const bool live = t.finished[s] == 0 && parent[0] == -1;
+  for (int r = tid; r < R; r += 256) s_next[r] = R;
+  __syncthreads();
+  for (int r = tid; r < R; r += 256) {
+    const int p = parent[r];
+    if (p >= 0 && p < r && t.tokens[base + r] == argmax[p]) atomicMin(&s_next[p], r);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    int A = -1;
+    if (live)
+      for (int r = 0; r < R; r = s_next[r]) s_path[++A] = r;
+    s_A = A;
+    t.accept[s] = max(A, 0);
+    t.run_len[s] = A;
+    t.old_len[s] = L;
+  }
+  __syncthreads();
+  const int A = s_A;
+  for (int i = tid; i < R; i += 256) {
+    const int r = i <= A ? s_path[i] : -1;
+    t.path[base + i] = r;
+    t.run[base + i] = r >= 0 ? argmax[r] : 0;
+  }
+  for (int i = tid; i < t.n_window_pages; i += 256) {
+    const int pg = L / DVS_PAGE_SIZE + i;
+    int id = L >= 0 && pg < t.max_pages ? t.table[(size_t)s * t.max_pages + pg] : -1;
+    if (id >= t.pool_pages) id = -1;
+    t.pages[(size_t)s * t.n_window_pages + i] = id;
+  }
+}
+
+constexpr int MOVE_LAYERS = 64;   // layers per launch (as kernel arguments)
+struct MovePools {
+  char* p[2 * MOVE_LAYERS];
+};
+
+// A wave a (sequence, layer, K or V, KV head).  path[i] >= i and rises, so a
+// slot is read before a later step writes it, and a wave's loads are complete
+// before the stores that wait for them.
+template <typename T>
+__global__ void __launch_bounds__(256) tree_move_kernel(TreeCommit t, MovePools pools, int n_pools,
+                                                        int Hkv, int D, int32_t* err) {
+  const long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (task >= (long long)t.S * n_pools * Hkv) return;
+  const int h = (int)(task % Hkv), pl = (int)(task / Hkv % n_pools), s = (int)(task / Hkv / n_pools);
+  const int L = t.old_len[s], k = t.kv_len[s] - L;
+  if (k <= 1) return;
+  const int32_t* path = t.path + (size_t)s * t.R;
+  const int32_t* pages = t.pages + (size_t)s * t.n_window_pages;
+  const int off = L % DVS_PAGE_SIZE;
+  if (path[k - 1] == k - 1) return;    // the path is the window's front already
+  T* pool = (T*)pools.p[pl];
+  const size_t head = (size_t)16 * D;
+  auto base_of = [&](int row) -> T* {
+    const int pg = pages[(off + row) >> 4];
+    return pg < 0 ? nullptr : pool + ((size_t)pg * Hkv + h) * head;
+  };
+  bool bad = false;
+  for (int i = 1; i < k; ++i) {
+    const int r = path[i];
+    if (r == i) continue;
+    const T* from = base_of(r);
+    T* to = base_of(i);
+    if (!from || !to) {
+      bad = true;
+      continue;
+    }
+    const int a = (off + r) & 15, b = (off + i) & 15;
+    if (pl & 1) {
+      for (int d = lane; d < D; d += 64) to[d * 16 + b] = from[d * 16 + a];
+    } else {
+      for (int d = lane; d < D; d += 64) to[b * D + d] = from[a * D + d];
+    }
+  }
+  if (bad && lane == 0) set_err(err, DVS_ERR_BAD_PAGE);
+}
+
+static size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+static int window_pages(int R) { return (R + DVS_PAGE_SIZE - 2) / DVS_PAGE_SIZE + 1; }
+
+template <typename T, bool ALIGNED>
+static void launch_append(const AppendParams& p, int D, unsigned grid, hipStream_t st) {
+  if (D == 128) hipLaunchKernelGGL((append_rope_kernel<T, 128, ALIGNED>), dim3(grid), dim3(256), 0, st, p);
+  else if (D == 96) hipLaunchKernelGGL((append_rope_kernel<T, 96, ALIGNED>), dim3(grid), dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((append_rope_kernel<T, 64, ALIGNED>), dim3(grid), dim3(256), 0, st, p);
+}
+
+}  // namespace dvs
+
+using namespace dvs;
+
+extern "C" int tree_masks(const int32_t* parent, int32_t S, int32_t R, int32_t* mask_out,
+                          int32_t* depth_out, int32_t* err_word, void* stream) {
+  clear_error();
+  DVS_CHECK_ARG(parent && mask_out, "tree_masks: NULL parent or mask_out");
+  DVS_CHECK_ARG(S >= 1 && R >= 1 && R <= TREE_MAX_ROWS, "tree_masks: need S >= 1, 1 <= R <= %d",
+                TREE_MAX_ROWS);
+  DVS_CHECK_ARG(R <= 32 || ((uintptr_t)mask_out & 7) == 0, "tree_masks: mask_out must start on 8 bytes");
+  hipStream_t st = (hipStream_t)stream;
+  if (R <= 64) {
+    hipLaunchKernelGGL(tree_masks_small_kernel, dim3((S + 3) / 4), dim3(256), 0, st, parent, S, R,
+                       mask_out, depth_out, err_word);
+  } else {
+    const int W4 = ((R + 31) / 32 + 3) / 4 * 4;
+    hipLaunchKernelGGL(tree_masks_kernel, dim3(S), dim3((R + 63) / 64 * 64),
+                       (size_t)R * (W4 + 4) * 4 + (size_t)R * 4, st, parent, R, mask_out, depth_out,
+                       err_word);
+  }
+  return launch_status("tree_masks");
+}
+
+extern "C" int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const void* k_new,
+                              int64_t k_seq, int64_t k_ld, const void* v_new, int64_t v_seq,
+                              int64_t v_ld, void* k_pool, void* v_pool, const int32_t* page_table,
+                              const int32_t* kv_len, const int32_t* depth, int32_t S, int32_t R,
+                              int32_t Hq, int32_t Hkv, int32_t D, int32_t rot_dim, float theta,
+                              int32_t max_pages, int32_t num_pool_pages, int32_t dtype, void* q_out,
+                              int32_t* err_word, void* stream) {
+  clear_error();
+  DVS_CHECK_ARG(k_new && v_new && k_pool && v_pool && page_table && kv_len,
+                "kv_append_rope: NULL array argument");
+  DVS_CHECK_ARG(!q == !q_out, "kv_append_rope: q and q_out go together");
+  DVS_CHECK_ARG(S >= 1 && R >= 1, "kv_append_rope: need S >= 1 and R >= 1");
+  DVS_CHECK_ARG(Hkv >= 1 && Hq >= (q ? 1 : 0), "kv_append_rope: need heads");
+  DVS_CHECK_ARG(max_pages >= 1 && num_pool_pages >= 1, "kv_append_rope: empty page table/pool");
+  DVS_CHECK_SUPPORTED(dtype == DVS_F32 || dtype == DVS_BF16, "kv_append_rope: dtype %d", dtype);
+  DVS_CHECK_SUPPORTED(D == 64 || D == 96 || D == 128, "kv_append_rope: head_dim %d", D);
+  DVS_CHECK_SUPPORTED(rot_dim >= 0 && rot_dim <= D && rot_dim % 16 == 0,
+                      "kv_append_rope: rot_dim must be a multiple of 16 of at most head_dim");
+  DVS_CHECK_ARG(theta > 0.f && isfinite(theta), "kv_append_rope: theta must be positive");
+  const int64_t qrow = (int64_t)Hq * D, krow = (int64_t)Hkv * D;
+  DVS_CHECK_ARG((!q || R == 1 || q_ld >= qrow) && (R == 1 || (k_ld >= krow && v_ld >= krow)),
+                "kv_append_rope: rows overlap");
+  DVS_CHECK_ARG(q != q_out || !q || ((R == 1 || q_ld == qrow) && (S == 1 || q_seq == R * qrow)),
+                "kv_append_rope: q is rotated in place only where its rows are dense");
+  const uintptr_t es = dtype == DVS_BF16 ? 2 : 4;
+  DVS_CHECK_ARG((((uintptr_t)k_pool | (uintptr_t)v_pool) & 15) == 0,
+                "kv_append_rope: the pools must start on 16 bytes");
+  DVS_CHECK_ARG((((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)q_out) & (es - 1)) == 0,
+                "kv_append_rope: rows must start on an element");
+  AppendParams p{};
+  p.q = q; p.k = k_new; p.v = v_new;
+  p.q_seq = q_seq; p.q_ld = q_ld; p.k_seq = k_seq; p.k_ld = k_ld; p.v_seq = v_seq; p.v_ld = v_ld;
+  p.k_pool = k_pool; p.v_pool = v_pool; p.q_out = q_out;
+  p.table = page_table; p.kv_len = kv_len; p.depth = depth; p.err = err_word;
+  p.S = S; p.R = R; p.Hq = q ? Hq : 0; p.Hkv = Hkv; p.max_pages = max_pages;
+  p.pool_pages = num_pool_pages; p.half = rot_dim / 2;
+  for (int i = 0; i < p.half; ++i)
+    p.turns[i] = pow((double)theta, -(double)i / p.half) * 0.63661977236758134308;
+  p.n_pages = window_pages(R);
+  // heads of a page over several workgroups where the pages alone do not fill
+  // the chip a few times over
+  const int heads = p.Hq + 2 * Hkv;
+  const long long pages = (long long)S * p.n_pages;
+  const int groups = (int)std::min<long long>(heads, std::max<long long>(1, 8LL * device_cus() / pages));
+  p.per_group = (heads + groups - 1) / groups;
+  p.n_groups = (heads + p.per_group - 1) / p.per_group;
+  DVS_CHECK_SUPPORTED(pages * p.n_groups < (1LL << 31), "kv_append_rope: grid too large");
+  const unsigned grid = (unsigned)(pages * p.n_groups);
+  auto on16 = [&](const void* b, int64_t seq, int64_t ld) {
+    return !b || ((((uintptr_t)b | (uintptr_t)(S > 1 ? seq : 0) * es | (uintptr_t)(R > 1 ? ld : 0) * es)) & 15) == 0;
+  };
+  const bool aligned = on16(q, q_seq, q_ld) && on16(k_new, k_seq, k_ld) && on16(v_new, v_seq, v_ld) &&
+                       on16(q_out, 0, 0);
+  hipStream_t st = (hipStream_t)stream;
+  if (dtype == DVS_BF16) {
+    if (aligned) launch_append<__bf16, true>(p, D, grid, st);
+    else launch_append<__bf16, false>(p, D, grid, st);
+  } else {
+    if (aligned) launch_append<float, true>(p, D, grid, st);
+    else launch_append<float, false>(p, D, grid, st);
+  }
+  return launch_status("kv_append_rope");
+}
+
+extern "C" size_t dvs_accept_tree_workspace_bytes(int32_t S, int32_t R) {
+  if (S < 1 || S > 1024 || R < 1 || R > TREE_MAX_ROWS) return 0;
+  return al256((size_t)S * 4 * (3 + window_pages(R) + 2 * (size_t)R));
+}
+
+extern "C" int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, int32_t n_layers,
+                                  int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t R,
+                                  const int32_t* parent, const int32_t* tokens,
+                                  const int32_t* argmax, int32_t* accept_out, int32_t* path_out,
+                                  void* workspace, size_t ws_bytes, void* stream) {
+  clear_error();
+  DVS_CHECK_ARG(st && st->kv_len && st->page_table && st->num_pages && st->free_stack &&
+                    st->free_top && st->boundary && st->out_tokens && st->out_count && st->finished,
+                "accept_commit_tree: NULL state or state array");
+  DVS_CHECK_ARG(parent && tokens && argmax, "accept_commit_tree: NULL parent, tokens or argmax");
+  DVS_CHECK_ARG(R >= 1 && R <= TREE_MAX_ROWS, "accept_commit_tree: need 1 <= R <= %d", TREE_MAX_ROWS);
+  DVS_CHECK_ARG(st->S >= 1 && st->S <= 1024, "accept_commit_tree: need 1 <= S <= 1024");
+  DVS_CHECK_ARG(st->max_pages >= 1 && st->num_pool_pages >= 1 && st->max_new >= 1,
+                "accept_commit_tree: need max_pages, num_pool_pages, max_new >= 1");
+  DVS_CHECK_ARG(layers && n_layers >= 1 && n_kv_heads >= 1, "accept_commit_tree: need layers and heads");
+  DVS_CHECK_SUPPORTED(dtype == DVS_F32 || dtype == DVS_BF16, "accept_commit_tree: dtype %d", dtype);
+  DVS_CHECK_SUPPORTED(head_dim == 64 || head_dim == 96 || head_dim == 128,
+                      "accept_commit_tree: head_dim %d", head_dim);
+  for (int l = 0; l < n_layers; ++l)
+    DVS_CHECK_ARG(layers[l].k_pool && layers[l].v_pool &&
+                      (((uintptr_t)layers[l].k_pool | (uintptr_t)layers[l].v_pool) & 15) == 0,
+                  "accept_commit_tree: layer %d needs pools that start on 16 bytes", l);
+  const size_t need = dvs_accept_tree_workspace_bytes(st->S, R);
+  if (!workspace || ws_bytes < need) {
+    set_error("accept_commit_tree: workspace needs %zu bytes, got %zu", need, ws_bytes);
+    return DVS_EWORKSPACE;
+  }
+  const int S = st->S;
+  TreeCommit t{};
+  t.S = S; t.R = R; t.max_pages = st->max_pages; t.pool_pages = st->num_pool_pages;
+  t.n_window_pages = window_pages(R);
+  t.parent = parent; t.tokens = tokens; t.argmax = argmax;
+  t.kv_len = st->kv_len; t.table = st->page_table; t.finished = st->finished;
+  int32_t* w = (int32_t*)workspace;
+  t.run_len = w; t.old_len = w + S;
+  t.accept = accept_out ? accept_out : w + 2 * S;
+  t.pages = w + 3 * S;
+  t.run = t.pages + (size_t)S * t.n_window_pages;
+  t.path = path_out ? path_out : t.run + (size_t)S * R;
+  hipStream_t hs = (hipStream_t)stream;
+  hipLaunchKernelGGL(tree_accept_kernel, dim3(S), dim3(256), 0, hs, t);
+  int rc = launch_status("accept_commit_tree(accept)");
+  if (rc) return rc;
+  if ((rc = commit_tree_run(st, R, t.run_len, t.run, stream))) return rc;
+  for (int l0 = 0; l0 < n_layers; l0 += MOVE_LAYERS) {
+    const int nl = std::min(n_layers - l0, MOVE_LAYERS);
+    MovePools pools{};
+    for (int l = 0; l < nl; ++l) {
+      pools.p[2 * l] = (char*)layers[l0 + l].k_pool;
+      pools.p[2 * l + 1] = (char*)layers[l0 + l].v_pool;
+    }
+    const long long tasks = (long long)S * 2 * nl * n_kv_heads;
+    const dim3 gr((unsigned)((tasks + 3) / 4));
+    if (dtype == DVS_BF16)
+      hipLaunchKernelGGL(tree_move_kernel<uint16_t>, gr, dim3(256), 0, hs, t, pools, 2 * nl, n_kv_heads, head_dim, st->err_word);
+    else
+      hipLaunchKernelGGL(tree_move_kernel<float>, gr, dim3(256), 0, hs, t, pools, 2 * nl, n_kv_heads, head_dim, st->err_word);
+    if ((rc = launch_status("accept_commit_tree(move)"))) return rc;
+  }
+  return DVS_OK;
+}

@@ -24,6 +24,7 @@ ERR_MAX_PAGES = 2
 ERR_NONFINITE = 4
 ERR_BAD_PAGE = 8
 ERR_BAD_SLOT = 32
+ERR_BAD_TREE = 64
 
 _lib = None
 
@@ -140,6 +141,16 @@ _SIGS["kv_release"] = ([ctypes.POINTER(DvsState), _c_ptr, _c_int, _c_ptr, _c_int
                         _c_ptr], _c_int)
 _SIGS["kv_compact"] = ([ctypes.POINTER(DvsState), _c_ptr, ctypes.POINTER(DvsLayer), _c_int, _c_int,
                         _c_int, _c_int, _c_ptr, _c_ptr, _c_size, _c_ptr], _c_int)
+
+_SIGS["tree_masks"] = ([_c_ptr, _c_int, _c_int, _c_ptr, _c_ptr, _c_ptr, _c_ptr], _c_int)
+_SIGS["kv_append_rope"] = ([_c_ptr, _c_long, _c_long] * 3 + [_c_ptr] * 5 + [_c_int] * 6 + [_c_f32] +
+                           [_c_int] * 3 + [_c_ptr] * 3, _c_int)
+_SIGS["dvs_tree_workspace_bytes"] = ([_c_int] * 7, _c_size)
+_SIGS["attn_tree"] = ([_c_ptr] * 6 + [_c_int] * 7 + [_c_f32, _c_int] + [_c_ptr] * 3 +
+                      [_c_size, _c_ptr], _c_int)
+_SIGS["dvs_accept_tree_workspace_bytes"] = ([_c_int, _c_int], _c_size)
+_SIGS["accept_commit_tree"] = ([ctypes.POINTER(DvsState), ctypes.POINTER(DvsLayer)] + [_c_int] * 5 +
+                               [_c_ptr] * 6 + [_c_size, _c_ptr], _c_int)
 
 EXPORTED = tuple(_SIGS)
 
@@ -839,7 +850,7 @@ def capture(fn) -> "torch.cuda.CUDAGraph":
     """Record the launches of ``fn`` (calls of this module that only enqueue:
     draft_verify_step, literal_round, attn_hybrid_block, argmax_accept,
     sample_filtered, accept_sampled, the commits, kv_fork, kv_release,
-    kv_compact; not diffusion_block or literal_round_refined, which read a count
+    kv_compact, tree_masks, kv_append_rope, attn_tree, accept_commit_tree; not diffusion_block or literal_round_refined, which read a count
     back from the device) into a HIP graph.  ``replay()`` re-runs them on the
     buffers' current contents: every input of a step (kv_len, pages, boundary,
     draft, ...) is read from device memory, so a replay is the next step.
@@ -1080,6 +1091,174 @@ def kv_compact(st: DeviceState, pools: KVPools, moved_out=None, workspace=None, 
                           _ptr(ws), ws.numel(), _stream(stream))
     _check(rc, "kv_compact")
     return moved_out
+
+
+# ---------------------------------------------------------------------------
+# a step over a tree of drafted tokens
+# ---------------------------------------------------------------------------
+
+def tree_masks(parent, mask_out=None, depth_out=None, err=None, stream=None):
+    """parent [S,R] int32 (-1: a root, < -1: padding) -> (mask [S,R,ceil(R/32)] int32:
+    bit j%32 of word j/32 of row r is set iff j is r or an ancestor; depth [S,R] int32,
+    -1 for padding)."""
+    S, R = _dev(parent, torch.int32, "parent", 2).shape
+    shape = (S, R, (R + 31) // 32)
+    if mask_out is None:
+        mask_out = _new(shape, torch.int32, parent.device, stream)
+    elif _dev(mask_out, torch.int32, "mask_out").shape != shape:
+        raise DvsError(f"mask_out must be {shape}")
+    if depth_out is None:
+        depth_out = _new((S, R), torch.int32, parent.device, stream)
+    elif _dev(depth_out, torch.int32, "depth_out").shape != (S, R):
+        raise DvsError("depth_out must be [S, R]")
+    _check_err(err)
+    _here(parent, mask_out, depth_out, err)
+    rc = lib().tree_masks(_ptr(parent), S, R, _ptr(mask_out), _ptr(depth_out), _ptr(err),
+                          _stream(stream))
+    _check(rc, "tree_masks")
+    return mask_out, depth_out
+
+
+def _rows(t, name, dtype, S, R, D):
+    """A [S,R,H,D] tensor whose heads lie side by side; its sequence and row strides."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise DvsError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != dtype:
+        raise DvsError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 4 or t.shape[0] != S or t.shape[1] != R or t.shape[3] != D:
+        raise DvsError(f"{name} must be [S, R, heads, D], got {tuple(t.shape)}")
+    seq, ld, head, one = t.stride()
+    if one != 1 or (t.shape[2] > 1 and head != D):
+        raise DvsError(f"{name}'s heads must be contiguous and side by side")
+    if seq < 0 or ld < 0:
+        raise DvsError(f"{name}'s strides must not be negative")
+    return seq, ld
+
+
+def _pool_pair(k_pool, v_pool, dtype):
+    P, Hkv, _, D = _dev(k_pool, dtype, "k_pool", 4).shape
+    _dev(v_pool, dtype, "v_pool", 4)
+    if k_pool.shape != (P, Hkv, 16, D) or v_pool.shape != (P, Hkv, D, 16):
+        raise DvsError("pools must be k [P,Hkv,16,D] and v [P,Hkv,D,16]")
+    return P, Hkv, D
+
+
+def _paged(page_table, kv_len, S):
+    _dev(page_table, torch.int32, "page_table", 2)
+    _dev(kv_len, torch.int32, "kv_len", 1)
+    if page_table.shape[0] != S or kv_len.shape[0] != S:
+        raise DvsError("page_table / kv_len must have S rows")
+
+
+def kv_append_rope(q, k_new, v_new, k_pool, v_pool, page_table, kv_len, depth=None,
+                   theta: float = 10000.0, rot_dim: int | None = None, q_out=None, err=None,
+                   stream=None):
+    """q [S,R,Hq,D] (may be None), k_new / v_new [S,R,Hkv,D]: rotated at kv_len + depth (depth
+    [S,R] int32; None: + row), keys and values appended to the pools at slots kv_len + row.
+    Rows may be strided (a fused projection's); heads lie side by side.  The first rot_dim
+    elements of a head turn (None: all).  Returns q_out [S,R,Hq,D]."""
+    dt = k_new.dtype
+    P, Hkv, D = _pool_pair(k_pool, v_pool, dt)
+    if k_new.dim() != 4 or k_new.shape[2] != Hkv or v_new.shape != k_new.shape:
+        raise DvsError("k_new / v_new must be [S, R, Hkv, D]")
+    S, R = k_new.shape[:2]
+    ks = _rows(k_new, "k_new", dt, S, R, D)
+    vs = _rows(v_new, "v_new", dt, S, R, D)
+    _paged(page_table, kv_len, S)
+    Hq, qs = 0, (0, 0)
+    if q is not None:
+        qs = _rows(q, "q", dt, S, R, D)
+        Hq = q.shape[2]
+        if q_out is None:
+            q_out = _new((S, R, Hq, D), dt, q.device, stream)
+        elif _dev(q_out, dt, "q_out").shape != (S, R, Hq, D):
+            raise DvsError("q_out must be [S, R, Hq, D]")
+    elif q_out is not None:
+        raise DvsError("q_out without q")
+    if depth is not None and _dev(depth, torch.int32, "depth").shape != (S, R):
+        raise DvsError("depth must be [S, R]")
+    _check_err(err)
+    _here(q, k_new, v_new, k_pool, v_pool, page_table, kv_len, depth, q_out, err)
+    rc = lib().kv_append_rope(_ptr(q), *qs, _ptr(k_new), *ks, _ptr(v_new), *vs, _ptr(k_pool),
+                              _ptr(v_pool), _ptr(page_table), _ptr(kv_len), _ptr(depth), S, R, Hq,
+                              Hkv, D, D if rot_dim is None else int(rot_dim), float(theta),
+                              page_table.shape[1], P, _dtype_code(k_new), _ptr(q_out), _ptr(err),
+                              _stream(stream))
+    _check(rc, "kv_append_rope")
+    return q_out
+
+
+def tree_workspace_bytes(S, R, Hq, Hkv, D, max_pages, dtype=torch.bfloat16) -> int:
+    code = dtype if isinstance(dtype, int) else DVS_F32 if dtype == torch.float32 else DVS_BF16
+    return int(lib().dvs_tree_workspace_bytes(S, R, Hq, Hkv, D, max_pages, code))
+
+
+def attn_tree(q, k_pool, v_pool, page_table, kv_len, mask, softmax_scale: float, out=None,
+              err=None, workspace=None, stream=None):
+    """Attention of q [S,R,Hq,D] over the cache below kv_len and, of the window's slots
+    [kv_len, kv_len + R), those whose bit is set in mask [S,R,ceil(R/32)] int32 (None: a
+    token-level causal window).  Returns out [S,R,Hq,D]."""
+    dt = q.dtype
+    S, R, Hq, D = _dev(q, dt, "q", 4).shape
+    P, Hkv, Dp = _pool_pair(k_pool, v_pool, dt)
+    if Dp != D:
+        raise DvsError("q and the pools must have the same head size")
+    _paged(page_table, kv_len, S)
+    if mask is not None and _dev(mask, torch.int32, "mask").shape != (S, R, (R + 31) // 32):
+        raise DvsError("mask must be [S, R, ceil(R / 32)]")
+    if out is None:
+        out = _new(q.shape, dt, q.device, stream)
+    elif _dev(out, dt, "out").shape != q.shape:
+        raise DvsError("out must be [S, R, Hq, D]")
+    _check_err(err)
+    _here(q, k_pool, v_pool, page_table, kv_len, mask, out, err, _buf(workspace))
+    code = _dtype_code(q)
+    ws = workspace.buf if workspace is not None else _new(
+        max(1, tree_workspace_bytes(S, R, Hq, Hkv, D, page_table.shape[1], code)), torch.uint8,
+        q.device, stream)
+    rc = lib().attn_tree(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(page_table), _ptr(kv_len),
+                         _ptr(mask), S, R, Hq, Hkv, D, page_table.shape[1], P,
+                         float(softmax_scale), code, _ptr(out), _ptr(err), _ptr(ws), ws.numel(),
+                         _stream(stream))
+    _check(rc, "attn_tree")
+    return out
+
+
+def accept_tree_workspace_bytes(S, R) -> int:
+    return int(lib().dvs_accept_tree_workspace_bytes(S, R))
+
+
+def accept_commit_tree(st: DeviceState, pools: KVPools, parent, tokens, argmax, eos_id: int = -1,
+                       accept_out=None, path_out=None, workspace=None, stream=None):
+    """Acceptance, commit and rollback of a tree window: parent, tokens and argmax (the
+    verifier's top-1) [S,R] int32.  The accepted path's cache slots move to the window's front
+    in every layer.  Returns (accept [S]: accepted rows below row 0, path [S,R]: the rows of the
+    path, then -1)."""
+    _check_pools(st, pools)
+    S, R = _dev(parent, torch.int32, "parent", 2).shape
+    _dev(tokens, torch.int32, "tokens", 2)
+    _dev(argmax, torch.int32, "argmax", 2)
+    if S != st.kv_len.shape[0] or tokens.shape != (S, R) or argmax.shape != (S, R):
+        raise DvsError("parent, tokens and argmax must be [S, R]")
+    if accept_out is None:
+        accept_out = _new((S,), torch.int32, parent.device, stream)
+    elif _dev(accept_out, torch.int32, "accept_out").shape != (S,):
+        raise DvsError("accept_out must be [S]")
+    if path_out is None:
+        path_out = _new((S, R), torch.int32, parent.device, stream)
+    elif _dev(path_out, torch.int32, "path_out").shape != (S, R):
+        raise DvsError("path_out must be [S, R]")
+    _here(st.kv_len, parent, tokens, argmax, accept_out, path_out, pools.keep[0][0],
+          _buf(workspace))
+    ws = workspace.buf if workspace is not None else _new(
+        max(1, accept_tree_workspace_bytes(S, R)), torch.uint8, parent.device, stream)
+    sd = _state_desc(st, eos_id)
+    rc = lib().accept_commit_tree(ctypes.byref(sd), pools.layers, len(pools.layers),
+                                  pools.n_kv_heads, pools.head_dim, pools.dtype, R, _ptr(parent),
+                                  _ptr(tokens), _ptr(argmax), _ptr(accept_out), _ptr(path_out),
+                                  _ptr(ws), ws.numel(), _stream(stream))
+    _check(rc, "accept_commit_tree")
+    return accept_out, path_out
 
 
 def prefill(model: DeviceModel, st: DeviceState, P: int, n_mask: int, prefix_tokens=None,
