@@ -2,81 +2,550 @@
 // in the paged cache already, over the cache and each row's ancestors.
 #include <math.h>
 
+#include <algorithm>
+
 #include "dvs_common.h"
 
 namespace dvs {
+
+static size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+__device__ __forceinline__ void store4(float* p, f32x4 v) { *(f32x4*)p = v; }
+__device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
+  *(bf16x4*)p = __builtin_convertvector(v, bf16x4);
+}
+
+constexpr int MAX_SEQS = 1024;      // sequences a launch takes
+constexpr float RESCALE_LOG2 = 8.f;
 
 struct TreeAttn {
   const void *q, *k_pool, *v_pool;
   const int32_t *table, *kv_len, *mask;
   void* out;
   int32_t* err;
-  int S, R, W, Hq, Hkv, G, max_pages, pool_pages;
-  float scale;
+  int S, R, W, Hq, Hkv, G, rows, n_rt, max_pages, pool_pages;
+  int split;       // items are cut where a wave's share ends, and merged by a launch of its own
+  int share_min;   // tiles of a share, at least
+  float scale_log2;
+  float* part_o;   // [slot][quad][lane] x 4
+  float* part_ml;  // [slot][group][lane] x (m, l)
+  int2* meta;      // [item] segments, share of the first
 };
 
-// A workgroup a (sequence, row, query head); 256 keys at a time, a thread a
-// key, then a thread an element of the head.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) tree_attn_plain_kernel(TreeAttn p) {
-  __shared__ float s_q[D], s_p[256], s_red[8];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int h = blockIdx.x % p.Hq, r = blockIdx.x / p.Hq % p.R, s = blockIdx.x / p.Hq / p.R;
-  const int kvh = h / p.G, L = p.kv_len[s];
-  if (L < 0 || (long long)L + p.R > (long long)p.max_pages * 16) {
-    if (tid == 0) set_err(p.err, DVS_ERR_MAX_PAGES);
-    return;
+// ---------------------------------------------------------------------------
+// Matrix instructions of 16 x 16: a lane is (m, quarter) or (n, quarter), with
+// m, n = lane & 15.  S^T[key, row] = K Q^T puts a query row in a lane's column
+// n, its keys in the four quarters; the exponentials are then the second
+// operand of O^T[d, row] += V^T P^T as they lie: the quarter's keys of P in a
+// lane are those of its piece of V.
+//
+// bf16: 32 keys a tile.  16x16x32 wants 8 consecutive keys a quarter of P, and
+// a result holds 4 rows a quarter: the first of two products takes the keys
+// 8 (m / 4) + m % 4, the second those 4 further on, so that their results side
+// by side are the keys 8 quarter .. + 7.
+// fp32: 16 keys a tile, 16x16x4: product i of four takes element i of every
+// lane's 16 bytes, in QK (4 elements of d a quarter) and PV (4 keys a quarter).
+//
+// Either way K and V are D / 16 pieces of 16 bytes a lane a tile, straight
+// from the cache page.
+// ---------------------------------------------------------------------------
+template <typename T>
+struct Tile;
+
+template <>
+struct Tile<__bf16> {
+  static constexpr int KEYS = 32, PAGES = 2, NK = 8, NS = 2;   // keys a lane, results
+  template <int D>
+  static __device__ __forceinline__ int k_page(int m, int) { return m >> 3; }
+  // offset in a page of a lane's piece 0 of K, and from there to piece i: the
+  // first and the second product's keys by turns
+  template <int D>
+  static __device__ __forceinline__ uint32_t k_off(int m, int quarter) {
+    return (uint32_t)(((8 * ((m >> 2) & 1) + (m & 3)) * D + quarter * 8) * 2);
   }
-  const size_t row = ((size_t)s * p.R + r) * p.Hq + h;
-  const uint32_t* bits = p.mask ? (const uint32_t*)p.mask + ((size_t)s * p.R + r) * p.W : nullptr;
-  bool any = !bits;
-  if (bits)
-    for (int i = 0; i < p.W; ++i) any |= bits[i] != 0;
-  const int T1 = any ? L + p.R : 0;
-  if (tid < D) s_q[tid] = (float)((const T*)p.q)[row * D + tid];
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, acc = 0.f;
-  const int d = tid % 128, part = tid / 128;
-  for (int t0 = 0; t0 < T1; t0 += 256) {
-    const int k = t0 + tid;
-    float sc = -INFINITY;
-    if (k < T1 && (k < L || (bits ? bits[(k - L) >> 5] >> ((k - L) & 31) & 1 : k - L <= r))) {
-      const int pg = p.table[(size_t)s * p.max_pages + (k >> 4)];
-      if (pg >= 0 && pg < p.pool_pages) {
-        const T* kr = (const T*)p.k_pool + (((size_t)pg * p.Hkv + kvh) * 16 + (k & 15)) * D;
-        float dot = 0.f;
-        for (int e = 0; e < D; ++e) dot = fmaf(s_q[e], (float)kr[e], dot);
-        sc = dot * p.scale;
+  template <int D>
+  static constexpr int k_piece(int i) { return ((i & 1) * 4 * D + (i >> 1) * 32) * 2; }
+  static __device__ __forceinline__ int v_page(int quarter) { return quarter >> 1; }
+  static __device__ __forceinline__ uint32_t v_off(int m, int quarter) {
+    return (uint32_t)((m * 16 + (quarter & 1) * 8) * 2);
+  }
+  // element of the head at which a lane's piece i of a query row starts
+  static constexpr int NQ_DIV = 32;
+  static __device__ __forceinline__ int q_elem(int quarter, int i) { return i * 32 + quarter * 8; }
+};
+
+template <>
+struct Tile<float> {
+  static constexpr int KEYS = 16, PAGES = 1, NK = 4, NS = 1;
+  template <int D>
+  static __device__ __forceinline__ int k_page(int, int) { return 0; }
+  template <int D>
+  static __device__ __forceinline__ uint32_t k_off(int m, int quarter) {
+    return (uint32_t)((m * D + quarter * 4) * 4);
+  }
+  template <int D>
+  static constexpr int k_piece(int i) { return i * 64; }
+  static __device__ __forceinline__ int v_page(int) { return 0; }
+  static __device__ __forceinline__ uint32_t v_off(int m, int quarter) {
+    return (uint32_t)((m * 16 + quarter * 4) * 4);
+  }
+  static constexpr int NQ_DIV = 16;
+  static __device__ __forceinline__ int q_elem(int quarter, int i) { return i * 16 + quarter * 4; }
+};
+
+__device__ __forceinline__ float rows_max(float v) {   // over the four quarters
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const f32x2 b = halves_pair(v);
+  return fmaxf(b[0], b[1]);
+}
+__device__ __forceinline__ float rows_sum(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const f32x2 b = halves_pair(v);
+  return b[0] + b[1];
+}
+
+// Bits i < N: whether window row r sees key key0 + i.  any: the row's mask has
+// a bit (it sees the cache).
+template <int N>
+__device__ __forceinline__ uint32_t seen_bits(const TreeAttn& p, const uint32_t* mask, int r, bool any,
+                                              int key0, int L) {
+  constexpr uint32_t ALL = (1u << N) - 1;
+  if (!any) return 0;
+  const int o = key0 - L;   // window slot of the first key
+  if (!mask) {
+    const int n = r - o + 1;
+    return n <= 0 ? 0 : (n >= N ? ALL : (1u << n) - 1);
+  }
+  if (o + N <= 0) return ALL;
+  const int lo = max(o, 0), w = lo >> 5, sh = lo & 31;
+  uint64_t bits = 0;
+  if (w < p.W) bits = mask[w];
+  if (w + 1 < p.W) bits |= (uint64_t)mask[w + 1] << 32;
+  uint32_t b = (uint32_t)(bits >> sh);
+  if (p.R - lo < 32) b &= p.R > lo ? (1u << (p.R - lo)) - 1 : 0;   // no slot past the window
+  if (o < 0) b = b << -o | ((1u << -o) - 1);
+  return b & ALL;
+}
+
+// One tile's softmax: scores to weights, with the row's reference maximum m
+// moved (and l and O rescaled) only where the tile exceeds it by 2^RESCALE_LOG2:
+// weights then stay below that, and the division by l is exact about it.
+template <int NS, int NG, int DG>
+__device__ __forceinline__ void softmax_tile(f32x4 (&s)[NG][NS], float scale_log2, float (&m)[NG],
+                                             float (&l)[NG], f32x4 (&o)[NG][DG]) {
+  bool move[NG], some = false;
+  float cand[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    float t = fmaxf(fmaxf(s[g][0][0], s[g][0][1]), fmaxf(s[g][0][2], s[g][0][3]));
+    if constexpr (NS == 2)
+      t = fmaxf(t, fmaxf(fmaxf(s[g][1][0], s[g][1][1]), fmaxf(s[g][1][2], s[g][1][3])));
+    cand[g] = rows_max(t) * scale_log2;
+    move[g] = cand[g] > m[g] + RESCALE_LOG2;
+    some |= move[g];
+  }
+  if (__ballot(some)) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const float a = move[g] ? __builtin_amdgcn_exp2f(m[g] - cand[g]) : 1.f;
+      l[g] *= a;
+      if (move[g]) m[g] = cand[g];
+#pragma unroll
+      for (int d = 0; d < DG; ++d) o[g][d] *= a;
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const float ms = m[g] == -INFINITY ? 0.f : m[g];
+#pragma unroll
+    for (int t = 0; t < NS; ++t) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[g][t][i] = __builtin_amdgcn_exp2f(fmaf(s[g][t][i], scale_log2, -ms));
+      l[g] += (s[g][t][0] + s[g][t][1]) + (s[g][t][2] + s[g][t][3]);
+    }
+  }
+}
+
+// Tiles before each sequence (s_seq[0 .. S]) and the lengths, by the whole
+// workgroup; sequences that do not fit their table have none.
+__device__ __forceinline__ void seq_tiles(const TreeAttn& p, int keys, int* s_seq, int* s_len, int* s_tot) {
+  const int tid = threadIdx.x, lane = tid & 63, nw = blockDim.x >> 6;
+  int carry = 0;
+  for (int s0 = 0; s0 < p.S; s0 += blockDim.x) {
+    const int s = s0 + tid;
+    int t = 0;
+    if (s < p.S) {
+      const int L = p.kv_len[s];
+      s_len[s] = L;
+      if (L < 0 || (long long)L + p.R > (long long)p.max_pages * DVS_PAGE_SIZE) {
+        if (blockIdx.x == 0) set_err(p.err, DVS_ERR_MAX_PAGES);
       } else {
-        set_err(p.err, DVS_ERR_BAD_PAGE);
+        t = (L + p.R + keys - 1) / keys;
       }
     }
-    float v = sc;
-    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-    if (lane == 0) s_red[w] = v;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int v = __shfl_up(t, off);
+      if (lane >= off) t += v;
+    }
+    if (s0) __syncthreads();
+    if (lane == 63) s_tot[tid >> 6] = t;
     __syncthreads();
-    const float mn = fmaxf(fmaxf(m, fmaxf(s_red[0], s_red[1])), fmaxf(s_red[2], s_red[3]));
-    const float al = m == -INFINITY ? 0.f : expf(m - mn);
-    const float e = sc == -INFINITY ? 0.f : expf(sc - mn);
-    s_p[tid] = sc == -INFINITY ? -1.f : e;
-    float sum = e;
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-    if (lane == 0) s_red[4 + w] = sum;
-    __syncthreads();
-    l = l * al + ((s_red[4] + s_red[5]) + (s_red[6] + s_red[7]));
-    m = mn;
-    acc *= al;
-    if (d < D)
-      for (int j = part; j < 256; j += 2) {
-        if (s_p[j] < 0.f) continue;
-        const int kk = t0 + j, pg = p.table[(size_t)s * p.max_pages + (kk >> 4)];
-        acc = fmaf(s_p[j], (float)((const T*)p.v_pool)[(((size_t)pg * p.Hkv + kvh) * D + d) * 16 + (kk & 15)], acc);
-      }
-    __syncthreads();
+    int before = carry;
+    for (int w = 0; w < nw; ++w) {
+      const int v = s_tot[w];
+      if (w < (tid >> 6)) before += v;
+      carry += v;
+    }
+    if (s < p.S) s_seq[1 + s] = before + t;
   }
-  s_p[tid] = acc;
+  if (tid == 0) s_seq[0] = 0;
   __syncthreads();
-  if (tid < D) ((T*)p.out)[row * D + tid] = (T)(l > 0.f ? (s_p[tid] + s_p[tid + 128]) / l : 0.f);
+}
+
+// The sequence that holds tile u of one item a sequence.
+__device__ __forceinline__ int find_seq(const int* s_seq, int S, int u) {
+  int lo = 0, hi = S;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (s_seq[mid] <= u) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Consecutive workgroups on one XCD (blockIdx goes round the eight): row tiles
+// of an item then find its keys in their L2.
+__device__ __forceinline__ int xcd_block() {
+  const int n = gridDim.x, q = n >> 3, rem = n & 7, x = blockIdx.x & 7, i = blockIdx.x >> 3;
+  return x * q + min(x, rem) + i;
+}
+
+// ---------------------------------------------------------------------------
+// Every wave on its own: NG groups of 16 query rows (row n of a KV head is
+// window row n / G, head n % G of its group) and a share of the key tiles,
+// straight from the cache into registers; the next tile's keys are on their
+// way under this one's softmax, its values under the next one's scores.
+// ---------------------------------------------------------------------------
+template <typename T, int D, int NG>
+__global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
+  using TL = Tile<T>;
+  constexpr int KEYS = TL::KEYS, NP = D / 16, NQP = D / TL::NQ_DIV, DG = D / 16, NS = TL::NS;
+  constexpr int PAGE_B = 16 * D * (int)sizeof(T);
+  __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[4];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int m16 = lane & 15, quarter = lane >> 4;
+  const int HN = p.Hkv * p.n_rt;
+  const int share_id = xcd_block() * 4 + w, n_shares = gridDim.x * 4;
+  int u = share_id, u_end = p.S * HN, share = 0;
+  if (p.split) {
+    seq_tiles(p, KEYS, s_seq, s_len, s_tot);
+    const int U = s_seq[p.S] * HN;
+    share = max((U + n_shares - 1) / n_shares, p.share_min);
+    u = min((long long)share_id * share, (long long)U);
+    u_end = min(u + share, U);
+  }
+  const char* kp = (const char*)p.k_pool;
+  const char* vp = (const char*)p.v_pool;
+  const uint32_t koff = TL::template k_off<D>(m16, quarter), voff = TL::v_off(m16, quarter);
+  const int kpage = TL::template k_page<D>(m16, quarter), vpage = TL::v_page(quarter);
+
+  while (u < u_end) {
+    int s, qi, j0, j1, tiles, k = 0, nseg = 1, L;
+    if (p.split) {
+      s = find_seq(s_seq, p.S, u / HN);
+      L = s_len[s];
+      tiles = s_seq[s + 1] - s_seq[s];
+      const int local = u - s_seq[s] * HN;
+      qi = local / tiles;
+      j0 = local - qi * tiles;
+      j1 = min(tiles, j0 + (u_end - u));
+      const int P0 = s_seq[s] * HN + qi * tiles;
+      k = share_id - P0 / share;
+      nseg = (P0 + tiles - 1) / share - P0 / share + 1;
+      u += j1 - j0;
+    } else {
+      s = u / HN;
+      qi = u - s * HN;
+      L = p.kv_len[s];
+      u += n_shares;
+      if (L < 0 || (long long)L + p.R > (long long)p.max_pages * DVS_PAGE_SIZE) {
+        if (lane == 0) set_err(p.err, DVS_ERR_MAX_PAGES);
+        continue;
+      }
+      j0 = 0;
+      j1 = tiles = (L + p.R + KEYS - 1) / KEYS;
+    }
+    s = __builtin_amdgcn_readfirstlane(s);
+    L = __builtin_amdgcn_readfirstlane(L);
+    const int it = s * HN + qi, kvh = qi / p.n_rt, rt = qi - kvh * p.n_rt;
+    if (p.split && k == 0 && lane == 0) p.meta[it] = int2{nseg, share_id};
+    const int n_valid = (L + p.R + 15) >> 4;
+    const int32_t* pt = p.table + (size_t)s * p.max_pages;
+    // the ids of the next 64 pages, a lane each
+    auto page_ids = [&](int j) {
+      int id = pt[min(j * TL::PAGES + lane, n_valid - 1)];
+      if (id < 0 || id >= p.pool_pages) {
+        set_err(p.err, DVS_ERR_BAD_PAGE);
+        id = 0;
+      }
+      return id;
+    };
+    int ids = page_ids(j0), ids_at = j0;
+    // this lane's query rows
+    int r[NG], h[NG];
+    bool valid[NG], any[NG];
+    const uint32_t* mask[NG];
+    u32x4 q[NG][NQP];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int n = (rt * NG + g) * 16 + m16;
+      valid[g] = n < p.rows;
+      r[g] = valid[g] ? n / p.G : 0;
+      h[g] = kvh * p.G + (valid[g] ? n - r[g] * p.G : 0);
+      const T* src = (const T*)p.q + (((size_t)s * p.R + r[g]) * p.Hq + h[g]) * D;
+#pragma unroll
+      for (int i = 0; i < NQP; ++i) q[g][i] = *(const u32x4*)(src + TL::q_elem(quarter, i));
+      mask[g] = p.mask ? (const uint32_t*)p.mask + ((size_t)s * p.R + r[g]) * p.W : nullptr;
+      any[g] = valid[g] && !p.mask;
+      if (valid[g] && p.mask)
+        for (int i = 0; i < p.W; ++i) any[g] |= (i == p.W - 1 && (p.R & 31) ? mask[g][i] & ((1u << (p.R & 31)) - 1) : mask[g][i]) != 0;
+    }
+    f32x4 o[NG][DG];
+    float m[NG], l[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      m[g] = -INFINITY;
+      l[g] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DG; ++d) o[g][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    u32x4 kf[NP], vf[NP];
+    auto base_of = [&](const char* pool, int j, int page) {
+      const int at = (j - ids_at) * TL::PAGES;
+      int id = __builtin_amdgcn_readlane(ids, at);
+      if constexpr (TL::PAGES == 2) {
+        const int id1 = __builtin_amdgcn_readlane(ids, at + 1);
+        id = page ? id1 : id;
+      }
+      return pool + ((size_t)(uint32_t)id * p.Hkv + kvh) * PAGE_B;
+    };
+    auto load_k = [&](int j) {
+      const char* b = base_of(kp, j, kpage) + koff;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) kf[i] = *(const u32x4*)(b + TL::template k_piece<D>(i));
+    };
+    auto load_v = [&](int j) {
+      const char* b = base_of(vp, j, vpage) + voff;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) vf[i] = *(const u32x4*)(b + i * 256 * sizeof(T));
+    };
+    load_k(j0);
+    load_v(j0);
+    for (int j = j0; j < j1; ++j) {
+      f32x4 sc[NG][NS];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+#pragma unroll
+        for (int t = 0; t < NS; ++t) sc[g][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+            sc[g][i & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, kf[i]), __builtin_bit_cast(bf16x8, q[g][i >> 1]), sc[g][i & 1], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              sc[g][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i][e]), __uint_as_float(q[g][i][e]),
+                                                              sc[g][0], 0, 0, 0);
+        }
+      }
+      const bool more = j + 1 < j1;
+      // the ids run out: those of the tiles from j on (this tile's are still
+      // needed for nothing, the next one's are)
+      if (more && (j + 2 - ids_at) * TL::PAGES > 64) {
+        ids_at = j + 1;
+        ids = page_ids(ids_at);
+      }
+      if (more) load_k(j + 1);
+      const int key0 = j * KEYS + quarter * TL::NK;
+      const bool masked = (j + 1) * KEYS > L;
+      if (masked) {
+        uint32_t un = 0;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const uint32_t b = seen_bits<TL::NK>(p, mask[g], r[g], any[g], key0, L);
+          un |= b;
+#pragma unroll
+          for (int i = 0; i < TL::NK; ++i)
+            if (!(b >> i & 1)) sc[g][i >> 2][i & 3] = -INFINITY;
+        }
+        // values that none of the wave's rows sees may be anything: zero
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) un |= __shfl_xor((int)un, off);
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2)
+              vf[i][e] &= (un >> (2 * e) & 1 ? 0xffffu : 0u) | (un >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+            else
+              vf[i][e] &= un >> e & 1 ? 0xffffffffu : 0u;
+          }
+      }
+      softmax_tile<NS, NG, DG>(sc, p.scale_log2, m, l, o);
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        if constexpr (sizeof(T) == 2) {
+          uint32_t pk[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            pk[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+                                                     f32x2{sc[g][e >> 1][2 * (e & 1)], sc[g][e >> 1][2 * (e & 1) + 1]}, bf16x2));
+          const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pk[0], pk[1], pk[2], pk[3]});
+#pragma unroll
+          for (int d = 0; d < DG; ++d)
+            o[g][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf, o[g][d], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int d = 0; d < DG; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              o[g][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[d][e]), sc[g][0][e], o[g][d], 0, 0, 0);
+        }
+      }
+      if (more) load_v(j + 1);
+    }
+    const size_t slot = (size_t)share_id * 2 + (k == 0 ? 1 : 0);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      l[g] = rows_sum(l[g]);
+      if (!any[g]) l[g] = 0.f;
+      if (nseg > 1) {
+        if (quarter == 0) *(f32x2*)(p.part_ml + ((slot * NG + g) * 16 + m16) * 2) = f32x2{m[g], l[g]};
+#pragma unroll
+        for (int d = 0; d < DG; ++d)
+          *(f32x4*)(p.part_o + ((slot * NG + g) * DG + d) * 256 + lane * 4) = o[g][d];
+      } else if (valid[g]) {
+        T* dst = (T*)p.out + (((size_t)s * p.R + r[g]) * p.Hq + h[g]) * D + quarter * 4;
+        const float inv = 1.f / l[g];
+#pragma unroll
+        for (int d = 0; d < DG; ++d) {
+          f32x4 x = o[g][d] * inv;
+          if (l[g] == 0.f) x = f32x4{0.f, 0.f, 0.f, 0.f};
+          store4(dst + d * 16, x);
+        }
+      }
+    }
+  }
+}
+
+// The segments of a split item, in their order: a wave a (group of 16 rows, 16
+// elements of the head).
+template <typename T, int D, int NG>
+__global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
+  constexpr int DG = D / 16, NQ = NG * DG, SB = 8;
+  const int lane = threadIdx.x & 63, m16 = lane & 15, quarter = lane >> 4;
+  const long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int HN = p.Hkv * p.n_rt;
+  const int it = (int)(task / NQ), gd = (int)(task - (long long)it * NQ), g = gd / DG, d = gd % DG;
+  if (it >= p.S * HN) return;
+  const int s = it / HN, qi = it - s * HN, kvh = qi / p.n_rt, rt = qi - kvh * p.n_rt;
+  const int2 mt = p.meta[it];
+  const int L = p.kv_len[s];
+  if (L < 0 || (long long)L + p.R > (long long)p.max_pages * DVS_PAGE_SIZE) return;
+  const int nseg = mt.x, first = mt.y;
+  if (nseg <= 1) return;
+  const int n = (rt * NG + g) * 16 + m16;
+  auto slot = [&](int c) { return (size_t)(first + c) * 2 + (c == 0 ? 1 : 0); };
+  auto ml_of = [&](int c) { return *(const f32x2*)(p.part_ml + ((slot(c) * NG + g) * 16 + m16) * 2); };
+  float M = -INFINITY;
+  for (int c0 = 0; c0 < nseg; c0 += SB) {
+    f32x2 v[SB];
+#pragma unroll
+    for (int b = 0; b < SB; ++b) v[b] = ml_of(min(c0 + b, nseg - 1));
+#pragma unroll
+    for (int b = 0; b < SB; ++b)
+      if (v[b][1] != 0.f) M = fmaxf(M, v[b][0]);
+  }
+  const float Ms = M == -INFINITY ? 0.f : M;
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int c0 = 0; c0 < nseg; c0 += SB) {
+    f32x2 ml[SB];
+    f32x4 x[SB];
+#pragma unroll
+    for (int b = 0; b < SB; ++b) {
+      const int c = min(c0 + b, nseg - 1);
+      ml[b] = ml_of(c);
+      x[b] = *(const f32x4*)(p.part_o + ((slot(c) * NG + g) * DG + d) * 256 + lane * 4);
+    }
+#pragma unroll
+    for (int b = 0; b < SB; ++b) {
+      if (c0 + b >= nseg || ml[b][1] == 0.f) continue;
+      const float e = __builtin_amdgcn_exp2f(ml[b][0] - Ms);
+      l = fmaf(e, ml[b][1], l);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] = fmaf(e, x[b][i], acc[i]);
+    }
+  }
+  if (n >= p.rows) return;
+  const int r = n / p.G, h = kvh * p.G + n - r * p.G;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  store4((T*)p.out + (((size_t)s * p.R + r) * p.Hq + h) * D + d * 16 + quarter * 4, acc * inv);
+}
+
+struct TreePlan {
+  int ng, n_rt, grid, split, share_min, seqs;   // seqs: sequences a launch takes
+  size_t off_ml, off_o, bytes;
+};
+
+static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, int dtype) {
+  TreePlan pl{};
+  const int rows = R * (Hq / Hkv);
+  const int keys = dtype == DVS_BF16 ? Tile<__bf16>::KEYS : Tile<float>::KEYS;
+  const int max_tiles = (max_pages * DVS_PAGE_SIZE + keys - 1) / keys;
+  pl.ng = rows > 16 ? 2 : 1;
+  pl.n_rt = (rows + pl.ng * 16 - 1) / (pl.ng * 16);
+  const long long per_seq = (long long)Hkv * pl.n_rt * max_tiles;
+  pl.seqs = (int)std::max<long long>(1, std::min<long long>(std::min(S, MAX_SEQS), (1LL << 30) / per_seq));
+  const long long items = (long long)pl.seqs * Hkv * pl.n_rt;
+  const int waves = device_cus() * 8;
+  pl.split = max_tiles > 8;
+  pl.share_min = 4;
+  const long long tiles = items * max_tiles;
+  pl.grid = (int)std::min<long long>(waves / 4, ((pl.split ? (tiles + pl.share_min - 1) / pl.share_min : items) + 3) / 4);
+  if (pl.split) {
+    const size_t slots = (size_t)pl.grid * 4 * 2;
+    pl.off_ml = al256((size_t)items * sizeof(int2));
+    pl.off_o = pl.off_ml + al256(slots * pl.ng * 16 * 2 * sizeof(float));
+    pl.bytes = pl.off_o + slots * pl.ng * 16 * D * sizeof(float);
+  } else {
+    pl.bytes = 256;
+  }
+  return pl;
+}
+
+template <typename T, int D, int NG>
+static void launch_wave(const TreePlan& pl, const TreeAttn& p, hipStream_t st) {
+  hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, NG>), dim3(pl.grid), dim3(256), 0, st, p);
+  if (pl.split) {
+    const long long tasks = (long long)p.S * p.Hkv * p.n_rt * NG * (D / 16);
+    hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, NG>), dim3((unsigned)((tasks + 3) / 4)), dim3(256), 0, st, p);
+  }
+}
+
+template <typename T, int D>
+static void launch_tree(const TreePlan& pl, const TreeAttn& p, hipStream_t st) {
+  if (pl.ng == 2) launch_wave<T, D, 2>(pl, p, st);
+  else launch_wave<T, D, 1>(pl, p, st);
 }
 
 }  // namespace dvs
@@ -88,7 +557,7 @@ extern "C" size_t dvs_tree_workspace_bytes(int32_t S, int32_t R, int32_t Hq, int
   if (S < 1 || R < 1 || R > 1024 || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 ||
       (D != 64 && D != 96 && D != 128) || max_pages < 1 || (dtype != DVS_F32 && dtype != DVS_BF16))
     return 0;
-  return 256;
+  return tree_plan(S, R, Hq, Hkv, D, max_pages, dtype).bytes;
 }
 
 extern "C" int attn_tree(const void* q, const void* k_pool, const void* v_pool,
@@ -107,24 +576,41 @@ extern "C" int attn_tree(const void* q, const void* k_pool, const void* v_pool,
   DVS_CHECK_SUPPORTED(D == 64 || D == 96 || D == 128, "attn_tree: head_dim %d", D);
   DVS_CHECK_ARG((((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_pool | (uintptr_t)v_pool) & 15) == 0,
                 "attn_tree: q, out and the pools must start on 16 bytes");
-  const size_t need = dvs_tree_workspace_bytes(S, R, Hq, Hkv, D, max_pages, dtype);
-  if (!workspace || ws_bytes < need) {
-    set_error("attn_tree: workspace needs %zu bytes, got %zu", need, ws_bytes);
+  const TreePlan pl = tree_plan(S, R, Hq, Hkv, D, max_pages, dtype);
+  if (!workspace || ws_bytes < pl.bytes) {
+    set_error("attn_tree: workspace needs %zu bytes, got %zu", pl.bytes, ws_bytes);
     return DVS_EWORKSPACE;
   }
+  DVS_CHECK_SUPPORTED((long long)Hkv * pl.n_rt * max_pages < (1LL << 30), "attn_tree: too many pages");
   TreeAttn p{};
-  p.q = q; p.k_pool = k_pool; p.v_pool = v_pool; p.table = page_table; p.kv_len = kv_len;
-  p.mask = tree_mask; p.out = out; p.err = err_word;
-  p.S = S; p.R = R; p.W = (R + 31) / 32; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv;
-  p.max_pages = max_pages; p.pool_pages = num_pool_pages; p.scale = softmax_scale;
-  const long long grid = (long long)S * R * Hq;
-  DVS_CHECK_SUPPORTED(grid < (1LL << 31), "attn_tree: grid too large");
+  p.k_pool = k_pool; p.v_pool = v_pool; p.err = err_word;
+  p.R = R; p.W = (R + 31) / 32; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.rows = R * p.G;
+  p.n_rt = pl.n_rt; p.max_pages = max_pages; p.pool_pages = num_pool_pages;
+  p.split = pl.split; p.share_min = pl.share_min;
+  p.scale_log2 = softmax_scale * 1.4426950408889634f;
+  p.meta = (int2*)workspace;
+  p.part_ml = (float*)((char*)workspace + pl.off_ml);
+  p.part_o = (float*)((char*)workspace + pl.off_o);
   hipStream_t st = (hipStream_t)stream;
-#define PLAIN(T)                                                                                      \
-  if (D == 128) hipLaunchKernelGGL((tree_attn_plain_kernel<T, 128>), dim3(grid), dim3(256), 0, st, p); \
-  else if (D == 96) hipLaunchKernelGGL((tree_attn_plain_kernel<T, 96>), dim3(grid), dim3(256), 0, st, p); \
-  else hipLaunchKernelGGL((tree_attn_plain_kernel<T, 64>), dim3(grid), dim3(256), 0, st, p);
-  if (dtype == DVS_BF16) { PLAIN(__bf16) } else { PLAIN(float) }
-#undef PLAIN
-  return launch_status("attn_tree");
+  const size_t row = (size_t)R * Hq * D * (dtype == DVS_BF16 ? 2 : 4);
+  for (int s0 = 0; s0 < S; s0 += pl.seqs) {
+    p.S = std::min(S - s0, pl.seqs);
+    p.q = (const char*)q + s0 * row;
+    p.out = (char*)out + s0 * row;
+    p.table = page_table + (size_t)s0 * max_pages;
+    p.kv_len = kv_len + s0;
+    p.mask = tree_mask ? tree_mask + (size_t)s0 * R * p.W : nullptr;
+    if (dtype == DVS_BF16) {
+      if (D == 128) launch_tree<__bf16, 128>(pl, p, st);
+      else if (D == 96) launch_tree<__bf16, 96>(pl, p, st);
+      else launch_tree<__bf16, 64>(pl, p, st);
+    } else {
+      if (D == 128) launch_tree<float, 128>(pl, p, st);
+      else if (D == 96) launch_tree<float, 96>(pl, p, st);
+      else launch_tree<float, 64>(pl, p, st);
+    }
+    const int rc = launch_status("attn_tree");
+    if (rc) return rc;
+  }
+  return DVS_OK;
 }
