@@ -17,6 +17,8 @@ __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
 
 constexpr int MAX_SEQS = 1024;      // sequences a launch takes
 constexpr float RESCALE_LOG2 = 8.f;
+constexpr int TILE_ROWS = 32, TILE_MIN_TILES = 2048, TILE_SHARE = 8;
+constexpr int WAVE_WHOLE = 8, WAVE_SHARE = 4;
 
 struct TreeAttn {
   const void *q, *k_pool, *v_pool;
@@ -24,6 +26,7 @@ struct TreeAttn {
   void* out;
   int32_t* err;
   int S, R, W, Hq, Hkv, G, rows, n_rt, max_pages, pool_pages;
+  int n_wide;      // row tiles of 128 (0: waves on their own)
   int split;       // items are cut where a wave's share ends, and merged by a launch of its own
   int share_min;   // tiles of a share, at least
   float scale_log2;
@@ -223,6 +226,60 @@ __device__ __forceinline__ int xcd_block() {
   return x * q + min(x, rem) + i;
 }
 
+// Whether a row's mask (NULL: causal) has a bit of the window.
+__device__ __forceinline__ bool sees_any(const TreeAttn& p, const uint32_t* mask) {
+  if (!mask) return true;
+  uint32_t bits = 0;
+  for (int i = 0; i < p.W; ++i) bits |= i == p.W - 1 && (p.R & 31) ? mask[i] & ((1u << (p.R & 31)) - 1) : mask[i];
+  return bits != 0;
+}
+
+// The two halves of word e of 8 bf16 values whose bits of `un` are set.
+__device__ __forceinline__ uint32_t pair_mask(uint32_t un, int e) {
+  return (un >> (2 * e) & 1 ? 0xffffu : 0u) | (un >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+}
+
+// The weights of a lane's 8 keys, rounded once (bf16: what the matrix
+// instruction takes; l is summed before the rounding).
+__device__ __forceinline__ bf16x8 weights_bf16(const f32x4 (&s)[2]) {
+  u32x4 pk;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    pk[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+                                             f32x2{s[e >> 1][2 * (e & 1)], s[e >> 1][2 * (e & 1) + 1]}, bf16x2));
+  return __builtin_bit_cast(bf16x8, pk);
+}
+
+// End of a segment: the output, or a part of it (O, m and l in 32 bits).  l is
+// 0 exactly for a row that sees nothing, whatever its O holds.
+template <typename T, int D, int NG>
+__device__ __forceinline__ void finish_rows(const TreeAttn& p, int s, const int (&r)[NG], const int (&h)[NG],
+                                            const bool (&valid)[NG], const bool (&any)[NG],
+                                            const float (&m)[NG], float (&l)[NG],
+                                            const f32x4 (&o)[NG][D / 16], int nseg, size_t slot) {
+  const int lane = threadIdx.x & 63, m16 = lane & 15, quarter = lane >> 4;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    l[g] = rows_sum(l[g]);
+    if (!any[g]) l[g] = 0.f;
+    if (nseg > 1) {
+      if (quarter == 0) *(f32x2*)(p.part_ml + ((slot * NG + g) * 16 + m16) * 2) = f32x2{m[g], l[g]};
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d)
+        *(f32x4*)(p.part_o + ((slot * NG + g) * (D / 16) + d) * 256 + lane * 4) = o[g][d];
+    } else if (valid[g]) {
+      T* dst = (T*)p.out + (((size_t)s * p.R + r[g]) * p.Hq + h[g]) * D + quarter * 4;
+      const float inv = 1.f / l[g];
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) {
+        f32x4 x = o[g][d] * inv;
+        if (l[g] == 0.f) x = f32x4{0.f, 0.f, 0.f, 0.f};
+        store4(dst + d * 16, x);
+      }
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Every wave on its own: NG groups of 16 query rows (row n of a KV head is
 // window row n / G, head n % G of its group) and a share of the key tiles,
@@ -309,9 +366,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
 #pragma unroll
       for (int i = 0; i < NQP; ++i) q[g][i] = *(const u32x4*)(src + TL::q_elem(quarter, i));
       mask[g] = p.mask ? (const uint32_t*)p.mask + ((size_t)s * p.R + r[g]) * p.W : nullptr;
-      any[g] = valid[g] && !p.mask;
-      if (valid[g] && p.mask)
-        for (int i = 0; i < p.W; ++i) any[g] |= (i == p.W - 1 && (p.R & 31) ? mask[g][i] & ((1u << (p.R & 31)) - 1) : mask[g][i]) != 0;
+      any[g] = valid[g] && sees_any(p, mask[g]);
     }
     f32x4 o[NG][DG];
     float m[NG], l[NG];
@@ -395,7 +450,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             if constexpr (sizeof(T) == 2)
-              vf[i][e] &= (un >> (2 * e) & 1 ? 0xffffu : 0u) | (un >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+              vf[i][e] &= pair_mask(un, e);
             else
               vf[i][e] &= un >> e & 1 ? 0xffffffffu : 0u;
           }
@@ -404,12 +459,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         if constexpr (sizeof(T) == 2) {
-          uint32_t pk[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            pk[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
-                                                     f32x2{sc[g][e >> 1][2 * (e & 1)], sc[g][e >> 1][2 * (e & 1) + 1]}, bf16x2));
-          const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pk[0], pk[1], pk[2], pk[3]});
+          const bf16x8 pf = weights_bf16(sc[g]);
 #pragma unroll
           for (int d = 0; d < DG; ++d)
             o[g][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf, o[g][d], 0, 0, 0);
@@ -423,27 +473,228 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
       }
       if (more) load_v(j + 1);
     }
-    const size_t slot = (size_t)share_id * 2 + (k == 0 ? 1 : 0);
+    finish_rows<T, D, NG>(p, s, r, h, valid, any, m, l, o, nseg, (size_t)share_id * 2 + (k == 0 ? 1 : 0));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Many query rows of a KV head (bf16): a workgroup of four waves, 32 rows each,
+// over 32-key tiles that all of them read from LDS.  A wave copies one page of
+// every tile, K (waves 0, 1) or V (2, 3), straight to LDS, STAGES - 1 tiles
+// ahead.  Row tiles of 128 rows take the same key range side by side on one
+// XCD (its L2 then gives the second reader what the first has fetched).
+//
+// LDS rows of K (a key, 2 D bytes) have their 16-byte chunks permuted so that
+// the 16 keys of one product, read at the same chunk, lie in 16 different bank
+// groups; in V (an element of the head, 32 bytes a page) the two halves swap.
+// The stages are variables of their own and the loop over them is unrolled:
+// the compiler then knows that a read of one does not touch the copies on
+// their way into the others, and does not wait for those.
+// ---------------------------------------------------------------------------
+template <int D>
+__device__ __forceinline__ int k_swizzle(int row) {
+  if constexpr (D == 128) return (row & 3) | ((row >> 1) & 12);
+  else if constexpr (D == 96) return (row >> 3) & 3;
+  else return ((row >> 1) & 1) | ((row >> 2) & 6);
+}
+__device__ __forceinline__ int v_swizzle(int d) { return ((d >> 2) ^ (d >> 3)) & 1; }
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {   // at most N vector loads on their way
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+}
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttn p) {
+  constexpr int KEYS = 32, NG = 2, DG = D / 16, STAGES = 4;
+  constexpr int PAGE_B = 32 * D, TILE_B = 2 * PAGE_B;   // bytes of a page, of a tile's K (or V)
+  constexpr int NPL = PAGE_B / 1024;                    // copies of a wave a tile
+  constexpr int STAGE_B = 2 * TILE_B;
+  __shared__ __attribute__((aligned(1024))) char st0[STAGE_B], st1[STAGE_B], st2[STAGE_B], st3[STAGE_B];
+  __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[4];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int m16 = lane & 15, quarter = lane >> 4;
+  const int block = xcd_block(), n_shares = gridDim.x / p.n_wide;
+  const int share_id = block / p.n_wide, rt = block - share_id * p.n_wide;
+  seq_tiles(p, KEYS, s_seq, s_len, s_tot);
+  const int U = s_seq[p.S] * p.Hkv;
+  const int share = max((U + n_shares - 1) / n_shares, p.share_min);
+  int u = (int)min((long long)share_id * share, (long long)U);
+  const int u_end = min(u + share, U);
+  // copies: lane's source offset in the page, of its 16 bytes of each 1 KB
+  const char* pool = (const char*)(w < 2 ? p.k_pool : p.v_pool);
+  uint32_t soff[NPL];
+#pragma unroll
+  for (int i = 0; i < NPL; ++i) {
+    const int off = i * 1024 + lane * 16;
+    if (w < 2) {
+      const int row = off / (2 * D), c = (off - row * 2 * D) >> 4;
+      soff[i] = row * 2 * D + ((c ^ k_swizzle<D>((w & 1) * 16 + row)) << 4);
+    } else {
+      const int d = off >> 5;
+      soff[i] = d * 32 + ((((off >> 4) & 1) ^ v_swizzle(d)) << 4);
+    }
+  }
+  // fragments: K of product t = 0 (t = 1: four rows on), chunk ks * 4 + quarter
+  const int krow = 8 * (m16 >> 2) + (m16 & 3), ksw = k_swizzle<D>(krow);
+  int kfrag[D / 32];
+#pragma unroll
+  for (int ks = 0; ks < D / 32; ++ks) kfrag[ks] = krow * 2 * D + (((ks * 4 + quarter) ^ ksw) << 4);
+  const int vfrag = TILE_B + (quarter >> 1) * PAGE_B + m16 * 32 + (((quarter & 1) ^ v_swizzle(m16)) << 4);
+  bool again = false;
+
+  while (u < u_end) {
+    const int s = __builtin_amdgcn_readfirstlane(find_seq(s_seq, p.S, u / p.Hkv));
+    const int L = __builtin_amdgcn_readfirstlane(s_len[s]);
+    const int tiles = s_seq[s + 1] - s_seq[s];
+    const int local = u - s_seq[s] * p.Hkv;
+    const int kvh = local / tiles, j0 = local - kvh * tiles, j1 = min(tiles, j0 + (u_end - u));
+    const int P0 = s_seq[s] * p.Hkv + kvh * tiles;
+    const int k = share_id - P0 / share, nseg = (P0 + tiles - 1) / share - P0 / share + 1;
+    u += j1 - j0;
+    const int sub = rt * 4 + w;                         // this wave's 32 rows of the item
+    const bool work = sub * 32 < p.rows;
+    const int it = (s * p.Hkv + kvh) * p.n_rt + sub;
+    if (work && k == 0 && lane == 0) p.meta[it] = int2{nseg, (share_id * p.n_wide + rt) * 4 + w};
+    const int n_valid = (L + p.R + 15) >> 4;
+    const int32_t* pt = p.table + (size_t)s * p.max_pages;
+    // the wave's page of the next 64 tiles, a lane each
+    auto page_ids = [&](int j) {
+      int id = pt[min((j + lane) * 2 + (w & 1), n_valid - 1)];
+      if (id < 0 || id >= p.pool_pages) {
+        set_err(p.err, DVS_ERR_BAD_PAGE);
+        id = 0;
+      }
+      return id;
+    };
+    int ids = page_ids(j0), ids_at = j0;
+    int r[NG], h[NG];
+    bool valid[NG], any[NG];
+    const uint32_t* mask[NG];
+    u32x4 q[NG][D / 32];
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      l[g] = rows_sum(l[g]);
-      if (!any[g]) l[g] = 0.f;
-      if (nseg > 1) {
-        if (quarter == 0) *(f32x2*)(p.part_ml + ((slot * NG + g) * 16 + m16) * 2) = f32x2{m[g], l[g]};
+      const int n = (sub * NG + g) * 16 + m16;
+      valid[g] = n < p.rows;
+      r[g] = valid[g] ? n / p.G : 0;
+      h[g] = kvh * p.G + (valid[g] ? n - r[g] * p.G : 0);
+      const __bf16* src = (const __bf16*)p.q + (((size_t)s * p.R + r[g]) * p.Hq + h[g]) * D + quarter * 8;
 #pragma unroll
-        for (int d = 0; d < DG; ++d)
-          *(f32x4*)(p.part_o + ((slot * NG + g) * DG + d) * 256 + lane * 4) = o[g][d];
-      } else if (valid[g]) {
-        T* dst = (T*)p.out + (((size_t)s * p.R + r[g]) * p.Hq + h[g]) * D + quarter * 4;
-        const float inv = 1.f / l[g];
-#pragma unroll
-        for (int d = 0; d < DG; ++d) {
-          f32x4 x = o[g][d] * inv;
-          if (l[g] == 0.f) x = f32x4{0.f, 0.f, 0.f, 0.f};
-          store4(dst + d * 16, x);
-        }
-      }
+      for (int i = 0; i < D / 32; ++i) q[g][i] = *(const u32x4*)(src + i * 32);
+      mask[g] = p.mask ? (const uint32_t*)p.mask + ((size_t)s * p.R + r[g]) * p.W : nullptr;
+      any[g] = valid[g] && sees_any(p, mask[g]);
     }
+    // The queries' loads end here, and the registers are then as if made anew:
+    // the compiler cannot tell inside the loop that they have ended, and would
+    // wait for the tiles' copies as well.
+    wait_loads<0>();
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) asm volatile("" : "+v"(q[g][i]));
+    asm volatile("" : "+v"(ids));
+    f32x4 o[NG][DG];
+    float m[NG], l[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      m[g] = -INFINITY;
+      l[g] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DG; ++d) o[g][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (again) __syncthreads();   // the last segment's tiles are read
+    again = true;
+    auto stage = [&](auto c) -> char* {
+      constexpr int I = decltype(c)::value % STAGES;
+      if constexpr (I == 0) return st0;
+      else if constexpr (I == 1) return st1;
+      else if constexpr (I == 2) return st2;
+      else return st3;
+    };
+    auto issue = [&](auto c, int j) {
+      if (j - ids_at >= 64) {
+        ids_at = j;
+        ids = page_ids(j);
+      }
+      const int id = __builtin_amdgcn_readlane(ids, j - ids_at);
+      const char* base = pool + ((size_t)(uint32_t)id * p.Hkv + kvh) * PAGE_B;
+      char* to = stage(c) + w * PAGE_B;
+#pragma unroll
+      for (int i = 0; i < NPL; ++i)
+        __builtin_amdgcn_global_load_lds((const void*)(base + soff[i]),
+                                         (__attribute__((address_space(3))) void*)(to + i * 1024), 16, 0, 0);
+    };
+    auto step = [&](auto c, int j) {
+      constexpr int C = decltype(c)::value;
+      // this wave's copies of tile j have arrived (those of later tiles may
+      // be on their way), then everybody's
+      if (j + STAGES - 1 <= j1) wait_loads<(STAGES - 2) * NPL>();
+      else if (j + 2 < j1) wait_loads<2 * NPL>();
+      else if (j + 1 < j1) wait_loads<NPL>();
+      else wait_loads<0>();
+      __builtin_amdgcn_s_barrier();
+      if (j + STAGES - 1 < j1) issue(IC<C + STAGES - 1>{}, j + STAGES - 1);
+      if (!work) return;
+      const char* tile = stage(c);
+      f32x4 sc[NG][2];
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) sc[g][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bf16x8 kf = *(const bf16x8*)(tile + kfrag[ks] + t * 4 * 2 * D);
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+            sc[g][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, q[g][ks]), sc[g][t], 0, 0, 0);
+        }
+      const int key0 = j * KEYS + quarter * 8;
+      const bool masked = (j + 1) * KEYS > L;
+      uint32_t un = 0xff;
+      if (masked) {
+        un = 0;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const uint32_t b = seen_bits<8>(p, mask[g], r[g], any[g], key0, L);
+          un |= b;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (!(b >> i & 1)) sc[g][i >> 2][i & 3] = -INFINITY;
+        }
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) un |= __shfl_xor((int)un, off);
+      }
+      softmax_tile<2, NG, DG>(sc, p.scale_log2, m, l, o);
+      bf16x8 pf[NG];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) pf[g] = weights_bf16(sc[g]);
+      u32x4 keep;
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) keep[e] = pair_mask(un, e);
+      }
+#pragma unroll
+      for (int d = 0; d < DG; ++d) {
+        u32x4 vf = *(const u32x4*)(tile + vfrag + d * 512);
+        if (masked) vf &= keep;
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+          o[g][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf[g], o[g][d], 0, 0, 0);
+      }
+    };
+    static_for<0, STAGES - 1>([&](auto c) {
+      if (j0 + decltype(c)::value < j1) issue(c, j0 + decltype(c)::value);
+    });
+    for (int j = j0; j < j1; j += STAGES)
+      static_for<0, STAGES>([&](auto c) {
+        if (j + decltype(c)::value < j1) step(c, j + decltype(c)::value);
+      });
+    if (!work) continue;
+    const size_t slot = (size_t)((share_id * p.n_wide + rt) * 4 + w) * 2 + (k == 0 ? 1 : 0);
+    finish_rows<__bf16, D, NG>(p, s, r, h, valid, any, m, l, o, nseg, slot);
   }
 }
 
@@ -464,7 +715,8 @@ __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
   const int nseg = mt.x, first = mt.y;
   if (nseg <= 1) return;
   const int n = (rt * NG + g) * 16 + m16;
-  auto slot = [&](int c) { return (size_t)(first + c) * 2 + (c == 0 ? 1 : 0); };
+  const int step = p.n_wide ? p.n_wide * 4 : 1;   // from a share's slot to the next one's
+  auto slot = [&](int c) { return (size_t)(first + c * step) * 2 + (c == 0 ? 1 : 0); };
   auto ml_of = [&](int c) { return *(const f32x2*)(p.part_ml + ((slot(c) * NG + g) * 16 + m16) * 2); };
   float M = -INFINITY;
   for (int c0 = 0; c0 < nseg; c0 += SB) {
@@ -503,7 +755,7 @@ __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
 }
 
 struct TreePlan {
-  int ng, n_rt, grid, split, share_min, seqs;   // seqs: sequences a launch takes
+  int ng, n_rt, n_wide, grid, split, share_min, seqs;   // seqs: sequences a launch takes
   size_t off_ml, off_o, bytes;
 };
 
@@ -517,11 +769,20 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
   const long long per_seq = (long long)Hkv * pl.n_rt * max_tiles;
   pl.seqs = (int)std::max<long long>(1, std::min<long long>(std::min(S, MAX_SEQS), (1LL << 30) / per_seq));
   const long long items = (long long)pl.seqs * Hkv * pl.n_rt;
-  const int waves = device_cus() * 8;
-  pl.split = max_tiles > 8;
-  pl.share_min = 4;
-  const long long tiles = items * max_tiles;
-  pl.grid = (int)std::min<long long>(waves / 4, ((pl.split ? (tiles + pl.share_min - 1) / pl.share_min : items) + 3) / 4);
+  const int cus = device_cus();
+  const long long kv_tiles = (long long)pl.seqs * Hkv * max_tiles;
+  if (dtype == DVS_BF16 && rows > TILE_ROWS && kv_tiles >= TILE_MIN_TILES) {
+    pl.n_wide = (rows + 127) / 128;
+    pl.split = 1;
+    pl.share_min = TILE_SHARE;
+    const long long shares = std::min<long long>(std::max(1, 2 * cus / pl.n_wide), (kv_tiles + TILE_SHARE - 1) / TILE_SHARE);
+    pl.grid = (int)(shares * pl.n_wide);
+  } else {
+    pl.split = max_tiles > WAVE_WHOLE;
+    pl.share_min = WAVE_SHARE;
+    const long long tiles = items * max_tiles;
+    pl.grid = (int)std::min<long long>(2 * cus, ((pl.split ? (tiles + WAVE_SHARE - 1) / WAVE_SHARE : items) + 3) / 4);
+  }
   if (pl.split) {
     const size_t slots = (size_t)pl.grid * 4 * 2;
     pl.off_ml = al256((size_t)items * sizeof(int2));
@@ -533,19 +794,20 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
   return pl;
 }
 
-template <typename T, int D, int NG>
-static void launch_wave(const TreePlan& pl, const TreeAttn& p, hipStream_t st) {
-  hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, NG>), dim3(pl.grid), dim3(256), 0, st, p);
-  if (pl.split) {
-    const long long tasks = (long long)p.S * p.Hkv * p.n_rt * NG * (D / 16);
-    hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, NG>), dim3((unsigned)((tasks + 3) / 4)), dim3(256), 0, st, p);
-  }
-}
-
 template <typename T, int D>
 static void launch_tree(const TreePlan& pl, const TreeAttn& p, hipStream_t st) {
-  if (pl.ng == 2) launch_wave<T, D, 2>(pl, p, st);
-  else launch_wave<T, D, 1>(pl, p, st);
+  if (pl.n_wide) {
+    if constexpr (sizeof(T) == 2) hipLaunchKernelGGL(tree_attn_tile_kernel<D>, dim3(pl.grid), dim3(256), 0, st, p);
+  } else if (pl.ng == 2) {
+    hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 2>), dim3(pl.grid), dim3(256), 0, st, p);
+  } else {
+    hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 1>), dim3(pl.grid), dim3(256), 0, st, p);
+  }
+  if (!pl.split) return;
+  const long long tasks = (long long)p.S * p.Hkv * p.n_rt * pl.ng * (D / 16);
+  const dim3 gr((unsigned)((tasks + 3) / 4));
+  if (pl.ng == 2) hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, 2>), gr, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, 1>), gr, dim3(256), 0, st, p);
 }
 
 }  // namespace dvs
@@ -586,7 +848,7 @@ extern "C" int attn_tree(const void* q, const void* k_pool, const void* v_pool,
   p.k_pool = k_pool; p.v_pool = v_pool; p.err = err_word;
   p.R = R; p.W = (R + 31) / 32; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.rows = R * p.G;
   p.n_rt = pl.n_rt; p.max_pages = max_pages; p.pool_pages = num_pool_pages;
-  p.split = pl.split; p.share_min = pl.share_min;
+  p.n_wide = pl.n_wide; p.split = pl.split; p.share_min = pl.share_min;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
   p.meta = (int2*)workspace;
   p.part_ml = (float*)((char*)workspace + pl.off_ml);
