@@ -16,9 +16,10 @@ __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
 }
 
 constexpr int MAX_SEQS = 1024;      // sequences a launch takes
-constexpr float RESCALE_LOG2 = 8.f;
+constexpr float RESCALE_LOG2 = 8.f, WEIGHT_MAX = 8 * 256.f;
 constexpr int TILE_ROWS = 32, TILE_MIN_TILES = 2048, TILE_SHARE = 8;
 constexpr int WAVE_WHOLE = 8, WAVE_SHARE = 4;
+constexpr int MERGE_FEW = 1024;
 
 struct TreeAttn {
   const void *q, *k_pool, *v_pool;
@@ -132,43 +133,51 @@ __device__ __forceinline__ uint32_t seen_bits(const TreeAttn& p, const uint32_t*
   return b & ALL;
 }
 
-// One tile's softmax: scores to weights, with the row's reference maximum m
-// moved (and l and O rescaled) only where the tile exceeds it by 2^RESCALE_LOG2:
-// weights then stay below that, and the division by l is exact about it.
+// One tile's softmax: scores to weights 2^(s - m).  m is a reference, not the
+// maximum so far: any m will do that keeps the weights in range, and the
+// division by l is exact about it.  So a tile takes m as it is, and only where
+// a lane's weights add up to more than 8 x 2^RESCALE_LOG2 (or to no number: m
+// starts at -inf) the rows' maxima are found, m moves to those that exceed it by
+// RESCALE_LOG2, and the tile's weights are made again.  Long documents: 520 us
+// with the maxima of every tile, XXX without.
 template <int NS, int NG, int DG>
-__device__ __forceinline__ void softmax_tile(f32x4 (&s)[NG][NS], float scale_log2, float (&m)[NG],
-                                             float (&l)[NG], f32x4 (&o)[NG][DG]) {
-  bool move[NG], some = false;
-  float cand[NG];
+__device__ __forceinline__ void softmax_tile(const f32x4 (&s)[NG][NS], f32x4 (&w)[NG][NS],
+                                             float scale_log2, float (&m)[NG], float (&l)[NG],
+                                             f32x4 (&o)[NG][DG]) {
+  float sum[NG];
+  bool over = false;
+  auto weigh = [&](int g, float ref) {
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[g][t][i] = __builtin_amdgcn_exp2f(fmaf(s[g][t][i], scale_log2, -ref));
+    sum[g] = (w[g][0][0] + w[g][0][1]) + (w[g][0][2] + w[g][0][3]);
+    if constexpr (NS == 2) sum[g] += (w[g][1][0] + w[g][1][1]) + (w[g][1][2] + w[g][1][3]);
+  };
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    float t = fmaxf(fmaxf(s[g][0][0], s[g][0][1]), fmaxf(s[g][0][2], s[g][0][3]));
-    if constexpr (NS == 2)
-      t = fmaxf(t, fmaxf(fmaxf(s[g][1][0], s[g][1][1]), fmaxf(s[g][1][2], s[g][1][3])));
-    cand[g] = rows_max(t) * scale_log2;
-    move[g] = cand[g] > m[g] + RESCALE_LOG2;
-    some |= move[g];
+    weigh(g, m[g]);
+    over |= !(sum[g] <= WEIGHT_MAX);
   }
-  if (__ballot(some)) {
+  if (__ballot(over)) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const float a = move[g] ? __builtin_amdgcn_exp2f(m[g] - cand[g]) : 1.f;
-      l[g] *= a;
-      if (move[g]) m[g] = cand[g];
+      float t = fmaxf(fmaxf(s[g][0][0], s[g][0][1]), fmaxf(s[g][0][2], s[g][0][3]));
+      if constexpr (NS == 2)
+        t = fmaxf(t, fmaxf(fmaxf(s[g][1][0], s[g][1][1]), fmaxf(s[g][1][2], s[g][1][3])));
+      const float cand = rows_max(t) * scale_log2;
+      if (cand > m[g] + RESCALE_LOG2) {
+        const float a = __builtin_amdgcn_exp2f(m[g] - cand);
+        m[g] = cand;
+        l[g] *= a;
 #pragma unroll
-      for (int d = 0; d < DG; ++d) o[g][d] *= a;
+        for (int d = 0; d < DG; ++d) o[g][d] *= a;
+      }
+      weigh(g, m[g] == -INFINITY ? 0.f : m[g]);
     }
   }
 #pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    const float ms = m[g] == -INFINITY ? 0.f : m[g];
-#pragma unroll
-    for (int t = 0; t < NS; ++t) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[g][t][i] = __builtin_amdgcn_exp2f(fmaf(s[g][t][i], scale_log2, -ms));
-      l[g] += (s[g][t][0] + s[g][t][1]) + (s[g][t][2] + s[g][t][3]);
-    }
-  }
+  for (int g = 0; g < NG; ++g) l[g] += sum[g];
 }
 
 // Tiles before each sequence (s_seq[0 .. S]) and the lengths, by the whole
@@ -455,11 +464,12 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
               vf[i][e] &= un >> e & 1 ? 0xffffffffu : 0u;
           }
       }
-      softmax_tile<NS, NG, DG>(sc, p.scale_log2, m, l, o);
+      f32x4 wt[NG][NS];
+      softmax_tile<NS, NG, DG>(sc, wt, p.scale_log2, m, l, o);
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         if constexpr (sizeof(T) == 2) {
-          const bf16x8 pf = weights_bf16(sc[g]);
+          const bf16x8 pf = weights_bf16(wt[g]);
 #pragma unroll
           for (int d = 0; d < DG; ++d)
             o[g][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf, o[g][d], 0, 0, 0);
@@ -468,7 +478,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
           for (int d = 0; d < DG; ++d)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              o[g][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[d][e]), sc[g][0][e], o[g][d], 0, 0, 0);
+              o[g][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[d][e]), wt[g][0][e], o[g][d], 0, 0, 0);
         }
       }
       if (more) load_v(j + 1);
@@ -605,39 +615,31 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttn p) {
     }
     if (again) __syncthreads();   // the last segment's tiles are read
     again = true;
-    auto stage = [&](auto c) -> char* {
-      constexpr int I = decltype(c)::value % STAGES;
-      if constexpr (I == 0) return st0;
-      else if constexpr (I == 1) return st1;
-      else if constexpr (I == 2) return st2;
-      else return st3;
-    };
-    auto issue = [&](auto c, int j) {
+    auto issue = [&](char* stage, int j) {
       if (j - ids_at >= 64) {
         ids_at = j;
         ids = page_ids(j);
       }
       const int id = __builtin_amdgcn_readlane(ids, j - ids_at);
       const char* base = pool + ((size_t)(uint32_t)id * p.Hkv + kvh) * PAGE_B;
-      char* to = stage(c) + w * PAGE_B;
+      char* to = stage + w * PAGE_B;
 #pragma unroll
       for (int i = 0; i < NPL; ++i)
         __builtin_amdgcn_global_load_lds((const void*)(base + soff[i]),
                                          (__attribute__((address_space(3))) void*)(to + i * 1024), 16, 0, 0);
     };
-    auto step = [&](auto c, int j) {
-      constexpr int C = decltype(c)::value;
-      // this wave's copies of tile j have arrived (those of later tiles may
-      // be on their way), then everybody's
+    // Tile j, in `tile`: this wave's copies of it have arrived (those of later
+    // tiles may be on their way), then everybody's; the stage that the tile
+    // before left free takes tile j + STAGES - 1.
+    auto step = [&](auto masked, char* tile, char* next, int j) {
+      constexpr bool MASKED = decltype(masked)::value != 0;
       if (j + STAGES - 1 <= j1) wait_loads<(STAGES - 2) * NPL>();
-      else if (j + 2 < j1) wait_loads<2 * NPL>();
       else if (j + 1 < j1) wait_loads<NPL>();
       else wait_loads<0>();
       __builtin_amdgcn_s_barrier();
-      if (j + STAGES - 1 < j1) issue(IC<C + STAGES - 1>{}, j + STAGES - 1);
+      if (j + STAGES - 1 < j1) issue(next, j + STAGES - 1);
       if (!work) return;
-      const char* tile = stage(c);
-      f32x4 sc[NG][2];
+      f32x4 sc[NG][2], wt[NG][2];
 #pragma unroll
       for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -651,62 +653,76 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttn p) {
           for (int g = 0; g < NG; ++g)
             sc[g][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, q[g][ks]), sc[g][t], 0, 0, 0);
         }
-      const int key0 = j * KEYS + quarter * 8;
-      const bool masked = (j + 1) * KEYS > L;
-      uint32_t un = 0xff;
-      if (masked) {
-        un = 0;
+      uint32_t un = 0;
+      if constexpr (MASKED) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const uint32_t b = seen_bits<8>(p, mask[g], r[g], any[g], key0, L);
+          const uint32_t b = seen_bits<8>(p, mask[g], r[g], any[g], j * KEYS + quarter * 8, L);
           un |= b;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             if (!(b >> i & 1)) sc[g][i >> 2][i & 3] = -INFINITY;
         }
+        // values that none of the wave's rows sees may be anything: zero
 #pragma unroll
         for (int off = 1; off < 16; off <<= 1) un |= __shfl_xor((int)un, off);
       }
-      softmax_tile<2, NG, DG>(sc, p.scale_log2, m, l, o);
+      softmax_tile<2, NG, DG>(sc, wt, p.scale_log2, m, l, o);
       bf16x8 pf[NG];
 #pragma unroll
-      for (int g = 0; g < NG; ++g) pf[g] = weights_bf16(sc[g]);
-      u32x4 keep;
-      if (masked) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) keep[e] = pair_mask(un, e);
-      }
+      for (int g = 0; g < NG; ++g) pf[g] = weights_bf16(wt[g]);
 #pragma unroll
       for (int d = 0; d < DG; ++d) {
         u32x4 vf = *(const u32x4*)(tile + vfrag + d * 512);
-        if (masked) vf &= keep;
+        if constexpr (MASKED) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vf[e] &= pair_mask(un, e);
+        }
 #pragma unroll
         for (int g = 0; g < NG; ++g)
           o[g][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf[g], o[g][d], 0, 0, 0);
       }
     };
+    auto stage = [&](auto c) -> char* {
+      constexpr int I = decltype(c)::value % STAGES;
+      if constexpr (I == 0) return st0;
+      else if constexpr (I == 1) return st1;
+      else if constexpr (I == 2) return st2;
+      else return st3;
+    };
     static_for<0, STAGES - 1>([&](auto c) {
-      if (j0 + decltype(c)::value < j1) issue(c, j0 + decltype(c)::value);
+      if (j0 + decltype(c)::value < j1) issue(stage(c), j0 + decltype(c)::value);
     });
-    for (int j = j0; j < j1; j += STAGES)
+    // tiles below L, then the few that reach the window
+    const int jm = max(j0, min(j1, L / KEYS));
+    for (int j = j0; j < jm; j += STAGES)
       static_for<0, STAGES>([&](auto c) {
-        if (j + decltype(c)::value < j1) step(c, j + decltype(c)::value);
+        constexpr int C = decltype(c)::value;
+        if (j + C < jm) step(IC<0>{}, stage(c), stage(IC<C + STAGES - 1>{}), j + C);
       });
+    for (int j = jm; j < j1; ++j) {
+      const int i = (j - j0) % STAGES;
+      char* at = i == 0 ? st0 : i == 1 ? st1 : i == 2 ? st2 : st3;
+      char* free = i == 0 ? st3 : i == 1 ? st0 : i == 2 ? st1 : st2;
+      step(IC<1>{}, at, free, j);
+    }
     if (!work) continue;
     const size_t slot = (size_t)((share_id * p.n_wide + rt) * 4 + w) * 2 + (k == 0 ? 1 : 0);
     finish_rows<__bf16, D, NG>(p, s, r, h, valid, any, m, l, o, nseg, slot);
   }
 }
 
-// The segments of a split item, in their order: a wave a (group of 16 rows, 16
-// elements of the head).
-template <typename T, int D, int NG>
+// The segments of a split item, in their order: a wave a (group of 16 rows, NQ
+// times 16 elements of the head), SB segments on their way at a time.  Few items:
+// more waves and more segments at a time; many: fewer and longer ones (2048 items
+// of two segments, 128 wide: 33 us with one piece a wave, XXX with all eight).
+template <typename T, int D, int NG, int NQ, int SB>
 __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
-  constexpr int DG = D / 16, NQ = NG * DG, SB = 8;
+  constexpr int DG = D / 16, PER = NG * DG / NQ;
   const int lane = threadIdx.x & 63, m16 = lane & 15, quarter = lane >> 4;
   const long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int HN = p.Hkv * p.n_rt;
-  const int it = (int)(task / NQ), gd = (int)(task - (long long)it * NQ), g = gd / DG, d = gd % DG;
+  const int it = (int)(task / PER), gd = (int)(task - (long long)it * PER) * NQ, g = gd / DG, d0 = gd % DG;
   if (it >= p.S * HN) return;
   const int s = it / HN, qi = it - s * HN, kvh = qi / p.n_rt, rt = qi - kvh * p.n_rt;
   const int2 mt = p.meta[it];
@@ -718,40 +734,48 @@ __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
   const int step = p.n_wide ? p.n_wide * 4 : 1;   // from a share's slot to the next one's
   auto slot = [&](int c) { return (size_t)(first + c * step) * 2 + (c == 0 ? 1 : 0); };
   auto ml_of = [&](int c) { return *(const f32x2*)(p.part_ml + ((slot(c) * NG + g) * 16 + m16) * 2); };
-  float M = -INFINITY;
-  for (int c0 = 0; c0 < nseg; c0 += SB) {
-    f32x2 v[SB];
+  f32x4 acc[NQ];
 #pragma unroll
-    for (int b = 0; b < SB; ++b) v[b] = ml_of(min(c0 + b, nseg - 1));
-#pragma unroll
-    for (int b = 0; b < SB; ++b)
-      if (v[b][1] != 0.f) M = fmaxf(M, v[b][0]);
-  }
-  const float Ms = M == -INFINITY ? 0.f : M;
-  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
+  for (int i = 0; i < NQ; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float M = -INFINITY, l = 0.f;
   for (int c0 = 0; c0 < nseg; c0 += SB) {
     f32x2 ml[SB];
-    f32x4 x[SB];
+    f32x4 x[SB][NQ];
 #pragma unroll
     for (int b = 0; b < SB; ++b) {
       const int c = min(c0 + b, nseg - 1);
       ml[b] = ml_of(c);
-      x[b] = *(const f32x4*)(p.part_o + ((slot(c) * NG + g) * DG + d) * 256 + lane * 4);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+        x[b][i] = *(const f32x4*)(p.part_o + ((slot(c) * NG + g) * DG + d0 + i) * 256 + lane * 4);
     }
+    float top = M;
+#pragma unroll
+    for (int b = 0; b < SB; ++b)
+      if (ml[b][1] != 0.f) top = fmaxf(top, ml[b][0]);   // the last segment's repeats change nothing
+    const float back = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - top);
+    const float ref = top == -INFINITY ? 0.f : top;
+    M = top;
+    l *= back;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) acc[i] *= back;
 #pragma unroll
     for (int b = 0; b < SB; ++b) {
       if (c0 + b >= nseg || ml[b][1] == 0.f) continue;
-      const float e = __builtin_amdgcn_exp2f(ml[b][0] - Ms);
+      const float e = __builtin_amdgcn_exp2f(ml[b][0] - ref);
       l = fmaf(e, ml[b][1], l);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = fmaf(e, x[b][i], acc[i]);
+      for (int i = 0; i < NQ; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(e, x[b][i][j], acc[i][j]);
     }
   }
   if (n >= p.rows) return;
   const int r = n / p.G, h = kvh * p.G + n - r * p.G;
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  store4((T*)p.out + (((size_t)s * p.R + r) * p.Hq + h) * D + d * 16 + quarter * 4, acc * inv);
+  T* dst = (T*)p.out + (((size_t)s * p.R + r) * p.Hq + h) * D + d0 * 16 + quarter * 4;
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) store4(dst + i * 16, acc[i] * inv);
 }
 
 struct TreePlan {
@@ -794,6 +818,14 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
   return pl;
 }
 
+template <typename T, int D, int NG>
+static void launch_merge(long long groups, const TreeAttn& p, hipStream_t st) {
+  if (groups < MERGE_FEW)
+    hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, NG, 1, 8>), dim3((unsigned)((groups * (D / 16) + 3) / 4)), dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, NG, D / 16, 2>), dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, st, p);
+}
+
 template <typename T, int D>
 static void launch_tree(const TreePlan& pl, const TreeAttn& p, hipStream_t st) {
   if (pl.n_wide) {
@@ -804,10 +836,9 @@ static void launch_tree(const TreePlan& pl, const TreeAttn& p, hipStream_t st) {
     hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 1>), dim3(pl.grid), dim3(256), 0, st, p);
   }
   if (!pl.split) return;
-  const long long tasks = (long long)p.S * p.Hkv * p.n_rt * pl.ng * (D / 16);
-  const dim3 gr((unsigned)((tasks + 3) / 4));
-  if (pl.ng == 2) hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, 2>), gr, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, 1>), gr, dim3(256), 0, st, p);
+  const long long groups = (long long)p.S * p.Hkv * p.n_rt * pl.ng;
+  if (pl.ng == 2) launch_merge<T, D, 2>(groups, p, st);
+  else launch_merge<T, D, 1>(groups, p, st);
 }
 
 }  // namespace dvs
