@@ -17,9 +17,9 @@ __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
 
 constexpr int MAX_SEQS = 1024;      // sequences a launch takes
 constexpr float RESCALE_LOG2 = 8.f, WEIGHT_MAX = 8 * 256.f;
-constexpr int TILE_ROWS = 32, TILE_MIN_TILES = 2048, TILE_SHARE = 8;
-constexpr int WAVE_WHOLE = 8, WAVE_SHARE = 4;
-constexpr int MERGE_FEW = 1024;
+constexpr int TILE_ROWS = 32;      // query rows of a KV head above which tiles go through LDS
+constexpr int WHOLE_TILES = 8;     // tiles of a table up to which a wave takes a whole item
+constexpr int MERGE_FEW = 1024;    // row groups up to which the merge takes more waves
 
 struct TreeAttn {
   const void *q, *k_pool, *v_pool;
@@ -27,7 +27,7 @@ struct TreeAttn {
   void* out;
   int32_t* err;
   int S, R, W, Hq, Hkv, G, rows, n_rt, max_pages, pool_pages;
-  int n_wide;      // row tiles of 128 (0: waves on their own)
+  int n_wide, wide_waves;   // row tiles of a workgroup's waves (0: waves on their own)
   int split;       // items are cut where a wave's share ends, and merged by a launch of its own
   int share_min;   // tiles of a share, at least
   float scale_log2;
@@ -138,25 +138,48 @@ __device__ __forceinline__ uint32_t seen_bits(const TreeAttn& p, const uint32_t*
 // division by l is exact about it.  So a tile takes m as it is, and only where
 // a lane's weights add up to more than 8 x 2^RESCALE_LOG2 (or to no number: m
 // starts at -inf) the rows' maxima are found, m moves to those that exceed it by
-// RESCALE_LOG2, and the tile's weights are made again.  Long documents: 520 us
-// with the maxima of every tile, XXX without.
-template <int NS, int NG, int DG>
-__device__ __forceinline__ void softmax_tile(const f32x4 (&s)[NG][NS], f32x4 (&w)[NG][NS],
+// RESCALE_LOG2, and the tile's weights are made again (long documents 540 us with
+// the maxima of every tile, 458 without).
+template <typename T>
+struct Weights;
+template <>
+struct Weights<__bf16> {   // a lane's 8 keys, rounded once: what the matrix instruction takes
+  typedef bf16x8 type;
+  // l is summed before the rounding
+  static __device__ __forceinline__ float make(const f32x4* s, float scale_log2, float ref, bf16x8& w) {
+    f32x4 e[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], scale_log2, -ref));
+    u32x4 pk;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      pk[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+                                               f32x2{e[i >> 1][2 * (i & 1)], e[i >> 1][2 * (i & 1) + 1]}, bf16x2));
+    w = __builtin_bit_cast(bf16x8, pk);
+    return ((e[0][0] + e[0][1]) + (e[0][2] + e[0][3])) + ((e[1][0] + e[1][1]) + (e[1][2] + e[1][3]));
+  }
+};
+template <>
+struct Weights<float> {    // 4 keys
+  typedef f32x4 type;
+  static __device__ __forceinline__ float make(const f32x4* s, float scale_log2, float ref, f32x4& w) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], scale_log2, -ref));
+    return (w[0] + w[1]) + (w[2] + w[3]);
+  }
+};
+
+template <typename T, int NS, int NG, int DG>
+__device__ __forceinline__ void softmax_tile(const f32x4 (&s)[NG][NS], typename Weights<T>::type (&w)[NG],
                                              float scale_log2, float (&m)[NG], float (&l)[NG],
                                              f32x4 (&o)[NG][DG]) {
   float sum[NG];
   bool over = false;
-  auto weigh = [&](int g, float ref) {
-#pragma unroll
-    for (int t = 0; t < NS; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[g][t][i] = __builtin_amdgcn_exp2f(fmaf(s[g][t][i], scale_log2, -ref));
-    sum[g] = (w[g][0][0] + w[g][0][1]) + (w[g][0][2] + w[g][0][3]);
-    if constexpr (NS == 2) sum[g] += (w[g][1][0] + w[g][1][1]) + (w[g][1][2] + w[g][1][3]);
-  };
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    weigh(g, m[g]);
+    sum[g] = Weights<T>::make(s[g], scale_log2, m[g], w[g]);
     over |= !(sum[g] <= WEIGHT_MAX);
   }
   if (__ballot(over)) {
@@ -173,35 +196,71 @@ __device__ __forceinline__ void softmax_tile(const f32x4 (&s)[NG][NS], f32x4 (&w
 #pragma unroll
         for (int d = 0; d < DG; ++d) o[g][d] *= a;
       }
-      weigh(g, m[g] == -INFINITY ? 0.f : m[g]);
+      sum[g] = Weights<T>::make(s[g], scale_log2, m[g] == -INFINITY ? 0.f : m[g], w[g]);
     }
   }
 #pragma unroll
   for (int g = 0; g < NG; ++g) l[g] += sum[g];
 }
 
-// Tiles before each sequence (s_seq[0 .. S]) and the lengths, by the whole
-// workgroup; sequences that do not fit their table have none.
-__device__ __forceinline__ void seq_tiles(const TreeAttn& p, int keys, int* s_seq, int* s_len, int* s_tot) {
+// The sequences' tiles side by side: how many lie before each of them, which
+// sequence a tile belongs to, and the lengths.  Sequences that do not fit their
+// table have none.  Up to 64: in registers, a lane a sequence, every wave for
+// itself; more: in LDS, by the whole workgroup.
+struct SeqTiles {
+  int S, total;
+  int upto, len;             // of sequence `lane`
+  const int *s_seq, *s_len;
+  bool in_lds;
+
+  __device__ __forceinline__ int before(int s) const {
+    if (in_lds) return s_seq[s];
+    return s == 0 ? 0 : __builtin_amdgcn_readlane(upto, s - 1);
+  }
+  __device__ __forceinline__ int length(int s) const {
+    return in_lds ? s_len[s] : __builtin_amdgcn_readlane(len, s);
+  }
+  __device__ __forceinline__ int find(int t) const {   // t < total
+    if (!in_lds) return __popcll(__ballot((threadIdx.x & 63) < S && upto <= t));
+    int lo = 0, hi = S;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (s_seq[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  }
+};
+
+__device__ __forceinline__ int scan64(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int o = __shfl_up(v, off);
+    if (lane >= off) v += o;
+  }
+  return v;
+}
+
+__device__ __forceinline__ SeqTiles seq_tiles(const TreeAttn& p, int keys, int* s_seq, int* s_len, int* s_tot) {
   const int tid = threadIdx.x, lane = tid & 63, nw = blockDim.x >> 6;
+  auto tiles_of = [&](int s, int L) {
+    if (s >= p.S) return 0;
+    if (L < 0 || (long long)L + p.R > (long long)p.max_pages * DVS_PAGE_SIZE) {
+      if (blockIdx.x == 0) set_err(p.err, DVS_ERR_MAX_PAGES);
+      return 0;
+    }
+    return (L + p.R + keys - 1) / keys;
+  };
+  if (p.S <= 64) {
+    const int L = p.kv_len[min(lane, p.S - 1)], upto = scan64(tiles_of(lane, L));
+    return SeqTiles{p.S, __builtin_amdgcn_readlane(upto, 63), upto, L, nullptr, nullptr, false};
+  }
   int carry = 0;
   for (int s0 = 0; s0 < p.S; s0 += blockDim.x) {
-    const int s = s0 + tid;
-    int t = 0;
-    if (s < p.S) {
-      const int L = p.kv_len[s];
-      s_len[s] = L;
-      if (L < 0 || (long long)L + p.R > (long long)p.max_pages * DVS_PAGE_SIZE) {
-        if (blockIdx.x == 0) set_err(p.err, DVS_ERR_MAX_PAGES);
-      } else {
-        t = (L + p.R + keys - 1) / keys;
-      }
-    }
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int v = __shfl_up(t, off);
-      if (lane >= off) t += v;
-    }
+    const int s = s0 + tid, L = s < p.S ? p.kv_len[s] : 0;
+    if (s < p.S) s_len[s] = L;
+    const int t = scan64(tiles_of(s, L));
     if (s0) __syncthreads();
     if (lane == 63) s_tot[tid >> 6] = t;
     __syncthreads();
@@ -215,17 +274,7 @@ __device__ __forceinline__ void seq_tiles(const TreeAttn& p, int keys, int* s_se
   }
   if (tid == 0) s_seq[0] = 0;
   __syncthreads();
-}
-
-// The sequence that holds tile u of one item a sequence.
-__device__ __forceinline__ int find_seq(const int* s_seq, int S, int u) {
-  int lo = 0, hi = S;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (s_seq[mid] <= u) lo = mid;
-    else hi = mid;
-  }
-  return lo;
+  return SeqTiles{p.S, s_seq[p.S], 0, 0, s_seq, s_len, true};
 }
 
 // Consecutive workgroups on one XCD (blockIdx goes round the eight): row tiles
@@ -238,25 +287,77 @@ __device__ __forceinline__ int xcd_block() {
 // Whether a row's mask (NULL: causal) has a bit of the window.
 __device__ __forceinline__ bool sees_any(const TreeAttn& p, const uint32_t* mask) {
   if (!mask) return true;
-  uint32_t bits = 0;
-  for (int i = 0; i < p.W; ++i) bits |= i == p.W - 1 && (p.R & 31) ? mask[i] & ((1u << (p.R & 31)) - 1) : mask[i];
+  const uint32_t last = mask[p.W - 1], first = mask[0];   // (the usual masks: one or two words)
+  uint32_t bits = last & (0xffffffffu >> (31 - ((p.R - 1) & 31)));
+  if (p.W > 1) bits |= first;
+  for (int i = 1; i < p.W - 1; ++i) bits |= mask[i];
   return bits != 0;
 }
 
-// The two halves of word e of 8 bf16 values whose bits of `un` are set.
-__device__ __forceinline__ uint32_t pair_mask(uint32_t un, int e) {
-  return (un >> (2 * e) & 1 ? 0xffffu : 0u) | (un >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+// A page id of the table, 0 (and the error) for one outside the pool.
+__device__ __forceinline__ int checked_page(const TreeAttn& p, int id) {
+  if (id >= 0 && id < p.pool_pages) return id;
+  set_err(p.err, DVS_ERR_BAD_PAGE);
+  return 0;
 }
 
-// The weights of a lane's 8 keys, rounded once (bf16: what the matrix
-// instruction takes; l is summed before the rounding).
-__device__ __forceinline__ bf16x8 weights_bf16(const f32x4 (&s)[2]) {
-  u32x4 pk;
+// A value that a row does not see must not reach it, and 0 times an infinity or a
+// NaN would.  In the window's tiles such values are therefore taken out of the
+// product, and added to the rows that see them (slots behind the last row hold
+// anything, others seldom such: finding out is a product with zeros, or in fp32
+// a multiplication each).  bits: of a lane's row and its quarter's keys;
+// value(key, d): the cache's.
+template <typename T, int NG, int DG, class F>
+__device__ __forceinline__ void clean_values(u32x4 (&vf)[DG], const uint32_t (&bits)[NG], f32x4 (&o)[NG][DG],
+                                             F value) {
+  const int quarter = (threadIdx.x & 63) >> 4;
+  bool found = false;
+  if constexpr (sizeof(T) == 2) {
+    f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    pk[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
-                                             f32x2{s[e >> 1][2 * (e & 1)], s[e >> 1][2 * (e & 1) + 1]}, bf16x2));
-  return __builtin_bit_cast(bf16x8, pk);
+    for (int d = 0; d < DG; ++d)
+      z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[d]), bf16x8{}, z, 0, 0, 0);
+    found = z[0] != 0.f || z[1] != 0.f || z[2] != 0.f || z[3] != 0.f;
+  } else {
+    float z = 0.f;
+#pragma unroll
+    for (int d = 0; d < DG; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z = fmaf(__uint_as_float(vf[d][e]), 0.f, z);
+    found = z != 0.f;
+  }
+  if (!__ballot(found)) return;
+#pragma unroll
+  for (int d = 0; d < DG; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((vf[d][e] & 0x7f800000) == 0x7f800000) vf[d][e] &= sizeof(T) == 2 ? 0xffff : 0;
+      if (sizeof(T) == 2 && (vf[d][e] & 0x7f80) == 0x7f80) vf[d][e] &= 0xffff0000;
+    }
+  constexpr int NK = Tile<T>::NK;
+  uint32_t sees[NG], some = 0;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    uint32_t b = bits[g] << quarter * NK;
+    b |= __shfl_xor((int)b, 16);
+    sees[g] = b | __shfl_xor((int)b, 32);
+    some |= sees[g];
+  }
+#pragma nounroll
+  for (int key = 0; key < Tile<T>::KEYS; ++key) {
+    if (!__ballot(some >> key & 1)) continue;
+#pragma unroll
+    for (int d = 0; d < DG; ++d) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = value(key, d * 16 + quarter * 4 + i);
+        const bool odd = (__float_as_uint(x) & 0x7f800000) == 0x7f800000;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) o[g][d][i] += odd && (sees[g] >> key & 1) ? x : 0.f;
+      }
+      __builtin_amdgcn_sched_barrier(0);   // (few registers are free here)
+    }
+  }
 }
 
 // End of a segment: the output, or a part of it (O, m and l in 32 bits).  l is
@@ -293,7 +394,16 @@ __device__ __forceinline__ void finish_rows(const TreeAttn& p, int s, const int 
 // Every wave on its own: NG groups of 16 query rows (row n of a KV head is
 // window row n / G, head n % G of its group) and a share of the key tiles,
 // straight from the cache into registers; the next tile's keys are on their
-// way under this one's softmax, its values under the next one's scores.
+// way under this one's softmax, its values under the next one's scores.  Shares
+// are equal numbers of tiles, wherever the sequences begin, so that ragged
+// lengths leave no wave idle; an item cut by shares is merged afterwards.
+//
+// What bounds it: single tokens over long caches, the cache (64 sequences of
+// 1k-8k, 4 of 16 heads, 294 MB: 70 us, 4.2 TB/s of the 5.2 that a copy
+// reaches); one sequence, latency: a wave's tiles one after the other, about
+// 0.9 us each, and the second launch (2000 keys: 14.9 us one row, 20 us 128);
+// fp32, the matrix instructions (32 sequences of 1k-4k, 64 rows: 162 us, half
+// their rate).
 // ---------------------------------------------------------------------------
 template <typename T, int D, int NG>
 __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
@@ -301,14 +411,15 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
   constexpr int KEYS = TL::KEYS, NP = D / 16, NQP = D / TL::NQ_DIV, DG = D / 16, NS = TL::NS;
   constexpr int PAGE_B = 16 * D * (int)sizeof(T);
   __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[4];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, quarter = lane >> 4;
   const int HN = p.Hkv * p.n_rt;
   const int share_id = xcd_block() * 4 + w, n_shares = gridDim.x * 4;
   int u = share_id, u_end = p.S * HN, share = 0;
+  SeqTiles seqs{};
   if (p.split) {
-    seq_tiles(p, KEYS, s_seq, s_len, s_tot);
-    const int U = s_seq[p.S] * HN;
+    seqs = seq_tiles(p, KEYS, s_seq, s_len, s_tot);
+    const int U = seqs.total * HN;
     share = max((U + n_shares - 1) / n_shares, p.share_min);
     u = min((long long)share_id * share, (long long)U);
     u_end = min(u + share, U);
@@ -321,14 +432,14 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
   while (u < u_end) {
     int s, qi, j0, j1, tiles, k = 0, nseg = 1, L;
     if (p.split) {
-      s = find_seq(s_seq, p.S, u / HN);
-      L = s_len[s];
-      tiles = s_seq[s + 1] - s_seq[s];
-      const int local = u - s_seq[s] * HN;
-      qi = local / tiles;
-      j0 = local - qi * tiles;
+      s = __builtin_amdgcn_readfirstlane(seqs.find(u / HN));
+      L = seqs.length(s);
+      const int U0 = seqs.before(s) * HN;
+      tiles = seqs.before(s + 1) - seqs.before(s);
+      qi = (u - U0) / tiles;
+      j0 = u - U0 - qi * tiles;
       j1 = min(tiles, j0 + (u_end - u));
-      const int P0 = s_seq[s] * HN + qi * tiles;
+      const int P0 = U0 + qi * tiles;
       k = share_id - P0 / share;
       nseg = (P0 + tiles - 1) / share - P0 / share + 1;
       u += j1 - j0;
@@ -350,15 +461,9 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
     if (p.split && k == 0 && lane == 0) p.meta[it] = int2{nseg, share_id};
     const int n_valid = (L + p.R + 15) >> 4;
     const int32_t* pt = p.table + (size_t)s * p.max_pages;
-    // the ids of the next 64 pages, a lane each
-    auto page_ids = [&](int j) {
-      int id = pt[min(j * TL::PAGES + lane, n_valid - 1)];
-      if (id < 0 || id >= p.pool_pages) {
-        set_err(p.err, DVS_ERR_BAD_PAGE);
-        id = 0;
-      }
-      return id;
-    };
+    // the ids of the next 64 pages, a lane each (checked only when the queries'
+    // loads have gone out too)
+    auto page_ids = [&](int j) { return pt[min(j * TL::PAGES + lane, n_valid - 1)]; };
     int ids = page_ids(j0), ids_at = j0;
     // this lane's query rows
     int r[NG], h[NG];
@@ -406,6 +511,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) vf[i] = *(const u32x4*)(b + i * 256 * sizeof(T));
     };
+    ids = checked_page(p, ids);
     load_k(j0);
     load_v(j0);
     for (int j = j0; j < j1; ++j) {
@@ -436,49 +542,40 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
       // needed for nothing, the next one's are)
       if (more && (j + 2 - ids_at) * TL::PAGES > 64) {
         ids_at = j + 1;
-        ids = page_ids(ids_at);
+        ids = checked_page(p, page_ids(ids_at));
       }
       if (more) load_k(j + 1);
       const int key0 = j * KEYS + quarter * TL::NK;
       const bool masked = (j + 1) * KEYS > L;
+      uint32_t bits[NG];
       if (masked) {
-        uint32_t un = 0;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const uint32_t b = seen_bits<TL::NK>(p, mask[g], r[g], any[g], key0, L);
-          un |= b;
+          const uint32_t b = bits[g] = seen_bits<TL::NK>(p, mask[g], r[g], any[g], key0, L);
 #pragma unroll
           for (int i = 0; i < TL::NK; ++i)
             if (!(b >> i & 1)) sc[g][i >> 2][i & 3] = -INFINITY;
         }
-        // values that none of the wave's rows sees may be anything: zero
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) un |= __shfl_xor((int)un, off);
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(T) == 2)
-              vf[i][e] &= pair_mask(un, e);
-            else
-              vf[i][e] &= un >> e & 1 ? 0xffffffffu : 0u;
-          }
       }
-      f32x4 wt[NG][NS];
-      softmax_tile<NS, NG, DG>(sc, wt, p.scale_log2, m, l, o);
+      typename Weights<T>::type pf[NG];
+      softmax_tile<T, NS, NG, DG>(sc, pf, p.scale_log2, m, l, o);
+      if (masked)
+        clean_values<T>(vf, bits, o, [&](int key, int d) {
+          const int page = __builtin_amdgcn_readfirstlane(checked_page(p, pt[min(j * TL::PAGES + (key >> 4), n_valid - 1)]));
+          return (float)((const T*)vp)[((size_t)page * p.Hkv + kvh) * 16 * D + d * 16 + (key & 15)];
+        });
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         if constexpr (sizeof(T) == 2) {
-          const bf16x8 pf = weights_bf16(wt[g]);
 #pragma unroll
           for (int d = 0; d < DG; ++d)
-            o[g][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf, o[g][d], 0, 0, 0);
+            o[g][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf[g], o[g][d], 0, 0, 0);
         } else {
 #pragma unroll
           for (int d = 0; d < DG; ++d)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              o[g][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[d][e]), wt[g][0][e], o[g][d], 0, 0, 0);
+              o[g][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[d][e]), pf[g][e], o[g][d], 0, 0, 0);
         }
       }
       if (more) load_v(j + 1);
@@ -488,15 +585,24 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
 }
 
 // ---------------------------------------------------------------------------
-// Many query rows of a KV head (bf16): a workgroup of four waves, 32 rows each,
-// over 32-key tiles that all of them read from LDS.  A wave copies one page of
-// every tile, K (waves 0, 1) or V (2, 3), straight to LDS, STAGES - 1 tiles
-// ahead.  Row tiles of 128 rows take the same key range side by side on one
-// XCD (its L2 then gives the second reader what the first has fetched).
+// Many query rows of a KV head (bf16): a workgroup of NW waves, 32 rows each, over
+// 32-key tiles that all of them read from LDS, copied there straight from the
+// cache, STAGES tiles at a time.  The next tile's scores are made under this
+// tile's softmax (matrix and vector unit), then this tile's values are added.
+//
+// Up to 128 rows: four waves, two workgroups a CU; more: eight waves over 256
+// rows, whose tiles go through LDS once where two workgroups would each copy
+// them (long documents 460 -> 441 us).
+//
+// What bounds it, long documents (256 rows, 1.44 GB, 0.36 PFLOP): the copies alone
+// take 253 us and the arithmetic alone 309, but with both at once the clock
+// falls from 2.4 to 1.9 GHz and the whole takes 445.  Taking the softmax and the
+// products in turns by two halves of the waves, 32x32 products, reads ahead of
+// their use and 64 rows a wave were all tried: 442 - 530.
 //
 // LDS rows of K (a key, 2 D bytes) have their 16-byte chunks permuted so that
-// the 16 keys of one product, read at the same chunk, lie in 16 different bank
-// groups; in V (an element of the head, 32 bytes a page) the two halves swap.
+// the 16 lanes that an access of 16 bytes serves at once (0-3, 12-15, 20-27 of
+// 32, or the others) lie in 16 different bank groups; V needs no such order.
 // The stages are variables of their own and the loop over them is unrolled:
 // the compiler then knows that a read of one does not touch the copies on
 // their way into the others, and does not wait for those.
@@ -504,10 +610,9 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
 template <int D>
 __device__ __forceinline__ int k_swizzle(int row) {
   if constexpr (D == 128) return (row & 3) | ((row >> 1) & 12);
-  else if constexpr (D == 96) return (row >> 3) & 3;
+  else if constexpr (D == 96) return ((row >> 2) & 2) ^ (((row >> 4) & 1) * 3);
   else return ((row >> 1) & 1) | ((row >> 2) & 6);
 }
-__device__ __forceinline__ int v_swizzle(int d) { return ((d >> 2) ^ (d >> 3)) & 1; }
 
 template <int N>
 __device__ __forceinline__ void wait_loads() {   // at most N vector loads on their way
@@ -515,35 +620,45 @@ __device__ __forceinline__ void wait_loads() {   // at most N vector loads on th
   __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
 }
 
-template <int D>
-__global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttn p) {
-  constexpr int KEYS = 32, NG = 2, DG = D / 16, STAGES = 4;
+__device__ __forceinline__ void barrier() {   // without a wait for this wave's loads
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int D, int NW>
+__global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) {
+  constexpr int KEYS = 32, NG = 2, DG = D / 16, STAGES = NW == 8 ? 6 : 4;
   constexpr int PAGE_B = 32 * D, TILE_B = 2 * PAGE_B;   // bytes of a page, of a tile's K (or V)
-  constexpr int NPL = PAGE_B / 1024;                    // copies of a wave a tile
+  constexpr int SEGS = PAGE_B / 1024;                   // copies of 1 KB a page
+  constexpr int NPL = 4 * SEGS / NW;                    // of a wave a tile: all of one page, or a part
+  static_assert(4 * SEGS % NW == 0 && SEGS % NPL == 0, "copies");
   constexpr int STAGE_B = 2 * TILE_B;
-  __shared__ __attribute__((aligned(1024))) char st0[STAGE_B], st1[STAGE_B], st2[STAGE_B], st3[STAGE_B];
+  __shared__ __attribute__((aligned(1024))) char st0[STAGE_B], st1[STAGE_B], st2[STAGE_B], st3[STAGE_B],
+      st4[STAGES > 4 ? STAGE_B : 16], st5[STAGES > 4 ? STAGE_B : 16];
   __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[4];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, quarter = lane >> 4;
   const int block = xcd_block(), n_shares = gridDim.x / p.n_wide;
   const int share_id = block / p.n_wide, rt = block - share_id * p.n_wide;
-  seq_tiles(p, KEYS, s_seq, s_len, s_tot);
-  const int U = s_seq[p.S] * p.Hkv;
+  const SeqTiles seqs = seq_tiles(p, KEYS, s_seq, s_len, s_tot);
+  const int U = seqs.total * p.Hkv;
   const int share = max((U + n_shares - 1) / n_shares, p.share_min);
   int u = (int)min((long long)share_id * share, (long long)U);
   const int u_end = min(u + share, U);
-  // copies: lane's source offset in the page, of its 16 bytes of each 1 KB
-  const char* pool = (const char*)(w < 2 ? p.k_pool : p.v_pool);
+  // copies: pages 0, 1 of K, then of V; lane's source offset in the page, of
+  // its 16 bytes of each 1 KB
+  const int cpage = w * NPL / SEGS, cseg = w * NPL % SEGS;
+  const char* pool = (const char*)(cpage < 2 ? p.k_pool : p.v_pool);
   uint32_t soff[NPL];
 #pragma unroll
   for (int i = 0; i < NPL; ++i) {
-    const int off = i * 1024 + lane * 16;
-    if (w < 2) {
+    const int off = (cseg + i) * 1024 + lane * 16;
+    if (cpage < 2) {
       const int row = off / (2 * D), c = (off - row * 2 * D) >> 4;
-      soff[i] = row * 2 * D + ((c ^ k_swizzle<D>((w & 1) * 16 + row)) << 4);
+      soff[i] = row * 2 * D + ((c ^ k_swizzle<D>(cpage * 16 + row)) << 4);
     } else {
-      const int d = off >> 5;
-      soff[i] = d * 32 + ((((off >> 4) & 1) ^ v_swizzle(d)) << 4);
+      soff[i] = off;
     }
   }
   // fragments: K of product t = 0 (t = 1: four rows on), chunk ks * 4 + quarter
@@ -551,33 +666,26 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttn p) {
   int kfrag[D / 32];
 #pragma unroll
   for (int ks = 0; ks < D / 32; ++ks) kfrag[ks] = krow * 2 * D + (((ks * 4 + quarter) ^ ksw) << 4);
-  const int vfrag = TILE_B + (quarter >> 1) * PAGE_B + m16 * 32 + (((quarter & 1) ^ v_swizzle(m16)) << 4);
+  const int vfrag = TILE_B + (quarter >> 1) * PAGE_B + m16 * 32 + ((quarter & 1) << 4);
   bool again = false;
 
   while (u < u_end) {
-    const int s = __builtin_amdgcn_readfirstlane(find_seq(s_seq, p.S, u / p.Hkv));
-    const int L = __builtin_amdgcn_readfirstlane(s_len[s]);
-    const int tiles = s_seq[s + 1] - s_seq[s];
-    const int local = u - s_seq[s] * p.Hkv;
-    const int kvh = local / tiles, j0 = local - kvh * tiles, j1 = min(tiles, j0 + (u_end - u));
-    const int P0 = s_seq[s] * p.Hkv + kvh * tiles;
+    const int s = __builtin_amdgcn_readfirstlane(seqs.find(u / p.Hkv));
+    const int L = __builtin_amdgcn_readfirstlane(seqs.length(s));
+    const int U0 = __builtin_amdgcn_readfirstlane(seqs.before(s)) * p.Hkv;
+    const int tiles = __builtin_amdgcn_readfirstlane(seqs.before(s + 1)) - U0 / p.Hkv;
+    const int kvh = (u - U0) / tiles, j0 = u - U0 - kvh * tiles, j1 = min(tiles, j0 + (u_end - u));
+    const int P0 = U0 + kvh * tiles;
     const int k = share_id - P0 / share, nseg = (P0 + tiles - 1) / share - P0 / share + 1;
     u += j1 - j0;
-    const int sub = rt * 4 + w;                         // this wave's 32 rows of the item
-    const bool work = sub * 32 < p.rows;
+    const int sub = rt * NW + w;                         // this wave's 32 rows of the item
+    const bool work = sub * NG * 16 < p.rows;
     const int it = (s * p.Hkv + kvh) * p.n_rt + sub;
-    if (work && k == 0 && lane == 0) p.meta[it] = int2{nseg, (share_id * p.n_wide + rt) * 4 + w};
+    if (work && k == 0 && lane == 0) p.meta[it] = int2{nseg, (share_id * p.n_wide + rt) * NW + w};
     const int n_valid = (L + p.R + 15) >> 4;
     const int32_t* pt = p.table + (size_t)s * p.max_pages;
     // the wave's page of the next 64 tiles, a lane each
-    auto page_ids = [&](int j) {
-      int id = pt[min((j + lane) * 2 + (w & 1), n_valid - 1)];
-      if (id < 0 || id >= p.pool_pages) {
-        set_err(p.err, DVS_ERR_BAD_PAGE);
-        id = 0;
-      }
-      return id;
-    };
+    auto page_ids = [&](int j) { return pt[min((j + lane) * 2 + (cpage & 1), n_valid - 1)]; };
     int ids = page_ids(j0), ids_at = j0;
     int r[NG], h[NG];
     bool valid[NG], any[NG];
@@ -603,6 +711,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttn p) {
     for (int g = 0; g < NG; ++g)
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) asm volatile("" : "+v"(q[g][i]));
+    ids = checked_page(p, ids);
     asm volatile("" : "+v"(ids));
     f32x4 o[NG][DG];
     float m[NG], l[NG];
@@ -618,28 +727,17 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttn p) {
     auto issue = [&](char* stage, int j) {
       if (j - ids_at >= 64) {
         ids_at = j;
-        ids = page_ids(j);
+        ids = checked_page(p, page_ids(j));
       }
       const int id = __builtin_amdgcn_readlane(ids, j - ids_at);
       const char* base = pool + ((size_t)(uint32_t)id * p.Hkv + kvh) * PAGE_B;
-      char* to = stage + w * PAGE_B;
+      char* to = stage + (w * NPL) * 1024;
 #pragma unroll
       for (int i = 0; i < NPL; ++i)
         __builtin_amdgcn_global_load_lds((const void*)(base + soff[i]),
                                          (__attribute__((address_space(3))) void*)(to + i * 1024), 16, 0, 0);
     };
-    // Tile j, in `tile`: this wave's copies of it have arrived (those of later
-    // tiles may be on their way), then everybody's; the stage that the tile
-    // before left free takes tile j + STAGES - 1.
-    auto step = [&](auto masked, char* tile, char* next, int j) {
-      constexpr bool MASKED = decltype(masked)::value != 0;
-      if (j + STAGES - 1 <= j1) wait_loads<(STAGES - 2) * NPL>();
-      else if (j + 1 < j1) wait_loads<NPL>();
-      else wait_loads<0>();
-      __builtin_amdgcn_s_barrier();
-      if (j + STAGES - 1 < j1) issue(next, j + STAGES - 1);
-      if (!work) return;
-      f32x4 sc[NG][2], wt[NG][2];
+    auto scores = [&](const char* tile, f32x4 (&sc)[NG][2]) {
 #pragma unroll
       for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -653,34 +751,50 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttn p) {
           for (int g = 0; g < NG; ++g)
             sc[g][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, q[g][ks]), sc[g][t], 0, 0, 0);
         }
-      uint32_t un = 0;
+    };
+    // Step j: the next tile's scores into `nxt` under this tile's softmax (`cur`
+    // holds its scores), then this tile's values.  At its start the next
+    // tile's copies are awaited, this wave's and by the barrier everybody's,
+    // and the stage of the tile before this one, which every wave is past,
+    // takes tile j + STAGES - 1.
+    auto step = [&](auto masked, auto last, const char* tile, const char* next, char* free, int j,
+                    f32x4 (&cur)[NG][2], f32x4 (&nxt)[NG][2]) {
+      constexpr bool MASKED = decltype(masked)::value != 0, LAST = decltype(last)::value != 0;
+      if constexpr (!LAST) {
+        if (j + STAGES - 2 < j1) wait_loads<(STAGES - 3) * NPL>();
+        else if (STAGES > 4 && j + 3 < j1) wait_loads<2 * NPL>();
+        else if (STAGES > 4 && j + 2 < j1) wait_loads<NPL>();
+        else wait_loads<0>();
+        barrier();
+        if (j + STAGES - 1 < j1) issue(free, j + STAGES - 1);
+      }
+      if (!work) return;
+      uint32_t bits[NG];
       if constexpr (MASKED) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const uint32_t b = seen_bits<8>(p, mask[g], r[g], any[g], j * KEYS + quarter * 8, L);
-          un |= b;
+          const uint32_t b = bits[g] = seen_bits<8>(p, mask[g], r[g], any[g], j * KEYS + quarter * 8, L);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            if (!(b >> i & 1)) sc[g][i >> 2][i & 3] = -INFINITY;
+            if (!(b >> i & 1)) cur[g][i >> 2][i & 3] = -INFINITY;
         }
-        // values that none of the wave's rows sees may be anything: zero
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) un |= __shfl_xor((int)un, off);
       }
-      softmax_tile<2, NG, DG>(sc, wt, p.scale_log2, m, l, o);
-      bf16x8 pf[NG];
+      if constexpr (!LAST) scores(next, nxt);
+      // the values' reads are on their way under the softmax
+      u32x4 vf[DG];
 #pragma unroll
-      for (int g = 0; g < NG; ++g) pf[g] = weights_bf16(wt[g]);
+      for (int d = 0; d < DG; ++d) vf[d] = *(const u32x4*)(tile + vfrag + d * 512);
+      bf16x8 pf[NG];
+      softmax_tile<__bf16, 2, NG, DG>(cur, pf, p.scale_log2, m, l, o);
+      if constexpr (MASKED)
+        clean_values<__bf16>(vf, bits, o, [&](int key, int d) {
+          return (float)*(const __bf16*)(tile + TILE_B + (key >> 4) * PAGE_B + d * 32 + (key & 15) * 2);
+        });
 #pragma unroll
       for (int d = 0; d < DG; ++d) {
-        u32x4 vf = *(const u32x4*)(tile + vfrag + d * 512);
-        if constexpr (MASKED) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) vf[e] &= pair_mask(un, e);
-        }
 #pragma unroll
         for (int g = 0; g < NG; ++g)
-          o[g][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf[g], o[g][d], 0, 0, 0);
+          o[g][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[d]), pf[g], o[g][d], 0, 0, 0);
       }
     };
     auto stage = [&](auto c) -> char* {
@@ -688,34 +802,60 @@ __global__ void __launch_bounds__(256, 2) tree_attn_tile_kernel(TreeAttn p) {
       if constexpr (I == 0) return st0;
       else if constexpr (I == 1) return st1;
       else if constexpr (I == 2) return st2;
-      else return st3;
+      else if constexpr (I == 3) return st3;
+      else if constexpr (I == 4) return st4;
+      else return st5;
     };
     static_for<0, STAGES - 1>([&](auto c) {
       if (j0 + decltype(c)::value < j1) issue(stage(c), j0 + decltype(c)::value);
     });
-    // tiles below L, then the few that reach the window
-    const int jm = max(j0, min(j1, L / KEYS));
+    if (j0 + STAGES - 2 < j1) wait_loads<(STAGES - 2) * NPL>();
+    else if (STAGES > 4 && j0 + 3 < j1) wait_loads<3 * NPL>();
+    else if (j0 + 2 < j1) wait_loads<2 * NPL>();
+    else if (j0 + 1 < j1) wait_loads<NPL>();
+    else wait_loads<0>();
+    barrier();
+    f32x4 sa[NG][2], sb[NG][2];
+    if (work) scores(st0, sa);
+    // steps below L whose tile is not the last, then those that reach the window
+    const int jm = max(j0, min(j1 - 1, L / KEYS));
     for (int j = j0; j < jm; j += STAGES)
       static_for<0, STAGES>([&](auto c) {
         constexpr int C = decltype(c)::value;
-        if (j + C < jm) step(IC<0>{}, stage(c), stage(IC<C + STAGES - 1>{}), j + C);
+        if (j + C < jm) {
+          if constexpr (C % 2 == 0) step(IC<0>{}, IC<0>{}, stage(c), stage(IC<C + 1>{}), stage(IC<C + STAGES - 1>{}), j + C, sa, sb);
+          else step(IC<0>{}, IC<0>{}, stage(c), stage(IC<C + 1>{}), stage(IC<C + STAGES - 1>{}), j + C, sb, sa);
+        }
       });
-    for (int j = jm; j < j1; ++j) {
+    auto at = [&](int j) {
       const int i = (j - j0) % STAGES;
-      char* at = i == 0 ? st0 : i == 1 ? st1 : i == 2 ? st2 : st3;
-      char* free = i == 0 ? st3 : i == 1 ? st0 : i == 2 ? st1 : st2;
-      step(IC<1>{}, at, free, j);
+      return i == 0 ? st0 : i == 1 ? st1 : i == 2 ? st2 : i == 3 ? st3 : i == 4 ? st4 : st5;
+    };
+    if ((jm - j0) & 1) {
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) sa[g][t] = sb[g][t];
     }
+    for (int j = jm; j + 1 < j1; ++j) {
+      step(IC<1>{}, IC<0>{}, at(j), at(j + 1), at(j + STAGES - 1), j, sa, sb);
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) sa[g][t] = sb[g][t];
+    }
+    step(IC<1>{}, IC<1>{}, at(j1 - 1), st0, st0, j1 - 1, sa, sb);
     if (!work) continue;
-    const size_t slot = (size_t)((share_id * p.n_wide + rt) * 4 + w) * 2 + (k == 0 ? 1 : 0);
+    const size_t slot = (size_t)((share_id * p.n_wide + rt) * NW + w) * 2 + (k == 0 ? 1 : 0);
     finish_rows<__bf16, D, NG>(p, s, r, h, valid, any, m, l, o, nseg, slot);
   }
 }
 
 // The segments of a split item, in their order: a wave a (group of 16 rows, NQ
 // times 16 elements of the head), SB segments on their way at a time.  Few items:
-// more waves and more segments at a time; many: fewer and longer ones (2048 items
-// of two segments, 128 wide: 33 us with one piece a wave, XXX with all eight).
+// more waves and more segments at a time; many: fewer and longer ones (pieces and
+// segments at a time, whole calls: long documents 1, 8 460 us; 8, 2 450; 4, 4 445;
+// serving 97.0, 96.7 and 94.4).
 template <typename T, int D, int NG, int NQ, int SB>
 __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
   constexpr int DG = D / 16, PER = NG * DG / NQ;
@@ -731,7 +871,7 @@ __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
   const int nseg = mt.x, first = mt.y;
   if (nseg <= 1) return;
   const int n = (rt * NG + g) * 16 + m16;
-  const int step = p.n_wide ? p.n_wide * 4 : 1;   // from a share's slot to the next one's
+  const int step = p.n_wide ? p.n_wide * p.wide_waves : 1;   // from a share's slot to the next one's
   auto slot = [&](int c) { return (size_t)(first + c * step) * 2 + (c == 0 ? 1 : 0); };
   auto ml_of = [&](int c) { return *(const f32x2*)(p.part_ml + ((slot(c) * NG + g) * 16 + m16) * 2); };
   f32x4 acc[NQ];
@@ -779,36 +919,57 @@ __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
 }
 
 struct TreePlan {
-  int ng, n_rt, n_wide, grid, split, share_min, seqs;   // seqs: sequences a launch takes
+  int ng, n_rt, n_wide, waves, grid, split, share_min, seqs;   // seqs: sequences a launch takes
   size_t off_ml, off_o, bytes;
 };
+
+constexpr long long MAX_ROWS = 1 << 20;   // query rows of a sequence, all heads
+
+static bool tree_fits(int R, int Hq, int max_pages) {   // what the kernels count in 32 bits
+  return (long long)R * Hq <= MAX_ROWS && (long long)R * Hq * max_pages < (1LL << 30);
+}
 
 static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, int dtype) {
   TreePlan pl{};
   const int rows = R * (Hq / Hkv);
   const int keys = dtype == DVS_BF16 ? Tile<__bf16>::KEYS : Tile<float>::KEYS;
-  const int max_tiles = (max_pages * DVS_PAGE_SIZE + keys - 1) / keys;
-  pl.ng = rows > 16 ? 2 : 1;
+  const int max_tiles = (int)(((long long)max_pages * DVS_PAGE_SIZE + keys - 1) / keys);
+  const int cus = device_cus();
+  // Two groups of 16 rows a wave read half the bytes a row.  fp32, whose products
+  // take long, only where every wave still has its 8 tiles (one / two groups, us:
+  // 128 rows, one sequence of 2048 30.1 / 33.8; 64 rows, 32 of 1k-4k 213 / 162).
+  pl.ng = rows > 16 && (dtype == DVS_BF16 || (long long)std::min(S, MAX_SEQS) * Hkv * ((rows + 31) / 32) * max_tiles >=
+                                                 8LL * 8 * cus) ? 2 : 1;
+  pl.waves = 4;
   pl.n_rt = (rows + pl.ng * 16 - 1) / (pl.ng * 16);
   const long long per_seq = (long long)Hkv * pl.n_rt * max_tiles;
-  pl.seqs = (int)std::max<long long>(1, std::min<long long>(std::min(S, MAX_SEQS), (1LL << 30) / per_seq));
+  pl.seqs = (int)std::max<long long>(1, std::min<long long>({S, MAX_SEQS, (1LL << 30) / per_seq,
+                                                             (1LL << 22) / ((long long)Hkv * pl.n_rt)}));
   const long long items = (long long)pl.seqs * Hkv * pl.n_rt;
-  const int cus = device_cus();
-  const long long kv_tiles = (long long)pl.seqs * Hkv * max_tiles;
-  if (dtype == DVS_BF16 && rows > TILE_ROWS && kv_tiles >= TILE_MIN_TILES) {
-    pl.n_wide = (rows + 127) / 128;
+  // Tiles of a share, at least: a part that is published costs as much as a few
+  // tiles, and the merge grows with the parts of an item; short caches are done
+  // sooner in smaller ones (128 rows, us, 4 / 8 tiles: 100 - 400 keys 21.7 / 24.7,
+  // one sequence of 16000 44.1 / 33.8; one row, 16000 keys: 32.5 / 27.4).
+  if (dtype == DVS_BF16 && rows > TILE_ROWS) {
+    // (waves on their own, us, against tiles in LDS: 64 rows, 32 sequences of
+    // 1k-8k 109 / 82; 128 rows, one of 2048 20.7 / 20.1; 60 rows, 16 of 1k-4k 34.9
+    // / 31.5)
+    pl.waves = rows > 128 && D != 96 ? 8 : 4;
+    pl.n_wide = (pl.n_rt + pl.waves - 1) / pl.waves;
     pl.split = 1;
-    pl.share_min = TILE_SHARE;
-    const long long shares = std::min<long long>(std::max(1, 2 * cus / pl.n_wide), (kv_tiles + TILE_SHARE - 1) / TILE_SHARE);
+    pl.share_min = max_tiles <= 32 ? 4 : std::max(8, max_tiles / 64);
+    const long long tiles = (long long)pl.seqs * Hkv * max_tiles;
+    const long long shares = std::min<long long>(std::max(1, (pl.waves == 8 ? 1 : 2) * cus / pl.n_wide),
+                                                 (tiles + pl.share_min - 1) / pl.share_min);
     pl.grid = (int)(shares * pl.n_wide);
   } else {
-    pl.split = max_tiles > WAVE_WHOLE;
-    pl.share_min = WAVE_SHARE;
+    pl.split = max_tiles > WHOLE_TILES;
+    pl.share_min = std::max(4, max_tiles / 64);
     const long long tiles = items * max_tiles;
-    pl.grid = (int)std::min<long long>(2 * cus, ((pl.split ? (tiles + WAVE_SHARE - 1) / WAVE_SHARE : items) + 3) / 4);
+    pl.grid = (int)std::min<long long>(2 * cus, ((pl.split ? (tiles + pl.share_min - 1) / pl.share_min : items) + 3) / 4);
   }
   if (pl.split) {
-    const size_t slots = (size_t)pl.grid * 4 * 2;
+    const size_t slots = (size_t)pl.grid * pl.waves * 2;
     pl.off_ml = al256((size_t)items * sizeof(int2));
     pl.off_o = pl.off_ml + al256(slots * pl.ng * 16 * 2 * sizeof(float));
     pl.bytes = pl.off_o + slots * pl.ng * 16 * D * sizeof(float);
@@ -820,20 +981,25 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
 
 template <typename T, int D, int NG>
 static void launch_merge(long long groups, const TreeAttn& p, hipStream_t st) {
+  constexpr int MANY = D == 96 ? 3 : 4;
   if (groups < MERGE_FEW)
     hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, NG, 1, 8>), dim3((unsigned)((groups * (D / 16) + 3) / 4)), dim3(256), 0, st, p);
   else
-    hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, NG, D / 16, 2>), dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((tree_attn_merge_kernel<T, D, NG, MANY, 4>), dim3((unsigned)((groups * (D / 16 / MANY) + 3) / 4)), dim3(256), 0, st, p);
 }
 
 template <typename T, int D>
 static void launch_tree(const TreePlan& pl, const TreeAttn& p, hipStream_t st) {
   if (pl.n_wide) {
-    if constexpr (sizeof(T) == 2) hipLaunchKernelGGL(tree_attn_tile_kernel<D>, dim3(pl.grid), dim3(256), 0, st, p);
-  } else if (pl.ng == 2) {
-    hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 2>), dim3(pl.grid), dim3(256), 0, st, p);
+    if constexpr (sizeof(T) == 2) {
+      // (a page of 96-wide heads is three copies, which eight waves cannot share evenly)
+      if constexpr (D != 96)
+        if (pl.waves == 8) hipLaunchKernelGGL((tree_attn_tile_kernel<D, 8>), dim3(pl.grid), dim3(512), 0, st, p);
+      if (pl.waves == 4) hipLaunchKernelGGL((tree_attn_tile_kernel<D, 4>), dim3(pl.grid), dim3(256), 0, st, p);
+    }
   } else {
-    hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 1>), dim3(pl.grid), dim3(256), 0, st, p);
+    if (pl.ng == 2) hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 2>), dim3(pl.grid), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 1>), dim3(pl.grid), dim3(256), 0, st, p);
   }
   if (!pl.split) return;
   const long long groups = (long long)p.S * p.Hkv * p.n_rt * pl.ng;
@@ -848,7 +1014,8 @@ using namespace dvs;
 extern "C" size_t dvs_tree_workspace_bytes(int32_t S, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
                                            int32_t max_pages, int32_t dtype) {
   if (S < 1 || R < 1 || R > 1024 || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 ||
-      (D != 64 && D != 96 && D != 128) || max_pages < 1 || (dtype != DVS_F32 && dtype != DVS_BF16))
+      (D != 64 && D != 96 && D != 128) || max_pages < 1 || (dtype != DVS_F32 && dtype != DVS_BF16) ||
+      !tree_fits(R, Hq, max_pages))
     return 0;
   return tree_plan(S, R, Hq, Hkv, D, max_pages, dtype).bytes;
 }
@@ -869,17 +1036,17 @@ extern "C" int attn_tree(const void* q, const void* k_pool, const void* v_pool,
   DVS_CHECK_SUPPORTED(D == 64 || D == 96 || D == 128, "attn_tree: head_dim %d", D);
   DVS_CHECK_ARG((((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_pool | (uintptr_t)v_pool) & 15) == 0,
                 "attn_tree: q, out and the pools must start on 16 bytes");
+  DVS_CHECK_SUPPORTED(tree_fits(R, Hq, max_pages), "attn_tree: R * Hq must be at most 2^20, its product with max_pages below 2^30");
   const TreePlan pl = tree_plan(S, R, Hq, Hkv, D, max_pages, dtype);
   if (!workspace || ws_bytes < pl.bytes) {
     set_error("attn_tree: workspace needs %zu bytes, got %zu", pl.bytes, ws_bytes);
     return DVS_EWORKSPACE;
   }
-  DVS_CHECK_SUPPORTED((long long)Hkv * pl.n_rt * max_pages < (1LL << 30), "attn_tree: too many pages");
   TreeAttn p{};
   p.k_pool = k_pool; p.v_pool = v_pool; p.err = err_word;
   p.R = R; p.W = (R + 31) / 32; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.rows = R * p.G;
   p.n_rt = pl.n_rt; p.max_pages = max_pages; p.pool_pages = num_pool_pages;
-  p.n_wide = pl.n_wide; p.split = pl.split; p.share_min = pl.share_min;
+  p.n_wide = pl.n_wide; p.wide_waves = pl.waves; p.split = pl.split; p.share_min = pl.share_min;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
   p.meta = (int2*)workspace;
   p.part_ml = (float*)((char*)workspace + pl.off_ml);

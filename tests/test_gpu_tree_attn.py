@@ -107,6 +107,81 @@ def test_flat_and_peaked_scores(dtype, spread):
     run(case, dtype, vis, i32(ot.words(vis)), spread=spread)
 
 
+# more query rows than a wave, a workgroup and a CU's two workgroups take, over several tiles, a
+# share that ends inside an item, and tables from a few pages to many
+@pytest.mark.parametrize("case", [
+    ([1500, 90], 33, 4, 4, 64), ([2100, 31, 700], 40, 8, 2, 64), ([1030, 1029], 64, 8, 2, 128),
+    ([900, 2000], 36, 16, 4, 96), ([640, 1300, 5], 70, 16, 4, 128), ([777], 130, 4, 2, 96),
+    ([50, 1, 0], 140, 4, 1, 64), ([1999, 64], 65, 8, 2, 128), ([96], 300, 4, 2, 128),
+    ([127, 128, 129], 40, 2, 1, 128)],
+    ids=lambda c: f"L{c[0][0]}x{len(c[0])}R{c[1]}H{c[2]}-{c[3]}D{c[4]}")
+def test_many_rows(case):
+    lens, R = case[:2]
+    vis, _, _ = ot.masks(random_parents(np.random.default_rng(R), len(lens), R))
+    run(case, "bf16", vis, i32(ot.words(vis)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", [([40, 7], 9, 4, 2, 64), ([100, 31], 20, 4, 2, 128),
+                                  ([70, 300], 30, 8, 2, 96), ([33], 40, 16, 2, 128)],
+                         ids=lambda c: f"R{c[1]}H{c[2]}-{c[3]}D{c[4]}")
+def test_rows_that_see_what_is_not_finite_and_rows_that_do_not(case, dtype):
+    """A drafted token's infinite or NaN value reaches its own row and its descendants', in the
+    elements that have it; the other rows' results stay the bits that they are without it."""
+    lens, R, Hq, Hkv, D = case
+    S = len(lens)
+    rng = np.random.default_rng(R)
+    parent = random_parents(rng, S, R)
+    vis, _, _ = ot.masks(parent)
+    st, k, v = cache(R, lens, R, Hkv, D, dtype)
+    q = dev(rounded(rng.standard_normal((S, R, Hq, D)), dtype), dtype)
+    bad = v.copy()
+    planted = []
+    for s, L in enumerate(lens):
+        for what, r, hk, d in ((np.inf, R // 3, 0, 1), (-np.inf, R // 2, Hkv - 1, D - 1),
+                               (np.nan, R - 1, 0, D // 2 + 3), (-np.inf, R // 3, 0, 5)):
+            bad[st.page_table[s, (L + r) // 16], hk, d, (L + r) % 16] = what
+            planted.append((s, r, hk, d, what))
+    words, scale = dvs.tree_masks(i32(parent))[0], 1 / math.sqrt(D)
+    args = i32(st.page_table), i32(st.kv_len), words, scale
+    want = to_f64(dvs.attn_tree(q, dev(k, dtype), dev(v, dtype), *args)).copy()
+    got = to_f64(dvs.attn_tree(q, dev(k, dtype), dev(bad, dtype), *args))
+    G = Hq // Hkv
+    hit = np.zeros(want.shape, bool)
+    for s, r, hk, d, what in planted:
+        for row in np.flatnonzero(vis[s, :, r]):
+            at = (s, row, slice(hk * G, hk * G + G), d)
+            assert np.all(np.isnan(got[at]) if np.isnan(what) else got[at] == what), (at, what)
+            hit[at] = True
+    assert np.array_equal(got[~hit], want[~hit])
+
+
+def test_fp32_batches_that_give_every_wave_two_groups():
+    rng = np.random.default_rng(2)
+    lens = [int(x) for x in rng.integers(0, 2000, 12)]
+    vis, _, _ = ot.masks(random_parents(rng, 12, 30))
+    run((lens, 30, 8, 4, 128), "f32", vis, i32(ot.words(vis)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_sequences_than_a_wave_has_lanes(dtype):
+    """The sequences' tiles are found in registers up to 64 of them, in LDS beyond."""
+    rng = np.random.default_rng(4)
+    lens = [int(x) for x in rng.integers(0, 300, 70)]
+    for R, Hq, Hkv in ((1, 4, 2), (40, 2, 2)):
+        vis, _, _ = ot.masks(random_parents(rng, 70, R))
+        run((lens, R, Hq, Hkv, 64), dtype, vis, i32(ot.words(vis)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_sequences_than_a_launch_takes(dtype):
+    """1030 sequences of a token or none, whose calls go out in two launches."""
+    lens = [i % 3 for i in range(1030)]
+    vis = np.ones((1030, 1, 1), bool)
+    vis[5::7] = False
+    run((lens, 1, 2, 1, 64), dtype, vis, i32(ot.words(vis)))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("R", [1, 9, 40])
 def test_long_ragged_batch(dtype, R):
