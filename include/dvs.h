@@ -714,7 +714,7 @@ int kv_compact(const dvs_state* st, int32_t* page_refs, const dvs_layer* layers,
  * tree_masks: mask_out [S, R, ceil(R / 32)]: bit j % 32 of word j / 32 of row
  *   r is set iff j is r or one of its ancestors (padding: no bit);
  *   depth_out [S, R] (may be NULL): ancestors of r (padding: -1).
- *   parent [S, R]; all int32.  Requirements: S >= 1, 1 <= R <= 1024, mask_out
+ *   parent [S, R]; all int32.  Requirements: 1 <= S < 2^22, 1 <= R <= 1024, mask_out
  *   on 8 bytes.
  * ---------------------------------------------------------------------- */
 int tree_masks(const int32_t* parent, int32_t S, int32_t R, int32_t* mask_out, int32_t* depth_out,

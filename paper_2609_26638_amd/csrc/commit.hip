@@ -30,6 +30,9 @@
 // finds its sequence's longest accepted prefix A (draft against the
 // verifier's top-1), then commits as above -- one launch for accept, commit
 // and rollback.
+//
+// accept_commit_tree's small steps do so as well: a wave accepts four trees, and
+// the threads of the first waves go on with the commit.
 #include "dvs_common.h"
 
 namespace dvs {
@@ -37,19 +40,19 @@ namespace dvs {
 constexpr int COMMIT_THREADS = 1024;
 constexpr int RUN_CHUNK = 8;
 
-__device__ __forceinline__ int block_exclusive_scan(int v, int* sh, int& total) {
+__device__ __forceinline__ int block_exclusive_scan(int v, int* sh, int threads, int& total) {
   // Hillis-Steele over the block in shared memory (S <= 1024; runs once).
   const int tid = threadIdx.x;
   sh[tid] = v;
   __syncthreads();
-  for (int off = 1; off < (int)blockDim.x; off <<= 1) {
+  for (int off = 1; off < threads; off <<= 1) {
     const int add = tid >= off ? sh[tid - off] : 0;
     __syncthreads();
     sh[tid] += add;
     __syncthreads();
   }
   const int incl = sh[tid];
-  total = sh[blockDim.x - 1];
+  total = sh[threads - 1];
   __syncthreads();
   return incl - v;
 }
@@ -94,7 +97,7 @@ __device__ __forceinline__ int run_token(const CommitParams& p, int s, int A, in
 constexpr int COMMIT_FAST_W = 32;
 
 template <bool FAST>
-__global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(CommitParams p) {
+__device__ __forceinline__ void commit_body(const CommitParams& p, int threads) {
   __shared__ int sh[COMMIT_THREADS];
   __shared__ int s_err;
   const int s = threadIdx.x;
@@ -216,8 +219,8 @@ __global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(CommitParams 
   const int push = live_seq && n > need ? n - need : 0;
   const int pop = live_seq && need > n ? need - n : 0;
   int tot_push = 0, tot_pop = 0;
-  const int push_off = block_exclusive_scan(push, sh, tot_push);
-  const int pop_off = block_exclusive_scan(pop, sh, tot_pop);
+  const int push_off = block_exclusive_scan(push, sh, threads, tot_push);
+  const int pop_off = block_exclusive_scan(pop, sh, threads, tot_pop);
   if (!FAST) top0 = *p.free_top;
   if (s == 0) {
     if (tot_pop > top0 + tot_push) atomicOr(&s_err, DVS_ERR_POOL_EXHAUSTED);
@@ -294,6 +297,79 @@ __global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(CommitParams 
   }
 }
 
+template <bool FAST>
+__global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(CommitParams p) {
+  commit_body<FAST>(p, blockDim.x);
+}
+
+// Trees of at most 64 rows, a row a lane, TREES of them a wave at a time.  The
+// accepted path is a 64-bit word: its rows rise, so that a row's place on it
+// is the number of bits below its own.
+constexpr int TREES = 4;
+
+__device__ __forceinline__ void accept_trees(const TreeCommit& t, int s0) {
+  const int lane = threadIdx.x & 63;
+  int p[TREES], token[TREES], top[TREES], L[TREES], fin[TREES];
+#pragma unroll
+  for (int i = 0; i < TREES; ++i) {
+    const int s = min(s0 + i, t.S - 1);
+    const size_t at = (size_t)s * t.R + min(lane, t.R - 1);
+    p[i] = t.parent[at];
+    token[i] = t.tokens[at];
+    top[i] = t.argmax[at];
+    L[i] = t.kv_len[s];
+    fin[i] = t.finished[s];
+  }
+#pragma unroll
+  for (int i = 0; i < TREES; ++i) {
+    const int s = s0 + i;
+    if (s >= t.S) break;
+    const bool child = p[i] >= 0 && p[i] < lane && lane < t.R;
+    const bool match = token[i] == __shfl(top[i], child ? p[i] : 0) && child;
+    uint64_t path = 0;
+    if (fin[i] == 0 && __builtin_amdgcn_readfirstlane(p[i]) == -1) {
+      int row = 0;
+      for (;;) {
+        path |= 1ull << row;
+        const uint64_t next = __ballot(match && p[i] == row);
+        if (!next) break;
+        row = __ffsll((unsigned long long)next) - 1;   // above this one: it ends
+      }
+    }
+    const int len = __popcll(path);
+    const size_t base = (size_t)s * t.R;
+    if (lane == 0) {
+      t.accept[s] = max(len - 1, 0);
+      t.run_len[s] = len - 1;
+      t.old_len[s] = L[i];
+    }
+    if (path >> lane & 1) {
+      const int at = __popcll(path & ((1ull << lane) - 1));
+      t.path[base + at] = lane;
+      t.run[base + at] = top[i];
+    }
+    if (lane >= len && lane < t.R) {
+      t.path[base + lane] = -1;
+      t.run[base + lane] = 0;
+    }
+    if (lane < t.n_window_pages) {
+      const int pg = L[i] / DVS_PAGE_SIZE + lane;
+      int id = L[i] >= 0 && pg < t.max_pages ? t.table[(size_t)s * t.max_pages + pg] : -1;
+      if (id >= t.pool_pages) id = -1;
+      t.pages[(size_t)s * t.n_window_pages + lane] = id;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(COMMIT_THREADS) tree_commit_kernel(CommitParams p, TreeCommit t) {
+  accept_trees(t, (threadIdx.x >> 6) * TREES);
+  __threadfence_block();
+  __syncthreads();
+  const int threads = (p.S + 63) / 64 * 64;
+  if (__builtin_amdgcn_readfirstlane((int)threadIdx.x) >= threads) return;   // a whole wave
+  commit_body<false>(p, threads);
+}
+
 }  // namespace dvs
 
 using namespace dvs;
@@ -306,7 +382,7 @@ static int launch_commit(const char* who, int32_t S, int32_t n_causal, int32_t n
                          int32_t* free_top, int32_t num_pool_pages, int32_t* boundary,
                          int32_t* draft, int32_t draft_width, int32_t* out_tokens,
                          int32_t* out_count, int32_t max_new, int32_t eos_id, int32_t* finished,
-                         int32_t* err_word, void* stream, int32_t idle_below = INT32_MIN) {
+                         int32_t* err_word, void* stream, const TreeCommit* tree = nullptr) {
   DVS_CHECK_ARG(argmax && kv_len && page_table && num_pages && free_stack &&
                     free_top && boundary && out_tokens && out_count && finished,
                 "%s: NULL array argument", who);
@@ -328,7 +404,7 @@ static int launch_commit(const char* who, int32_t S, int32_t n_causal, int32_t n
                                      (n_mask == n_causal * draft_group && draft_group >= draft_width)),
                 "%s: mask rows must be n_causal groups of draft_group >= draft_width rows", who);
   p.accept_len = accept_len; p.accept_here = accept_here; p.accept_out = accept_out;
-  p.idle_below = idle_below;
+  p.idle_below = tree ? 0 : INT32_MIN;
   p.draft_group = draft_group;
   p.argmax = argmax; p.kv_len = kv_len; p.page_table = page_table;
   p.num_pages = num_pages; p.free_stack = free_stack; p.free_top = free_top;
@@ -339,7 +415,10 @@ static int launch_commit(const char* who, int32_t S, int32_t n_causal, int32_t n
   const int threads = ((S + 63) / 64) * 64;
   const bool fast = accept_here && !lead && draft_group == 0 && n_causal <= COMMIT_FAST_W &&
                     draft_width <= COMMIT_FAST_W;
-  if (fast)
+  if (tree && tree_accept_in_commit(*tree))
+    hipLaunchKernelGGL(tree_commit_kernel, dim3(1), dim3((S + TREES - 1) / TREES * 64), 0,
+                       (hipStream_t)stream, p, *tree);
+  else if (fast)
     hipLaunchKernelGGL(kv_commit_kernel<true>, dim3(1), dim3(threads), 0, (hipStream_t)stream, p);
   else
     hipLaunchKernelGGL(kv_commit_kernel<false>, dim3(1), dim3(threads), 0, (hipStream_t)stream, p);
@@ -351,13 +430,18 @@ namespace dvs {
 // accept_commit_tree: run[s, 0 .. run_len[s]] are the tokens that the accepted
 // path commits (both the run's drafts and its last token); run_len < 0: the
 // sequence has no tree this step.
-int commit_tree_run(const dvs_state* st, int R, const int32_t* run_len, const int32_t* run,
-                    void* stream) {
-  return launch_commit("accept_commit_tree", st->S, R, 0, R, nullptr, run_len, 0, nullptr, 0, run,
+int commit_tree_run(const dvs_state* st, const TreeCommit& t, void* stream) {
+  return launch_commit("accept_commit_tree", st->S, t.R, 0, t.R, nullptr, t.run_len, 0, nullptr, 0, t.run,
                        st->kv_len, st->page_table, st->num_pages, st->max_pages, st->free_stack,
-                       st->free_top, st->num_pool_pages, st->boundary, const_cast<int32_t*>(run), R,
+                       st->free_top, st->num_pool_pages, st->boundary, t.run, t.R,
                        st->out_tokens, st->out_count, st->max_new, st->eos_id, st->finished,
-                       st->err_word, stream, 0);
+                       st->err_word, stream, &t);
+}
+
+// 16 waves of 4 trees of up to 64 rows (whole calls, us: 8 sequences of 64 rows 18.4,
+// by two launches 21.2; 64 of 33 rows 18.3 and 21.2).
+bool tree_accept_in_commit(const TreeCommit& t) {
+  return t.R <= 64 && t.S <= COMMIT_THREADS / 64 * TREES;
 }
 
 }  // namespace dvs

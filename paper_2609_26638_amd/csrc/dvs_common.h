@@ -72,9 +72,16 @@ bool attn_chunk_ok(int chunk_keys);
 size_t attn_counter_bytes(int S, int R, int Hq, int Hkv, int D, int max_pages, int chunk_keys,
                           int dtype);
 
-// The commit of accept_commit_tree (commit.hip).
-int commit_tree_run(const dvs_state* st, int R, const int32_t* run_len, const int32_t* run,
-                    void* stream);
+// accept_commit_tree: a step's trees and what its launches hand on.
+struct TreeCommit {
+  int S, R, max_pages, pool_pages, n_window_pages;
+  const int32_t *parent, *tokens, *argmax, *kv_len, *table, *finished;
+  int32_t *accept, *path;                      // outputs (or workspace)
+  int32_t *run_len, *old_len, *pages, *run;    // workspace
+};
+// Whether the commit's launch accepts as well; the commit (commit.hip).
+bool tree_accept_in_commit(const TreeCommit& t);
+int commit_tree_run(const dvs_state* st, const TreeCommit& t, void* stream);
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));

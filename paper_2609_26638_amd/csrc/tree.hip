@@ -23,9 +23,8 @@ constexpr int TREE_MAX_ROWS = 1024;
 // lane.  Pointer doubling inside the wave (log2 64 rounds of mask(r) |=
 // mask(up r), up r = up(up r)) gives every row's ancestors among the 64 as one
 // 64-bit word; the topmost of them, its lowest bit, names the parent further
-// up by which the chain leaves the wave's rows.  The waves then finish in
-// order, 64 rows a step, each row taking over the words of that parent, which
-// an earlier wave has finished.
+// up by which the chain leaves the wave's rows.  With these in LDS a row goes up
+// its chain a block of 64 rows at a time, a word of its mask a block.
 // ---------------------------------------------------------------------------
 struct MaskRow {
   uint64_t in;   // ancestors among the wave's rows, itself among them
@@ -37,19 +36,24 @@ __device__ __forceinline__ uint64_t shfl64(uint64_t v, int src) {
   return (uint64_t)hi << 32 | lo;
 }
 
-// p: the row's parent, or below -1 for a row of the padding.
-__device__ __forceinline__ MaskRow wave_ancestors(int p, int first, int lane) {
-  uint64_t in = 1ull << lane;
-  int up = p >= first ? p - first : -1;
+// N blocks of 64 rows at a time, block i from row first + i * step.  p: the row's
+// parent, or below -1 for a row of the padding.
+template <int N>
+__device__ __forceinline__ void wave_ancestors(const int (&p)[N], int first, int step, int lane, MaskRow (&m)[N]) {
 #pragma unroll
-  for (int round = 0; round < 6; ++round) {
-    const int src = up >= 0 ? up : lane;
-    const uint64_t other = shfl64(in, src);
-    const int next = __shfl(up, src);
-    in |= other;
-    up = up >= 0 ? next : -1;
-  }
-  return MaskRow{in, __shfl(p, __ffsll((unsigned long long)in) - 1)};
+  for (int i = 0; i < N; ++i) m[i] = MaskRow{1ull << lane, p[i] >= first + i * step ? p[i] - first - i * step : -1};
+#pragma unroll
+  for (int round = 0; round < 6; ++round)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int src = m[i].up >= 0 ? m[i].up : lane;
+      const uint64_t other = shfl64(m[i].in, src);
+      const int next = __shfl(m[i].up, src);
+      m[i].in |= other;
+      m[i].up = m[i].up >= 0 ? next : -1;
+    }
+#pragma unroll
+  for (int i = 0; i < N; ++i) m[i].up = __shfl(p[i], __ffsll((unsigned long long)m[i].in) - 1);
 }
 
 // A row's parent as the kernels take it: a row that names itself or a later
@@ -70,9 +74,10 @@ __global__ void __launch_bounds__(256) tree_masks_small_kernel(const int32_t* __
                                                                int32_t* __restrict__ err) {
   const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (s >= S) return;
-  int p = -2;
-  if (lane < R) p = checked_parent(parent[(size_t)s * R + lane], lane, err);
-  const MaskRow m = wave_ancestors(p, 0, lane);
+  const int p[1] = {lane < R ? checked_parent(parent[(size_t)s * R + lane], lane, err) : -2};
+  MaskRow rows[1];
+  wave_ancestors(p, 0, 0, lane, rows);
+  const MaskRow m = rows[0];
   if (lane >= R) return;
   const bool in_tree = m.up == -1;
   const size_t at = (size_t)s * R + lane;
@@ -84,40 +89,82 @@ __global__ void __launch_bounds__(256) tree_masks_small_kernel(const int32_t* __
     mask[at] = (int32_t)(uint32_t)w;
 }
 
-// More rows: a workgroup a sequence, the masks in LDS.  Rows are 16 bytes more
-// than their words apart, which spreads the lanes' 16-byte accesses over the
-// banks.
-__global__ void __launch_bounds__(1024) tree_masks_kernel(const int32_t* __restrict__ parent, int R,
-                                                          int32_t* __restrict__ mask,
-                                                          int32_t* __restrict__ depth,
-                                                          int32_t* __restrict__ err) {
-  extern __shared__ __attribute__((aligned(16))) uint32_t rows_lds[];
-  const int W = (R + 31) / 32, W4 = (W + 3) / 4 * 4, ld = W4 + 4;
-  int* s_depth = (int*)(rows_lds + (size_t)R * ld);
-  const int s = blockIdx.x, r = threadIdx.x, lane = r & 63, first = r & ~63;
+// More rows, up to NB blocks of 64: a workgroup takes 256 of a sequence's, makes
+// the blocks up to its last row, then a wave its 64 rows' words, in registers,
+// which go out through LDS, side by side.  The words to write bound it (128
+// sequences of 1000 rows, 17 MB: 7.8 us; copied row by row from the parent's in 16
+// steps of a workgroup a sequence: 18.4).  The first words reach memory late, after
+// a chain of parents that is all latency.
+template <int NB>
+__global__ void __launch_bounds__(256) tree_masks_kernel(const int32_t* __restrict__ parent, int R,
+                                                         int parts, bool wide, int32_t* __restrict__ mask,
+                                                         int32_t* __restrict__ depth,
+                                                         int32_t* __restrict__ err) {
+  constexpr int LD = 2 * NB + 4;   // words of a staged row: 16 lanes' 16 bytes in 16 bank groups
+  __shared__ uint64_t s_in[NB * 64];
+  __shared__ int s_up[NB * 64];
+  __shared__ __attribute__((aligned(16))) uint32_t s_out[4][64 * LD];
+  const int s = blockIdx.x / parts, part = blockIdx.x - s * parts;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, W = (R + 31) / 32;
   const size_t base = (size_t)s * R;
-  int p = -2;
-  if (r < R) p = checked_parent(parent[base + r], r, err);
-  const MaskRow m = wave_ancestors(p, first, lane);
-  for (int f = 0; f < R; f += 64) {
-    if (f == first && r < R) {
-      int d = -1;
-      if (m.up == -1) d = 0;
-      else if (m.up >= 0) d = s_depth[m.up] < 0 ? -1 : s_depth[m.up] + 1;
-      if (d >= 0) d += __popcll(m.in) - 1;
-      s_depth[r] = d;
-      uint32_t* row = rows_lds + (size_t)r * ld;
-      const uint32_t* over = m.up >= 0 && d >= 0 ? rows_lds + (size_t)m.up * ld : nullptr;
-      for (int w = 0; w < W4; w += 4)
-        *(u32x4*)(row + w) = over && w < first / 32 ? *(const u32x4*)(over + w) : u32x4{0, 0, 0, 0};
-      if (d >= 0) *(u32x2*)(row + first / 32) = u32x2{(uint32_t)m.in, (uint32_t)(m.in >> 32)};
-    }
-    __syncthreads();
+  const int blocks = min((R + 63) / 64, part * 4 + 4);
+  constexpr int N = (NB + 3) / 4;
+  int p[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int b = i * 4 + w, r = b * 64 + lane;
+    p[i] = b < blocks && r < R ? parent[base + r] : -2;
   }
-  if (r < R && depth) depth[base + r] = s_depth[r];
-  for (int i = r; i < R * W; i += blockDim.x) {
-    const int row = i / W, w = i - row * W;
-    mask[base * W + i] = (int32_t)rows_lds[(size_t)row * ld + w];
+#pragma unroll
+  for (int i = 0; i < N; ++i) p[i] = checked_parent(p[i], (i * 4 + w) * 64 + lane, err);
+  MaskRow m[N];
+  wave_ancestors(p, w * 64, 256, lane, m);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int b = i * 4 + w, r = b * 64 + lane;
+    if (b < blocks) {
+      s_in[r] = m[i].in;
+      s_up[r] = m[i].up;
+    }
+  }
+  __syncthreads();
+  const int first = part * 256 + w * 64, r = first + lane;
+  const bool live = first < R;
+  u32x4 word[NB / 2];
+  int up = live ? r : -2, d = -1;
+#pragma unroll
+  for (int b = NB - 1; b >= 0; --b) {
+    uint64_t m = 0;
+    if (up >= b * 64) {   // (the chain's next row is in block b: those above are done)
+      m = s_in[up];
+      up = s_up[up];
+      d += __popcll(m);
+    }
+    word[b / 2][b % 2 * 2] = (uint32_t)m;
+    word[b / 2][b % 2 * 2 + 1] = (uint32_t)(m >> 32);
+  }
+  if (live) {
+    if (r < R && depth) depth[base + r] = up == -1 ? d : -1;
+#pragma unroll
+    for (int i = 0; i < NB / 2; ++i)
+      *(u32x4*)(s_out[w] + lane * LD + i * 4) = up == -1 ? word[i] : u32x4{0, 0, 0, 0};
+  }
+  __syncthreads();
+  if (!live) return;
+  uint32_t* to = (uint32_t*)mask + (base + first) * W;
+  const int unit = wide ? 4 : 1, per_row = W / unit, n = min(64, R - first) * per_row;
+  int row = lane / per_row, c = lane - row * per_row;
+  const int drow = 64 / per_row, dc = 64 - drow * per_row;
+  for (int i = lane; i < n; i += 64) {
+    const uint32_t* from = s_out[w] + row * LD + c * unit;
+    if (wide) *(u32x4*)(to + i * 4) = *(const u32x4*)from;
+    else to[i] = *from;
+    row += drow;
+    c += dc;
+    if (c >= per_row) {
+      c -= per_row;
+      ++row;
+    }
   }
 }
 
@@ -287,15 +334,9 @@ __global__ void __launch_bounds__(256) append_rope_kernel(AppendParams p) {
 // commits with its pages; the path's cache slots then move from kv_len +
 // path[i] to kv_len + i in every layer.  The commit may give pages of the
 // window back before the move: the move goes by the page ids noted here, and
-// nothing writes to a page that was given back in between.
+// nothing writes to a page that was given back in between.  Small steps are
+// accepted and committed by one launch (commit.hip); this kernel is for the others.
 // ---------------------------------------------------------------------------
-struct TreeCommit {
-  int S, R, max_pages, pool_pages, n_window_pages;
-  const int32_t *parent, *tokens, *argmax, *kv_len, *table, *finished;
-  int32_t *accept, *path;                      // outputs (or workspace)
-  int32_t *run_len, *old_len, *pages, *run;    // workspace
-};
-
 __global__ void __launch_bounds__(256) tree_accept_kernel(TreeCommit t) {
   __shared__ int s_next[TREE_MAX_ROWS];
   __shared__ int s_path[TREE_MAX_ROWS];
@@ -342,11 +383,12 @@ struct MovePools {
 };
 
 // A wave a (sequence, layer, K or V, KV head).  path[i] >= i and rises, so a
-// slot is read before a later step writes it, and a wave's loads are complete
-// before the stores that wait for them.
+// slot is read before a later step writes it: MOVE slots are read together, then
+// written.  Their rows and pages are found 64 at a time, a lane each.
 template <typename T>
 __global__ void __launch_bounds__(256) tree_move_kernel(TreeCommit t, MovePools pools, int n_pools,
                                                         int Hkv, int D, int32_t* err) {
+  constexpr int MOVE = 8, WORDS = 128 * (int)sizeof(T) / 4 / 64;   // words a lane of a slot of K
   const long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (task >= (long long)t.S * n_pools * Hkv) return;
@@ -356,31 +398,58 @@ __global__ void __launch_bounds__(256) tree_move_kernel(TreeCommit t, MovePools 
   const int32_t* path = t.path + (size_t)s * t.R;
   const int32_t* pages = t.pages + (size_t)s * t.n_window_pages;
   const int off = L % DVS_PAGE_SIZE;
-  if (path[k - 1] == k - 1) return;    // the path is the window's front already
-  T* pool = (T*)pools.p[pl];
-  const size_t head = (size_t)16 * D;
-  auto base_of = [&](int row) -> T* {
-    const int pg = pages[(off + row) >> 4];
-    return pg < 0 ? nullptr : pool + ((size_t)pg * Hkv + h) * head;
-  };
+  char* pool = pools.p[pl];
+  const size_t head = (size_t)16 * D * sizeof(T);
   bool bad = false;
-  for (int i = 1; i < k; ++i) {
-    const int r = path[i];
-    if (r == i) continue;
-    const T* from = base_of(r);
-    T* to = base_of(i);
-    if (!from || !to) {
-      bad = true;
-      continue;
-    }
-    const int a = (off + r) & 15, b = (off + i) & 15;
-    if (pl & 1) {
-      for (int d = lane; d < D; d += 64) to[d * 16 + b] = from[d * 16 + a];
-    } else {
-      for (int d = lane; d < D; d += 64) to[b * D + d] = from[a * D + d];
+  for (int i0 = 1; i0 < k; i0 += 64) {
+    const int i = min(i0 + lane, k - 1), r = path[i];
+    const int pf = pages[(off + r) >> 4], pt = pages[(off + i) >> 4];
+    const int slots = ((off + r) & 15) << 4 | ((off + i) & 15);
+    const bool moves = i0 + lane < k && r != i;
+    bad |= moves && (pf < 0 || pt < 0);
+    uint64_t todo = __ballot(moves && pf >= 0 && pt >= 0);
+    while (todo) {
+      char *from[MOVE], *to[MOVE];
+      int n = 0;
+#pragma unroll
+      for (int b = 0; b < MOVE; ++b) {
+        const int at = todo ? __ffsll((unsigned long long)todo) - 1 : 0;
+        if (todo) n = b + 1;
+        todo &= todo - 1;
+        const int ab = __builtin_amdgcn_readlane(slots, at);
+        const size_t step = pl & 1 ? sizeof(T) : D * sizeof(T);
+        from[b] = pool + ((size_t)__builtin_amdgcn_readlane(pf, at) * Hkv + h) * head + (ab >> 4) * step;
+        to[b] = pool + ((size_t)__builtin_amdgcn_readlane(pt, at) * Hkv + h) * head + (ab & 15) * step;
+      }
+      if (pl & 1) {
+        T x[MOVE][2];
+#pragma unroll
+        for (int b = 0; b < MOVE; ++b)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (b < n && e * 64 + lane < D) x[b][e] = *(const T*)(from[b] + (e * 64 + lane) * 16 * sizeof(T));
+#pragma unroll
+        for (int b = 0; b < MOVE; ++b)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (b < n && e * 64 + lane < D) *(T*)(to[b] + (e * 64 + lane) * 16 * sizeof(T)) = x[b][e];
+      } else {
+        const int words = D * (int)sizeof(T) / 4;
+        uint32_t x[MOVE][WORDS];
+#pragma unroll
+        for (int b = 0; b < MOVE; ++b)
+#pragma unroll
+          for (int e = 0; e < WORDS; ++e)
+            if (b < n && e * 64 + lane < words) x[b][e] = *(const uint32_t*)(from[b] + (e * 64 + lane) * 4);
+#pragma unroll
+        for (int b = 0; b < MOVE; ++b)
+#pragma unroll
+          for (int e = 0; e < WORDS; ++e)
+            if (b < n && e * 64 + lane < words) *(uint32_t*)(to[b] + (e * 64 + lane) * 4) = x[b][e];
+      }
     }
   }
-  if (bad && lane == 0) set_err(err, DVS_ERR_BAD_PAGE);
+  if (__ballot(bad) && lane == 0) set_err(err, DVS_ERR_BAD_PAGE);
 }
 
 static size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -405,15 +474,22 @@ extern "C" int tree_masks(const int32_t* parent, int32_t S, int32_t R, int32_t* 
   DVS_CHECK_ARG(S >= 1 && R >= 1 && R <= TREE_MAX_ROWS, "tree_masks: need S >= 1, 1 <= R <= %d",
                 TREE_MAX_ROWS);
   DVS_CHECK_ARG(R <= 32 || ((uintptr_t)mask_out & 7) == 0, "tree_masks: mask_out must start on 8 bytes");
+  DVS_CHECK_SUPPORTED(S < (1 << 22), "tree_masks: more than 2^22 sequences");
   hipStream_t st = (hipStream_t)stream;
   if (R <= 64) {
     hipLaunchKernelGGL(tree_masks_small_kernel, dim3((S + 3) / 4), dim3(256), 0, st, parent, S, R,
                        mask_out, depth_out, err_word);
   } else {
-    const int W4 = ((R + 31) / 32 + 3) / 4 * 4;
-    hipLaunchKernelGGL(tree_masks_kernel, dim3(S), dim3((R + 63) / 64 * 64),
-                       (size_t)R * (W4 + 4) * 4 + (size_t)R * 4, st, parent, R, mask_out, depth_out,
-                       err_word);
+    const int parts = (R + 255) / 256, W = (R + 31) / 32;
+    const bool wide = W % 4 == 0 && ((uintptr_t)mask_out & 15) == 0;
+    auto launch = [&](auto nb) {
+      hipLaunchKernelGGL(tree_masks_kernel<decltype(nb)::value>, dim3((unsigned)(S * parts)), dim3(256), 0, st,
+                         parent, R, parts, wide, mask_out, depth_out, err_word);
+    };
+    if (R <= 128) launch(IC<2>{});
+    else if (R <= 256) launch(IC<4>{});
+    else if (R <= 512) launch(IC<8>{});
+    else launch(IC<16>{});
   }
   return launch_status("tree_masks");
 }
@@ -454,8 +530,13 @@ extern "C" int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const 
   p.table = page_table; p.kv_len = kv_len; p.depth = depth; p.err = err_word;
   p.S = S; p.R = R; p.Hq = q ? Hq : 0; p.Hkv = Hkv; p.max_pages = max_pages;
   p.pool_pages = num_pool_pages; p.half = rot_dim / 2;
-  for (int i = 0; i < p.half; ++i)
-    p.turns[i] = pow((double)theta, -(double)i / p.half) * 0.63661977236758134308;
+  // (by products in 64-bit mantissas, which keep all of a double's bits: 64 pow()
+  // take longer than the launch)
+  if (p.half) {
+    const long double ratio = powl((long double)theta, -1.0L / p.half);
+    long double turn = 0.636619772367581343075535L;
+    for (int i = 0; i < p.half; ++i, turn *= ratio) p.turns[i] = (double)turn;
+  }
   p.n_pages = window_pages(R);
   // heads of a page over several workgroups where the pages alone do not fill
   // the chip a few times over
@@ -464,7 +545,7 @@ extern "C" int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const 
   const int groups = (int)std::min<long long>(heads, std::max<long long>(1, 8LL * device_cus() / pages));
   p.per_group = (heads + groups - 1) / groups;
   p.n_groups = (heads + p.per_group - 1) / p.per_group;
-  DVS_CHECK_SUPPORTED(pages * p.n_groups < (1LL << 31), "kv_append_rope: grid too large");
+  DVS_CHECK_SUPPORTED(pages * p.n_groups < (1LL << 24), "kv_append_rope: grid too large");
   const unsigned grid = (unsigned)(pages * p.n_groups);
   auto on16 = [&](const void* b, int64_t seq, int64_t ld) {
     return !b || ((((uintptr_t)b | (uintptr_t)(S > 1 ? seq : 0) * es | (uintptr_t)(R > 1 ? ld : 0) * es)) & 15) == 0;
@@ -527,10 +608,12 @@ extern "C" int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, 
   t.run = t.pages + (size_t)S * t.n_window_pages;
   t.path = path_out ? path_out : t.run + (size_t)S * R;
   hipStream_t hs = (hipStream_t)stream;
-  hipLaunchKernelGGL(tree_accept_kernel, dim3(S), dim3(256), 0, hs, t);
-  int rc = launch_status("accept_commit_tree(accept)");
-  if (rc) return rc;
-  if ((rc = commit_tree_run(st, R, t.run_len, t.run, stream))) return rc;
+  int rc;
+  if (!tree_accept_in_commit(t)) {
+    hipLaunchKernelGGL(tree_accept_kernel, dim3(S), dim3(256), 0, hs, t);
+    if ((rc = launch_status("accept_commit_tree(accept)"))) return rc;
+  }
+  if ((rc = commit_tree_run(st, t, stream))) return rc;
   for (int l0 = 0; l0 < n_layers; l0 += MOVE_LAYERS) {
     const int nl = std::min(n_layers - l0, MOVE_LAYERS);
     MovePools pools{};

@@ -1129,10 +1129,11 @@ def _rows(t, name, dtype, S, R, D):
         raise DvsError(f"{name} must be a CUDA (HIP) tensor")
     if t.dtype != dtype:
         raise DvsError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 4 or t.shape[0] != S or t.shape[1] != R or t.shape[3] != D:
-        raise DvsError(f"{name} must be [S, R, heads, D], got {tuple(t.shape)}")
+    shape = t.shape
+    if len(shape) != 4 or shape[0] != S or shape[1] != R or shape[3] != D:
+        raise DvsError(f"{name} must be [S, R, heads, D], got {tuple(shape)}")
     seq, ld, head, one = t.stride()
-    if one != 1 or (t.shape[2] > 1 and head != D):
+    if one != 1 or (shape[2] > 1 and head != D):
         raise DvsError(f"{name}'s heads must be contiguous and side by side")
     if seq < 0 or ld < 0:
         raise DvsError(f"{name}'s strides must not be negative")
