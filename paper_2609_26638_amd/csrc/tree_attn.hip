@@ -17,9 +17,8 @@ __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
 
 constexpr int MAX_SEQS = 1024;      // sequences a launch takes
 constexpr float RESCALE_LOG2 = 8.f, WEIGHT_MAX = 8 * 256.f;
-constexpr int TILE_ROWS = 32;      // query rows of a KV head above which tiles go through LDS
-constexpr int WHOLE_TILES = 8;     // tiles of a table up to which a wave takes a whole item
-constexpr int MERGE_FEW = 1024;    // row groups up to which the merge takes more waves
+constexpr int TILE_ROWS = 32;   // query rows of a KV head above which tiles go through LDS
+constexpr int MERGE_FEW = 1024; // row groups up to which the merge takes more waves
 
 struct TreeAttn {
   const void *q, *k_pool, *v_pool;
@@ -277,6 +276,28 @@ __device__ __forceinline__ SeqTiles seq_tiles(const TreeAttn& p, int keys, int* 
   return SeqTiles{p.S, s_seq[p.S], 0, 0, s_seq, s_len, true};
 }
 
+// The key tiles [u, u_end) of share `id` of n, in order of sequences, then items of
+// a sequence (per_seq of them).  Split: equal shares of at least share_min
+// tiles, which cut items; else whole items.
+struct Share {
+  int u, u_end, size;
+};
+__device__ __forceinline__ Share share_of(const TreeAttn& p, const SeqTiles& seqs, int per_seq, int id, int n) {
+  const int U = seqs.total * per_seq;
+  if (p.split) {
+    const int size = max((U + n - 1) / n, p.share_min);
+    const int u = (int)min((long long)id * size, (long long)U);
+    return Share{u, min(u + size, U), size};
+  }
+  auto start = [&](uint32_t i) {
+    const int s = i / per_seq;
+    if (s >= p.S) return U;
+    return seqs.before(s) * per_seq + (int)(i - s * per_seq) * (seqs.before(s + 1) - seqs.before(s));
+  };
+  const uint32_t items = p.S * per_seq;   // at most 2^22, n at most 2 a CU
+  return Share{start(id * items / n), start((id + 1) * items / n), 1};
+}
+
 // Consecutive workgroups on one XCD (blockIdx goes round the eight): row tiles
 // of an item then find its keys in their L2.
 __device__ __forceinline__ int xcd_block() {
@@ -284,15 +305,52 @@ __device__ __forceinline__ int xcd_block() {
   return x * q + min(x, rem) + i;
 }
 
-// Whether a row's mask (NULL: causal) has a bit of the window.
-__device__ __forceinline__ bool sees_any(const TreeAttn& p, const uint32_t* mask) {
-  if (!mask) return true;
-  const uint32_t last = mask[p.W - 1], first = mask[0];   // (the usual masks: one or two words)
-  uint32_t bits = last & (0xffffffffu >> (31 - ((p.R - 1) & 31)));
-  if (p.W > 1) bits |= first;
-  for (int i = 1; i < p.W - 1; ++i) bits |= mask[i];
-  return bits != 0;
-}
+// A lane's NG query rows: row n of a KV head is window row n / G, head n % G of
+// its group.  Every load is sent out before any is waited for.  any: the row's
+// mask (NULL: causal) has a bit of the window.
+template <typename T, int D, int NG>
+struct Rows {
+  static constexpr int NQ = D / Tile<T>::NQ_DIV;
+  int first, kvh, r[NG];
+  bool any[NG];
+  u32x4 q[NG][NQ];
+
+  __device__ __forceinline__ bool valid(const TreeAttn& p, int g) const {
+    return first + g * 16 + (int)(threadIdx.x & 15) < p.rows;
+  }
+  // the row in q and out (one that is not there: the first)
+  __device__ __forceinline__ size_t at(const TreeAttn& p, int s, int g) const {
+    const int h = valid(p, g) ? first + g * 16 + (int)(threadIdx.x & 15) - r[g] * p.G : 0;
+    return (((size_t)s * p.R + r[g]) * p.Hq + kvh * p.G + h) * D;
+  }
+  __device__ __forceinline__ const uint32_t* mask(const TreeAttn& p, int s, int g) const {
+    return p.mask ? (const uint32_t*)p.mask + ((size_t)s * p.R + r[g]) * p.W : nullptr;
+  }
+
+  __device__ __forceinline__ void load(const TreeAttn& p, int s, int kv_head, int first_row) {
+    const int lane = threadIdx.x & 63, m16 = lane & 15, quarter = lane >> 4;
+    first = first_row;
+    kvh = kv_head;
+    uint32_t bits[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      r[g] = valid(p, g) ? (first + g * 16 + m16) / p.G : 0;
+      const T* src = (const T*)p.q + at(p, s, g);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) q[g][i] = *(const u32x4*)(src + Tile<T>::q_elem(quarter, i));
+      bits[g] = 1;
+    }
+    if (p.mask) {
+#pragma unroll
+      for (int g = 0; g < NG; ++g) bits[g] = mask(p, s, g)[p.W - 1] & (0xffffffffu >> (31 - ((p.R - 1) & 31)));
+      for (int i = 0; i < p.W - 1; ++i)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) bits[g] |= mask(p, s, g)[i];
+    }
+#pragma unroll
+    for (int g = 0; g < NG; ++g) any[g] = valid(p, g) && bits[g] != 0;
+  }
+};
 
 // A page id of the table, 0 (and the error) for one outside the pool.
 __device__ __forceinline__ int checked_page(const TreeAttn& p, int id) {
@@ -306,10 +364,10 @@ __device__ __forceinline__ int checked_page(const TreeAttn& p, int id) {
 // product, and added to the rows that see them (slots behind the last row hold
 // anything, others seldom such: finding out is a product with zeros, or in fp32
 // a multiplication each).  bits: of a lane's row and its quarter's keys;
-// value(key, d): the cache's.
+// values(key): the key's, 16 elements from one of the head to the next.
 template <typename T, int NG, int DG, class F>
 __device__ __forceinline__ void clean_values(u32x4 (&vf)[DG], const uint32_t (&bits)[NG], f32x4 (&o)[NG][DG],
-                                             F value) {
+                                             F values) {
   const int quarter = (threadIdx.x & 63) >> 4;
   bool found = false;
   if constexpr (sizeof(T) == 2) {
@@ -346,11 +404,13 @@ __device__ __forceinline__ void clean_values(u32x4 (&vf)[DG], const uint32_t (&b
 #pragma nounroll
   for (int key = 0; key < Tile<T>::KEYS; ++key) {
     if (!__ballot(some >> key & 1)) continue;
+    const char* v = (const char*)values(key);
+    const uint32_t off = quarter * 64 * (uint32_t)sizeof(T);
 #pragma unroll
     for (int d = 0; d < DG; ++d) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = value(key, d * 16 + quarter * 4 + i);
+        const float x = (float)*(const T*)(v + off + (d * 16 + i) * 16 * (int)sizeof(T));
         const bool odd = (__float_as_uint(x) & 0x7f800000) == 0x7f800000;
 #pragma unroll
         for (int g = 0; g < NG; ++g) o[g][d][i] += odd && (sees[g] >> key & 1) ? x : 0.f;
@@ -363,22 +423,21 @@ __device__ __forceinline__ void clean_values(u32x4 (&vf)[DG], const uint32_t (&b
 // End of a segment: the output, or a part of it (O, m and l in 32 bits).  l is
 // 0 exactly for a row that sees nothing, whatever its O holds.
 template <typename T, int D, int NG>
-__device__ __forceinline__ void finish_rows(const TreeAttn& p, int s, const int (&r)[NG], const int (&h)[NG],
-                                            const bool (&valid)[NG], const bool (&any)[NG],
+__device__ __forceinline__ void finish_rows(const TreeAttn& p, int s, const Rows<T, D, NG>& row,
                                             const float (&m)[NG], float (&l)[NG],
                                             const f32x4 (&o)[NG][D / 16], int nseg, size_t slot) {
   const int lane = threadIdx.x & 63, m16 = lane & 15, quarter = lane >> 4;
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     l[g] = rows_sum(l[g]);
-    if (!any[g]) l[g] = 0.f;
+    if (!row.any[g]) l[g] = 0.f;
     if (nseg > 1) {
       if (quarter == 0) *(f32x2*)(p.part_ml + ((slot * NG + g) * 16 + m16) * 2) = f32x2{m[g], l[g]};
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
         *(f32x4*)(p.part_o + ((slot * NG + g) * (D / 16) + d) * 256 + lane * 4) = o[g][d];
-    } else if (valid[g]) {
-      T* dst = (T*)p.out + (((size_t)s * p.R + r[g]) * p.Hq + h[g]) * D + quarter * 4;
+    } else if (row.valid(p, g)) {
+      T* dst = (T*)p.out + row.at(p, s, g) + quarter * 4;
       const float inv = 1.f / l[g];
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
@@ -390,98 +449,117 @@ __device__ __forceinline__ void finish_rows(const TreeAttn& p, int s, const int 
   }
 }
 
+// The same where the workgroup's waves hold parts of one segment: joined in LDS,
+// a wave every fourth 16 elements of the head.
+template <typename T, int D, int NG>
+__device__ __forceinline__ void finish_together(const TreeAttn& p, int s, const Rows<T, D, NG>& row,
+                                                const float (&m)[NG], float (&l)[NG],
+                                                const f32x4 (&o)[NG][D / 16], int nseg, size_t slot,
+                                                f32x4* s_o, f32x2* s_ml) {
+  constexpr int DG = D / 16;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, m16 = lane & 15, quarter = lane >> 4;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    l[g] = rows_sum(l[g]);
+    s_ml[(w * NG + g) * 64 + lane] = f32x2{m[g], row.any[g] ? l[g] : 0.f};
+#pragma unroll
+    for (int d = 0; d < DG; ++d) s_o[((w * NG + g) * DG + d) * 64 + lane] = o[g][d];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    f32x2 ml[4];
+    float M = -INFINITY, sum = 0.f, e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      ml[i] = s_ml[(i * NG + g) * 64 + lane];
+      if (ml[i][1] != 0.f) M = fmaxf(M, ml[i][0]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      e[i] = ml[i][1] != 0.f ? __builtin_amdgcn_exp2f(ml[i][0] - M) : 0.f;
+      if (ml[i][1] != 0.f) sum = fmaf(e[i], ml[i][1], sum);
+    }
+    if (nseg > 1 && w == 0 && quarter == 0)
+      *(f32x2*)(p.part_ml + ((slot * NG + g) * 16 + m16) * 2) = f32x2{M, sum};
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T* dst = (T*)p.out + row.at(p, s, g) + quarter * 4;
+#pragma unroll
+    for (int d0 = 0; d0 < DG; d0 += 4) {
+      const int d = d0 + w;
+      if (d >= DG) break;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 y = s_o[((i * NG + g) * DG + d) * 64 + lane];
+        if (ml[i][1] != 0.f) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = fmaf(e[i], y[j], x[j]);
+        }
+      }
+      if (nseg > 1) *(f32x4*)(p.part_o + ((slot * NG + g) * DG + d) * 256 + lane * 4) = x;
+      else if (row.valid(p, g)) store4(dst + d * 16, x * inv);
+    }
+  }
+  __syncthreads();
+}
+
 // ---------------------------------------------------------------------------
-// Every wave on its own: NG groups of 16 query rows (row n of a KV head is
-// window row n / G, head n % G of its group) and a share of the key tiles,
-// straight from the cache into registers; the next tile's keys are on their
-// way under this one's softmax, its values under the next one's scores.  Shares
-// are equal numbers of tiles, wherever the sequences begin, so that ragged
-// lengths leave no wave idle; an item cut by shares is merged afterwards.
+// Few query rows of a KV head: a workgroup takes NG groups of 16 of them and a run
+// of key tiles, a quarter of it a wave, straight from the cache into registers:
+// the next tile's keys are on their way under this one's softmax, its values
+// under the next one's scores.  The waves' results are joined in LDS (a wave on
+// its own, with a part of its own for the merge, took, us: 64 sequences of 1k-8k,
+// one row 117 / 111; 32 of 1k-8k, 16 rows 75 / 67; one of 16000, one row 28 / 21).
 //
-// What bounds it: single tokens over long caches, the cache (64 sequences of
-// 1k-8k, 4 of 16 heads, 294 MB: 70 us, 4.2 TB/s of the 5.2 that a copy
-// reaches); one sequence, latency: a wave's tiles one after the other, about
-// 0.9 us each, and the second launch (2000 keys: 14.9 us one row, 20 us 128);
-// fp32, the matrix instructions (32 sequences of 1k-4k, 64 rows: 162 us, half
-// their rate).
+// What bounds it: long caches, the cache (64 sequences, one row, 556 MB: 111 us,
+// 5.0 TB/s of the 5.2 that a copy reaches); one sequence, latency: the lengths,
+// then the page ids, then keys and values, 1 - 2 us each, then the second launch
+// (2000 keys, one row 13.7 us, 128 rows 15.0); fp32, the matrix instructions (32
+// sequences of 1k-4k, 64 rows: 149 us, half their rate).
 // ---------------------------------------------------------------------------
 template <typename T, int D, int NG>
 __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
   using TL = Tile<T>;
-  constexpr int KEYS = TL::KEYS, NP = D / 16, NQP = D / TL::NQ_DIV, DG = D / 16, NS = TL::NS;
+  constexpr int KEYS = TL::KEYS, NP = D / 16, DG = D / 16, NS = TL::NS;
   constexpr int PAGE_B = 16 * D * (int)sizeof(T);
   __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[4];
+  __shared__ f32x4 s_o[4 * NG * DG * 64];
+  __shared__ f32x2 s_ml[4 * NG * 64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, quarter = lane >> 4;
   const int HN = p.Hkv * p.n_rt;
-  const int share_id = xcd_block() * 4 + w, n_shares = gridDim.x * 4;
-  int u = share_id, u_end = p.S * HN, share = 0;
-  SeqTiles seqs{};
-  if (p.split) {
-    seqs = seq_tiles(p, KEYS, s_seq, s_len, s_tot);
-    const int U = seqs.total * HN;
-    share = max((U + n_shares - 1) / n_shares, p.share_min);
-    u = min((long long)share_id * share, (long long)U);
-    u_end = min(u + share, U);
-  }
+  const int share_id = xcd_block(), n_shares = gridDim.x;
+  const SeqTiles seqs = seq_tiles(p, KEYS, s_seq, s_len, s_tot);
+  const Share sh = share_of(p, seqs, HN, share_id, n_shares);
+  const int u_end = __builtin_amdgcn_readfirstlane(sh.u_end), share = __builtin_amdgcn_readfirstlane(sh.size);
+  int u = __builtin_amdgcn_readfirstlane(sh.u);
   const char* kp = (const char*)p.k_pool;
   const char* vp = (const char*)p.v_pool;
   const uint32_t koff = TL::template k_off<D>(m16, quarter), voff = TL::v_off(m16, quarter);
   const int kpage = TL::template k_page<D>(m16, quarter), vpage = TL::v_page(quarter);
 
   while (u < u_end) {
-    int s, qi, j0, j1, tiles, k = 0, nseg = 1, L;
-    if (p.split) {
-      s = __builtin_amdgcn_readfirstlane(seqs.find(u / HN));
-      L = seqs.length(s);
-      const int U0 = seqs.before(s) * HN;
-      tiles = seqs.before(s + 1) - seqs.before(s);
-      qi = (u - U0) / tiles;
-      j0 = u - U0 - qi * tiles;
-      j1 = min(tiles, j0 + (u_end - u));
-      const int P0 = U0 + qi * tiles;
-      k = share_id - P0 / share;
-      nseg = (P0 + tiles - 1) / share - P0 / share + 1;
-      u += j1 - j0;
-    } else {
-      s = u / HN;
-      qi = u - s * HN;
-      L = p.kv_len[s];
-      u += n_shares;
-      if (L < 0 || (long long)L + p.R > (long long)p.max_pages * DVS_PAGE_SIZE) {
-        if (lane == 0) set_err(p.err, DVS_ERR_MAX_PAGES);
-        continue;
-      }
-      j0 = 0;
-      j1 = tiles = (L + p.R + KEYS - 1) / KEYS;
-    }
-    s = __builtin_amdgcn_readfirstlane(s);
-    L = __builtin_amdgcn_readfirstlane(L);
+    const int s = __builtin_amdgcn_readfirstlane(seqs.find(u / HN));
+    const int L = __builtin_amdgcn_readfirstlane(seqs.length(s));
+    const int U0 = __builtin_amdgcn_readfirstlane(seqs.before(s)) * HN;
+    const int tiles = __builtin_amdgcn_readfirstlane(seqs.before(s + 1)) - U0 / HN;
+    const int qi = (u - U0) / tiles, first = u - U0 - qi * tiles, n = min(tiles - first, u_end - u);
+    const int P0 = U0 + qi * tiles;
+    const int k = p.split ? share_id - P0 / share : 0;
+    const int nseg = p.split ? (P0 + tiles - 1) / share - P0 / share + 1 : 1;
+    u += n;
+    const int j0 = first + n * w / 4, j1 = first + n * (w + 1) / 4;   // this wave's
     const int it = s * HN + qi, kvh = qi / p.n_rt, rt = qi - kvh * p.n_rt;
-    if (p.split && k == 0 && lane == 0) p.meta[it] = int2{nseg, share_id};
+    if (p.split && k == 0 && threadIdx.x == 0) p.meta[it] = int2{nseg, share_id};
     const int n_valid = (L + p.R + 15) >> 4;
     const int32_t* pt = p.table + (size_t)s * p.max_pages;
     // the ids of the next 64 pages, a lane each (checked only when the queries'
     // loads have gone out too)
     auto page_ids = [&](int j) { return pt[min(j * TL::PAGES + lane, n_valid - 1)]; };
     int ids = page_ids(j0), ids_at = j0;
-    // this lane's query rows
-    int r[NG], h[NG];
-    bool valid[NG], any[NG];
-    const uint32_t* mask[NG];
-    u32x4 q[NG][NQP];
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const int n = (rt * NG + g) * 16 + m16;
-      valid[g] = n < p.rows;
-      r[g] = valid[g] ? n / p.G : 0;
-      h[g] = kvh * p.G + (valid[g] ? n - r[g] * p.G : 0);
-      const T* src = (const T*)p.q + (((size_t)s * p.R + r[g]) * p.Hq + h[g]) * D;
-#pragma unroll
-      for (int i = 0; i < NQP; ++i) q[g][i] = *(const u32x4*)(src + TL::q_elem(quarter, i));
-      mask[g] = p.mask ? (const uint32_t*)p.mask + ((size_t)s * p.R + r[g]) * p.W : nullptr;
-      any[g] = valid[g] && sees_any(p, mask[g]);
-    }
+    Rows<T, D, NG> row;
+    row.load(p, s, kvh, rt * NG * 16);
     f32x4 o[NG][DG];
     float m[NG], l[NG];
 #pragma unroll
@@ -512,8 +590,10 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
       for (int i = 0; i < NP; ++i) vf[i] = *(const u32x4*)(b + i * 256 * sizeof(T));
     };
     ids = checked_page(p, ids);
-    load_k(j0);
-    load_v(j0);
+    if (j0 < j1) {
+      load_k(j0);
+      load_v(j0);
+    }
     for (int j = j0; j < j1; ++j) {
       f32x4 sc[NG][NS];
 #pragma unroll
@@ -527,13 +607,13 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
 #pragma unroll
           for (int g = 0; g < NG; ++g)
             sc[g][i & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, kf[i]), __builtin_bit_cast(bf16x8, q[g][i >> 1]), sc[g][i & 1], 0, 0, 0);
+                __builtin_bit_cast(bf16x8, kf[i]), __builtin_bit_cast(bf16x8, row.q[g][i >> 1]), sc[g][i & 1], 0, 0, 0);
         } else {
 #pragma unroll
           for (int g = 0; g < NG; ++g)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              sc[g][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i][e]), __uint_as_float(q[g][i][e]),
+              sc[g][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i][e]), __uint_as_float(row.q[g][i][e]),
                                                               sc[g][0], 0, 0, 0);
         }
       }
@@ -551,7 +631,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
       if (masked) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const uint32_t b = bits[g] = seen_bits<TL::NK>(p, mask[g], r[g], any[g], key0, L);
+          const uint32_t b = bits[g] = seen_bits<TL::NK>(p, row.mask(p, s, g), row.r[g], row.any[g], key0, L);
 #pragma unroll
           for (int i = 0; i < TL::NK; ++i)
             if (!(b >> i & 1)) sc[g][i >> 2][i & 3] = -INFINITY;
@@ -560,9 +640,9 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
       typename Weights<T>::type pf[NG];
       softmax_tile<T, NS, NG, DG>(sc, pf, p.scale_log2, m, l, o);
       if (masked)
-        clean_values<T>(vf, bits, o, [&](int key, int d) {
+        clean_values<T>(vf, bits, o, [&](int key) {
           const int page = __builtin_amdgcn_readfirstlane(checked_page(p, pt[min(j * TL::PAGES + (key >> 4), n_valid - 1)]));
-          return (float)((const T*)vp)[((size_t)page * p.Hkv + kvh) * 16 * D + d * 16 + (key & 15)];
+          return (const T*)(vp + ((size_t)(uint32_t)page * p.Hkv + kvh) * PAGE_B) + (key & 15);
         });
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
@@ -580,7 +660,8 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
       }
       if (more) load_v(j + 1);
     }
-    finish_rows<T, D, NG>(p, s, r, h, valid, any, m, l, o, nseg, (size_t)share_id * 2 + (k == 0 ? 1 : 0));
+    const size_t slot = (size_t)share_id * 2 + (k == 0 ? 1 : 0);
+    finish_together<T, D, NG>(p, s, row, m, l, o, nseg, slot, s_o, s_ml);
   }
 }
 
@@ -642,10 +723,9 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
   const int block = xcd_block(), n_shares = gridDim.x / p.n_wide;
   const int share_id = block / p.n_wide, rt = block - share_id * p.n_wide;
   const SeqTiles seqs = seq_tiles(p, KEYS, s_seq, s_len, s_tot);
-  const int U = seqs.total * p.Hkv;
-  const int share = max((U + n_shares - 1) / n_shares, p.share_min);
-  int u = (int)min((long long)share_id * share, (long long)U);
-  const int u_end = min(u + share, U);
+  const Share sh = share_of(p, seqs, p.Hkv, share_id, n_shares);
+  const int u_end = __builtin_amdgcn_readfirstlane(sh.u_end), share = __builtin_amdgcn_readfirstlane(sh.size);
+  int u = __builtin_amdgcn_readfirstlane(sh.u);
   // copies: pages 0, 1 of K, then of V; lane's source offset in the page, of
   // its 16 bytes of each 1 KB
   const int cpage = w * NPL / SEGS, cseg = w * NPL % SEGS;
@@ -676,33 +756,20 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
     const int tiles = __builtin_amdgcn_readfirstlane(seqs.before(s + 1)) - U0 / p.Hkv;
     const int kvh = (u - U0) / tiles, j0 = u - U0 - kvh * tiles, j1 = min(tiles, j0 + (u_end - u));
     const int P0 = U0 + kvh * tiles;
-    const int k = share_id - P0 / share, nseg = (P0 + tiles - 1) / share - P0 / share + 1;
+    const int k = p.split ? share_id - P0 / share : 0;
+    const int nseg = p.split ? (P0 + tiles - 1) / share - P0 / share + 1 : 1;
     u += j1 - j0;
     const int sub = rt * NW + w;                         // this wave's 32 rows of the item
     const bool work = sub * NG * 16 < p.rows;
     const int it = (s * p.Hkv + kvh) * p.n_rt + sub;
-    if (work && k == 0 && lane == 0) p.meta[it] = int2{nseg, (share_id * p.n_wide + rt) * NW + w};
+    if (p.split && work && k == 0 && lane == 0) p.meta[it] = int2{nseg, (share_id * p.n_wide + rt) * NW + w};
     const int n_valid = (L + p.R + 15) >> 4;
     const int32_t* pt = p.table + (size_t)s * p.max_pages;
     // the wave's page of the next 64 tiles, a lane each
     auto page_ids = [&](int j) { return pt[min((j + lane) * 2 + (cpage & 1), n_valid - 1)]; };
     int ids = page_ids(j0), ids_at = j0;
-    int r[NG], h[NG];
-    bool valid[NG], any[NG];
-    const uint32_t* mask[NG];
-    u32x4 q[NG][D / 32];
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const int n = (sub * NG + g) * 16 + m16;
-      valid[g] = n < p.rows;
-      r[g] = valid[g] ? n / p.G : 0;
-      h[g] = kvh * p.G + (valid[g] ? n - r[g] * p.G : 0);
-      const __bf16* src = (const __bf16*)p.q + (((size_t)s * p.R + r[g]) * p.Hq + h[g]) * D + quarter * 8;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) q[g][i] = *(const u32x4*)(src + i * 32);
-      mask[g] = p.mask ? (const uint32_t*)p.mask + ((size_t)s * p.R + r[g]) * p.W : nullptr;
-      any[g] = valid[g] && sees_any(p, mask[g]);
-    }
+    Rows<__bf16, D, NG> row;
+    row.load(p, s, kvh, sub * NG * 16);
     // The queries' loads end here, and the registers are then as if made anew:
     // the compiler cannot tell inside the loop that they have ended, and would
     // wait for the tiles' copies as well.
@@ -710,7 +777,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) asm volatile("" : "+v"(q[g][i]));
+      for (int i = 0; i < D / 32; ++i) asm volatile("" : "+v"(row.q[g][i]));
     ids = checked_page(p, ids);
     asm volatile("" : "+v"(ids));
     f32x4 o[NG][DG];
@@ -749,7 +816,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
           const bf16x8 kf = *(const bf16x8*)(tile + kfrag[ks] + t * 4 * 2 * D);
 #pragma unroll
           for (int g = 0; g < NG; ++g)
-            sc[g][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, q[g][ks]), sc[g][t], 0, 0, 0);
+            sc[g][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8, row.q[g][ks]), sc[g][t], 0, 0, 0);
         }
     };
     // Step j: the next tile's scores into `nxt` under this tile's softmax (`cur`
@@ -773,7 +840,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
       if constexpr (MASKED) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          const uint32_t b = bits[g] = seen_bits<8>(p, mask[g], r[g], any[g], j * KEYS + quarter * 8, L);
+          const uint32_t b = bits[g] = seen_bits<8>(p, row.mask(p, s, g), row.r[g], row.any[g], j * KEYS + quarter * 8, L);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             if (!(b >> i & 1)) cur[g][i >> 2][i & 3] = -INFINITY;
@@ -787,8 +854,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
       bf16x8 pf[NG];
       softmax_tile<__bf16, 2, NG, DG>(cur, pf, p.scale_log2, m, l, o);
       if constexpr (MASKED)
-        clean_values<__bf16>(vf, bits, o, [&](int key, int d) {
-          return (float)*(const __bf16*)(tile + TILE_B + (key >> 4) * PAGE_B + d * 32 + (key & 15) * 2);
+        clean_values<__bf16>(vf, bits, o, [&](int key) {
+          return (const __bf16*)(tile + TILE_B + (key >> 4) * PAGE_B) + (key & 15);
         });
 #pragma unroll
       for (int d = 0; d < DG; ++d) {
@@ -847,7 +914,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
     step(IC<1>{}, IC<1>{}, at(j1 - 1), st0, st0, j1 - 1, sa, sb);
     if (!work) continue;
     const size_t slot = (size_t)((share_id * p.n_wide + rt) * NW + w) * 2 + (k == 0 ? 1 : 0);
-    finish_rows<__bf16, D, NG>(p, s, r, h, valid, any, m, l, o, nseg, slot);
+    finish_rows<__bf16, D, NG>(p, s, row, m, l, o, nseg, slot);
   }
 }
 
@@ -935,39 +1002,46 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
   const int keys = dtype == DVS_BF16 ? Tile<__bf16>::KEYS : Tile<float>::KEYS;
   const int max_tiles = (int)(((long long)max_pages * DVS_PAGE_SIZE + keys - 1) / keys);
   const int cus = device_cus();
-  // Two groups of 16 rows a wave read half the bytes a row.  fp32, whose products
-  // take long, only where every wave still has its 8 tiles (one / two groups, us:
-  // 128 rows, one sequence of 2048 30.1 / 33.8; 64 rows, 32 of 1k-4k 213 / 162).
-  pl.ng = rows > 16 && (dtype == DVS_BF16 || (long long)std::min(S, MAX_SEQS) * Hkv * ((rows + 31) / 32) * max_tiles >=
-                                                 8LL * 8 * cus) ? 2 : 1;
-  pl.waves = 4;
+  // Few tiles: 16 rows a wave, and not the tiles through LDS, so that there are as
+  // many waves as can be (us, 16 rows a wave / otherwise: 128 rows, one sequence
+  // of 2048 15.0 / 19.7, one of 16000 43 / 31; 8 of 1k-2k, 32 rows 18.5 / 23.9, 64
+  // rows 21.1 / 22.0, 128 rows 27.7 / 25.1; fp32, one of 2048, 128 rows 24.4 / 29.2,
+  // 32 of 1k-4k, 64 rows 204 / 149).  Short tables need no merge, and may be more:
+  // 16 of 300-900, 128 rows 21.2 / 28.3.
+  const long long a_wave = (long long)std::min(S, MAX_SEQS) * Hkv * ((rows + 15) / 16) * max_tiles / (8 * cus);
+  const bool few = a_wave < (max_tiles <= 32 ? 8 : 4);
+  const bool wide = dtype == DVS_BF16 && rows > TILE_ROWS && !few;
+  pl.ng = rows > 16 && !few ? 2 : 1;
   pl.n_rt = (rows + pl.ng * 16 - 1) / (pl.ng * 16);
   const long long per_seq = (long long)Hkv * pl.n_rt * max_tiles;
   pl.seqs = (int)std::max<long long>(1, std::min<long long>({S, MAX_SEQS, (1LL << 30) / per_seq,
                                                              (1LL << 22) / ((long long)Hkv * pl.n_rt)}));
   const long long items = (long long)pl.seqs * Hkv * pl.n_rt;
-  // Tiles of a share, at least: a part that is published costs as much as a few
-  // tiles, and the merge grows with the parts of an item; short caches are done
-  // sooner in smaller ones (128 rows, us, 4 / 8 tiles: 100 - 400 keys 21.7 / 24.7,
-  // one sequence of 16000 44.1 / 33.8; one row, 16000 keys: 32.5 / 27.4).
-  if (dtype == DVS_BF16 && rows > TILE_ROWS) {
-    // (waves on their own, us, against tiles in LDS: 64 rows, 32 sequences of
-    // 1k-8k 109 / 82; 128 rows, one of 2048 20.7 / 20.1; 60 rows, 16 of 1k-4k 34.9
-    // / 31.5)
+  // (waves on their own, us, against tiles in LDS: 64 rows, 32 sequences of 1k-8k
+  // 108 / 79; 256 rows, 8 of 1k-2k 38.5 / 34.8; 60 rows, 16 of 1k-4k 30.3 / 29.3)
+  if (wide) {
     pl.waves = rows > 128 && D != 96 ? 8 : 4;
     pl.n_wide = (pl.n_rt + pl.waves - 1) / pl.waves;
-    pl.split = 1;
-    pl.share_min = max_tiles <= 32 ? 4 : std::max(8, max_tiles / 64);
-    const long long tiles = (long long)pl.seqs * Hkv * max_tiles;
-    const long long shares = std::min<long long>(std::max(1, (pl.waves == 8 ? 1 : 2) * cus / pl.n_wide),
-                                                 (tiles + pl.share_min - 1) / pl.share_min);
-    pl.grid = (int)(shares * pl.n_wide);
+    pl.grid = std::max(1, (pl.waves == 8 ? 1 : 2) * cus / pl.n_wide);
   } else {
-    pl.split = max_tiles > WHOLE_TILES;
-    pl.share_min = std::max(4, max_tiles / 64);
-    const long long tiles = items * max_tiles;
-    pl.grid = (int)std::min<long long>(2 * cus, ((pl.split ? (tiles + pl.share_min - 1) / pl.share_min : items) + 3) / 4);
+    pl.waves = 1;
+    pl.grid = 2 * cus;
   }
+  // Whole items, and no merge, where a wave's tiles then are at most 8 more than
+  // with all cut to equal shares: a merge and its launch take that long (cut /
+  // whole, us: 64 sequences of 200-500, 16 rows 20.3 / 13.1; 256 of 100-400, 32 rows
+  // 58.6 / 38.5; 128 of 500-1900 87.9 / 75.1).  Only tables of up to 64 tiles: lengths
+  // differ, and a long one must not be left to a wave.
+  // Tiles of a share, at least: the merge grows with the parts of an item (one
+  // sequence of 16000, one row, 8 / 16 / 32 tiles 27.4 / 21.4 / 23.5 us).
+  const int per = wide ? 1 : 4;   // waves that share a segment's tiles
+  const long long units = (long long)pl.seqs * Hkv * (wide ? 1 : pl.n_rt), tiles = units * max_tiles;
+  const long long whole = (units + pl.grid - 1) / pl.grid * ((max_tiles + per - 1) / per);
+  const long long cut = std::max(1LL, tiles / ((long long)pl.grid * per));
+  pl.split = max_tiles > 64 || whole - cut > 8;
+  pl.share_min = wide ? (max_tiles <= 32 ? 4 : std::max(8, max_tiles / 64)) : std::max(4, max_tiles / 32);
+  pl.grid = (int)std::min<long long>(pl.grid, pl.split ? (tiles + pl.share_min - 1) / pl.share_min : units);
+  if (wide) pl.grid *= pl.n_wide;
   if (pl.split) {
     const size_t slots = (size_t)pl.grid * pl.waves * 2;
     pl.off_ml = al256((size_t)items * sizeof(int2));

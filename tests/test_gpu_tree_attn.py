@@ -29,7 +29,7 @@ def check(got, want, size, dtype):
         assert max_rel_err(got[live], want[live]) <= 1e-5
 
 
-def run(case, dtype, vis, words, spread=1.0, tail=np.nan, seed=0, **kw):
+def run(case, dtype, vis, words, spread=1.0, tail=np.nan, seed=0, columns=0, **kw):
     lens, R, Hq, Hkv, D = case
     st, k, v = cache(seed + R, lens, R, Hkv, D, dtype, spread=spread, tail=tail)
     rng = np.random.default_rng(seed)
@@ -42,7 +42,10 @@ def run(case, dtype, vis, words, spread=1.0, tail=np.nan, seed=0, **kw):
     scale = 1 / math.sqrt(D)
     want, size = ot.attention(q.astype(float), k, v, st.page_table, st.kv_len, vis, scale)
     err = zero_err()
-    out = dvs.attn_tree(dev(q, dtype), dev(k, dtype), dev(v, dtype), i32(st.page_table),
+    table = st.page_table
+    if table.shape[1] < columns:   # entries behind a sequence's pages are not read
+        table = np.pad(table, ((0, 0), (0, columns - table.shape[1])), constant_values=1 << 30)
+    out = dvs.attn_tree(dev(q, dtype), dev(k, dtype), dev(v, dtype), i32(table),
                         i32(st.kv_len), words, scale, err=err, **kw)
     assert int(err) == 0
     got = to_f64(out)
@@ -154,6 +157,31 @@ def test_rows_that_see_what_is_not_finite_and_rows_that_do_not(case, dtype):
             assert np.all(np.isnan(got[at]) if np.isnan(what) else got[at] == what), (at, what)
             hit[at] = True
     assert np.array_equal(got[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("columns", [130, 300, 1100])
+@pytest.mark.parametrize("case", CASES[2:], ids=lambda c: f"L{c[0][0]}x{len(c[0])}R{c[1]}H{c[2]}-{c[3]}D{c[4]}")
+def test_wide_tables(case, columns, dtype):
+    """A table of many more pages than the sequences have: items in parts, few or many shares."""
+    lens, R = case[:2]
+    vis, _, _ = ot.masks(random_parents(np.random.default_rng(R + columns), len(lens), R))
+    run(case, dtype, vis, i32(ot.words(vis)), columns=columns)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", [(40, 1, 4, 2, 64), (70, 5, 8, 2, 128), (33, 9, 8, 2, 96),
+                                  (64, 33, 4, 4, 64), (65, 40, 8, 2, 128), (48, 17, 8, 1, 96)],
+                         ids=lambda c: f"S{c[0]}R{c[1]}H{c[2]}-{c[3]}D{c[4]}")
+@pytest.mark.parametrize("columns", [0, 300])
+def test_ragged_batches(case, columns, dtype):
+    """Many sequences of nothing to 400 tokens, whole items or parts of them to a workgroup."""
+    S, R, *rest = case
+    rng = np.random.default_rng(S)
+    lens = [int(x) for x in rng.integers(0, 400, S)]
+    lens[3] = lens[S - 1] = 0
+    vis, _, _ = ot.masks(random_parents(rng, S, R))
+    run((lens, R, *rest), dtype, vis, i32(ot.words(vis)), columns=columns)
 
 
 def test_fp32_batches_that_give_every_wave_two_groups():
