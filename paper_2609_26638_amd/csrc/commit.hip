@@ -96,8 +96,15 @@ __device__ __forceinline__ int run_token(const CommitParams& p, int s, int A, in
 // and per dependent step); the results are the general path's.
 constexpr int COMMIT_FAST_W = 32;
 
-template <bool FAST>
-__device__ __forceinline__ void commit_body(const CommitParams& p, int threads) {
+// A sequence's state as tree_commit_kernel has it already: the words, loaded
+// before the acceptance, and the run in LDS (run_len < 0: no tree this step).
+struct TreeRun {
+  int kv_len, num_pages, out_count, finished, free_top, run_len;
+  const int* run;
+};
+
+template <bool FAST, bool TREE>
+__device__ __forceinline__ void commit_body(const CommitParams& p, int threads, const TreeRun& tree) {
   __shared__ int sh[COMMIT_THREADS];
   __shared__ int s_err;
   const int s = threadIdx.x;
@@ -110,8 +117,7 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads) 
   int last_tok = 0;
   constexpr int FW = FAST ? COMMIT_FAST_W : 1;
   int dv[FW], av[FW], nx[FW];   // FAST: draft row, verify top-1, next draft
-  int top0 = 0;
-  if (FAST) top0 = *p.free_top;
+  const int top0 = TREE ? tree.free_top : *p.free_top;
   if (FAST && live_seq) {
     const int nd = p.n_causal - 1;
     const int32_t* drow = p.draft + (size_t)s * p.draft_width;
@@ -157,10 +163,17 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads) 
     if (need > p.max_pages || n < 0 || n > p.max_pages || L < 0)
       atomicOr(&s_err, DVS_ERR_MAX_PAGES);
   } else if (!FAST && live_seq) {
-    L = p.kv_len[s];
-    n = p.num_pages[s];
-    cnt = p.out_count[s];
-    fin = p.finished[s] != 0 || (p.accept_len && p.accept_len[s] < p.idle_below);
+    if (TREE) {
+      L = tree.kv_len;
+      n = tree.num_pages;
+      cnt = tree.out_count;
+      fin = tree.finished != 0 || tree.run_len < 0;
+    } else {
+      L = p.kv_len[s];
+      n = p.num_pages[s];
+      cnt = p.out_count[s];
+      fin = p.finished[s] != 0 || (p.accept_len && p.accept_len[s] < p.idle_below);
+    }
     if (!fin && p.accept_here) {
       // longest prefix with d_j == a_j = argmax[s, j-1], j <= n_causal - 1,
       // compared RUN_CHUNK positions at a time (independent loads first)
@@ -184,7 +197,8 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads) 
     }
     if (live_seq && p.accept_here && p.accept_out) p.accept_out[s] = fin ? 0 : A;
     if (!fin) {
-      if (!p.accept_here) A = p.accept_len ? p.accept_len[s] : p.n_causal - 1;
+      if (TREE) A = tree.run_len;
+      else if (!p.accept_here) A = p.accept_len ? p.accept_len[s] : p.n_causal - 1;
       A = A < 0 ? 0 : (A > p.n_causal - 1 ? p.n_causal - 1 : A);
       // run = [a0,] d_1..d_A, a_{A+1} (last index jl); keep up to the first
       // stop token / budget.  Tokens are fetched RUN_CHUNK at a time
@@ -195,7 +209,8 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads) 
       for (int j0 = 0; j0 <= jl && !done; j0 += RUN_CHUNK) {
         int tk[RUN_CHUNK];
 #pragma unroll
-        for (int u = 0; u < RUN_CHUNK; ++u) tk[u] = run_token(p, s, A, min(j0 + u, jl));
+        for (int u = 0; u < RUN_CHUNK; ++u)
+          tk[u] = TREE ? tree.run[min(j0 + u, jl)] : run_token(p, s, A, min(j0 + u, jl));
 #pragma unroll
         for (int u = 0; u < RUN_CHUNK; ++u) {
           if (done || j0 + u > jl) continue;
@@ -221,7 +236,6 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads) 
   int tot_push = 0, tot_pop = 0;
   const int push_off = block_exclusive_scan(push, sh, threads, tot_push);
   const int pop_off = block_exclusive_scan(pop, sh, threads, tot_pop);
-  if (!FAST) top0 = *p.free_top;
   if (s == 0) {
     if (tot_pop > top0 + tot_push) atomicOr(&s_err, DVS_ERR_POOL_EXHAUSTED);
     if (top0 + tot_push > p.pool_pages || top0 < 0) atomicOr(&s_err, DVS_ERR_POOL_EXHAUSTED);
@@ -272,7 +286,8 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads) 
       for (int j0 = 0; j0 < k; j0 += RUN_CHUNK) {   // loads of a chunk first, then its stores
         int tk[RUN_CHUNK];
 #pragma unroll
-        for (int u = 0; u < RUN_CHUNK; ++u) tk[u] = run_token(p, s, A, min(j0 + u, k - 1));
+        for (int u = 0; u < RUN_CHUNK; ++u)
+          tk[u] = TREE ? tree.run[min(j0 + u, k - 1)] : run_token(p, s, A, min(j0 + u, k - 1));
 #pragma unroll
         for (int u = 0; u < RUN_CHUNK; ++u)
           if (j0 + u < k) ot[cnt + j0 + u] = tk[u];
@@ -299,7 +314,7 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads) 
 
 template <bool FAST>
 __global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(CommitParams p) {
-  commit_body<FAST>(p, blockDim.x);
+  commit_body<FAST, false>(p, blockDim.x, TreeRun{});
 }
 
 // Trees of at most 64 rows, a row a lane, TREES of them a wave at a time.  The
@@ -307,7 +322,9 @@ __global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(CommitParams 
 // is the number of bits below its own.
 constexpr int TREES = 4;
 
-__device__ __forceinline__ void accept_trees(const TreeCommit& t, int s0) {
+constexpr int RUN_LD = 65;   // a sequence's run in LDS: sequences side by side read the same place of theirs
+
+__device__ __forceinline__ void accept_trees(const TreeCommit& t, int s0, int* s_run, int* s_len) {
   const int lane = threadIdx.x & 63;
   int p[TREES], token[TREES], top[TREES], L[TREES], fin[TREES];
 #pragma unroll
@@ -340,18 +357,15 @@ __device__ __forceinline__ void accept_trees(const TreeCommit& t, int s0) {
     const size_t base = (size_t)s * t.R;
     if (lane == 0) {
       t.accept[s] = max(len - 1, 0);
-      t.run_len[s] = len - 1;
       t.old_len[s] = L[i];
+      s_len[s] = len - 1;
     }
     if (path >> lane & 1) {
       const int at = __popcll(path & ((1ull << lane) - 1));
       t.path[base + at] = lane;
-      t.run[base + at] = top[i];
+      s_run[s * RUN_LD + at] = top[i];
     }
-    if (lane >= len && lane < t.R) {
-      t.path[base + lane] = -1;
-      t.run[base + lane] = 0;
-    }
+    if (lane >= len && lane < t.R) t.path[base + lane] = -1;
     if (lane < t.n_window_pages) {
       const int pg = L[i] / DVS_PAGE_SIZE + lane;
       int id = L[i] >= 0 && pg < t.max_pages ? t.table[(size_t)s * t.max_pages + pg] : -1;
@@ -362,12 +376,15 @@ __device__ __forceinline__ void accept_trees(const TreeCommit& t, int s0) {
 }
 
 __global__ void __launch_bounds__(COMMIT_THREADS) tree_commit_kernel(CommitParams p, TreeCommit t) {
-  accept_trees(t, (threadIdx.x >> 6) * TREES);
-  __threadfence_block();
+  __shared__ int s_run[COMMIT_THREADS / 64 * TREES * RUN_LD], s_len[COMMIT_THREADS / 64 * TREES];
+  const int s = min((int)threadIdx.x, p.S - 1);
+  TreeRun tree{p.kv_len[s], p.num_pages[s], p.out_count[s], p.finished[s], *p.free_top, 0, s_run + s * RUN_LD};
+  accept_trees(t, (threadIdx.x >> 6) * TREES, s_run, s_len);
   __syncthreads();
   const int threads = (p.S + 63) / 64 * 64;
   if (__builtin_amdgcn_readfirstlane((int)threadIdx.x) >= threads) return;   // a whole wave
-  commit_body<false>(p, threads);
+  tree.run_len = s_len[s];
+  commit_body<false, true>(p, threads, tree);
 }
 
 }  // namespace dvs
@@ -438,8 +455,9 @@ int commit_tree_run(const dvs_state* st, const TreeCommit& t, void* stream) {
                        st->err_word, stream, &t);
 }
 
-// 16 waves of 4 trees of up to 64 rows (whole calls, us: 8 sequences of 64 rows 18.4,
-// by two launches 21.2; 64 of 33 rows 18.3 and 21.2).
+// 16 waves of 4 trees of up to 64 rows (whole calls, us: 8 sequences of 64 rows 17.5,
+// by two launches 21.2; 64 of 33 rows 17.8 and 21.2; the launch itself 7.3 and 8.7,
+// a chain of about six round trips to memory).
 bool tree_accept_in_commit(const TreeCommit& t) {
   return t.R <= 64 && t.S <= COMMIT_THREADS / 64 * TREES;
 }

@@ -211,6 +211,14 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _new_like(t, stream):
+    """The same for one of a contiguous tensor's shape and type (half a us less to ask for)."""
+    if stream is None:
+        return torch.empty_like(t)
+    with _on(stream):
+        return torch.empty_like(t)
+
+
 def _dev(t, dtype, name, ndim=None):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise DvsError(f"{name} must be a CUDA (HIP) tensor")
@@ -1112,7 +1120,7 @@ def tree_masks(parent, mask_out=None, depth_out=None, err=None, stream=None):
     elif _dev(mask_out, torch.int32, "mask_out").shape != shape:
         raise DvsError(f"mask_out must be {shape}")
     if depth_out is None:
-        depth_out = _new((S, R), torch.int32, parent.device, stream)
+        depth_out = _new_like(parent, stream)
     elif _dev(depth_out, torch.int32, "depth_out").shape != (S, R):
         raise DvsError("depth_out must be [S, R]")
     _check_err(err)
@@ -1212,7 +1220,7 @@ def attn_tree(q, k_pool, v_pool, page_table, kv_len, mask, softmax_scale: float,
     if mask is not None and _dev(mask, torch.int32, "mask").shape != (S, R, (R + 31) // 32):
         raise DvsError("mask must be [S, R, ceil(R / 32)]")
     if out is None:
-        out = _new(q.shape, dt, q.device, stream)
+        out = _new_like(q, stream)
     elif _dev(out, dt, "out").shape != q.shape:
         raise DvsError("out must be [S, R, Hq, D]")
     _check_err(err)
@@ -1250,7 +1258,7 @@ def accept_commit_tree(st: DeviceState, pools: KVPools, parent, tokens, argmax, 
     elif _dev(accept_out, torch.int32, "accept_out").shape != (S,):
         raise DvsError("accept_out must be [S]")
     if path_out is None:
-        path_out = _new((S, R), torch.int32, parent.device, stream)
+        path_out = _new_like(parent, stream)
     elif _dev(path_out, torch.int32, "path_out").shape != (S, R):
         raise DvsError("path_out must be [S, R]")
     _here(st.kv_len, parent, tokens, argmax, accept_out, path_out, pools.keep[0][0],
