@@ -773,8 +773,11 @@ int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const void* k_new
  *   the sequence then mean nothing).
  *   workspace >= dvs_tree_workspace_bytes(...) bytes on 256, no initialisation
  *   needed.  Calls that share it must not overlap in time.
- * Requirements: Hq % Hkv == 0, D in {64, 96, 128}, S >= 1, 1 <= R <= 1024, q,
- * out and the pools on 16 bytes, softmax_scale > 0.
+ * Requirements: Hq % Hkv == 0, D in {64, 96, 128}, S >= 1, 1 <= R <= 1024,
+ * R * Hq <= 2^20, R * Hq * max_pages < 2^30, q, out and the pools on 16 bytes,
+ * softmax_scale > 0.  Sequences, masks and page tables of any width; the choice
+ * of kernels goes by the sizes above, the longest table among them, not by
+ * kv_len.
  * ---------------------------------------------------------------------- */
 size_t dvs_tree_workspace_bytes(int32_t S, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
                                 int32_t max_pages, int32_t dtype);

@@ -16,7 +16,7 @@ __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
 }
 
 constexpr int MAX_SEQS = 1024;      // sequences a launch takes
-constexpr float RESCALE_LOG2 = 8.f, WEIGHT_MAX = 8 * 256.f;
+constexpr float WEIGHT_MAX = 2048.f, RESCALE_LOG2 = 11.5f;   // (2^11.5 is above the first)
 constexpr int TILE_ROWS = 32;   // query rows of a KV head above which tiles go through LDS
 constexpr int MERGE_FEW = 1024; // row groups up to which the merge takes more waves
 
@@ -135,10 +135,11 @@ __device__ __forceinline__ uint32_t seen_bits(const TreeAttn& p, const uint32_t*
 // One tile's softmax: scores to weights 2^(s - m).  m is a reference, not the
 // maximum so far: any m will do that keeps the weights in range, and the
 // division by l is exact about it.  So a tile takes m as it is, and only where
-// a lane's weights add up to more than 8 x 2^RESCALE_LOG2 (or to no number: m
-// starts at -inf) the rows' maxima are found, m moves to those that exceed it by
-// RESCALE_LOG2, and the tile's weights are made again (long documents 540 us with
-// the maxima of every tile, 458 without).
+// a lane's weights add up to more than WEIGHT_MAX (or to no number: m starts at
+// -inf) the rows' maxima are found, m moves to those that exceed it by RESCALE_LOG2,
+// and the tile's weights are made again (long documents 540 us with the maxima
+// of every tile, 458 without).  A row that moves would have called for it by
+// itself: what it gives does not depend on the rows beside it.
 template <typename T>
 struct Weights;
 template <>
@@ -348,7 +349,13 @@ struct Rows {
         for (int g = 0; g < NG; ++g) bits[g] |= mask(p, s, g)[i];
     }
 #pragma unroll
-    for (int g = 0; g < NG; ++g) any[g] = valid(p, g) && bits[g] != 0;
+    for (int g = 0; g < NG; ++g) {
+      any[g] = valid(p, g) && bits[g] != 0;
+      // (padding: NaN there would take every tile's slower way)
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+        if (!any[g]) q[g][i] = u32x4{0, 0, 0, 0};
+    }
   }
 };
 
@@ -677,7 +684,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
 //
 // What bounds it, long documents (256 rows, 1.44 GB, 0.36 PFLOP): the copies alone
 // take 253 us and the arithmetic alone 309, but with both at once the clock
-// falls from 2.4 to 1.9 GHz and the whole takes 445.  Taking the softmax and the
+// falls from 2.4 to 1.9 GHz and the whole takes 410 - 430.  Taking the softmax and the
 // products in turns by two halves of the waves, 32x32 products, reads ahead of
 // their use and 64 rows a wave were all tried: 442 - 530.
 //
@@ -1116,6 +1123,7 @@ extern "C" int attn_tree(const void* q, const void* k_pool, const void* v_pool,
     set_error("attn_tree: workspace needs %zu bytes, got %zu", pl.bytes, ws_bytes);
     return DVS_EWORKSPACE;
   }
+  DVS_CHECK_ARG(((uintptr_t)workspace & 255) == 0, "attn_tree: workspace must start on 256 bytes");
   TreeAttn p{};
   p.k_pool = k_pool; p.v_pool = v_pool; p.err = err_word;
   p.R = R; p.W = (R + 31) / 32; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.rows = R * p.G;

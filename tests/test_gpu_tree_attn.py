@@ -128,7 +128,8 @@ def test_many_rows(case):
 @pytest.mark.parametrize("case", [([40, 7], 9, 4, 2, 64), ([100, 31], 20, 4, 2, 128),
                                   ([70, 300], 30, 8, 2, 96), ([33], 40, 16, 2, 128)],
                          ids=lambda c: f"R{c[1]}H{c[2]}-{c[3]}D{c[4]}")
-def test_rows_that_see_what_is_not_finite_and_rows_that_do_not(case, dtype):
+@pytest.mark.parametrize("columns", [0, 1100, 4200])
+def test_rows_that_see_what_is_not_finite_and_rows_that_do_not(case, columns, dtype):
     """A drafted token's infinite or NaN value reaches its own row and its descendants', in the
     elements that have it; the other rows' results stay the bits that they are without it."""
     lens, R, Hq, Hkv, D = case
@@ -146,7 +147,8 @@ def test_rows_that_see_what_is_not_finite_and_rows_that_do_not(case, dtype):
             bad[st.page_table[s, (L + r) // 16], hk, d, (L + r) % 16] = what
             planted.append((s, r, hk, d, what))
     words, scale = dvs.tree_masks(i32(parent))[0], 1 / math.sqrt(D)
-    args = i32(st.page_table), i32(st.kv_len), words, scale
+    table = np.pad(st.page_table, ((0, 0), (0, max(0, columns - st.page_table.shape[1]))))
+    args = i32(table), i32(st.kv_len), words, scale
     want = to_f64(dvs.attn_tree(q, dev(k, dtype), dev(v, dtype), *args)).copy()
     got = to_f64(dvs.attn_tree(q, dev(k, dtype), dev(bad, dtype), *args))
     G = Hq // Hkv
@@ -157,6 +159,33 @@ def test_rows_that_see_what_is_not_finite_and_rows_that_do_not(case, dtype):
             assert np.all(np.isnan(got[at]) if np.isnan(what) else got[at] == what), (at, what)
             hit[at] = True
     assert np.array_equal(got[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("columns", [0, 1100, 4200])
+@pytest.mark.parametrize("R,Hq,D", [(14, 4, 64), (30, 8, 128)])
+def test_padded_queries_may_hold_anything(R, Hq, D, columns, dtype):
+    """The other rows' results are the same bits whatever padded rows hold; so are those of rows
+    beside one whose scores are large."""
+    rng = np.random.default_rng(R)
+    lens = [500, 90]
+    st, k, v = cache(R, lens, R, 2, D, dtype)
+    parent = random_parents(rng, 2, R, padding=False)
+    parent[:, R // 2::3] = -2
+    parent[:, R - 1] = 0
+    vis, _, _ = ot.masks(parent)
+    table = np.pad(st.page_table, ((0, 0), (0, max(0, columns - st.page_table.shape[1]))))
+    args = (dev(k, dtype), dev(v, dtype), i32(table), i32(st.kv_len), i32(ot.words(vis)), D ** -0.5)
+    q = rounded(rng.standard_normal((2, R, Hq, D)), dtype)
+    want = to_f64(dvs.attn_tree(dev(q, dtype), *args))
+    for what in (np.nan, np.inf, 1e30):
+        other = q.copy()
+        other[~vis.any(-1)] = rounded(what, dtype)
+        other[:, R - 1] = rounded(40 * q[:, R - 1], dtype)
+        got = to_f64(dvs.attn_tree(dev(other, dtype), *args))
+        assert np.all(got[~vis.any(-1)] == 0)
+        np.testing.assert_array_equal(got[:, :R - 1], want[:, :R - 1])
+        assert np.all(np.isfinite(got))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -171,7 +200,8 @@ def test_wide_tables(case, columns, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("case", [(40, 1, 4, 2, 64), (70, 5, 8, 2, 128), (33, 9, 8, 2, 96),
-                                  (64, 33, 4, 4, 64), (65, 40, 8, 2, 128), (48, 17, 8, 1, 96)],
+                                  (64, 33, 4, 4, 64), (65, 40, 8, 2, 128), (48, 17, 8, 1, 96),
+                                  (100, 33, 8, 4, 64), (90, 40, 6, 2, 96), (70, 40, 8, 2, 96)],
                          ids=lambda c: f"S{c[0]}R{c[1]}H{c[2]}-{c[3]}D{c[4]}")
 @pytest.mark.parametrize("columns", [0, 300])
 def test_ragged_batches(case, columns, dtype):

@@ -60,7 +60,9 @@ def _attn(**kw):
     (dict(Hkv=0), -1), (dict(D=32), -2), (dict(max_pages=0), -1), (dict(pool=0), -1),
     (dict(scale=0.0), -1), (dict(scale=float("nan")), -1), (dict(dtype=3), -2), (dict(ws=N), -4),
     (dict(nbytes=16), -4), (dict(q=ctypes.c_void_p(0x1008)), -1),
-    (dict(vp=ctypes.c_void_p(0x1004)), -1), (dict(out=ctypes.c_void_p(0x1002)), -1)])
+    (dict(vp=ctypes.c_void_p(0x1004)), -1), (dict(out=ctypes.c_void_p(0x1002)), -1),
+    (dict(ws=ctypes.c_void_p(0x1080)), -1), (dict(Hq=1 << 20, Hkv=1, R=2), -2),
+    (dict(max_pages=1 << 28), -2)])
 def test_attn_tree_refuses(kw, rc):
     assert _attn(**kw) == rc
     assert b"attn_tree" in dvs.lib().dvs_last_error()
