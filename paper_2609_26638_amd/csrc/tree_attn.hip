@@ -17,7 +17,6 @@ __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
 
 constexpr int MAX_SEQS = 1024;      // sequences a launch takes
 constexpr float WEIGHT_MAX = 2048.f, RESCALE_LOG2 = 11.5f;   // (2^11.5 is above the first)
-constexpr int TILE_ROWS = 32;   // query rows of a KV head above which tiles go through LDS
 constexpr int MERGE_FEW = 1024; // row groups up to which the merge takes more waves
 
 struct TreeAttn {
@@ -26,7 +25,7 @@ struct TreeAttn {
   void* out;
   int32_t* err;
   int S, R, W, Hq, Hkv, G, rows, n_rt, max_pages, pool_pages;
-  int n_wide, wide_waves;   // row tiles of a workgroup's waves (0: waves on their own)
+  int n_wide;      // workgroups of NW waves over an item's rows (0: tiles not through LDS)
   int split;       // items are cut where a wave's share ends, and merged by a launch of its own
   int share_min;   // tiles of a share, at least
   float scale_log2;
@@ -512,7 +511,7 @@ __device__ __forceinline__ void finish_together(const TreeAttn& p, int s, const 
 }
 
 // ---------------------------------------------------------------------------
-// Few query rows of a KV head: a workgroup takes NG groups of 16 of them and a run
+// Few query rows of a KV head, or few tiles: a workgroup takes NG groups of 16 of them and a run
 // of key tiles, a quarter of it a wave, straight from the cache into registers:
 // the next tile's keys are on their way under this one's softmax, its values
 // under the next one's scores.  The waves' results are joined in LDS (a wave on
@@ -673,14 +672,10 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
 }
 
 // ---------------------------------------------------------------------------
-// Many query rows of a KV head (bf16): a workgroup of NW waves, 32 rows each, over
-// 32-key tiles that all of them read from LDS, copied there straight from the
-// cache, STAGES tiles at a time.  The next tile's scores are made under this
-// tile's softmax (matrix and vector unit), then this tile's values are added.
-//
-// Up to 128 rows: four waves, two workgroups a CU; more: eight waves over 256
-// rows, whose tiles go through LDS once where two workgroups would each copy
-// them (long documents 460 -> 441 us).
+// Many query rows of a KV head (bf16): a workgroup of eight waves, 16 or 32 rows
+// each, over 32-key tiles that all of them read from LDS, copied there straight
+// from the cache, STAGES tiles at a time.  The next tile's scores are made under
+// this tile's softmax (matrix and vector unit), then this tile's values are added.
 //
 // What bounds it, long documents (256 rows, 1.44 GB, 0.36 PFLOP): the copies alone
 // take 253 us and the arithmetic alone 309, but with both at once the clock
@@ -714,16 +709,19 @@ __device__ __forceinline__ void barrier() {   // without a wait for this wave's 
   asm volatile("" ::: "memory");
 }
 
-template <int D, int NW>
+constexpr int NW = 8;   // its waves
+
+template <int D, int NG>
 __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) {
-  constexpr int KEYS = 32, NG = 2, DG = D / 16, STAGES = NW == 8 ? 6 : 4;
+  constexpr int KEYS = 32, DG = D / 16, STAGES = 6;
   constexpr int PAGE_B = 32 * D, TILE_B = 2 * PAGE_B;   // bytes of a page, of a tile's K (or V)
   constexpr int SEGS = PAGE_B / 1024;                   // copies of 1 KB a page
-  constexpr int NPL = 4 * SEGS / NW;                    // of a wave a tile: all of one page, or a part
-  static_assert(4 * SEGS % NW == 0 && SEGS % NPL == 0, "copies");
+  // copies of a wave a tile, all of one page: half a page, or where that is no
+  // whole number (three to a page) two, and the third by the other wave, twice
+  constexpr int NPL = (SEGS + 1) / 2;
   constexpr int STAGE_B = 2 * TILE_B;
-  __shared__ __attribute__((aligned(1024))) char st0[STAGE_B], st1[STAGE_B], st2[STAGE_B], st3[STAGE_B],
-      st4[STAGES > 4 ? STAGE_B : 16], st5[STAGES > 4 ? STAGE_B : 16];
+  __shared__ __attribute__((aligned(1024))) char st0[STAGE_B], st1[STAGE_B], st2[STAGE_B], st3[STAGE_B], st4[STAGE_B],
+      st5[STAGE_B];
   __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[4];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, quarter = lane >> 4;
@@ -735,12 +733,13 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
   int u = __builtin_amdgcn_readfirstlane(sh.u);
   // copies: pages 0, 1 of K, then of V; lane's source offset in the page, of
   // its 16 bytes of each 1 KB
-  const int cpage = w * NPL / SEGS, cseg = w * NPL % SEGS;
+  const int cpage = w >> 1;
+  auto seg = [&](int i) { return min((w & 1) * NPL + i, SEGS - 1); };
   const char* pool = (const char*)(cpage < 2 ? p.k_pool : p.v_pool);
   uint32_t soff[NPL];
 #pragma unroll
   for (int i = 0; i < NPL; ++i) {
-    const int off = (cseg + i) * 1024 + lane * 16;
+    const int off = seg(i) * 1024 + lane * 16;
     if (cpage < 2) {
       const int row = off / (2 * D), c = (off - row * 2 * D) >> 4;
       soff[i] = row * 2 * D + ((c ^ k_swizzle<D>(cpage * 16 + row)) << 4);
@@ -805,11 +804,11 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
       }
       const int id = __builtin_amdgcn_readlane(ids, j - ids_at);
       const char* base = pool + ((size_t)(uint32_t)id * p.Hkv + kvh) * PAGE_B;
-      char* to = stage + (w * NPL) * 1024;
+      char* to = stage + cpage * PAGE_B;
 #pragma unroll
       for (int i = 0; i < NPL; ++i)
         __builtin_amdgcn_global_load_lds((const void*)(base + soff[i]),
-                                         (__attribute__((address_space(3))) void*)(to + i * 1024), 16, 0, 0);
+                                         (__attribute__((address_space(3))) void*)(to + seg(i) * 1024), 16, 0, 0);
     };
     auto scores = [&](const char* tile, f32x4 (&sc)[NG][2]) {
 #pragma unroll
@@ -836,8 +835,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
       constexpr bool MASKED = decltype(masked)::value != 0, LAST = decltype(last)::value != 0;
       if constexpr (!LAST) {
         if (j + STAGES - 2 < j1) wait_loads<(STAGES - 3) * NPL>();
-        else if (STAGES > 4 && j + 3 < j1) wait_loads<2 * NPL>();
-        else if (STAGES > 4 && j + 2 < j1) wait_loads<NPL>();
+        else if (j + 3 < j1) wait_loads<2 * NPL>();
+        else if (j + 2 < j1) wait_loads<NPL>();
         else wait_loads<0>();
         barrier();
         if (j + STAGES - 1 < j1) issue(free, j + STAGES - 1);
@@ -884,7 +883,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
       if (j0 + decltype(c)::value < j1) issue(stage(c), j0 + decltype(c)::value);
     });
     if (j0 + STAGES - 2 < j1) wait_loads<(STAGES - 2) * NPL>();
-    else if (STAGES > 4 && j0 + 3 < j1) wait_loads<3 * NPL>();
+    else if (j0 + 3 < j1) wait_loads<3 * NPL>();
     else if (j0 + 2 < j1) wait_loads<2 * NPL>();
     else if (j0 + 1 < j1) wait_loads<NPL>();
     else wait_loads<0>();
@@ -945,7 +944,7 @@ __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
   const int nseg = mt.x, first = mt.y;
   if (nseg <= 1) return;
   const int n = (rt * NG + g) * 16 + m16;
-  const int step = p.n_wide ? p.n_wide * p.wide_waves : 1;   // from a share's slot to the next one's
+  const int step = p.n_wide ? p.n_wide * NW : 1;   // from a share's slot to the next one's
   auto slot = [&](int c) { return (size_t)(first + c * step) * 2 + (c == 0 ? 1 : 0); };
   auto ml_of = [&](int c) { return *(const f32x2*)(p.part_ml + ((slot(c) * NG + g) * 16 + m16) * 2); };
   f32x4 acc[NQ];
@@ -993,7 +992,7 @@ __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
 }
 
 struct TreePlan {
-  int ng, n_rt, n_wide, waves, grid, split, share_min, seqs;   // seqs: sequences a launch takes
+  int ng, n_rt, n_wide, grid, split, share_min, seqs;   // seqs: sequences a launch takes
   size_t off_ml, off_o, bytes;
 };
 
@@ -1017,21 +1016,25 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
   // 16 of 300-900, 128 rows 21.2 / 28.3.
   const long long a_wave = (long long)std::min(S, MAX_SEQS) * Hkv * ((rows + 15) / 16) * max_tiles / (8 * cus);
   const bool few = a_wave < (max_tiles <= 32 ? 8 : 4);
-  const bool wide = dtype == DVS_BF16 && rows > TILE_ROWS && !few;
-  pl.ng = rows > 16 && !few ? 2 : 1;
+  // Tiles through LDS otherwise, for more than 16 rows (us, waves on their own /
+  // through LDS: 32 rows, 32 sequences of 1k-8k 73.2 / 69.5, 16 of 3k-6k 44.6 / 38.5;
+  // 16 rows, 32 of 1k-8k 64.7 / 66.5), in short tables for more than 32 (32 rows,
+  // 256 of 100-400 38.9 / 44.4).
+  const bool wide = dtype == DVS_BF16 && !few && rows > (max_tiles <= 32 ? 32 : 16);
+  pl.ng = !few && rows > (wide ? NW * 16 : 16) ? 2 : 1;
   pl.n_rt = (rows + pl.ng * 16 - 1) / (pl.ng * 16);
   const long long per_seq = (long long)Hkv * pl.n_rt * max_tiles;
   pl.seqs = (int)std::max<long long>(1, std::min<long long>({S, MAX_SEQS, (1LL << 30) / per_seq,
                                                              (1LL << 22) / ((long long)Hkv * pl.n_rt)}));
   const long long items = (long long)pl.seqs * Hkv * pl.n_rt;
-  // (waves on their own, us, against tiles in LDS: 64 rows, 32 sequences of 1k-8k
-  // 108 / 79; 256 rows, 8 of 1k-2k 38.5 / 34.8; 60 rows, 16 of 1k-4k 30.3 / 29.3)
+  // Through LDS: a workgroup a CU, whose waves take 16 rows each up to 128 rows, 32
+  // beyond (128 rows, two workgroups of four waves of 32 / eight of 16, us: 32 of 1k-8k
+  // 92 / 87.5, 64 of 1k-1.9k 66.8 / 48.5); two workgroups where the registers are enough
+  // (heads of 64, 128 rows, 32 of 1k-8k, one / two 54.7 / 51.0).
   if (wide) {
-    pl.waves = rows > 128 && D != 96 ? 8 : 4;
-    pl.n_wide = (pl.n_rt + pl.waves - 1) / pl.waves;
-    pl.grid = std::max(1, (pl.waves == 8 ? 1 : 2) * cus / pl.n_wide);
+    pl.n_wide = (pl.n_rt + NW - 1) / NW;
+    pl.grid = std::max(1, (D == 64 && pl.ng == 1 ? 2 : 1) * cus / pl.n_wide);
   } else {
-    pl.waves = 1;
     pl.grid = 2 * cus;
   }
   // Whole items, and no merge, where a wave's tiles then are at most 8 more than
@@ -1050,7 +1053,7 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
   pl.grid = (int)std::min<long long>(pl.grid, pl.split ? (tiles + pl.share_min - 1) / pl.share_min : units);
   if (wide) pl.grid *= pl.n_wide;
   if (pl.split) {
-    const size_t slots = (size_t)pl.grid * pl.waves * 2;
+    const size_t slots = (size_t)pl.grid * (wide ? NW : 1) * 2;
     pl.off_ml = al256((size_t)items * sizeof(int2));
     pl.off_o = pl.off_ml + al256(slots * pl.ng * 16 * 2 * sizeof(float));
     pl.bytes = pl.off_o + slots * pl.ng * 16 * D * sizeof(float);
@@ -1073,10 +1076,8 @@ template <typename T, int D>
 static void launch_tree(const TreePlan& pl, const TreeAttn& p, hipStream_t st) {
   if (pl.n_wide) {
     if constexpr (sizeof(T) == 2) {
-      // (a page of 96-wide heads is three copies, which eight waves cannot share evenly)
-      if constexpr (D != 96)
-        if (pl.waves == 8) hipLaunchKernelGGL((tree_attn_tile_kernel<D, 8>), dim3(pl.grid), dim3(512), 0, st, p);
-      if (pl.waves == 4) hipLaunchKernelGGL((tree_attn_tile_kernel<D, 4>), dim3(pl.grid), dim3(256), 0, st, p);
+      if (pl.ng == 2) hipLaunchKernelGGL((tree_attn_tile_kernel<D, 2>), dim3(pl.grid), dim3(NW * 64), 0, st, p);
+      else hipLaunchKernelGGL((tree_attn_tile_kernel<D, 1>), dim3(pl.grid), dim3(NW * 64), 0, st, p);
     }
   } else {
     if (pl.ng == 2) hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 2>), dim3(pl.grid), dim3(256), 0, st, p);
@@ -1128,7 +1129,7 @@ extern "C" int attn_tree(const void* q, const void* k_pool, const void* v_pool,
   p.k_pool = k_pool; p.v_pool = v_pool; p.err = err_word;
   p.R = R; p.W = (R + 31) / 32; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.rows = R * p.G;
   p.n_rt = pl.n_rt; p.max_pages = max_pages; p.pool_pages = num_pool_pages;
-  p.n_wide = pl.n_wide; p.wide_waves = pl.waves; p.split = pl.split; p.share_min = pl.share_min;
+  p.n_wide = pl.n_wide; p.split = pl.split; p.share_min = pl.share_min;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
   p.meta = (int2*)workspace;
   p.part_ml = (float*)((char*)workspace + pl.off_ml);
