@@ -185,10 +185,10 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stream(stream=None):
+def _stream(stream=None, dev=None):
     # (the current stream's handle without an object for it: 0.1 us a call, not 3)
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if dev is None else dev)
     return stream.cuda_stream
 
 
@@ -425,11 +425,12 @@ def top1_confidence(logits, argmax_out=None, conf_out=None, err=None, stream=Non
 # ---------------------------------------------------------------------------
 
 def _here(*tensors):
-    """Refuses tensors that are not on the current device, whose stream takes the call."""
+    """Refuses tensors that are not on the current device, whose stream takes the call; the device."""
     dev = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise DvsError(f"tensors must be on the current device {dev}, got {t.device}")
+    return dev
 
 
 def _scratch(workspace, nbytes, device, stream):
@@ -1124,9 +1125,9 @@ def tree_masks(parent, mask_out=None, depth_out=None, err=None, stream=None):
     elif _dev(depth_out, torch.int32, "depth_out").shape != (S, R):
         raise DvsError("depth_out must be [S, R]")
     _check_err(err)
-    _here(parent, mask_out, depth_out, err)
-    rc = lib().tree_masks(_ptr(parent), S, R, _ptr(mask_out), _ptr(depth_out), _ptr(err),
-                          _stream(stream))
+    dev = _here(parent, mask_out, depth_out, err)
+    rc = lib().tree_masks(parent.data_ptr(), S, R, mask_out.data_ptr(), depth_out.data_ptr(), _ptr(err),
+                          _stream(stream, dev))
     _check(rc, "tree_masks")
     return mask_out, depth_out
 
@@ -1191,12 +1192,12 @@ def kv_append_rope(q, k_new, v_new, k_pool, v_pool, page_table, kv_len, depth=No
     if depth is not None and _dev(depth, torch.int32, "depth").shape != (S, R):
         raise DvsError("depth must be [S, R]")
     _check_err(err)
-    _here(q, k_new, v_new, k_pool, v_pool, page_table, kv_len, depth, q_out, err)
-    rc = lib().kv_append_rope(_ptr(q), *qs, _ptr(k_new), *ks, _ptr(v_new), *vs, _ptr(k_pool),
-                              _ptr(v_pool), _ptr(page_table), _ptr(kv_len), _ptr(depth), S, R, Hq,
+    dev = _here(q, k_new, v_new, k_pool, v_pool, page_table, kv_len, depth, q_out, err)
+    rc = lib().kv_append_rope(_ptr(q), *qs, k_new.data_ptr(), *ks, v_new.data_ptr(), *vs, k_pool.data_ptr(),
+                              v_pool.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(), _ptr(depth), S, R, Hq,
                               Hkv, D, D if rot_dim is None else int(rot_dim), float(theta),
                               page_table.shape[1], P, _dtype_code(k_new), _ptr(q_out), _ptr(err),
-                              _stream(stream))
+                              _stream(stream, dev))
     _check(rc, "kv_append_rope")
     return q_out
 
@@ -1224,15 +1225,15 @@ def attn_tree(q, k_pool, v_pool, page_table, kv_len, mask, softmax_scale: float,
     elif _dev(out, dt, "out").shape != q.shape:
         raise DvsError("out must be [S, R, Hq, D]")
     _check_err(err)
-    _here(q, k_pool, v_pool, page_table, kv_len, mask, out, err, _buf(workspace))
+    dev = _here(q, k_pool, v_pool, page_table, kv_len, mask, out, err, _buf(workspace))
     code = _dtype_code(q)
     ws = workspace.buf if workspace is not None else _new(
         max(1, tree_workspace_bytes(S, R, Hq, Hkv, D, page_table.shape[1], code)), torch.uint8,
         q.device, stream)
-    rc = lib().attn_tree(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(page_table), _ptr(kv_len),
+    rc = lib().attn_tree(q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(),
                          _ptr(mask), S, R, Hq, Hkv, D, page_table.shape[1], P,
-                         float(softmax_scale), code, _ptr(out), _ptr(err), _ptr(ws), ws.numel(),
-                         _stream(stream))
+                         float(softmax_scale), code, out.data_ptr(), _ptr(err), ws.data_ptr(), ws.numel(),
+                         _stream(stream, dev))
     _check(rc, "attn_tree")
     return out
 
@@ -1261,15 +1262,15 @@ def accept_commit_tree(st: DeviceState, pools: KVPools, parent, tokens, argmax, 
         path_out = _new_like(parent, stream)
     elif _dev(path_out, torch.int32, "path_out").shape != (S, R):
         raise DvsError("path_out must be [S, R]")
-    _here(st.kv_len, parent, tokens, argmax, accept_out, path_out, pools.keep[0][0],
-          _buf(workspace))
+    dev = _here(st.kv_len, parent, tokens, argmax, accept_out, path_out, pools.keep[0][0],
+                _buf(workspace))
     ws = workspace.buf if workspace is not None else _new(
         max(1, accept_tree_workspace_bytes(S, R)), torch.uint8, parent.device, stream)
     sd = _state_desc(st, eos_id)
     rc = lib().accept_commit_tree(ctypes.byref(sd), pools.layers, len(pools.layers),
-                                  pools.n_kv_heads, pools.head_dim, pools.dtype, R, _ptr(parent),
-                                  _ptr(tokens), _ptr(argmax), _ptr(accept_out), _ptr(path_out),
-                                  _ptr(ws), ws.numel(), _stream(stream))
+                                  pools.n_kv_heads, pools.head_dim, pools.dtype, R, parent.data_ptr(),
+                                  tokens.data_ptr(), argmax.data_ptr(), accept_out.data_ptr(), path_out.data_ptr(),
+                                  ws.data_ptr(), ws.numel(), _stream(stream, dev))
     _check(rc, "accept_commit_tree")
     return accept_out, path_out
 
