@@ -27,7 +27,6 @@ struct TreeAttn {
   int S, R, W, Hq, Hkv, G, rows, n_rt, max_pages, pool_pages;
   int n_wide;      // workgroups of NW waves over an item's rows (0: tiles not through LDS)
   int split;       // items are cut where a wave's share ends, and merged by a launch of its own
-  int share_min;   // tiles of a share, at least
   float scale_log2;
   float* part_o;   // [slot][quad][lane] x 4
   float* part_ml;  // [slot][group][lane] x (m, l)
@@ -276,33 +275,44 @@ __device__ __forceinline__ SeqTiles seq_tiles(const TreeAttn& p, int keys, int* 
   return SeqTiles{p.S, s_seq[p.S], 0, 0, s_seq, s_len, true};
 }
 
-// The key tiles [u, u_end) of share `id` of n, in order of sequences, then items of
-// a sequence (per_seq of them).  Split: equal shares of at least share_min
-// tiles, which cut items; else whole items.
+// Consecutive workgroups on one XCD (blockIdx goes round the eight): row tiles
+// of an item then find its keys in their L2.
+__device__ __forceinline__ int xcd_block(int n) {   // of n workgroups
+  const int q = n >> 3, rem = n & 7, x = blockIdx.x & 7, i = blockIdx.x >> 3;
+  return x * q + min(x, rem) + i;
+}
+
+// This workgroup's share of the key tiles, in order of sequences, then items of a
+// sequence (per_seq of them): [u, u_end) of share `id`, whose row tile is rt of
+// `wide`.  Split: equal shares, which cut items; else whole items.
+// A share has some tiles at least, by the sequences' mean length: the merge grows
+// with the parts of an item (us, one sequence, one row: 16000 keys in shares of 8 /
+// 16 / 32 tiles 27.4 / 21.4 / 23.5, 8000 of 8 / 10 18.6 / 18.0; 8 of 100-400, 128 rows, 4
+// / 8 21.7 / 24.7).  Workgroups that this leaves without any are the last, so that
+// the others lie on all XCDs (one of 16000: 28 on three of them, 21.7 on all; 8
+// of 500 in tables of 32768, 16 rows, 20.4 / 10.7).
 struct Share {
-  int u, u_end, size;
+  int id, rt, u, u_end, size;
 };
-__device__ __forceinline__ Share share_of(const TreeAttn& p, const SeqTiles& seqs, int per_seq, int id, int n) {
+__device__ __forceinline__ Share share_of(const TreeAttn& p, const SeqTiles& seqs, int per_seq, int wide) {
   const int U = seqs.total * per_seq;
+  int n = gridDim.x / wide, size = 1;
   if (p.split) {
-    const int size = max((U + n - 1) / n, p.share_min);
-    const int u = (int)min((long long)id * size, (long long)U);
-    return Share{u, min(u + size, U), size};
+    const int mean = seqs.total / p.S;
+    const int least = p.n_wide ? (mean <= 32 ? 4 : max(8, mean / 64)) : max(4, mean / 24);
+    size = max((U + n - 1) / n, least);
+    n = (U + size - 1) / size;
   }
+  if ((int)blockIdx.x >= n * wide) return Share{0, 0, 0, 0, size};
+  const int block = xcd_block(n * wide), id = block / wide, rt = block - id * wide;
+  if (p.split) return Share{id, rt, id * size, (int)min((long long)(id + 1) * size, (long long)U), size};
   auto start = [&](uint32_t i) {
     const int s = i / per_seq;
     if (s >= p.S) return U;
     return seqs.before(s) * per_seq + (int)(i - s * per_seq) * (seqs.before(s + 1) - seqs.before(s));
   };
   const uint32_t items = p.S * per_seq;   // at most 2^22, n at most 2 a CU
-  return Share{start(id * items / n), start((id + 1) * items / n), 1};
-}
-
-// Consecutive workgroups on one XCD (blockIdx goes round the eight): row tiles
-// of an item then find its keys in their L2.
-__device__ __forceinline__ int xcd_block() {
-  const int n = gridDim.x, q = n >> 3, rem = n & 7, x = blockIdx.x & 7, i = blockIdx.x >> 3;
-  return x * q + min(x, rem) + i;
+  return Share{id, rt, start(id * items / n), start((id + 1) * items / n), size};
 }
 
 // A lane's NG query rows: row n of a KV head is window row n / G, head n % G of
@@ -535,9 +545,9 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, quarter = lane >> 4;
   const int HN = p.Hkv * p.n_rt;
-  const int share_id = xcd_block(), n_shares = gridDim.x;
   const SeqTiles seqs = seq_tiles(p, KEYS, s_seq, s_len, s_tot);
-  const Share sh = share_of(p, seqs, HN, share_id, n_shares);
+  const Share sh = share_of(p, seqs, HN, 1);
+  const int share_id = __builtin_amdgcn_readfirstlane(sh.id);
   const int u_end = __builtin_amdgcn_readfirstlane(sh.u_end), share = __builtin_amdgcn_readfirstlane(sh.size);
   int u = __builtin_amdgcn_readfirstlane(sh.u);
   const char* kp = (const char*)p.k_pool;
@@ -703,8 +713,11 @@ __device__ __forceinline__ void wait_loads() {   // at most N vector loads on th
   __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
 }
 
-__device__ __forceinline__ void barrier() {   // without a wait for this wave's loads
+// Without a wait for this wave's copies; its reads of LDS have ended (what they
+// read may be overwritten once every wave is past).
+__device__ __forceinline__ void barrier() {
   asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -725,10 +738,9 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
   __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[4];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, quarter = lane >> 4;
-  const int block = xcd_block(), n_shares = gridDim.x / p.n_wide;
-  const int share_id = block / p.n_wide, rt = block - share_id * p.n_wide;
   const SeqTiles seqs = seq_tiles(p, KEYS, s_seq, s_len, s_tot);
-  const Share sh = share_of(p, seqs, p.Hkv, share_id, n_shares);
+  const Share sh = share_of(p, seqs, p.Hkv, p.n_wide);
+  const int share_id = __builtin_amdgcn_readfirstlane(sh.id), rt = __builtin_amdgcn_readfirstlane(sh.rt);
   const int u_end = __builtin_amdgcn_readfirstlane(sh.u_end), share = __builtin_amdgcn_readfirstlane(sh.size);
   int u = __builtin_amdgcn_readfirstlane(sh.u);
   // copies: pages 0, 1 of K, then of V; lane's source offset in the page, of
@@ -992,7 +1004,7 @@ __global__ void __launch_bounds__(256) tree_attn_merge_kernel(TreeAttn p) {
 }
 
 struct TreePlan {
-  int ng, n_rt, n_wide, grid, split, share_min, seqs;   // seqs: sequences a launch takes
+  int ng, n_rt, n_wide, grid, split, seqs;   // seqs: sequences a launch takes
   size_t off_ml, off_o, bytes;
 };
 
@@ -1042,15 +1054,12 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
   // whole, us: 64 sequences of 200-500, 16 rows 20.3 / 13.1; 256 of 100-400, 32 rows
   // 58.6 / 38.5; 128 of 500-1900 87.9 / 75.1).  Only tables of up to 64 tiles: lengths
   // differ, and a long one must not be left to a wave.
-  // Tiles of a share, at least: the merge grows with the parts of an item (one
-  // sequence of 16000, one row, 8 / 16 / 32 tiles 27.4 / 21.4 / 23.5 us).
   const int per = wide ? 1 : 4;   // waves that share a segment's tiles
   const long long units = (long long)pl.seqs * Hkv * (wide ? 1 : pl.n_rt), tiles = units * max_tiles;
   const long long whole = (units + pl.grid - 1) / pl.grid * ((max_tiles + per - 1) / per);
   const long long cut = std::max(1LL, tiles / ((long long)pl.grid * per));
   pl.split = max_tiles > 64 || whole - cut > 8;
-  pl.share_min = wide ? (max_tiles <= 32 ? 4 : std::max(8, max_tiles / 64)) : std::max(4, max_tiles / 32);
-  pl.grid = (int)std::min<long long>(pl.grid, pl.split ? (tiles + pl.share_min - 1) / pl.share_min : units);
+  pl.grid = (int)std::min<long long>(pl.grid, pl.split ? (tiles + 3) / 4 : units);
   if (wide) pl.grid *= pl.n_wide;
   if (pl.split) {
     const size_t slots = (size_t)pl.grid * (wide ? NW : 1) * 2;
@@ -1129,7 +1138,7 @@ extern "C" int attn_tree(const void* q, const void* k_pool, const void* v_pool,
   p.k_pool = k_pool; p.v_pool = v_pool; p.err = err_word;
   p.R = R; p.W = (R + 31) / 32; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv; p.rows = R * p.G;
   p.n_rt = pl.n_rt; p.max_pages = max_pages; p.pool_pages = num_pool_pages;
-  p.n_wide = pl.n_wide; p.split = pl.split; p.share_min = pl.share_min;
+  p.n_wide = pl.n_wide; p.split = pl.split;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
   p.meta = (int2*)workspace;
   p.part_ml = (float*)((char*)workspace + pl.off_ml);
