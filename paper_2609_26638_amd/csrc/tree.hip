@@ -179,8 +179,9 @@ __global__ void __launch_bounds__(256) tree_masks_kernel(const int32_t* __restri
 // written in whole 16-byte pieces (8 or 4 slots of an element).
 //
 // What bounds it: prefills, the rows read and written (8 x 1088 rows of 16 + 2 x 4
-// heads of 96, 80 MB: 17.2 us, 4.7 TB/s of the 5.2 that a copy reaches); single
-// tokens, latency (lengths, then page and row, then stores: 6.7 us for 64).
+// heads of 96, 80 MB: 17.2 us, 4.7 TB/s of the 5.2 that a copy reaches; 17.7 without
+// the loads ahead and with a head of V at a time); single
+// tokens, latency (lengths, then page and row, then stores: 5.2 us for 64).
 // ---------------------------------------------------------------------------
 struct AppendParams {
   const void *q, *k, *v;
@@ -225,7 +226,8 @@ __global__ void __launch_bounds__(256) append_rope_kernel(AppendParams p) {
   constexpr int PAIRS = D / (2 * N);    // items of a row: two pieces each
   constexpr int VLD = D + 16 / sizeof(T);
   __shared__ float2 s_cs[16][65];
-  __shared__ __attribute__((aligned(16))) T s_v[16 * VLD];
+  constexpr int VH = 8 / (int)sizeof(T);   // heads of V in LDS at a time
+  __shared__ __attribute__((aligned(16))) T s_v[VH * 16 * VLD];
   __shared__ int s_live[16];
   const int tid = threadIdx.x;
   const int g = blockIdx.x % p.n_groups, sp = blockIdx.x / p.n_groups;
@@ -242,6 +244,33 @@ __global__ void __launch_bounds__(256) append_rope_kernel(AppendParams p) {
   const bool in_pool = page >= 0 && page < p.pool_pages;
   if (!in_pool && g == 0 && tid == 0) set_err(p.err, DVS_ERR_BAD_PAGE);
   const int u0 = g * p.per_group, u1 = min(u0 + p.per_group, p.Hq + 2 * p.Hkv);
+  const T* q = (const T*)p.q + s * p.q_seq;
+  const T* k = (const T*)p.k + s * p.k_seq;
+  const T* v = (const T*)p.v + s * p.v_seq;
+  // queries and keys: the first pieces are on their way under the angles, the
+  // next ones under a piece's products
+  const int items = (min(u1, p.Hq + p.Hkv) - u0) * 16 * PAIRS;
+  Piece<T, ALIGNED> na, nb;
+  auto place = [&](int i, int& u, int& j, int& lo, int& hi, bool& turn) {
+    const int c = i % PAIRS;
+    j = i / PAIRS % 16;
+    u = u0 + i / (16 * PAIRS);
+    turn = c * N < p.half;
+    lo = turn ? c * N : 2 * p.half + 2 * (c * N - p.half);
+    hi = turn ? p.half + c * N : lo + N;
+  };
+  auto fetch = [&](int i) {
+    int u, j, lo, hi;
+    bool turn;
+    if (i >= items) return;
+    place(i, u, j, lo, hi, turn);
+    const int r = r0 + j;
+    if (r < 0 || r >= p.R) return;
+    const T* src = u >= p.Hq ? k + r * p.k_ld + (u - p.Hq) * D : q + r * p.q_ld + (long long)u * D;
+    na.load(src + lo);
+    nb.load(src + hi);
+  };
+  fetch(tid);
   // live rows and their angles
   for (int i = tid; i < 16 * max(p.half, 1); i += 256) {
     const int j = i % 16, e = i / 16, r = r0 + j;
@@ -261,21 +290,15 @@ __global__ void __launch_bounds__(256) append_rope_kernel(AppendParams p) {
     }
   }
   __syncthreads();
-  const T* q = (const T*)p.q + s * p.q_seq;
-  const T* k = (const T*)p.k + s * p.k_seq;
-  const T* v = (const T*)p.v + s * p.v_seq;
-  // queries and keys
-  const int ur = min(u1, p.Hq + p.Hkv);
-  for (int i = tid; i < (ur - u0) * 16 * PAIRS; i += 256) {
-    const int c = i % PAIRS, j = i / PAIRS % 16, u = u0 + i / (16 * PAIRS), r = r0 + j;
+  for (int i = tid; i < items; i += 256) {
+    int u, j, lo, hi;
+    bool turn;
+    place(i, u, j, lo, hi, turn);
+    const int r = r0 + j;
     const bool key = u >= p.Hq;
+    Piece<T, ALIGNED> a = na, b = nb;
+    fetch(i + 256);
     if (!s_live[j] || (key && !in_pool)) continue;
-    const T* src = key ? k + r * p.k_ld + (u - p.Hq) * D : q + r * p.q_ld + (long long)u * D;
-    const bool turn = c * N < p.half;
-    const int lo = turn ? c * N : 2 * p.half + 2 * (c * N - p.half), hi = turn ? p.half + c * N : lo + N;
-    Piece<T, ALIGNED> a, b;
-    a.load(src + lo);
-    b.load(src + hi);
     if (turn) {
 #pragma unroll
       for (int e = 0; e < N; ++e) {
@@ -296,34 +319,34 @@ __global__ void __launch_bounds__(256) append_rope_kernel(AppendParams p) {
     }
   }
   if (!in_pool) return;
-  // values
-  for (int u = max(u0, p.Hq + p.Hkv); u < u1; ++u) {
-    const int h = u - p.Hq - p.Hkv;
+  // values, VH heads at a time
+  for (int ub = max(u0, p.Hq + p.Hkv); ub < u1; ub += VH) {
+    const int nh = min(VH, u1 - ub), h0 = ub - p.Hq - p.Hkv;
     __syncthreads();
-    for (int i = tid; i < 16 * (D / N); i += 256) {
-      const int c = i % (D / N), j = i / (D / N);
+    for (int i = tid; i < nh * 16 * (D / N); i += 256) {
+      const int c = i % (D / N), j = i / (D / N) % 16, h = i / (16 * (D / N));
       if (!s_live[j]) continue;
       Piece<T, ALIGNED> x;
-      x.load(v + (r0 + j) * p.v_ld + h * D + c * N);
-      ((Piece<T, true>&)x).store(s_v + j * VLD + c * N);
+      x.load(v + (r0 + j) * p.v_ld + (h0 + h) * D + c * N);
+      ((Piece<T, true>&)x).store(s_v + (h * 16 + j) * VLD + c * N);
     }
     __syncthreads();
-    T* dst = (T*)p.v_pool + ((size_t)page * p.Hkv + h) * D * 16;
-    for (int i = tid; i < D * (16 / N); i += 256) {
-      const int d = i / (16 / N), j0 = i % (16 / N) * N;
+    T* dst = (T*)p.v_pool + ((size_t)page * p.Hkv + h0) * D * 16;   // (a page's heads lie side by side)
+    for (int i = tid; i < nh * D * (16 / N); i += 256) {
+      const int hd = i / (16 / N), j0 = i % (16 / N) * N, h = hd / D, d = hd - h * D;
       Piece<T, true> x;
       int live = 0;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        x.e[e] = s_v[(j0 + e) * VLD + d];
+        x.e[e] = s_v[(h * 16 + j0 + e) * VLD + d];
         live += s_live[j0 + e];
       }
       if (live == N) {
-        x.store(dst + d * 16 + j0);
+        x.store(dst + hd * 16 + j0);
       } else if (live) {
 #pragma unroll
         for (int e = 0; e < N; ++e)
-          if (s_live[j0 + e]) dst[d * 16 + j0 + e] = x.e[e];
+          if (s_live[j0 + e]) dst[hd * 16 + j0 + e] = x.e[e];
       }
     }
   }
@@ -544,10 +567,11 @@ extern "C" int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const 
   }
   p.n_pages = window_pages(R);
   // heads of a page over several workgroups where the pages alone do not fill
-  // the chip a few times over
+  // the chip a few times over; fewer where a page has few rows to write (64 single
+  // tokens, four / eight workgroups a CU 5.1 / 6.1 us; prefills 18.7 / 17.7)
   const int heads = p.Hq + 2 * Hkv;
   const long long pages = (long long)S * p.n_pages;
-  const int groups = (int)std::min<long long>(heads, std::max<long long>(1, 8LL * device_cus() / pages));
+  const int groups = (int)std::min<long long>(heads, std::max<long long>(1, (R < DVS_PAGE_SIZE ? 4LL : 8LL) * device_cus() / pages));
   p.per_group = (heads + groups - 1) / groups;
   p.n_groups = (heads + p.per_group - 1) / p.per_group;
   DVS_CHECK_SUPPORTED(pages * p.n_groups < (1LL << 24), "kv_append_rope: grid too large");
