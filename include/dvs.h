@@ -746,7 +746,8 @@ int tree_masks(const int32_t* parent, int32_t S, int32_t R, int32_t* mask_out, i
  * The cache outside the appended slots is neither read nor written.
  * Requirements: S, R, Hkv >= 1 (with q: Hq >= 1), D in {64, 96, 128}, rot_dim
  * a multiple of 16 in [0, D], theta > 0, rows at the alignment of their
- * elements (ones that start on 16 bytes take the faster copies).
+ * elements (ones that start on 16 bytes take the faster copies), S * (R / 16 + 2)
+ * below 2^24 / (Hq + 2 Hkv).
  * ---------------------------------------------------------------------- */
 int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const void* k_new, int64_t k_seq,
                    int64_t k_ld, const void* v_new, int64_t v_seq, int64_t v_ld, void* k_pool,

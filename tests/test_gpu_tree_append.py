@@ -169,6 +169,32 @@ def test_append_in_place_without_queries_and_other_bases():
                            q_out=torch.as_strided(x, (S, R, Hq, D), (R * Hq * D, Hq * D, D, 1)))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,D,rot", [(4, 6, 64, 64), (1, 9, 96, 32), (24, 3, 128, 128)])
+def test_append_of_a_large_batch_is_that_of_its_parts(Hq, Hkv, D, rot, dtype):
+    """A workgroup takes the more heads of a page the more pages there are: the same bits."""
+    S, R = 720, 33
+    rng = np.random.default_rng(D)
+    lens = rng.integers(0, 20, S)
+    st, kp, vp = cache(D, lens, R, Hkv, D, dtype)
+    parent = random_parents(rng, S, R)
+    depth = i32(ot.masks(parent)[1])
+    parts = [dev(rng.standard_normal((S, R, h, D)), dtype) for h in (Hq, Hkv, Hkv)]
+    table, kv_len = i32(st.page_table), i32(st.kv_len)
+    a, b = ([dev(kp, dtype), dev(vp, dtype)] for _ in range(2))
+    kw = dict(rot_dim=rot)
+    out = dvs.kv_append_rope(*parts, *a, table, kv_len, depth=depth, **kw, q_out=torch.zeros_like(parts[0]))
+    for s in range(0, S, 40):
+        c = slice(s, s + 40)
+        got = dvs.kv_append_rope(*(p[c] for p in parts), *b, table[c], kv_len[c], depth=depth[c],
+                                 **kw, q_out=torch.zeros_like(parts[0][c]))
+        assert torch.equal(out[c], got)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    dvs.kv_append_rope(*parts, *b, table, kv_len, depth=depth, **kw, q_out=parts[0])
+    live = depth >= 0
+    assert torch.equal(parts[0][live], out[live])
+
+
 def test_append_far_positions_keep_their_angle():
     """At position 16 million, where 32 bits no longer tell neighbouring angles apart, with the
     cache's own length short: the depth carries the distance."""
