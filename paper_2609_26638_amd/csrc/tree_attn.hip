@@ -26,7 +26,7 @@ struct TreeAttn {
   int32_t* err;
   int S, R, W, Hq, Hkv, G, rows, n_rt, max_pages, pool_pages;
   int n_wide;      // workgroups of NW waves over an item's rows (0: tiles not through LDS)
-  int split;       // items are cut where a wave's share ends, and merged by a launch of its own
+  int split;       // items are cut where a share ends, and merged by a launch of its own
   float scale_log2;
   float* part_o;   // [slot][quad][lane] x 4
   float* part_ml;  // [slot][group][lane] x (m, l)
@@ -1020,14 +1020,14 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
   const int keys = dtype == DVS_BF16 ? Tile<__bf16>::KEYS : Tile<float>::KEYS;
   const int max_tiles = (int)(((long long)max_pages * DVS_PAGE_SIZE + keys - 1) / keys);
   const int cus = device_cus();
-  // Few tiles: 16 rows a wave, and not the tiles through LDS, so that there are as
-  // many waves as can be (us, 16 rows a wave / otherwise: 128 rows, one sequence
-  // of 2048 15.0 / 19.7, one of 16000 43 / 31; 8 of 1k-2k, 32 rows 18.5 / 23.9, 64
-  // rows 21.1 / 22.0, 128 rows 27.7 / 25.1; fp32, one of 2048, 128 rows 24.4 / 29.2,
-  // 32 of 1k-4k, 64 rows 204 / 149).  Short tables need no merge, and may be more:
-  // 16 of 300-900, 128 rows 21.2 / 28.3.
+  // Few tiles (under three a wave of 16 rows): 16 rows a wave, and not the tiles
+  // through LDS, so that there are as many waves as can be (us, 16 rows a wave /
+  // otherwise: 256 rows, one sequence of 2048 19.7 / 26.8; 128 rows, one of 4000 20.0
+  // / 20.8, of 8000 25.7 / 24.2, of 16000 43 / 30; 64 rows, 8 of 1k-2k 21.3 / 20.2; fp32,
+  // 128 rows, one of 2048 24.4 / 29.2, 64 rows, 32 of 1k-4k 204 / 149).  Short tables
+  // need no merge, and may be more: 16 of 300-900, 128 rows 21.4 / 23.2.
   const long long a_wave = (long long)std::min(S, MAX_SEQS) * Hkv * ((rows + 15) / 16) * max_tiles / (8 * cus);
-  const bool few = a_wave < (max_tiles <= 32 ? 8 : 4);
+  const bool few = a_wave < (max_tiles <= 32 ? 8 : 3);
   // Tiles through LDS otherwise, for more than 16 rows (us, waves on their own /
   // through LDS: 32 rows, 32 sequences of 1k-8k 73.2 / 69.5, 16 of 3k-6k 44.6 / 38.5;
   // 16 rows, 32 of 1k-8k 64.7 / 66.5), in short tables for more than 32 (32 rows,
