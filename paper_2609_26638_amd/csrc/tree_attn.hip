@@ -16,6 +16,7 @@ __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
 }
 
 constexpr int MAX_SEQS = 1024;      // sequences a launch takes
+constexpr int FW = 4, NW = 8;       // waves of a workgroup: few query rows, many
 constexpr float WEIGHT_MAX = 2048.f, RESCALE_LOG2 = 11.5f;   // (2^11.5 is above the first)
 constexpr int MERGE_FEW = 1024; // row groups up to which the merge takes more waves
 
@@ -240,8 +241,11 @@ __device__ __forceinline__ int scan64(int v) {
   return v;
 }
 
-__device__ __forceinline__ SeqTiles seq_tiles(const TreeAttn& p, int keys, int* s_seq, int* s_len, int* s_tot) {
-  const int tid = threadIdx.x, lane = tid & 63, nw = blockDim.x >> 6;
+// By a workgroup of WAVES waves (s_tot: a word each).
+template <int WAVES>
+__device__ __forceinline__ SeqTiles seq_tiles(const TreeAttn& p, int keys, int (&s_seq)[MAX_SEQS + 1],
+                                              int (&s_len)[MAX_SEQS], int (&s_tot)[WAVES]) {
+  const int tid = threadIdx.x, lane = tid & 63;
   auto tiles_of = [&](int s, int L) {
     if (s >= p.S) return 0;
     if (L < 0 || (long long)L + p.R > (long long)p.max_pages * DVS_PAGE_SIZE) {
@@ -255,7 +259,7 @@ __device__ __forceinline__ SeqTiles seq_tiles(const TreeAttn& p, int keys, int* 
     return SeqTiles{p.S, __builtin_amdgcn_readlane(upto, 63), upto, L, nullptr, nullptr, false};
   }
   int carry = 0;
-  for (int s0 = 0; s0 < p.S; s0 += blockDim.x) {
+  for (int s0 = 0; s0 < p.S; s0 += WAVES * 64) {
     const int s = s0 + tid, L = s < p.S ? p.kv_len[s] : 0;
     if (s < p.S) s_len[s] = L;
     const int t = scan64(tiles_of(s, L));
@@ -263,7 +267,8 @@ __device__ __forceinline__ SeqTiles seq_tiles(const TreeAttn& p, int keys, int* 
     if (lane == 63) s_tot[tid >> 6] = t;
     __syncthreads();
     int before = carry;
-    for (int w = 0; w < nw; ++w) {
+#pragma nounroll
+    for (int w = 0; w < WAVES; ++w) {
       const int v = s_tot[w];
       if (w < (tid >> 6)) before += v;
       carry += v;
@@ -484,15 +489,15 @@ __device__ __forceinline__ void finish_together(const TreeAttn& p, int s, const 
   __syncthreads();
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    f32x2 ml[4];
-    float M = -INFINITY, sum = 0.f, e[4];
+    f32x2 ml[FW];
+    float M = -INFINITY, sum = 0.f, e[FW];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < FW; ++i) {
       ml[i] = s_ml[(i * NG + g) * 64 + lane];
       if (ml[i][1] != 0.f) M = fmaxf(M, ml[i][0]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < FW; ++i) {
       e[i] = ml[i][1] != 0.f ? __builtin_amdgcn_exp2f(ml[i][0] - M) : 0.f;
       if (ml[i][1] != 0.f) sum = fmaf(e[i], ml[i][1], sum);
     }
@@ -501,12 +506,12 @@ __device__ __forceinline__ void finish_together(const TreeAttn& p, int s, const 
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T* dst = (T*)p.out + row.at(p, s, g) + quarter * 4;
 #pragma unroll
-    for (int d0 = 0; d0 < DG; d0 += 4) {
+    for (int d0 = 0; d0 < DG; d0 += FW) {
       const int d = d0 + w;
       if (d >= DG) break;
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < FW; ++i) {
         const f32x4 y = s_o[((i * NG + g) * DG + d) * 64 + lane];
         if (ml[i][1] != 0.f) {
 #pragma unroll
@@ -535,17 +540,17 @@ __device__ __forceinline__ void finish_together(const TreeAttn& p, int s, const 
 // sequences of 1k-4k, 64 rows: 149 us, half their rate).
 // ---------------------------------------------------------------------------
 template <typename T, int D, int NG>
-__global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
+__global__ void __launch_bounds__(FW * 64, 2) tree_attn_wave_kernel(TreeAttn p) {
   using TL = Tile<T>;
   constexpr int KEYS = TL::KEYS, NP = D / 16, DG = D / 16, NS = TL::NS;
   constexpr int PAGE_B = 16 * D * (int)sizeof(T);
-  __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[4];
-  __shared__ f32x4 s_o[4 * NG * DG * 64];
-  __shared__ f32x2 s_ml[4 * NG * 64];
+  __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[FW];
+  __shared__ f32x4 s_o[FW * NG * DG * 64];
+  __shared__ f32x2 s_ml[FW * NG * 64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, quarter = lane >> 4;
   const int HN = p.Hkv * p.n_rt;
-  const SeqTiles seqs = seq_tiles(p, KEYS, s_seq, s_len, s_tot);
+  const SeqTiles seqs = seq_tiles<FW>(p, KEYS, s_seq, s_len, s_tot);
   const Share sh = share_of(p, seqs, HN, 1);
   const int share_id = __builtin_amdgcn_readfirstlane(sh.id);
   const int u_end = __builtin_amdgcn_readfirstlane(sh.u_end), share = __builtin_amdgcn_readfirstlane(sh.size);
@@ -565,7 +570,7 @@ __global__ void __launch_bounds__(256, 2) tree_attn_wave_kernel(TreeAttn p) {
     const int k = p.split ? share_id - P0 / share : 0;
     const int nseg = p.split ? (P0 + tiles - 1) / share - P0 / share + 1 : 1;
     u += n;
-    const int j0 = first + n * w / 4, j1 = first + n * (w + 1) / 4;   // this wave's
+    const int j0 = first + n * w / FW, j1 = first + n * (w + 1) / FW;   // this wave's
     const int it = s * HN + qi, kvh = qi / p.n_rt, rt = qi - kvh * p.n_rt;
     if (p.split && k == 0 && threadIdx.x == 0) p.meta[it] = int2{nseg, share_id};
     const int n_valid = (L + p.R + 15) >> 4;
@@ -722,8 +727,6 @@ __device__ __forceinline__ void barrier() {
   asm volatile("" ::: "memory");
 }
 
-constexpr int NW = 8;   // its waves
-
 template <int D, int NG>
 __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) {
   constexpr int KEYS = 32, DG = D / 16, STAGES = 6;
@@ -735,10 +738,10 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
   constexpr int STAGE_B = 2 * TILE_B;
   __shared__ __attribute__((aligned(1024))) char st0[STAGE_B], st1[STAGE_B], st2[STAGE_B], st3[STAGE_B], st4[STAGE_B],
       st5[STAGE_B];
-  __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[4];
+  __shared__ int s_seq[MAX_SEQS + 1], s_len[MAX_SEQS], s_tot[NW];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m16 = lane & 15, quarter = lane >> 4;
-  const SeqTiles seqs = seq_tiles(p, KEYS, s_seq, s_len, s_tot);
+  const SeqTiles seqs = seq_tiles<NW>(p, KEYS, s_seq, s_len, s_tot);
   const Share sh = share_of(p, seqs, p.Hkv, p.n_wide);
   const int share_id = __builtin_amdgcn_readfirstlane(sh.id), rt = __builtin_amdgcn_readfirstlane(sh.rt);
   const int u_end = __builtin_amdgcn_readfirstlane(sh.u_end), share = __builtin_amdgcn_readfirstlane(sh.size);
@@ -1054,7 +1057,7 @@ static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, i
   // whole, us: 64 sequences of 200-500, 16 rows 20.3 / 13.1; 256 of 100-400, 32 rows
   // 58.6 / 38.5; 128 of 500-1900 87.9 / 75.1).  Only tables of up to 64 tiles: lengths
   // differ, and a long one must not be left to a wave.
-  const int per = wide ? 1 : 4;   // waves that share a segment's tiles
+  const int per = wide ? 1 : FW;   // waves that share a segment's tiles
   const long long units = (long long)pl.seqs * Hkv * (wide ? 1 : pl.n_rt), tiles = units * max_tiles;
   const long long whole = (units + pl.grid - 1) / pl.grid * ((max_tiles + per - 1) / per);
   const long long cut = std::max(1LL, tiles / ((long long)pl.grid * per));
@@ -1089,8 +1092,8 @@ static void launch_tree(const TreePlan& pl, const TreeAttn& p, hipStream_t st) {
       else hipLaunchKernelGGL((tree_attn_tile_kernel<D, 1>), dim3(pl.grid), dim3(NW * 64), 0, st, p);
     }
   } else {
-    if (pl.ng == 2) hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 2>), dim3(pl.grid), dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 1>), dim3(pl.grid), dim3(256), 0, st, p);
+    if (pl.ng == 2) hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 2>), dim3(pl.grid), dim3(FW * 64), 0, st, p);
+    else hipLaunchKernelGGL((tree_attn_wave_kernel<T, D, 1>), dim3(pl.grid), dim3(FW * 64), 0, st, p);
   }
   if (!pl.split) return;
   const long long groups = (long long)p.S * p.Hkv * p.n_rt * pl.ng;
