@@ -13,6 +13,7 @@ import numpy as np
 
 from . import decode
 
+ERR_BAD_PAGE = 8
 ERR_BAD_TREE = 64
 PAGE = 16
 
@@ -108,9 +109,16 @@ def accepted(parent, tokens, argmax):
             return path
 
 
+def kept(st, s, run, eos_id):
+    """How many tokens of a run the budget and the stop token leave."""
+    n = min(len(run), max(0, st.out_tokens.shape[1] - int(st.out_count[s])))
+    return run.index(eos_id) + 1 if eos_id >= 0 and eos_id in run[:n] else n
+
+
 def accept_commit(st, pools, parent, tokens, argmax, eos_id=-1):
     """Returns (error word, accepted [S], path [S, R]).  pools: K pools at even,
-    V pools at odd places."""
+    V pools at odd places.  With an error, a slot to be moved whose page or whose
+    target's is outside the pool among them, nothing is changed."""
     S, R = parent.shape
     took, path = np.zeros(S, np.int32), np.full((S, R), -1, np.int32)
     runs, idle = [[] for _ in range(S)], []
@@ -122,6 +130,15 @@ def accept_commit(st, pools, parent, tokens, argmax, eos_id=-1):
         took[s], path[s, :len(p)] = len(p) - 1, p
         runs[s] = [int(argmax[s, r]) for r in p]
     before, table, fin = st.kv_len.copy(), st.page_table.copy(), st.finished.copy()
+    bad = 0
+    for s in set(range(S)) - set(idle):
+        moves = [(i, int(path[s, i])) for i in range(kept(st, s, runs[s], eos_id)) if path[s, i] != i]
+        pages = [(int(before[s]) + t) // PAGE for m in moves for t in m]
+        ids = [int(table[s, g]) for g in pages if 0 <= g < st.max_pages]
+        if any(not 0 <= x < st.pool_pages for x in ids):
+            bad = ERR_BAD_PAGE
+    if bad:
+        return bad | decode.kv_commit(st.copy(), took, argmax, R, 0, eos_id, block_runs=runs), took, path
     err = decode.kv_commit(st, took, argmax, R, 0, eos_id, block_runs=runs)
     if err:
         return err, took, path

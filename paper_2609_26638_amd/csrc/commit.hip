@@ -65,6 +65,7 @@ struct CommitParams {
   int32_t* accept_out;         // accept_here: A per sequence (may be NULL)
   int draft_group;             // > 0: next draft from mask group A (groups of this many rows)
   int idle_below;              // accept_len < idle_below: the sequence sits this step out
+  const int32_t* movable;      // tokens that the cache can follow, per sequence (NULL: any number)
   const int32_t* argmax;
   int32_t* kv_len;
   int32_t* page_table;
@@ -99,7 +100,7 @@ constexpr int COMMIT_FAST_W = 32;
 // A sequence's state as tree_commit_kernel has it already: the words, loaded
 // before the acceptance, and the run in LDS (run_len < 0: no tree this step).
 struct TreeRun {
-  int kv_len, num_pages, out_count, finished, free_top, run_len;
+  int kv_len, num_pages, out_count, finished, free_top, run_len, movable;
   const int* run;
 };
 
@@ -225,6 +226,7 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads, 
         }
       }
       if (cnt + k >= p.max_new) stop = true;
+      if (TREE ? k > tree.movable : p.movable && k > p.movable[s]) atomicOr(&s_err, DVS_ERR_BAD_PAGE);
     }
     // new length: + k, or + k - 1 when kv_len already counts the kept x0
     need = (L + k - (p.lead && !fin ? 1 : 0) + p.window + DVS_PAGE_SIZE - 1) / DVS_PAGE_SIZE;
@@ -324,9 +326,9 @@ constexpr int TREES = 4;
 
 constexpr int RUN_LD = 65;   // a sequence's run in LDS: sequences side by side read the same place of theirs
 
-__device__ __forceinline__ void accept_trees(const TreeCommit& t, int s0, int* s_run, int* s_len) {
+__device__ __forceinline__ void accept_trees(const TreeCommit& t, int s0, int* s_run, int* s_len, int* s_movable) {
   const int lane = threadIdx.x & 63;
-  int p[TREES], token[TREES], top[TREES], L[TREES], fin[TREES];
+  int p[TREES], token[TREES], top[TREES], L[TREES], fin[TREES], page[TREES];
 #pragma unroll
   for (int i = 0; i < TREES; ++i) {
     const int s = min(s0 + i, t.S - 1);
@@ -337,6 +339,9 @@ __device__ __forceinline__ void accept_trees(const TreeCommit& t, int s0, int* s
     L[i] = t.kv_len[s];
     fin[i] = t.finished[s];
   }
+#pragma unroll
+  for (int i = 0; i < TREES; ++i)
+    page[i] = lane < t.n_window_pages ? tree_window_page(t, min(s0 + i, t.S - 1), L[i], lane) : 0;
 #pragma unroll
   for (int i = 0; i < TREES; ++i) {
     const int s = s0 + i;
@@ -353,37 +358,37 @@ __device__ __forceinline__ void accept_trees(const TreeCommit& t, int s0, int* s
         row = __ffsll((unsigned long long)next) - 1;   // above this one: it ends
       }
     }
-    const int len = __popcll(path);
+    const int len = __popcll(path), at = __popcll(path & ((1ull << lane) - 1)), off = L[i] & (DVS_PAGE_SIZE - 1);
     const size_t base = (size_t)s * t.R;
+    // slots that move and whose page, or the page they move to, is none of the pool's
+    const int from = __shfl(page[i], (off + lane) >> 4), to = __shfl(page[i], (off + at) >> 4);
+    const uint64_t bad = __ballot((path >> lane & 1) && lane != at && (from < 0 || to < 0));
     if (lane == 0) {
       t.accept[s] = max(len - 1, 0);
       t.old_len[s] = L[i];
       s_len[s] = len - 1;
+      s_movable[s] = bad ? __popcll(path & ((bad & -bad) - 1)) : len;
     }
     if (path >> lane & 1) {
-      const int at = __popcll(path & ((1ull << lane) - 1));
       t.path[base + at] = lane;
       s_run[s * RUN_LD + at] = top[i];
     }
     if (lane >= len && lane < t.R) t.path[base + lane] = -1;
-    if (lane < t.n_window_pages) {
-      const int pg = L[i] / DVS_PAGE_SIZE + lane;
-      int id = L[i] >= 0 && pg < t.max_pages ? t.table[(size_t)s * t.max_pages + pg] : -1;
-      if (id >= t.pool_pages) id = -1;
-      t.pages[(size_t)s * t.n_window_pages + lane] = id;
-    }
+    if (lane < t.n_window_pages) t.pages[(size_t)s * t.n_window_pages + lane] = page[i];
   }
 }
 
 __global__ void __launch_bounds__(COMMIT_THREADS) tree_commit_kernel(CommitParams p, TreeCommit t) {
-  __shared__ int s_run[COMMIT_THREADS / 64 * TREES * RUN_LD], s_len[COMMIT_THREADS / 64 * TREES];
+  constexpr int MAX_TREES = COMMIT_THREADS / 64 * TREES;
+  __shared__ int s_run[MAX_TREES * RUN_LD], s_len[MAX_TREES], s_movable[MAX_TREES];
   const int s = min((int)threadIdx.x, p.S - 1);
-  TreeRun tree{p.kv_len[s], p.num_pages[s], p.out_count[s], p.finished[s], *p.free_top, 0, s_run + s * RUN_LD};
-  accept_trees(t, (threadIdx.x >> 6) * TREES, s_run, s_len);
+  TreeRun tree{p.kv_len[s], p.num_pages[s], p.out_count[s], p.finished[s], *p.free_top, 0, 0, s_run + s * RUN_LD};
+  accept_trees(t, (threadIdx.x >> 6) * TREES, s_run, s_len, s_movable);
   __syncthreads();
   const int threads = (p.S + 63) / 64 * 64;
   if (__builtin_amdgcn_readfirstlane((int)threadIdx.x) >= threads) return;   // a whole wave
   tree.run_len = s_len[s];
+  tree.movable = s_movable[s];
   commit_body<false, true>(p, threads, tree);
 }
 
@@ -422,6 +427,7 @@ static int launch_commit(const char* who, int32_t S, int32_t n_causal, int32_t n
                 "%s: mask rows must be n_causal groups of draft_group >= draft_width rows", who);
   p.accept_len = accept_len; p.accept_here = accept_here; p.accept_out = accept_out;
   p.idle_below = tree ? 0 : INT32_MIN;
+  p.movable = tree ? tree->movable : nullptr;
   p.draft_group = draft_group;
   p.argmax = argmax; p.kv_len = kv_len; p.page_table = page_table;
   p.num_pages = num_pages; p.free_stack = free_stack; p.free_top = free_top;

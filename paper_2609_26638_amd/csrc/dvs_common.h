@@ -77,8 +77,16 @@ struct TreeCommit {
   int S, R, max_pages, pool_pages, n_window_pages;
   const int32_t *parent, *tokens, *argmax, *kv_len, *table, *finished;
   int32_t *accept, *path;                      // outputs (or workspace)
-  int32_t *run_len, *old_len, *pages, *run;    // workspace
+  int32_t *run_len, *old_len, *movable, *pages, *run;    // workspace
 };
+// Page i of a sequence's window, -1 for an id outside the pool.  (No slot behind
+// the table or of a negative length is moved: the commit refuses such a sequence.)
+__device__ __forceinline__ int tree_window_page(const TreeCommit& t, int s, int L, int i) {
+  const int pg = L / DVS_PAGE_SIZE + i;
+  if (L < 0 || pg >= t.max_pages) return 0;
+  const int id = t.table[(size_t)s * t.max_pages + pg];
+  return id >= 0 && id < t.pool_pages ? id : -1;
+}
 // Whether the commit's launch accepts as well; the commit (commit.hip).
 bool tree_accept_in_commit(const TreeCommit& t);
 int commit_tree_run(const dvs_state* st, const TreeCommit& t, void* stream);

@@ -361,19 +361,24 @@ __global__ void __launch_bounds__(256) append_rope_kernel(AppendParams p) {
 // commits with its pages; the path's cache slots then move from kv_len +
 // path[i] to kv_len + i in every layer.  The commit may give pages of the
 // window back before the move: the move goes by the page ids noted here, and
-// nothing writes to a page that was given back in between.  Small steps are
-// accepted and committed by one launch (commit.hip); this kernel is for the others.
+// nothing writes to a page that was given back in between.  A slot that cannot
+// move, for a page outside the pool, is found here too, so that a commit that
+// needs it changes nothing.  Small steps are accepted and committed by one launch
+// (commit.hip); this kernel is for the others.
 // ---------------------------------------------------------------------------
 __global__ void __launch_bounds__(256) tree_accept_kernel(TreeCommit t) {
   __shared__ int s_next[TREE_MAX_ROWS];
   __shared__ int s_path[TREE_MAX_ROWS];
-  __shared__ int s_A;
+  __shared__ int s_page[TREE_MAX_ROWS / DVS_PAGE_SIZE + 2];
+  __shared__ int s_A, s_movable;
   const int s = blockIdx.x, tid = threadIdx.x, R = t.R;
   const size_t base = (size_t)s * R;
   const int32_t *parent = t.parent + base, *argmax = t.argmax + base;
   const int L = t.kv_len[s];
   const bool live = t.finished[s] == 0 && parent[0] == -1;
   for (int r = tid; r < R; r += 256) s_next[r] = R;
+  for (int i = tid; i < t.n_window_pages; i += 256)
+    t.pages[(size_t)s * t.n_window_pages + i] = s_page[i] = tree_window_page(t, s, L, i);
   __syncthreads();
   for (int r = tid; r < R; r += 256) {
     const int p = parent[r];
@@ -385,23 +390,21 @@ __global__ void __launch_bounds__(256) tree_accept_kernel(TreeCommit t) {
     if (live)
       for (int r = 0; r < R; r = s_next[r]) s_path[++A] = r;
     s_A = A;
+    s_movable = A + 1;
     t.accept[s] = max(A, 0);
     t.run_len[s] = A;
     t.old_len[s] = L;
   }
   __syncthreads();
-  const int A = s_A;
+  const int A = s_A, off = L & (DVS_PAGE_SIZE - 1);
   for (int i = tid; i < R; i += 256) {
     const int r = i <= A ? s_path[i] : -1;
     t.path[base + i] = r;
     t.run[base + i] = r >= 0 ? argmax[r] : 0;
+    if (r > i && (s_page[(off + r) >> 4] < 0 || s_page[(off + i) >> 4] < 0)) atomicMin(&s_movable, i);
   }
-  for (int i = tid; i < t.n_window_pages; i += 256) {
-    const int pg = L / DVS_PAGE_SIZE + i;
-    int id = L >= 0 && pg < t.max_pages ? t.table[(size_t)s * t.max_pages + pg] : -1;
-    if (id >= t.pool_pages) id = -1;
-    t.pages[(size_t)s * t.n_window_pages + i] = id;
-  }
+  __syncthreads();
+  if (tid == 0) t.movable[s] = s_movable;
 }
 
 constexpr int MOVE_LAYERS = 64;   // layers per launch (as kernel arguments)
@@ -415,7 +418,7 @@ struct MovePools {
 // sequences, 16 layers, 4 heads of 96: 5.0 us, one slot at a time 5.6.
 template <typename T>
 __global__ void __launch_bounds__(256) tree_move_kernel(TreeCommit t, MovePools pools, int n_pools,
-                                                        int Hkv, int D, int32_t* err) {
+                                                        int Hkv, int D) {
   constexpr int MOVE = 8, WORDS = 128 * (int)sizeof(T) / 4 / 64;   // words a lane of a slot of K
   const long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
@@ -428,14 +431,11 @@ __global__ void __launch_bounds__(256) tree_move_kernel(TreeCommit t, MovePools 
   const int off = L % DVS_PAGE_SIZE;
   char* pool = pools.p[pl];
   const size_t head = (size_t)16 * D * sizeof(T);
-  bool bad = false;
   for (int i0 = 1; i0 < k; i0 += 64) {
     const int i = min(i0 + lane, k - 1), r = path[i];
     const int pf = pages[(off + r) >> 4], pt = pages[(off + i) >> 4];
     const int slots = ((off + r) & 15) << 4 | ((off + i) & 15);
-    const bool moves = i0 + lane < k && r != i;
-    bad |= moves && (pf < 0 || pt < 0);
-    uint64_t todo = __ballot(moves && pf >= 0 && pt >= 0);
+    uint64_t todo = __ballot(i0 + lane < k && r != i);   // (the commit saw to their pages)
     while (todo) {
       char *from[MOVE], *to[MOVE];
       int n = 0;
@@ -477,7 +477,6 @@ __global__ void __launch_bounds__(256) tree_move_kernel(TreeCommit t, MovePools 
       }
     }
   }
-  if (__ballot(bad) && lane == 0) set_err(err, DVS_ERR_BAD_PAGE);
 }
 
 static size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -594,7 +593,7 @@ extern "C" int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const 
 
 extern "C" size_t dvs_accept_tree_workspace_bytes(int32_t S, int32_t R) {
   if (S < 1 || S > 1024 || R < 1 || R > TREE_MAX_ROWS) return 0;
-  return al256((size_t)S * 4 * (3 + window_pages(R) + 2 * (size_t)R));
+  return al256((size_t)S * 4 * (4 + window_pages(R) + 2 * (size_t)R));
 }
 
 extern "C" int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, int32_t n_layers,
@@ -633,7 +632,8 @@ extern "C" int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, 
   int32_t* w = (int32_t*)workspace;
   t.run_len = w; t.old_len = w + S;
   t.accept = accept_out ? accept_out : w + 2 * S;
-  t.pages = w + 3 * S;
+  t.movable = w + 3 * S;
+  t.pages = w + 4 * S;
   t.run = t.pages + (size_t)S * t.n_window_pages;
   t.path = path_out ? path_out : t.run + (size_t)S * R;
   hipStream_t hs = (hipStream_t)stream;
@@ -653,9 +653,9 @@ extern "C" int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, 
     const long long tasks = (long long)S * 2 * nl * n_kv_heads;
     const dim3 gr((unsigned)((tasks + 3) / 4));
     if (dtype == DVS_BF16)
-      hipLaunchKernelGGL(tree_move_kernel<uint16_t>, gr, dim3(256), 0, hs, t, pools, 2 * nl, n_kv_heads, head_dim, st->err_word);
+      hipLaunchKernelGGL(tree_move_kernel<uint16_t>, gr, dim3(256), 0, hs, t, pools, 2 * nl, n_kv_heads, head_dim);
     else
-      hipLaunchKernelGGL(tree_move_kernel<float>, gr, dim3(256), 0, hs, t, pools, 2 * nl, n_kv_heads, head_dim, st->err_word);
+      hipLaunchKernelGGL(tree_move_kernel<float>, gr, dim3(256), 0, hs, t, pools, 2 * nl, n_kv_heads, head_dim);
     if ((rc = launch_status("accept_commit_tree(move)"))) return rc;
   }
   return DVS_OK;
