@@ -107,7 +107,8 @@ const char* dvs_last_error(void);
  *                zero-filled before its first call with a given shape (S, R,
  *                heads, D, max_pages, chunk_keys); its leading bytes are
  *                split-merge counters that every call leaves zero again, so
- *                later calls of the same shape need no clearing.
+ *                later calls of the same shape need no clearing (unless another
+ *                function was given the same memory in between).
  *                Calls that share a workspace must not overlap in time.
  * Requirements: Hq % Hkv == 0, D in {64, 96, 128}, R >= 1, S >= 1, all
  * pointers non-NULL (except err_word), softmax_scale > 0.

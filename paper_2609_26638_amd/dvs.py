@@ -253,7 +253,9 @@ class Workspace:
     """Zero-initialised device scratch.  attn_hybrid_block keeps split-merge
     counters at its start, which must be zero when a call shape first uses
     it and which every call leaves zero; `shape` remembers the last shape so
-    a change of shape clears the buffer again."""
+    a change of shape, or a call of another kind in between, clears the buffer
+    again.  (A captured call does not look again when it is replayed: a graph's
+    attn_hybrid_block calls need a workspace that nothing else uses.)"""
 
     def __init__(self, nbytes: int, device="cuda"):
         self.buf = torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=device)
@@ -433,8 +435,15 @@ def _here(*tensors):
     return dev
 
 
+def _lent(workspace):
+    """A given workspace's buffer, for a call that may leave anything in it: attn_hybrid_block
+    clears it before it counts there again."""
+    workspace.shape = None
+    return workspace.buf
+
+
 def _scratch(workspace, nbytes, device, stream):
-    return workspace.buf if workspace is not None else _new(nbytes, torch.uint8, device, stream)
+    return _lent(workspace) if workspace is not None else _new(nbytes, torch.uint8, device, stream)
 
 
 def _buf(workspace):
@@ -1227,7 +1236,7 @@ def attn_tree(q, k_pool, v_pool, page_table, kv_len, mask, softmax_scale: float,
     _check_err(err)
     dev = _here(q, k_pool, v_pool, page_table, kv_len, mask, out, err, _buf(workspace))
     code = _dtype_code(q)
-    ws = workspace.buf if workspace is not None else _new(
+    ws = _lent(workspace) if workspace is not None else _new(
         max(1, tree_workspace_bytes(S, R, Hq, Hkv, D, page_table.shape[1], code)), torch.uint8,
         q.device, stream)
     rc = lib().attn_tree(q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(),
@@ -1264,7 +1273,7 @@ def accept_commit_tree(st: DeviceState, pools: KVPools, parent, tokens, argmax, 
         raise DvsError("path_out must be [S, R]")
     dev = _here(st.kv_len, parent, tokens, argmax, accept_out, path_out, pools.keep[0][0],
                 _buf(workspace))
-    ws = workspace.buf if workspace is not None else _new(
+    ws = _lent(workspace) if workspace is not None else _new(
         max(1, accept_tree_workspace_bytes(S, R)), torch.uint8, parent.device, stream)
     sd = _state_desc(st, eos_id)
     rc = lib().accept_commit_tree(ctypes.byref(sd), pools.layers, len(pools.layers),
