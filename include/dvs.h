@@ -748,7 +748,7 @@ int tree_masks(const int32_t* parent, int32_t S, int32_t R, int32_t* mask_out, i
  * Requirements: S, R, Hkv >= 1 (with q: Hq >= 1), D in {64, 96, 128}, rot_dim
  * a multiple of 16 in [0, D], theta > 0, rows at the alignment of their
  * elements (ones that start on 16 bytes take the faster copies), S * (R / 16 + 2)
- * below 2^24 / (Hq + 2 Hkv).
+ * below 2^24 / (Hq + 2 Hkv), max_pages < 2^27 - 3.
  * ---------------------------------------------------------------------- */
 int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const void* k_new, int64_t k_seq,
                    int64_t k_ld, const void* v_new, int64_t v_seq, int64_t v_ld, void* k_pool,
@@ -776,7 +776,7 @@ int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const void* k_new
  *   workspace >= dvs_tree_workspace_bytes(...) bytes on 256, no initialisation
  *   needed.  Calls that share it must not overlap in time.
  * Requirements: Hq % Hkv == 0, D in {64, 96, 128}, S >= 1, 1 <= R <= 1024,
- * R * Hq <= 2^20, R * Hq * max_pages < 2^30, q, out and the pools on 16 bytes,
+ * R * Hq <= 2^20, R * Hq * max_pages < 2^30, max_pages < 2^27 - 3, q, out and the pools on 16 bytes,
  * softmax_scale > 0.  Sequences, masks and page tables of any width; the choice
  * of kernels goes by the sizes above, the longest table among them, not by
  * kv_len.
@@ -812,7 +812,8 @@ int attn_tree(const void* q, const void* k_pool, const void* v_pool, const int32
  *           -1 for the other sequences); both may be NULL.
  *   workspace >= dvs_accept_tree_workspace_bytes(S, R) bytes, no
  *           initialisation needed.  Calls that share it must not overlap.
- * Requirements: 1 <= S <= 1024, 1 <= R <= 1024, head_dim in {64, 96, 128}.
+ * Requirements: 1 <= S <= 1024, 1 <= R <= 1024, head_dim in {64, 96, 128},
+ * max_pages < 2^27 - 3.
  * ---------------------------------------------------------------------- */
 size_t dvs_accept_tree_workspace_bytes(int32_t S, int32_t R);
 int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, int32_t n_layers,

@@ -72,6 +72,10 @@ bool attn_chunk_ok(int chunk_keys);
 size_t attn_counter_bytes(int S, int R, int Hq, int Hkv, int D, int max_pages, int chunk_keys,
                           int dtype);
 
+// Widest page table of the tree calls: positions, and the keys of a tile behind
+// the last one, stay within 31 bits.
+constexpr int TREE_MAX_PAGES = (1 << 27) - 4;
+
 // accept_commit_tree: a step's trees and what its launches hand on.
 struct TreeCommit {
   int S, R, max_pages, pool_pages, n_window_pages;

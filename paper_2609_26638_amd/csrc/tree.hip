@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(256) tree_move_kernel(TreeCommit t, MovePools 
 
 static size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-static int window_pages(int R) { return (R + DVS_PAGE_SIZE - 2) / DVS_PAGE_SIZE + 1; }
+static int window_pages(int R) { return (int)((R + DVS_PAGE_SIZE - 2LL) / DVS_PAGE_SIZE) + 1; }
 
 template <typename T, bool ALIGNED>
 static void launch_append(const AppendParams& p, int D, unsigned grid, hipStream_t st) {
@@ -535,6 +535,7 @@ extern "C" int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const 
   DVS_CHECK_ARG(S >= 1 && R >= 1, "kv_append_rope: need S >= 1 and R >= 1");
   DVS_CHECK_ARG(Hkv >= 1 && Hq >= (q ? 1 : 0), "kv_append_rope: need heads");
   DVS_CHECK_ARG(max_pages >= 1 && num_pool_pages >= 1, "kv_append_rope: empty page table/pool");
+  DVS_CHECK_SUPPORTED(max_pages <= TREE_MAX_PAGES, "kv_append_rope: max_pages must be below 2^27 - 3");
   DVS_CHECK_SUPPORTED(dtype == DVS_F32 || dtype == DVS_BF16, "kv_append_rope: dtype %d", dtype);
   DVS_CHECK_SUPPORTED(D == 64 || D == 96 || D == 128, "kv_append_rope: head_dim %d", D);
   DVS_CHECK_SUPPORTED(rot_dim >= 0 && rot_dim <= D && rot_dim % 16 == 0,
@@ -610,6 +611,7 @@ extern "C" int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, 
   DVS_CHECK_ARG(st->S >= 1 && st->S <= 1024, "accept_commit_tree: need 1 <= S <= 1024");
   DVS_CHECK_ARG(st->max_pages >= 1 && st->num_pool_pages >= 1 && st->max_new >= 1,
                 "accept_commit_tree: need max_pages, num_pool_pages, max_new >= 1");
+  DVS_CHECK_SUPPORTED(st->max_pages <= TREE_MAX_PAGES, "accept_commit_tree: max_pages must be below 2^27 - 3");
   DVS_CHECK_ARG(layers && n_layers >= 1 && n_kv_heads >= 1, "accept_commit_tree: need layers and heads");
   DVS_CHECK_SUPPORTED(dtype == DVS_F32 || dtype == DVS_BF16, "accept_commit_tree: dtype %d", dtype);
   DVS_CHECK_SUPPORTED(head_dim == 64 || head_dim == 96 || head_dim == 128,

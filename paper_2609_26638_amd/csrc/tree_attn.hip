@@ -1014,7 +1014,7 @@ struct TreePlan {
 constexpr long long MAX_ROWS = 1 << 20;   // query rows of a sequence, all heads
 
 static bool tree_fits(int R, int Hq, int max_pages) {   // what the kernels count in 32 bits
-  return (long long)R * Hq <= MAX_ROWS && (long long)R * Hq * max_pages < (1LL << 30);
+  return (long long)R * Hq <= MAX_ROWS && (long long)R * Hq * max_pages < (1LL << 30) && max_pages <= TREE_MAX_PAGES;
 }
 
 static TreePlan tree_plan(int S, int R, int Hq, int Hkv, int D, int max_pages, int dtype) {
@@ -1130,7 +1130,7 @@ extern "C" int attn_tree(const void* q, const void* k_pool, const void* v_pool,
   DVS_CHECK_SUPPORTED(D == 64 || D == 96 || D == 128, "attn_tree: head_dim %d", D);
   DVS_CHECK_ARG((((uintptr_t)q | (uintptr_t)out | (uintptr_t)k_pool | (uintptr_t)v_pool) & 15) == 0,
                 "attn_tree: q, out and the pools must start on 16 bytes");
-  DVS_CHECK_SUPPORTED(tree_fits(R, Hq, max_pages), "attn_tree: R * Hq must be at most 2^20, its product with max_pages below 2^30");
+  DVS_CHECK_SUPPORTED(tree_fits(R, Hq, max_pages), "attn_tree: R * Hq must be at most 2^20, its product with max_pages below 2^30, max_pages below 2^27 - 3");
   const TreePlan pl = tree_plan(S, R, Hq, Hkv, D, max_pages, dtype);
   if (!workspace || ws_bytes < pl.bytes) {
     set_error("attn_tree: workspace needs %zu bytes, got %zu", pl.bytes, ws_bytes);
