@@ -89,6 +89,11 @@ __device__ __forceinline__ int run_token(const CommitParams& p, int s, int A, in
   return j < A ? p.draft[(size_t)s * p.draft_width + j] : p.argmax[(size_t)s * p.R + A];
 }
 
+// (64 bits: a length that no table holds must not come out as few pages)
+__device__ __forceinline__ int pages_of(long long positions) {
+  return (int)((positions + DVS_PAGE_SIZE - 1) / DVS_PAGE_SIZE);
+}
+
 // FAST: acceptance here, no lead token, no draft groups, at most
 // COMMIT_FAST_W causal rows and draft slots.  A sequence's whole draft row,
 // its verify rows' top-1 and the next draft's rows are loaded at once, with
@@ -160,7 +165,7 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads, 
       }
       if (cnt + k >= p.max_new) stop = true;
     }
-    need = (L + k + p.window + DVS_PAGE_SIZE - 1) / DVS_PAGE_SIZE;
+    need = pages_of((long long)L + k + p.window);
     if (need > p.max_pages || n < 0 || n > p.max_pages || L < 0)
       atomicOr(&s_err, DVS_ERR_MAX_PAGES);
   } else if (!FAST && live_seq) {
@@ -229,7 +234,7 @@ __device__ __forceinline__ void commit_body(const CommitParams& p, int threads, 
       if (TREE ? k > tree.movable : p.movable && k > p.movable[s]) atomicOr(&s_err, DVS_ERR_BAD_PAGE);
     }
     // new length: + k, or + k - 1 when kv_len already counts the kept x0
-    need = (L + k - (p.lead && !fin ? 1 : 0) + p.window + DVS_PAGE_SIZE - 1) / DVS_PAGE_SIZE;
+    need = pages_of((long long)L + k - (p.lead && !fin ? 1 : 0) + p.window);
     if (need > p.max_pages || n < 0 || n > p.max_pages || L < 0)
       atomicOr(&s_err, DVS_ERR_MAX_PAGES);
   }
