@@ -806,7 +806,8 @@ int attn_tree(const void* q, const void* k_pool, const void* v_pool, const int32
  * ceil((kv_len + R) / 16).  Errors as kv_commit (nothing is changed, the cache
  * neither), and DVS_ERR_BAD_PAGE, likewise, where a slot that has to move lies in,
  * or moves to, a page whose id is outside the pool.
- *   layers: only k_pool and v_pool are read; they start on 16 bytes.
+ *   layers: only k_pool and v_pool are read; they start on 16 bytes.  Layers may
+ *           share a cache (both pools, which then moves once).
  *   parent, tokens, argmax [S, R] int32 (tokens[s, 0] is not read)
  *   accept_out [S] = A, path_out [S, R] = p_0 .. p_A, then -1 (A = 0 and all
  *           -1 for the other sequences); both may be NULL.

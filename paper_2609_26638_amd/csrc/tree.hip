@@ -620,6 +620,10 @@ extern "C" int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, 
     DVS_CHECK_ARG(layers[l].k_pool && layers[l].v_pool &&
                       (((uintptr_t)layers[l].k_pool | (uintptr_t)layers[l].v_pool) & 15) == 0,
                   "accept_commit_tree: layer %d needs pools that start on 16 bytes", l);
+  for (int l = 0; l < n_layers; ++l)
+    for (int e = 0; e < l; ++e)
+      DVS_CHECK_ARG((layers[e].k_pool == layers[l].k_pool) == (layers[e].v_pool == layers[l].v_pool),
+                    "accept_commit_tree: layers %d and %d share one of their two pools", e, l);
   const size_t need = dvs_accept_tree_workspace_bytes(st->S, R);
   if (!workspace || ws_bytes < need) {
     set_error("accept_commit_tree: workspace needs %zu bytes, got %zu", need, ws_bytes);
@@ -645,13 +649,19 @@ extern "C" int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, 
     if ((rc = launch_status("accept_commit_tree(accept)"))) return rc;
   }
   if ((rc = commit_tree_run(st, t, stream))) return rc;
-  for (int l0 = 0; l0 < n_layers; l0 += MOVE_LAYERS) {
-    const int nl = std::min(n_layers - l0, MOVE_LAYERS);
+  for (int l = 0; l < n_layers;) {
     MovePools pools{};
-    for (int l = 0; l < nl; ++l) {
-      pools.p[2 * l] = (char*)layers[l0 + l].k_pool;
-      pools.p[2 * l + 1] = (char*)layers[l0 + l].v_pool;
+    int nl = 0;
+    for (; l < n_layers && nl < MOVE_LAYERS; ++l) {
+      // a cache that several layers share moves once: a second wave on the same
+      // slots would read what the first has moved
+      bool moved = false;
+      for (int e = 0; e < l; ++e) moved |= layers[e].k_pool == layers[l].k_pool;
+      if (moved) continue;
+      pools.p[2 * nl] = (char*)layers[l].k_pool;
+      pools.p[2 * nl++ + 1] = (char*)layers[l].v_pool;
     }
+    if (!nl) break;
     const long long tasks = (long long)S * 2 * nl * n_kv_heads;
     const dim3 gr((unsigned)((tasks + 3) / 4));
     if (dtype == DVS_BF16)
