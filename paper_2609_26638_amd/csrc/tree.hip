@@ -624,6 +624,9 @@ extern "C" int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, 
     for (int e = 0; e < l; ++e)
       DVS_CHECK_ARG((layers[e].k_pool == layers[l].k_pool) == (layers[e].v_pool == layers[l].v_pool),
                     "accept_commit_tree: layers %d and %d share one of their two pools", e, l);
+  // (the move's grid: 2^32 threads are too many, and the state would be committed by then)
+  DVS_CHECK_SUPPORTED((long long)st->S * 2 * std::min(n_layers, MOVE_LAYERS) * n_kv_heads < (1LL << 26) - 3,
+                      "accept_commit_tree: sequences, layers and heads make too large a grid");
   const size_t need = dvs_accept_tree_workspace_bytes(st->S, R);
   if (!workspace || ws_bytes < need) {
     set_error("accept_commit_tree: workspace needs %zu bytes, got %zu", need, ws_bytes);

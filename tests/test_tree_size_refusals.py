@@ -30,3 +30,13 @@ def test_tables_wider_than_31_bits_of_positions():
     assert _attn(**one, max_pages=WIDEST, nbytes=16) == -4
     st = _state(max_pages=WIDEST)
     assert _commit(st=ctypes.byref(st), nbytes=16) == -4
+
+
+@needs_lib
+def test_moves_of_more_threads_than_a_launch_has():
+    st = _state(S=1024)
+    nbytes = dvs.accept_tree_workspace_bytes(1024, 4)
+    # two layers: 1024 * 4 * heads tasks
+    assert _commit(st=ctypes.byref(st), nbytes=nbytes, heads=1 << 14) == -2
+    assert _commit(st=ctypes.byref(st), nbytes=nbytes, heads=2 ** 31 - 1) == -2
+    assert _commit(st=ctypes.byref(st), nbytes=16, heads=(1 << 14) - 1) == -4
