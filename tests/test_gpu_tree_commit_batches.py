@@ -2,7 +2,10 @@
 both sides of the sizes that it takes (64 sequences, 64 rows), against the oracle."""
 import numpy as np
 import pytest
+import torch
 
+from oracle import tree as ot
+from paper_2609_26638_amd import dvs
 from tests.test_gpu_tree_append import i32
 from tests.test_gpu_tree_commit import Both, drafted
 from tests.tree_util import random_parents
@@ -58,3 +61,37 @@ def test_each_sequence_keeps_a_run_of_its_own(S):
     want = b.commit(parent, tokens, argmax)
     assert want[1].tolist() == [R - 1 - s for s in range(S)]
     assert b.st.out_tokens[S - 1, :R - S + 1].tolist() == [1000 * (S - 1) + i + 1 for i in range(R - S)] + [-6 - S]
+
+
+@pytest.mark.parametrize("S,R", [(3, 20), (64, 64), (3, 100), (1024, 9)])
+def test_outputs_may_be_left_out(S, R):
+    """NULL accept_out and path_out: the same state and cache, with a workspace of any contents."""
+    rng = np.random.default_rng(R)
+    b = Both(R, rng.integers(0, 60, S).tolist(), R, layers=2, heads=1, max_new=2 * R, extra=S * (R // 16 + 2))
+    widen(b, 1, R)
+    b.st.out_count[:] = 0
+    b.dev.out_count.zero_()
+    parent = random_parents(rng, S, R)
+    tokens, argmax = drafted(rng, parent)
+    want = ot.accept_commit(b.st, b.pools, parent, tokens, argmax)
+    assert want[0] == 0 and want[1].max() > 0
+    words = [i32(a) for a in (parent, tokens, argmax)]
+    ws = torch.full((dvs.accept_tree_workspace_bytes(S, R),), 255, dtype=torch.uint8, device="cuda")
+    rc = dvs.lib().accept_commit_tree(dvs._state_desc(b.dev, -1), b.handle.layers, len(b.handle.layers),
+                                      b.handle.n_kv_heads, b.handle.head_dim, b.handle.dtype, R,
+                                      *(w.data_ptr() for w in words), None, None, ws.data_ptr(), ws.numel(),
+                                      dvs._stream())
+    assert rc == 0
+    torch.cuda.synchronize()
+    assert int(b.dev.err) == 0
+    b.same()
+
+
+@pytest.mark.parametrize("R", [7, 64, 100, 1024])
+def test_masks_without_depths(R):
+    parent = i32(random_parents(np.random.default_rng(R), 5, R))
+    want = dvs.tree_masks(parent)[0]
+    mask = torch.full_like(want, -1)
+    rc = dvs.lib().tree_masks(parent.data_ptr(), 5, R, mask.data_ptr(), None, None, dvs._stream())
+    assert rc == 0
+    assert torch.equal(mask, want)
