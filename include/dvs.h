@@ -764,9 +764,10 @@ int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const void* k_new
  * (slots [L, L + R), L = kv_len[s]).  Row r sees key position k iff
  *     k < L,  or  L <= k < L + R and bit k - L of its mask is set
  * (tree_mask NULL: k <= L + r); a row without any bit sees nothing, not the
- * cache either: its output is 0.  Slots that a row does not see may hold
- * anything.  out[s,r,h,:] = sum_k softmax_k(softmax_scale <q[s,r,h], K_k>) V_k,
- * query head h reading KV head h / (Hq / Hkv).
+ * cache either: its output is 0, as is that of a row with scores of -inf only.
+ * Slots that a row does not see may hold anything.  out[s,r,h,:] = sum_k
+ * softmax_k(softmax_scale <q[s,r,h], K_k>) V_k, query head h reading KV head
+ * h / (Hq / Hkv).
  *   q, out [S, R, Hq, D]; pools, page_table, kv_len as attn_hybrid_block;
  *   tree_mask [S, R, ceil(R / 32)] int32 (tree_masks makes it; any other bits
  *   do as well) or NULL.
@@ -776,10 +777,10 @@ int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const void* k_new
  *   workspace >= dvs_tree_workspace_bytes(...) bytes on 256, no initialisation
  *   needed.  Calls that share it must not overlap in time.
  * Requirements: Hq % Hkv == 0, D in {64, 96, 128}, S >= 1, 1 <= R <= 1024,
- * R * Hq <= 2^20, R * Hq * max_pages < 2^30, max_pages < 2^27 - 3, q, out and the pools on 16 bytes,
- * softmax_scale > 0.  Sequences, masks and page tables of any width; the choice
- * of kernels goes by the sizes above, the longest table among them, not by
- * kv_len.
+ * R * Hq <= 2^20, R * Hq * max_pages < 2^30, max_pages < 2^27 - 3, q, out and
+ * the pools on 16 bytes, softmax_scale > 0.  Otherwise sequences, masks and page
+ * tables of any width; the choice of kernels goes by the sizes above, the longest
+ * table among them, not by kv_len.
  * ---------------------------------------------------------------------- */
 size_t dvs_tree_workspace_bytes(int32_t S, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
                                 int32_t max_pages, int32_t dtype);

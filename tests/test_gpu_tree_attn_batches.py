@@ -1,13 +1,14 @@
 """GPU: attn_tree over batches of hundreds of sequences, whose lengths every wave of a workgroup
-counts, with the tiles through LDS and without."""
+counts, with the tiles through LDS and without; rows whose scores are all -inf."""
 import numpy as np
 import pytest
 
 from oracle import tree as ot
 from paper_2609_26638_amd import dvs
-from tests.test_gpu_tree_append import i32
+from tests.gpu_util import to_f64
+from tests.test_gpu_tree_append import dev, i32
 from tests.test_gpu_tree_attn import run
-from tests.tree_util import random_parents
+from tests.tree_util import cache, random_parents, rounded
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +40,26 @@ def test_hundreds_of_sequences_fp32(case):
     lens = [int(x) for x in rng.integers(0, 150, S)]
     vis, _, _ = ot.masks(random_parents(rng, S, R))
     run((lens, R, *rest), "f32", vis, i32(ot.words(vis)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("columns", [0, 1100])
+@pytest.mark.parametrize("R,Hq,Hkv,D", [(3, 4, 2, 64), (40, 8, 2, 128), (20, 4, 1, 96)])
+def test_rows_with_scores_of_minus_infinity_only(R, Hq, Hkv, D, columns, dtype):
+    """3e38 * -4 leaves 32 bits: such a row gives 0, the rows beside it what they give without it."""
+    lens = [300, 45]
+    st, k, v = cache(R, lens, R, Hkv, D, dtype)
+    k[..., 0] = -4
+    rng = np.random.default_rng(R)
+    q = rounded(rng.standard_normal((2, R, Hq, D)), dtype)
+    parent = random_parents(rng, 2, R, padding=False)
+    table = np.pad(st.page_table, ((0, 0), (0, max(0, columns - st.page_table.shape[1]))))
+    args = (dev(k, dtype), dev(v, dtype), i32(table), i32(st.kv_len), dvs.tree_masks(i32(parent))[0], D ** -0.5)
+    want = to_f64(dvs.attn_tree(dev(q, dtype), *args))
+    row = R // 2
+    q[:, row] = 0
+    q[:, row, :, 0] = rounded(3e38, dtype)
+    got = to_f64(dvs.attn_tree(dev(q, dtype), *args))
+    assert np.all(got[:, row] == 0)
+    others = np.arange(R) != row
+    np.testing.assert_array_equal(got[:, others], want[:, others])
