@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(256) tree_masks_small_kernel(const int32_t* __
 // More rows, up to NB blocks of 64: a workgroup takes 256 of a sequence's, makes
 // the blocks up to its last row, then a wave its 64 rows' words, in registers,
 // which go out through LDS, side by side.  The words to write bound it (128
-// sequences of 1000 rows, 17 MB: 7.8 us; copied row by row from the parent's in 16
+// sequences of 1000 rows, 17 MB: 8.1 us; copied row by row from the parent's in 16
 // steps of a workgroup a sequence: 18.4).  The first words reach memory late, after
 // a chain of parents that is all latency.
 template <int NB>
@@ -179,9 +179,9 @@ __global__ void __launch_bounds__(256) tree_masks_kernel(const int32_t* __restri
 // written in whole 16-byte pieces (8 or 4 slots of an element).
 //
 // What bounds it: prefills, the rows read and written (8 x 1088 rows of 16 + 2 x 4
-// heads of 96, 80 MB: 17.2 us, 4.7 TB/s of the 5.2 that a copy reaches; 17.7 without
-// the loads ahead and with a head of V at a time); single
-// tokens, latency (lengths, then page and row, then stores: 5.2 us for 64).
+// heads of 96, 80 MB: 17.4 us, 4.6 TB/s of the 5.1 that a copy reaches; half a us
+// more without the loads ahead and with a head of V at a time); single
+// tokens, latency (lengths, then page and row, then stores: 6.2 us for 64).
 // ---------------------------------------------------------------------------
 struct AppendParams {
   const void *q, *k, *v;
@@ -415,7 +415,7 @@ struct MovePools {
 // A wave a (sequence, layer, K or V, KV head).  path[i] >= i and rises, so a
 // slot is read before a later step writes it: MOVE slots are read together, then
 // written.  Their rows and pages are found 64 at a time, a lane each.  Latency: 8
-// sequences, 16 layers, 4 heads of 96: 5.0 us, one slot at a time 5.6.
+// sequences, 16 layers, 4 heads of 96: 5.0 - 5.5 us, 0.6 more a slot at a time.
 template <typename T>
 __global__ void __launch_bounds__(256) tree_move_kernel(TreeCommit t, MovePools pools, int n_pools,
                                                         int Hkv, int D) {
@@ -568,7 +568,7 @@ extern "C" int kv_append_rope(const void* q, int64_t q_seq, int64_t q_ld, const 
   p.n_pages = window_pages(R);
   // heads of a page over several workgroups where the pages alone do not fill
   // the chip a few times over; fewer where a page has few rows to write (64 single
-  // tokens, four / eight workgroups a CU 5.1 / 6.1 us; prefills 18.7 / 17.7)
+  // tokens, four / eight workgroups a CU 6.2 / 7.2 us; prefills 18.9 / 17.4)
   const int heads = p.Hq + 2 * Hkv;
   const long long pages = (long long)S * p.n_pages;
   const int groups = (int)std::min<long long>(heads, std::max<long long>(1, (R < DVS_PAGE_SIZE ? 4LL : 8LL) * device_cus() / pages));

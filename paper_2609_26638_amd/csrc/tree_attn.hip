@@ -442,7 +442,8 @@ __device__ __forceinline__ void clean_values(u32x4 (&vf)[DG], const uint32_t (&b
 }
 
 // End of a segment: the output, or a part of it (O, m and l in 32 bits).  l is
-// 0 exactly for a row that sees nothing, whatever its O holds.
+// 0 exactly for a row that sees nothing (or no score above -inf), whatever its O
+// holds.
 template <typename T, int D, int NG>
 __device__ __forceinline__ void finish_rows(const TreeAttn& p, int s, const Rows<T, D, NG>& row,
                                             const float (&m)[NG], float (&l)[NG],
@@ -534,7 +535,7 @@ __device__ __forceinline__ void finish_together(const TreeAttn& p, int s, const 
 // one row 117 / 111; 32 of 1k-8k, 16 rows 75 / 67; one of 16000, one row 28 / 21).
 //
 // What bounds it: long caches, the cache (64 sequences, one row, 556 MB: 111 us,
-// 5.0 TB/s of the 5.2 that a copy reaches); one sequence, latency: the lengths,
+// 5.0 TB/s of the 5.1 - 5.2 that a copy reaches); one sequence, latency: the lengths,
 // then the page ids, then keys and values, 1 - 2 us each, then the second launch
 // (2000 keys, one row 13.7 us, 128 rows 15.0); fp32, the matrix instructions (32
 // sequences of 1k-4k, 64 rows: 149 us, half their rate).
@@ -692,11 +693,14 @@ __global__ void __launch_bounds__(FW * 64, 2) tree_attn_wave_kernel(TreeAttn p) 
 // from the cache, STAGES tiles at a time.  The next tile's scores are made under
 // this tile's softmax (matrix and vector unit), then this tile's values are added.
 //
-// What bounds it, long documents (256 rows, 1.44 GB, 0.36 PFLOP): the copies alone
-// take 253 us and the arithmetic alone 309, but with both at once the clock
-// falls from 2.4 to 1.9 GHz and the whole takes 410 - 430.  Taking the softmax and the
-// products in turns by two halves of the waves, 32x32 products, reads ahead of
-// their use and 64 rows a wave were all tried: 442 - 530.
+// What bounds it, long documents (256 rows, 1.44 GB, 0.36 PFLOP; 410 - 430 us): no
+// unit alone.  A SIMD's matrix core is busy for 42% of the time, its vector ALU
+// for 41, both at once for 8, neither for 25, and 36% of a wave's cycles are
+// waits; the cache is read once (1.001 of its bytes), without bank conflicts in
+// LDS.  The copies alone take 253 us, the arithmetic alone 309; with both the
+// clock falls from 2.4 to 1.7 - 2.0 GHz.  Taking the softmax and the products in turns
+// by two halves of the waves, 32x32 products, reads ahead of their use and 64 rows
+// a wave were all tried: 442 - 530.
 //
 // LDS rows of K (a key, 2 D bytes) have their 16-byte chunks permuted so that
 // the 16 lanes that an access of 16 bytes serves at once (0-3, 12-15, 20-27 of
@@ -780,7 +784,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tree_attn_tile_kernel(TreeAttn p) 
     const int k = p.split ? share_id - P0 / share : 0;
     const int nseg = p.split ? (P0 + tiles - 1) / share - P0 / share + 1 : 1;
     u += j1 - j0;
-    const int sub = rt * NW + w;                         // this wave's 32 rows of the item
+    const int sub = rt * NW + w;                         // this wave's NG * 16 rows of the item
     const bool work = sub * NG * 16 < p.rows;
     const int it = (s * p.Hkv + kvh) * p.n_rt + sub;
     if (p.split && work && k == 0 && lane == 0) p.meta[it] = int2{nseg, (share_id * p.n_wide + rt) * NW + w};

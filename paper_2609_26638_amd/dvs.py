@@ -872,8 +872,9 @@ def capture(fn) -> "torch.cuda.CUDAGraph":
     """Record the launches of ``fn`` (calls of this module that only enqueue:
     draft_verify_step, literal_round, attn_hybrid_block, argmax_accept,
     sample_filtered, accept_sampled, the commits, kv_fork, kv_release,
-    kv_compact, tree_masks, kv_append_rope, attn_tree, accept_commit_tree; not diffusion_block or literal_round_refined, which read a count
-    back from the device) into a HIP graph.  ``replay()`` re-runs them on the
+    kv_compact, tree_masks, kv_append_rope, attn_tree, accept_commit_tree; not
+    diffusion_block or literal_round_refined, which read a count back from the
+    device) into a HIP graph.  ``replay()`` re-runs them on the
     buffers' current contents: every input of a step (kv_len, pages, boundary,
     draft, ...) is read from device memory, so a replay is the next step.
     The library clears its counters with kernels, never with a memset node.
