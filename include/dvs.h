@@ -815,8 +815,7 @@ int attn_tree(const void* q, const void* k_pool, const void* v_pool, const int32
  *   workspace >= dvs_accept_tree_workspace_bytes(S, R) bytes, no
  *           initialisation needed.  Calls that share it must not overlap.
  * Requirements: 1 <= S <= 1024, 1 <= R <= 1024, head_dim in {64, 96, 128},
- * max_pages < 2^27 - 3, S * n_kv_heads below 2^25 / n_layers (64 of them at most
- * count).
+ * max_pages < 2^27 - 3, S * n_kv_heads * min(n_layers, 64) <= 2^25 - 2.
  * ---------------------------------------------------------------------- */
 size_t dvs_accept_tree_workspace_bytes(int32_t S, int32_t R);
 int accept_commit_tree(const dvs_state* st, const dvs_layer* layers, int32_t n_layers,

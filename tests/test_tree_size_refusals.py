@@ -40,3 +40,7 @@ def test_moves_of_more_threads_than_a_launch_has():
     assert _commit(st=ctypes.byref(st), nbytes=nbytes, heads=1 << 14) == -2
     assert _commit(st=ctypes.byref(st), nbytes=nbytes, heads=2 ** 31 - 1) == -2
     assert _commit(st=ctypes.byref(st), nbytes=16, heads=(1 << 14) - 1) == -4
+    # the largest product that is taken: 1 * 1 * (2^25 - 2) with one layer, 2^25 - 1 is not
+    st = _state(S=1)
+    assert _commit(st=ctypes.byref(st), nbytes=16, n=1, heads=2 ** 25 - 2) == -4
+    assert _commit(st=ctypes.byref(st), nbytes=16, n=1, heads=2 ** 25 - 1) == -2
